@@ -469,6 +469,128 @@ BLOAD_API int bload_plan_static(const int32_t* d_lengths, int64_t n, int32_t t_b
                                 bload_plan_info_t* info);
 
 /*
+ * Layers on packed batches.  A model that trains on packed blocks mixes information along the slots, and must do so
+ * inside sequences only.  The calls below take the per-slot positions that bload_pack writes,
+ *     d_pos[q, s] = position of slot s of block q in its sequence, -1 on padding         (int32 [block_count, t_block])
+ * as their only description of the packing: slot s belongs to the sequence that starts at slot s - d_pos[q, s].  The
+ * positions of a sequence have to be 0, 1, 2, ... in consecutive slots and slot 0 of a block has to start a sequence
+ * (or be padding), as in every block of a plan; other contents give unspecified values, never an access outside
+ * the buffers.  Padding slots receive zeros (rotary: their input unchanged), and what their inputs hold is not used.
+ *
+ * Common rules: block_count >= 0 (0 does nothing), 1 <= t_block <= BLOAD_MAX_T_BLOCK.  Element types are BLOAD_F32,
+ * BLOAD_F16 and BLOAD_BF16, one for all tensors of a call; statistics, states and sums are held in 32 bits and every
+ * output is rounded once.  Outputs must not overlap inputs or each other, except where a call says so.  Repeated calls
+ * on equal inputs give identical bits: no sum depends on the order in which blocks of threads run.  Asynchronous on
+ * `stream`; nothing is allocated; capturable.  Errors: NULL, ARG, ALIGN, UNSUPPORTED, WORKSPACE, CUDA as documented at
+ * each call, all before anything is launched.
+ */
+#define BLOAD_F32 0
+#define BLOAD_F16 1
+#define BLOAD_BF16 2
+
+/* A tensor [block_count, t_block, heads, head_dim] by strides in ELEMENTS; the elements of a head are contiguous.
+ * Slices of a fused projection and [block, head, slot, element] layouts are expressed this way. */
+typedef struct {
+    void* data;
+    int64_t block_stride, slot_stride, head_stride;
+} bload_heads_t;
+
+/*
+ * bload_rotary -- rotary positions that restart with every sequence.  For each head of each frame at position p, with
+ * n = rot_dim / 2 and a_i = float(p) * d_inv_freq[i] (one rounding to 32 bits), i < n:
+ *     (u, w) = (x[i], x[n + i])          interleaved == 0
+ *            = (x[2 i], x[2 i + 1])      interleaved == 1
+ *     (u, w) -> factor * (u cos a_i - w sin a_i,  w cos a_i + u sin a_i)
+ * Elements from rot_dim on, and padding slots, are copied.  d_inv_freq (float[n], device) holds base^(-2 i / rot_dim)
+ * or any stretched form of it for long contexts; `factor` is the scale some of those apply to the rotated part.
+ * bload_rotary_grad is the gradient: it takes dy as `x` and writes dx to `y` (the same turn by -a_i).
+ * y may be x itself (same data and strides).  rot_dim is even, 0 <= rot_dim <= head_dim; heads >= 1, head_dim >= 1.
+ * Errors: NULL, ARG (sizes, rot_dim, strides < 0, a broadcast y), ALIGN (data not aligned to the element),
+ * UNSUPPORTED (dtype, t_block), CUDA.
+ */
+BLOAD_API int bload_rotary(const int32_t* d_pos, int64_t block_count, int32_t t_block, int32_t heads, int32_t head_dim,
+                           int32_t dtype, const bload_heads_t* x, const bload_heads_t* y, const float* d_inv_freq,
+                           int32_t rot_dim, int32_t interleaved, float factor, void* stream);
+BLOAD_API int bload_rotary_grad(const int32_t* d_pos, int64_t block_count, int32_t t_block, int32_t heads,
+                                int32_t head_dim, int32_t dtype, const bload_heads_t* dy, const bload_heads_t* dx,
+                                const float* d_inv_freq, int32_t rot_dim, int32_t interleaved, float factor,
+                                void* stream);
+
+/*
+ * bload_attention / bload_attention_grad -- attention inside the sequences of a block.  For head h and slot i of a
+ * sequence, over the slots j of the same sequence (j <= i if causal; |i - j| < window if window > 0):
+ *     s_ij = scale * q_i . k_j;   if softcap > 0: s_ij = softcap * tanh(s_ij / softcap);
+ *     if d_slopes: s_ij -= d_slopes[h] * |i - j|
+ *     out_i = sum_j softmax_j(s_ij) v_j;        lse[q, h, i] = log sum_j exp(s_ij)   (natural logarithm)
+ * Query head h reads key and value head h / (heads / kv_heads).  On padding out = 0 and lse = -inf.  A key slot that
+ * is not allowed has no influence, whatever it holds (infinities and NaN included).  A row whose allowed scores are
+ * all -inf gives zeros and lse = -inf.
+ *
+ *   q, out, dout, dq  [block_count, t_block, heads, head_dim]          k, v, dk, dv  [.., kv_heads, head_dim]
+ *   d_lse             float [block_count, heads, t_block]; NULL in bload_attention: not written
+ *   d_delta           float [block_count, heads, t_block], written by bload_attention_grad: sum over the head of
+ *                     dout * out, which both of its kernels need
+ * bload_attention_grad takes out and d_lse of the forward call with the same arguments, and dout, and writes dq, dk, dv
+ * (gradients of shared key heads are summed over their query heads).
+ *
+ * dtype BLOAD_F16 or BLOAD_BF16; head_dim a multiple of 8, at most 128; data 16-byte aligned and strides multiples of 8
+ * elements (all dimensions longer than 1), strides below 2^39 elements; scale and softcap finite, softcap >= 0;
+ * d_slopes float[heads] (device) or NULL; window >= 0.
+ * Errors: NULL, ARG (sizes, heads not a multiple of kv_heads, strides <= 0, values), ALIGN, UNSUPPORTED (dtype, head_dim,
+ * t_block), CUDA.
+ */
+typedef struct {
+    int64_t block_count;
+    int32_t t_block, heads, kv_heads, head_dim, dtype;
+    int32_t causal, window;
+    float scale, softcap;
+    const int32_t* d_pos;
+    const float* d_slopes;
+    bload_heads_t q, k, v, out;
+    float* d_lse;
+    bload_heads_t dout, dq, dk, dv; /* gradient only */
+    float* d_delta;                 /* gradient only */
+} bload_attention_t;
+BLOAD_API int bload_attention(const bload_attention_t* a, void* stream);
+BLOAD_API int bload_attention_grad(const bload_attention_t* a, void* stream);
+
+/*
+ * bload_recurrence / bload_recurrence_grad -- a gated linear recurrence along the slots of each block, per channel,
+ * that restarts at every sequence start:
+ *     f_s = sigmoid(gate_s);     h_s = f_s * h_{s-1} + (1 - f_s) * x_s,    h_{s-1} = 0 where a sequence starts at s
+ * and, for the gradient dh of a loss with respect to every h_s,
+ *     g_s = dh_s + (f_{s+1} * g_{s+1} if the sequence continues at s + 1);
+ *     dx_s = (1 - f_s) g_s;      dgate_s = g_s (h_{s-1} - x_s) f_s (1 - f_s).
+ * Padding slots get h = 0, dgate = dx = 0.  gate, x, h, dh, dgate, dx are [block_count, t_block, channels] with
+ * contiguous channels, strides in elements; data aligned to the element (16-byte aligned data and strides that are
+ * multiples of 16 bytes take the fast path).
+ *
+ *   d_carry  float [block_count, ceil(t_block / BLOAD_RECURRENCE_RUN), channels]: the state that enters each run of
+ *            BLOAD_RECURRENCE_RUN slots, written by the forward call and read by the gradient, which rebuilds h from it
+ *            in 32 bits instead of reading the rounded h; 16-byte aligned; NULL in the forward call: not kept
+ *   d_work   scratch of bload_recurrence_work_bytes bytes, 256-byte aligned, for both calls (NULL when that is 0)
+ * Errors: NULL, ARG (sizes, strides < 0, a broadcast output), ALIGN, WORKSPACE, UNSUPPORTED (dtype, t_block), CUDA.
+ */
+#define BLOAD_RECURRENCE_RUN 64
+typedef struct {
+    void* data;
+    int64_t block_stride, slot_stride;
+} bload_channels_t;
+typedef struct {
+    int64_t block_count, channels;
+    int32_t t_block, dtype;
+    const int32_t* d_pos;
+    bload_channels_t gate, x, h; /* h: forward only */
+    float* d_carry;
+    void* d_work;
+    size_t work_bytes;
+    bload_channels_t dh, dgate, dx; /* gradient only */
+} bload_recurrence_t;
+BLOAD_API size_t bload_recurrence_work_bytes(int64_t block_count, int32_t t_block, int64_t channels);
+BLOAD_API int bload_recurrence(const bload_recurrence_t* a, void* stream);
+BLOAD_API int bload_recurrence_grad(const bload_recurrence_t* a, void* stream);
+
+/*
  * bload_rank_range -- the share of one data-parallel rank, host only.
  *
  * The paper's motivation (section "Problem Statement and Current Limitations"): with data-parallel

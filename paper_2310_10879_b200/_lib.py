@@ -20,6 +20,8 @@ MAX_T_BLOCK = 32768
 EXPORTS = ("bload_plan_sizes", "bload_plan", "bload_plan_async", "bload_plan_finish", "bload_rank_range", "bload_pack", "bload_unpack", "bload_stats", "bload_epoch", "bload_epoch_stage_times",
            "bload_pack_repeat_last", "bload_var_offsets", "bload_pack_var", "bload_unpack_var", "bload_var_offsets2d", "bload_pack_var2d",
            "bload_unpack_var2d", "bload_carry_prev", "bload_reset_state", "bload_valid_sum",
+           "bload_rotary", "bload_rotary_grad", "bload_attention", "bload_attention_grad", "bload_recurrence_work_bytes",
+           "bload_recurrence", "bload_recurrence_grad",
            "bload_plan_static", "bload_chunk_work_bytes", "bload_chunk_count", "bload_plan_chunks", "bload_set_plan_timing", "bload_plan_stage_times", "bload_kernel_launches", "bload_last_copy_kernel", "bload_debug_status", "bload_bulk_copy_timeouts",
            "bload_strerror", "bload_version")
 
@@ -119,6 +121,14 @@ def load() -> C.CDLL:
     L.bload_epoch.argtypes = [vp, i64, i32, u64, vp, C.c_size_t, vp, C.c_size_t, C.POINTER(EpochIO), vp, vp,
                               C.POINTER(PlanInfo)]
     L.bload_epoch_stage_times.argtypes = [C.POINTER(C.c_float * 5)]
+    L.bload_rotary.argtypes = [vp, i64, i32, i32, i32, i32, C.POINTER(HeadsTensor), C.POINTER(HeadsTensor), vp, i32, i32,
+                               C.c_float, vp]
+    L.bload_rotary_grad.argtypes = L.bload_rotary.argtypes
+    L.bload_attention.argtypes = [C.POINTER(AttentionArgs), vp]
+    L.bload_attention_grad.argtypes = L.bload_attention.argtypes
+    L.bload_recurrence_work_bytes.argtypes = [i64, i32, i64]
+    L.bload_recurrence.argtypes = [C.POINTER(RecurrenceArgs), vp]
+    L.bload_recurrence_grad.argtypes = L.bload_recurrence.argtypes
     L.bload_set_plan_timing.argtypes = [C.c_int]
     L.bload_plan_stage_times.argtypes = [C.POINTER(C.c_float * 4)]
     L.bload_strerror.argtypes = [C.c_int]
@@ -128,12 +138,13 @@ def load() -> C.CDLL:
     L.bload_version.argtypes = []
     L.bload_kernel_launches.argtypes = []
     for name in EXPORTS:
-        if name not in ("bload_strerror", "bload_kernel_launches", "bload_last_copy_kernel", "bload_debug_status", "bload_bulk_copy_timeouts", "bload_chunk_work_bytes"):
+        if name not in ("bload_strerror", "bload_kernel_launches", "bload_last_copy_kernel", "bload_debug_status", "bload_bulk_copy_timeouts", "bload_chunk_work_bytes", "bload_recurrence_work_bytes"):
             getattr(L, name).restype = C.c_int
     L.bload_kernel_launches.restype = C.c_int64
     L.bload_bulk_copy_timeouts.argtypes = []
     L.bload_bulk_copy_timeouts.restype = C.c_int64
     L.bload_chunk_work_bytes.restype = C.c_size_t
+    L.bload_recurrence_work_bytes.restype = C.c_size_t
     L.bload_last_copy_kernel.restype = C.c_char_p
     _lib = L
     return L
@@ -525,3 +536,192 @@ def bload_rank_range(n_blocks: int, world_size: int, rank: int, batch_blocks: in
     if rc:
         raise BloadError(rc, "bload_rank_range")
     return int(b.value), int(c.value)
+
+
+# ---- layers on packed batches: everything below takes the per-slot positions that bload_pack writes ----------------
+
+F32, F16, BF16 = 0, 1, 2
+RECURRENCE_RUN = 64
+
+
+class HeadsTensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("block_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class AttentionArgs(C.Structure):
+    _fields_ = [("block_count", C.c_int64), ("t_block", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32),
+                ("scale", C.c_float), ("softcap", C.c_float), ("d_pos", C.c_void_p), ("d_slopes", C.c_void_p),
+                ("q", HeadsTensor), ("k", HeadsTensor), ("v", HeadsTensor), ("out", HeadsTensor), ("d_lse", C.c_void_p),
+                ("dout", HeadsTensor), ("dq", HeadsTensor), ("dk", HeadsTensor), ("dv", HeadsTensor),
+                ("d_delta", C.c_void_p)]
+
+
+class ChannelsTensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("block_stride", C.c_int64), ("slot_stride", C.c_int64)]
+
+
+class RecurrenceArgs(C.Structure):
+    _fields_ = [("block_count", C.c_int64), ("channels", C.c_int64), ("t_block", C.c_int32), ("dtype", C.c_int32),
+                ("d_pos", C.c_void_p), ("gate", ChannelsTensor), ("x", ChannelsTensor), ("h", ChannelsTensor),
+                ("d_carry", C.c_void_p), ("d_work", C.c_void_p), ("work_bytes", C.c_size_t), ("dh", ChannelsTensor),
+                ("dgate", ChannelsTensor), ("dx", ChannelsTensor)]
+
+
+def _element_type(t, where: str) -> int:
+    import torch
+    code = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}.get(t.dtype)
+    if code is None:
+        raise TypeError("%s: float32, float16 or bfloat16 tensors, not %s" % (where, t.dtype))
+    return code
+
+
+def _positions(pos, where: str):
+    import torch
+    if pos.dtype != torch.int32 or pos.dim() != 2 or not pos.is_cuda or not pos.is_contiguous():
+        raise TypeError("%s: pos must be a contiguous CUDA int32 tensor [blocks, t_block], as bload_pack writes it" % where)
+    if pos.device.index != torch.cuda.current_device():
+        raise ValueError("%s: pos is on %s, the current device is cuda:%d" % (where, pos.device, torch.cuda.current_device()))
+    return pos.shape
+
+
+def _strided(cls, name, t, shape, like, where: str):
+    """A strided tensor argument; the last dimension has to be contiguous."""
+    if t.dtype != like.dtype or t.device != like.device:
+        raise TypeError("%s: %s is %s on %s, expected %s on %s" % (where, name, t.dtype, t.device, like.dtype, like.device))
+    if t.shape != shape:
+        raise ValueError("%s: %s has shape %s, expected %s" % (where, name, tuple(t.shape), tuple(shape)))
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError("%s: the last dimension of %s must be contiguous" % (where, name))
+    return cls(t.data_ptr(), *st[:-1])
+
+
+def _flat32(name, t, count: int, like, where: str):
+    """A contiguous float32 argument, or None."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.device != like.device or not t.is_contiguous() or t.numel() != count:
+        raise TypeError("%s: %s must be a contiguous float32 tensor of %d elements on %s" % (where, name, count, like.device))
+    return t.data_ptr()
+
+
+def _rotary(fn, where, pos, x, y, inv_freq, interleaved, factor, stream) -> None:
+    b, t = _positions(pos, where)
+    if x.dim() != 4 or x.device != pos.device:
+        raise ValueError("%s: tensors are [blocks, t_block, heads, head_dim] on the device of pos" % where)
+    h, d = x.shape[2:]
+    shape = (b, t, h, d)
+    xs = _strided(HeadsTensor, "input", x, shape, x, where)
+    ys = _strided(HeadsTensor, "output", y, shape, x, where)
+    n = inv_freq.numel()
+    rc = fn(pos.data_ptr(), b, t, h, d, _element_type(x, where), C.byref(xs), C.byref(ys),
+            _flat32("inv_freq", inv_freq, n, x, where), 2 * n, 1 if interleaved else 0, factor, _stream(stream))
+    if rc:
+        raise BloadError(rc, where)
+
+
+def bload_rotary(pos, x, y, inv_freq, interleaved: bool = False, factor: float = 1.0, stream=None) -> None:
+    """y = rotary positions applied to x [blocks, t_block, heads, head_dim] (strided; y may be x).  pos: int32 [blocks,
+    t_block] from bload_pack; inv_freq: float32 [rot_dim / 2], the elements from rot_dim on are copied."""
+    _rotary(load().bload_rotary, "bload_rotary", pos, x, y, inv_freq, interleaved, factor, stream)
+
+
+def bload_rotary_grad(pos, dy, dx, inv_freq, interleaved: bool = False, factor: float = 1.0, stream=None) -> None:
+    """dx = gradient of bload_rotary's input, from the gradient dy of its output (dx may be dy)."""
+    _rotary(load().bload_rotary_grad, "bload_rotary_grad", pos, dy, dx, inv_freq, interleaved, factor, stream)
+
+
+def _attention_args(where, pos, q, k, v, out, lse, scale, softcap, slopes, causal, window) -> AttentionArgs:
+    b, t = _positions(pos, where)
+    if q.dim() != 4 or k.dim() != 4 or q.device != pos.device:
+        raise ValueError("%s: tensors are [blocks, t_block, heads, head_dim] on the device of pos" % where)
+    h, d = q.shape[2:]
+    hk = k.shape[2]
+    qs, ks = (b, t, h, d), (b, t, hk, d)
+    a = AttentionArgs(b, t, h, hk, d, _element_type(q, where), 1 if causal else 0, window,
+                      d ** -0.5 if scale is None else scale, softcap, pos.data_ptr(), _flat32("slopes", slopes, h, q, where))
+    a.q = _strided(HeadsTensor, "q", q, qs, q, where)
+    a.k = _strided(HeadsTensor, "k", k, ks, q, where)
+    a.v = _strided(HeadsTensor, "v", v, ks, q, where)
+    a.out = _strided(HeadsTensor, "out", out, qs, q, where)
+    a.d_lse = _flat32("lse", lse, b * h * t, q, where)
+    return a
+
+
+def bload_attention(pos, q, k, v, out, lse=None, scale: float | None = None, softcap: float = 0.0, slopes=None,
+                    causal: bool = True, window: int = 0, stream=None) -> None:
+    """Attention inside the sequences of packed blocks.  q, out: [blocks, t_block, heads, head_dim], k, v: [.., kv_heads, ..]
+    (float16 or bfloat16, strided); pos: int32 [blocks, t_block] from bload_pack; lse: float32 [blocks, heads, t_block] or
+    None (needed for the gradient).  scale defaults to head_dim ** -0.5; softcap > 0 caps scores by a tanh; slopes: float32
+    [heads], subtracts slope * |i - j|; window > 0 keeps |i - j| < window."""
+    a = _attention_args("bload_attention", pos, q, k, v, out, lse, scale, softcap, slopes, causal, window)
+    rc = load().bload_attention(C.byref(a), _stream(stream))
+    if rc:
+        raise BloadError(rc, "bload_attention")
+
+
+def bload_attention_grad(pos, q, k, v, out, lse, dout, dq, dk, dv, delta, scale: float | None = None, softcap: float = 0.0,
+                         slopes=None, causal: bool = True, window: int = 0, stream=None) -> None:
+    """dq, dk, dv of bload_attention from dout, with out and lse of the forward call.  delta: float32 [blocks, heads,
+    t_block], written (the row sums of dout * out)."""
+    where = "bload_attention_grad"
+    a = _attention_args(where, pos, q, k, v, out, lse, scale, softcap, slopes, causal, window)
+    a.dout = _strided(HeadsTensor, "dout", dout, q.shape, q, where)
+    a.dq = _strided(HeadsTensor, "dq", dq, q.shape, q, where)
+    a.dk = _strided(HeadsTensor, "dk", dk, k.shape, q, where)
+    a.dv = _strided(HeadsTensor, "dv", dv, k.shape, q, where)
+    a.d_delta = _flat32("delta", delta, lse.numel(), q, where)
+    rc = load().bload_attention_grad(C.byref(a), _stream(stream))
+    if rc:
+        raise BloadError(rc, where)
+
+
+def bload_recurrence_buffers(pos, x):
+    """(carry, work) for bload_recurrence and its gradient on x [blocks, t_block, channels]: the float32 states that the
+    forward call keeps for the gradient, [blocks, ceil(t_block / 64), channels], and scratch (None when none is needed)."""
+    import torch
+    b, t = pos.shape
+    carry = torch.empty((b, -(-t // RECURRENCE_RUN), x.shape[-1]), dtype=torch.float32, device=x.device)
+    n = load().bload_recurrence_work_bytes(b, t, x.shape[-1])
+    return carry, torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+
+
+def _recurrence_args(where, pos, gate, x, carry, work) -> RecurrenceArgs:
+    b, t = _positions(pos, where)
+    if x.dim() != 3 or x.device != pos.device:
+        raise ValueError("%s: tensors are [blocks, t_block, channels] on the device of pos" % where)
+    c = x.shape[2]
+    a = RecurrenceArgs(b, c, t, _element_type(x, where), pos.data_ptr())
+    a.gate = _strided(ChannelsTensor, "gate", gate, x.shape, x, where)
+    a.x = _strided(ChannelsTensor, "x", x, (b, t, c), x, where)
+    a.d_carry = _flat32("carry", carry, b * -(-t // RECURRENCE_RUN) * c, x, where)
+    if work is not None:
+        if work.device != x.device or not work.is_contiguous():
+            raise TypeError("%s: work must be a contiguous tensor on %s" % (where, x.device))
+        a.d_work, a.work_bytes = work.data_ptr(), work.numel() * work.element_size()
+    return a
+
+
+def bload_recurrence(pos, gate, x, h, carry=None, work=None, stream=None) -> None:
+    """h_s = f_s h_{s-1} + (1 - f_s) x_s with f = sigmoid(gate), restarted at every sequence start.  gate, x, h: [blocks,
+    t_block, channels] (float32, float16 or bfloat16, strided); carry, work from bload_recurrence_buffers (carry None:
+    no gradient will be asked for)."""
+    a = _recurrence_args("bload_recurrence", pos, gate, x, carry, work)
+    a.h = _strided(ChannelsTensor, "h", h, x.shape, x, "bload_recurrence")
+    rc = load().bload_recurrence(C.byref(a), _stream(stream))
+    if rc:
+        raise BloadError(rc, "bload_recurrence")
+
+
+def bload_recurrence_grad(pos, gate, x, carry, dh, dgate, dx, work=None, stream=None) -> None:
+    """dgate and dx of bload_recurrence from dh, the gradient with respect to every h; carry is the forward call's."""
+    where = "bload_recurrence_grad"
+    a = _recurrence_args(where, pos, gate, x, carry, work)
+    a.dh = _strided(ChannelsTensor, "dh", dh, x.shape, x, where)
+    a.dgate = _strided(ChannelsTensor, "dgate", dgate, x.shape, x, where)
+    a.dx = _strided(ChannelsTensor, "dx", dx, x.shape, x, where)
+    rc = load().bload_recurrence_grad(C.byref(a), _stream(stream))
+    if rc:
+        raise BloadError(rc, where)

@@ -56,7 +56,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False, defin
     if not force and not stale(lib, extra):
         return lib
     tmp = lib + ".tmp%d" % os.getpid()
-    cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
+    cmd = [nvcc_path(), "--threads", "0", "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
            "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if debug:
