@@ -45,8 +45,8 @@ extern "C" {
 #define BLOAD_ERR_ALIGN (-5)       /* a device pointer is not aligned as documented */
 #define BLOAD_ERR_UNSUPPORTED (-6) /* t_block above BLOAD_MAX_T_BLOCK, unknown policy */
 #define BLOAD_ERR_CUDA (-7)        /* a CUDA runtime call or launch failed */
-#define BLOAD_ERR_TIMEOUT (-8)     /* reserved: a bounded device-side wait expired.  No kernel of this version waits on a
-                                      flag (the only waits are for the hardware's own copy groups), so no call returns it */
+#define BLOAD_ERR_TIMEOUT (-8)     /* reserved: a bounded device-side wait expired.  No call returns it: calls do not
+                                      synchronise, and the layers count such waits (bload_device_timeouts) */
 #define BLOAD_ERR_PLAN (-9)        /* info/plan do not describe a finished plan */
 
 #define BLOAD_MAX_T_BLOCK 32768
@@ -482,7 +482,8 @@ BLOAD_API int bload_plan_static(const int32_t* d_lengths, int64_t n, int32_t t_b
  * output is rounded once.  Outputs must not overlap inputs or each other, except where a call says so.  Repeated calls
  * on equal inputs give identical bits: no sum depends on the order in which blocks of threads run.  Asynchronous on
  * `stream`; nothing is allocated; capturable.  Errors: NULL, ARG, ALIGN, UNSUPPORTED, WORKSPACE, CUDA as documented at
- * each call, all before anything is launched.
+ * each call, all before anything is launched.  A device-side wait that expired (it cannot, short of a hardware fault)
+ * leaves that call's outputs incomplete and is counted by bload_device_timeouts.
  */
 #define BLOAD_F32 0
 #define BLOAD_F16 1
@@ -589,6 +590,13 @@ typedef struct {
 BLOAD_API size_t bload_recurrence_work_bytes(int64_t block_count, int32_t t_block, int64_t channels);
 BLOAD_API int bload_recurrence(const bload_recurrence_t* a, void* stream);
 BLOAD_API int bload_recurrence_grad(const bload_recurrence_t* a, void* stream);
+
+/*
+ * bload_device_timeouts -- number of bounded device-side waits (of the attention kernels: on their own copies, matrix
+ * products and arithmetic) that gave up since the library was loaded.  Anything but
+ * 0 means incomplete outputs.  Synchronises the device; -1 if that fails.
+ */
+BLOAD_API int64_t bload_device_timeouts(void);
 
 /*
  * bload_rank_range -- the share of one data-parallel rank, host only.

@@ -21,7 +21,7 @@ EXPORTS = ("bload_plan_sizes", "bload_plan", "bload_plan_async", "bload_plan_fin
            "bload_pack_repeat_last", "bload_var_offsets", "bload_pack_var", "bload_unpack_var", "bload_var_offsets2d", "bload_pack_var2d",
            "bload_unpack_var2d", "bload_carry_prev", "bload_reset_state", "bload_valid_sum",
            "bload_rotary", "bload_rotary_grad", "bload_attention", "bload_attention_grad", "bload_recurrence_work_bytes",
-           "bload_recurrence", "bload_recurrence_grad",
+           "bload_recurrence", "bload_recurrence_grad", "bload_device_timeouts",
            "bload_plan_static", "bload_chunk_work_bytes", "bload_chunk_count", "bload_plan_chunks", "bload_set_plan_timing", "bload_plan_stage_times", "bload_kernel_launches", "bload_last_copy_kernel", "bload_debug_status", "bload_bulk_copy_timeouts",
            "bload_strerror", "bload_version")
 
@@ -138,9 +138,11 @@ def load() -> C.CDLL:
     L.bload_version.argtypes = []
     L.bload_kernel_launches.argtypes = []
     for name in EXPORTS:
-        if name not in ("bload_strerror", "bload_kernel_launches", "bload_last_copy_kernel", "bload_debug_status", "bload_bulk_copy_timeouts", "bload_chunk_work_bytes", "bload_recurrence_work_bytes"):
+        if name not in ("bload_strerror", "bload_kernel_launches", "bload_last_copy_kernel", "bload_debug_status", "bload_bulk_copy_timeouts", "bload_chunk_work_bytes", "bload_recurrence_work_bytes", "bload_device_timeouts"):
             getattr(L, name).restype = C.c_int
     L.bload_kernel_launches.restype = C.c_int64
+    L.bload_device_timeouts.argtypes = []
+    L.bload_device_timeouts.restype = C.c_int64
     L.bload_bulk_copy_timeouts.argtypes = []
     L.bload_bulk_copy_timeouts.restype = C.c_int64
     L.bload_chunk_work_bytes.restype = C.c_size_t
@@ -725,3 +727,8 @@ def bload_recurrence_grad(pos, gate, x, carry, dh, dgate, dx, work=None, stream=
     rc = load().bload_recurrence_grad(C.byref(a), _stream(stream))
     if rc:
         raise BloadError(rc, where)
+
+
+def bload_device_timeouts() -> int:
+    """Bounded device-side waits of the layers' kernels that gave up (0 unless the hardware failed)."""
+    return int(load().bload_device_timeouts())

@@ -1,37 +1,870 @@
-// Attention inside the sequences of packed blocks and its gradients.
+// Attention inside the sequences of packed blocks, and its gradients, on the fifth-generation tensor cores.
+//
+//   k29_attention       128 queries per CTA: scores S = Q K^T and out += P V per tile of 128 keys
+//   k30_attention_grad  <queries>: 128 queries per CTA, dq;  <keys>: 128 keys per CTA, dk and dv
+//
+// Every row (a query, or a key of the second gradient kernel) may see one interval of slots [lo, hi] -- its sequence, cut by
+// causality and by the window -- so a CTA walks the tiles from the smallest lo of its rows to their largest hi, and a tile's
+// mask is a range of columns per row.  Products run in 16 bits with sums in 32; scores, statistics, probabilities and
+// accumulators are held in 32 bits, and P and dS are rounded to the inputs' type as operands of the second product.
+//
+// Hidden slots must have no influence, but a product multiplies them by zero, and 0 * NaN is not 0.  So a tile that is hidden
+// from any row of the CTA is scanned (one multiply-add by zero per pair of elements): infinities and NaN on padding are
+// cleared in shared memory, and if a frame holds any, the CTA's rows are computed once more, one at a time, by the loops of
+// bload_attention_rows.cuh, which never touch a hidden slot.
+#include <cuda.h>
+
+#include <type_traits>
+
 #include "bload_attention_rows.cuh"
 #include "bload_internal.cuh"
+#include "bload_tc.cuh"
 
 namespace bload {
 
 namespace {
 
-enum { kForward, kDq, kDkv };
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kNever = 1 << 30;
 
-// A warp per row: the simplest form that is right for every case.
-template <typename T, int WHAT>
-__global__ void __launch_bounds__(256) k29_attention_rows(AttnParams p, AttnTensors<T> a)
+__device__ unsigned int g_timeouts;  // bounded waits that gave up (bload_device_timeouts)
+
+template <bool BF16>
+struct Element {
+    using type = __half;
+};
+template <>
+struct Element<true> {
+    using type = __nv_bfloat16;
+};
+
+// The interval of the other side that row `row` of this warp's rows row0 .. row0 + 31 may see.
+__device__ __forceinline__ rows::Span span_of(const AttnParams& p, const int32_t* pos, int row, bool keys, int lane)
 {
-    const int lane = threadIdx.x & 31;
-    const int heads = WHAT == kDkv ? p.kv_heads : p.heads;
-    const int64_t items = p.blocks * heads * p.t, warps = ((int64_t)gridDim.x * blockDim.x) >> 5;
-    for (int64_t item = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; item < items; item += warps) {
-        const int i = (int)(item % p.t);
-        const int h = (int)(item / p.t % heads);
-        const int64_t b = item / p.t / heads;
-        if (WHAT == kForward) rows::forward_row(p, a, b, h, i, lane);
-        if (WHAT == kDq) rows::dq_row(p, a, b, h, i, lane);
-        if (WHAT == kDkv) rows::dkv_row(p, a, b, h, i, lane);
+    const int row0 = row - lane;
+    const int here = row < p.t ? pos[row] : -1;
+    int end = row + 1;
+    if (keys || !p.causal) {  // (uniform) the sequence of a row ends at the next start or padding in the warp, or behind it
+        const unsigned stops = __ballot_sync(0xffffffffu, here <= 0) & ~((2u << lane) - 1);
+        const int last = __shfl_sync(0xffffffffu, here, 31);
+        int behind = row0 + 32;
+        if (last >= 0) behind = warp_seq_end(pos, p.t, row0 + 31, lane);
+        end = stops ? row0 + __ffs(stops) - 1 : behind;
+    }
+    if (here < 0) return {kNever, -1};
+    rows::Span s;
+    if (keys) {
+        s.lo = p.causal ? row : max(row - here, 0);
+        s.hi = end - 1;
+    } else {
+        s.lo = max(row - here, 0);
+        s.hi = p.causal ? row : end - 1;
+    }
+    s.lo = max(s.lo, row - (p.window - 1));
+    s.hi = min(s.hi, row + (p.window - 1));
+    return s;
+}
+
+// columns [lo, hi] of 32
+__device__ __forceinline__ uint32_t column_mask(int lo, int hi)
+{
+    lo = max(lo, 0);
+    hi = min(hi, 31);
+    return lo > hi ? 0u : (0xffffffffu << lo) & (0xffffffffu >> (31 - hi));
+}
+
+// The intervals of a CTA's rows together.
+struct Reach {
+    int lo, hi;         // smallest lo, largest hi
+    int all_lo, all_hi; // [all_lo, all_hi] is seen by every row that sees anything
+};
+template <int WARPS>
+struct ReachShared {
+    int lo[WARPS], hi[WARPS], all_lo[WARPS], all_hi[WARPS];
+};
+template <int WARPS>
+__device__ __forceinline__ void put_reach(ReachShared<WARPS>& sh, int warp, int lane, const rows::Span& s)
+{
+    const bool some = s.lo <= s.hi;
+    const int lo = __reduce_min_sync(0xffffffffu, some ? s.lo : kNever), hi = __reduce_max_sync(0xffffffffu, some ? s.hi : -1);
+    const int all_lo = __reduce_max_sync(0xffffffffu, some ? s.lo : -1), all_hi = __reduce_min_sync(0xffffffffu, some ? s.hi : kNever);
+    if (lane == 0) {
+        sh.lo[warp] = lo;
+        sh.hi[warp] = hi;
+        sh.all_lo[warp] = all_lo;
+        sh.all_hi[warp] = all_hi;
+    }
+}
+template <int WARPS>
+__device__ __forceinline__ Reach get_reach(const ReachShared<WARPS>& sh)
+{
+    Reach r{sh.lo[0], sh.hi[0], sh.all_lo[0], sh.all_hi[0]};
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) {
+        r.lo = min(r.lo, sh.lo[w]);
+        r.hi = max(r.hi, sh.hi[w]);
+        r.all_lo = max(r.all_lo, sh.all_lo[w]);
+        r.all_hi = min(r.all_hi, sh.all_hi[w]);
+    }
+    return r;
+}
+
+// score in units of log2 from q.k, with the cap and the distance bias; `inner` = d score / d (scale q.k)
+struct Modifier {
+    float by, inv_cap2, cap2, slope2;  // scale * log2e; 2 log2e * scale / cap; cap * log2e; slope * log2e
+    __device__ __forceinline__ Modifier(const AttnParams& p, int h)
+    {
+        by = p.scale * kLog2e;
+        inv_cap2 = p.cap > 0.0f ? 2.0f * kLog2e * p.scale / p.cap : 0.0f;
+        cap2 = p.cap * kLog2e;
+        slope2 = p.slopes ? p.slopes[h] * kLog2e : 0.0f;
+    }
+    // tanh(y) = 1 - 2 / (1 + exp(2 y)): an absolute error of some 2^-23 of the cap, whatever y
+    __device__ __forceinline__ float operator()(float qk, float apart, float& inner) const
+    {
+        float x = qk * by;
+        inner = 1.0f;
+        if (cap2 > 0.0f) {
+            const float th = fmaf(-2.0f, tc::inverse_fast(1.0f + tc::exp2_fast(qk * inv_cap2)), 1.0f);
+            x = cap2 * th;
+            inner = fmaf(-th, th, 1.0f);
+        }
+        return fmaf(-slope2, fabsf(apart), x);
+    }
+};
+
+// Scans a tile [ROWS][DP] in shared memory with THREADS threads for infinities and NaN.  Those on padding (or behind the
+// block's last slot, where copies fill in zeros anyway) are cleared; true if a frame holds one.
+template <bool BF16, int ROWS, int DP, int THREADS>
+__device__ __forceinline__ bool scan_tile(const AttnParams& p, const int32_t* pos, uint8_t* tile, int row0, int tid)
+{
+    uint32_t acc = 0;
+    constexpr int kChunks = ROWS * DP / 8 / THREADS;
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+        const uint4 x = *reinterpret_cast<const uint4*>(tile + (k * THREADS + tid) * 16);
+        acc = tc::probe<BF16>(tc::probe<BF16>(acc, x.x), x.y);
+        acc = tc::probe<BF16>(tc::probe<BF16>(acc, x.z), x.w);
+    }
+    if (!(acc & 0x7fff7fffu)) return false;
+    bool found = false;
+    for (int k = 0; k < kChunks; ++k) {
+        uint4* at = reinterpret_cast<uint4*>(tile + (k * THREADS + tid) * 16);
+        const uint4 x = *at;
+        if (!(tc::probe<BF16>(tc::probe<BF16>(tc::probe<BF16>(tc::probe<BF16>(0u, x.x), x.y), x.z), x.w) & 0x7fff7fffu)) continue;
+        const int row = row0 + (k * THREADS + tid) / 8 % ROWS;
+        if (row >= p.t || pos[row] < 0)
+            *at = make_uint4(0, 0, 0, 0);
+        else
+            found = true;
+    }
+    return found;
+}
+
+// 32 columns of a row in tensor memory, times `by`, to 64 bytes of a staged output tile (128-byte rows, swizzled)
+template <bool BF16>
+__device__ __forceinline__ void stage_columns(uint8_t* tile, int row, int column, const float (&x)[32])
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        uint4 w;
+        w.x = tc::pack<BF16>(x[8 * c], x[8 * c + 1]);
+        w.y = tc::pack<BF16>(x[8 * c + 2], x[8 * c + 3]);
+        w.z = tc::pack<BF16>(x[8 * c + 4], x[8 * c + 5]);
+        w.w = tc::pack<BF16>(x[8 * c + 6], x[8 * c + 7]);
+        *reinterpret_cast<uint4*>(tile + row * 128 + (((column / 8 + c) ^ (row & 7)) * 16)) = w;
     }
 }
 
-template <typename T, int WHAT>
-cudaError_t launch(const AttnParams& p, const AttnTensors<T>& a, cudaStream_t st)
+// ---- forward ------------------------------------------------------------------------------------------------------
+
+struct ForwardMaps {
+    CUtensorMap q, k, v, out;  // boxes of 128, 128, 128, 32 rows by 64 elements
+};
+
+template <int DP>
+struct ForwardTile {
+    static constexpr int kKeys = 128;
+    static constexpr int kStages = DP == 64 ? 2 : 1;
+    static constexpr int kTile = 128 * DP * 2;  // bytes of a tile of 128 rows
+    static constexpr int kShared = kTile * (1 + 2 * kStages) + 1024;
+};
+
+// Warps 0 to 3 own a query row per thread: scores from tensor memory, running maximum and sum, P back to tensor memory over
+// the scores.  Warp 4 copies tiles in, warp 5 issues the products.  256 of the 512 columns of tensor memory and less than half
+// of the shared memory, so that two CTAs share an SM and one's products run under the other's exponentials.
+template <bool BF16, int DP, bool MOD>
+__global__ void __launch_bounds__(192, 2)
+    k29_attention(const AttnParams p, const AttnTensors<typename Element<BF16>::type> a, const __grid_constant__ ForwardMaps maps)
 {
-    const int64_t items = p.blocks * (WHAT == kDkv ? p.kv_heads : p.heads) * p.t, grid = (items + 7) / 8;
-    k29_attention_rows<T, WHAT><<<(unsigned)(grid < 148 * 64 ? grid : 148 * 64), 256, 0, st>>>(p, a);
+    using Tile = ForwardTile<DP>;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t bars[3 + 4 * Tile::kStages + 1];
+    __shared__ uint32_t tmem_base;
+    __shared__ int dead, junk;
+    __shared__ ReachShared<4> reach_shared;
+
+    uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* const q_tile = tiles;
+    uint8_t* const k_tiles = tiles + Tile::kTile;
+    uint8_t* const v_tiles = k_tiles + Tile::kStages * Tile::kTile;
+    const uint32_t bar0 = tc::smem_of(bars);
+    const uint32_t q_full = bar0, s_full = bar0 + 8, p_full = bar0 + 16, o_done = bar0 + 24, k_full = bar0 + 32,
+                   k_free = k_full + 8 * Tile::kStages, v_full = k_free + 8 * Tile::kStages, v_free = v_full + 8 * Tile::kStages;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int q_tiles = (p.t + 127) / 128;
+    const int64_t bh = blockIdx.x % (p.blocks * p.heads);
+    const int i0 = (q_tiles - 1 - (int)(blockIdx.x / (p.blocks * p.heads))) * 128;  // the longest rows of a long sequence first
+    const int h = (int)(bh % p.heads), hk = h / p.group, b = (int)(bh / p.heads);
+    const int32_t* const pos = p.pos + (int64_t)b * p.t;
+    const int row = i0 + tid;  // of threads 0 to 127
+
+    rows::Span span{kNever, -1};
+    if (warp < 4) {
+        span = span_of(p, pos, row, false, lane);
+        put_reach(reach_shared, warp, lane, span);
+        if (tid == 0) dead = junk = 0;
+    } else if (warp == 4) {
+        if (lane == 0) {
+            tc::bar_init(q_full, 1);
+            tc::bar_init(s_full, 1);
+            tc::bar_init(p_full, 128);
+            tc::bar_init(o_done, 1);
+            for (int s = 0; s < 4 * Tile::kStages; ++s) tc::bar_init(k_full + 8 * s, 1);
+            tc::bar_init_done();
+        }
+    } else {
+        tc::tmem_alloc<256>(tc::smem_of(&tmem_base));
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = tmem_base, o_at = tmem, s_at = tmem + 128;
+    const Reach reach = get_reach(reach_shared);
+    const int n = reach.hi < 0 ? 0 : (reach.hi - reach.lo) / Tile::kKeys + 1;
+    float m = -INFINITY, l = 0.0f;  // running maximum (log2 units; may lag by kLag) and sum
+
+    if (warp == 4) {
+        if (lane == 0 && n > 0) {
+            bool ok = true;
+            tc::bar_expect(q_full, Tile::kTile);
+            for (int x = 0; x < DP; x += 64) tc::tensor_load(tc::smem_of(q_tile) + x * 256, &maps.q, x, i0, h, b, q_full);
+            int issued = 0;
+            for (int i = 0; i < n && ok; ++i, ++issued) {
+                const int s = i % Tile::kStages;
+                const uint32_t parity = (i / Tile::kStages + 1) & 1;
+                const int j0 = reach.lo + i * Tile::kKeys;
+                if (!(ok = tc::bar_wait(k_free + 8 * s, parity))) break;
+                tc::bar_expect(k_full + 8 * s, Tile::kTile);
+                for (int x = 0; x < DP; x += 64)
+                    tc::tensor_load(tc::smem_of(k_tiles) + s * Tile::kTile + x * 256, &maps.k, x, j0, hk, b, k_full + 8 * s);
+                if (!(ok = tc::bar_wait(v_free + 8 * s, parity))) {
+                    tc::bar_wait(k_full + 8 * s, (i / Tile::kStages) & 1);  // a copy in flight ends before the CTA does
+                    break;
+                }
+                tc::bar_expect(v_full + 8 * s, Tile::kTile);
+                for (int x = 0; x < DP; x += 64)
+                    tc::tensor_load(tc::smem_of(v_tiles) + s * Tile::kTile + x * 256, &maps.v, x, j0, hk, b, v_full + 8 * s);
+            }
+            if (!ok) {
+                dead = 1;
+                tc::bar_wait(q_full, 0);
+                for (int i = max(0, issued - Tile::kStages); i < issued; ++i) {
+                    tc::bar_wait(k_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
+                    tc::bar_wait(v_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
+                }
+            }
+        }
+    } else if (warp == 5) {
+        if (lane == 0 && n > 0) {
+            bool ok = tc::bar_wait(q_full, 0);
+            for (int i = 0; i < n && ok; ++i) {
+                const int s = i % Tile::kStages;
+                const uint32_t parity = (i / Tile::kStages) & 1;
+                // the scores take the place of the last tile's P: the product that reads it has to be over
+                ok = tc::bar_wait(k_full + 8 * s, parity) && (i == 0 || tc::bar_wait(o_done, (i - 1) & 1));
+                if (!ok) break;
+                tc::fence_after();
+                tc::product_rows<BF16, 128, DP>(s_at, tc::smem_of(q_tile), tc::smem_of(k_tiles) + s * Tile::kTile);
+                tc::products_arrive(k_free + 8 * s);
+                tc::products_arrive(s_full);
+                ok = tc::bar_wait(v_full + 8 * s, parity) && tc::bar_wait(p_full, i & 1);
+                if (!ok) break;
+                tc::fence_after();
+                tc::product_across<BF16, 128, DP>(o_at, s_at, tc::smem_of(v_tiles) + s * Tile::kTile, i > 0);
+                tc::products_arrive(v_free + 8 * s);
+                tc::products_arrive(o_done);
+            }
+            if (!ok) {
+                dead = 1;
+                tc::products_arrive(q_full);  // its second phase: products in flight end before the CTA does
+                tc::bar_wait(q_full, 1);
+            }
+        }
+    } else {
+        const Modifier modify(p, h);
+        const uint32_t lanes = (uint32_t)warp << 21;  // this warp's 32 lanes of tensor memory
+        const float by = modify.by;
+        bool found = false;
+        for (int i = 0; i < n; ++i) {
+            const int st = i % Tile::kStages;
+            const int j0 = reach.lo + i * Tile::kKeys;
+            if (!__all_sync(0xffffffffu, tc::bar_wait(s_full, i & 1))) {
+                dead = 1;
+                break;
+            }
+            tc::fence_after();
+            uint32_t s[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tc::tmem_load(s[c], s_at + lanes + 32 * c);
+            tc::tmem_loaded();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tc::settle(s[c]);
+            const bool clear = __all_sync(0xffffffffu, span.lo <= j0 && span.hi >= j0 + Tile::kKeys - 1);
+            float top = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint32_t mask = clear ? 0xffffffffu : column_mask(span.lo - j0 - 32 * c, span.hi - j0 - 32 * c);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    float x = __uint_as_float(s[c][e]);
+                    if (MOD) {
+                        float inner;
+                        x = modify(x, (float)(row - j0 - 32 * c - e), inner);
+                    }
+                    if (!clear) x = (mask >> e) & 1 ? x : -INFINITY;
+                    s[c][e] = __float_as_uint(x);
+                }
+            }
+            if (!MOD && by < 0.0f) {  // a negative scale turns the order around
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float x = __uint_as_float(s[c][e]);
+                        top = fmaxf(top, x == -INFINITY ? x : x * by);
+                    }
+            } else {
+                float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) t4[e & 3] = fmaxf(t4[e & 3], __uint_as_float(s[c][e]));
+                top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+                if (!MOD) top = top == -INFINITY ? top : top * by;
+            }
+            // The maximum that scales the exponentials may lag behind by a factor of 2^8: the result is the same, and the
+            // accumulator in tensor memory is rescaled only when a row has moved further than that.
+            constexpr float kLag = 8.0f;
+            const bool move = top > m + kLag || (m == -INFINITY && top > m);
+            if (__any_sync(0xffffffffu, move)) {
+                const float now = move ? top : m;
+                const float down = m == now || m == -INFINITY ? (m == now ? 1.0f : 0.0f) : tc::exp2_fast(m - now);
+                l *= down;
+                m = now;
+                if (i > 0) {
+#pragma unroll
+                    for (int c = 0; c < DP / 32; ++c) {
+                        uint32_t o[32];
+                        tc::tmem_load(o, o_at + lanes + 32 * c);
+                        tc::tmem_loaded();
+                        tc::settle(o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * down);
+                        tc::tmem_store(o_at + lanes + 32 * c, o);
+                    }
+                }
+            }
+            const float off = m == -INFINITY ? 0.0f : m;
+            float sum[4] = {};
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t w[32];
+#pragma unroll
+                for (int e = 0; e < 64; e += 2) {
+                    float x0 = __uint_as_float(s[2 * c + e / 32][e % 32]), x1 = __uint_as_float(s[2 * c + e / 32][e % 32 + 1]);
+                    if (!MOD) {
+                        const bool h0 = !clear && x0 == -INFINITY, h1 = !clear && x1 == -INFINITY;
+                        x0 = fmaf(x0, by, -off);
+                        x1 = fmaf(x1, by, -off);
+                        if (by <= 0.0f) {  // (hidden columns stay at -inf)
+                            x0 = h0 ? -INFINITY : x0;
+                            x1 = h1 ? -INFINITY : x1;
+                        }
+                    } else {
+                        x0 -= off;
+                        x1 -= off;
+                    }
+                    const float p0 = tc::exp2_fast(x0), p1 = tc::exp2_fast(x1);
+                    sum[e & 2] += p0;
+                    sum[(e & 2) + 1] += p1;
+                    w[e / 2] = tc::pack<BF16>(p0, p1);
+                }
+                tc::tmem_store(s_at + lanes + 32 * c, w);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            if (j0 < reach.all_lo || j0 + Tile::kKeys - 1 > reach.all_hi) {  // hidden from some row: no junk may reach the product
+                if (!tc::bar_wait(v_full + 8 * st, (i / Tile::kStages) & 1)) dead = 1;
+                found |= scan_tile<BF16, 128, DP, 128>(p, pos, v_tiles + st * Tile::kTile, j0, tid);
+                tc::writes_to_async();
+            }
+            tc::tmem_stored();
+            tc::fence_before();
+            tc::bar_arrive(p_full);
+        }
+        if (found) junk = 1;
+    }
+    __syncthreads();
+    if (dead) {
+        if (tid == 0) atomicAdd(&g_timeouts, 1u);
+    } else if (junk) {
+        for (int r = warp; r < 128; r += 6)
+            if (i0 + r < p.t) rows::forward_row(p, a, b, h, i0 + r, lane);
+    } else if (warp < 4) {
+        const uint32_t lanes = (uint32_t)warp << 21;
+        const bool empty = l == 0.0f;
+        const float inv = 1.0f / l;
+        if (n > 0 && !tc::bar_wait(o_done, (n - 1) & 1)) atomicAdd(&g_timeouts, 1u);
+        tc::fence_after();
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) {
+            uint32_t o[32];
+            if (n > 0) {
+                tc::tmem_load(o, o_at + lanes + 32 * c);
+                tc::tmem_loaded();
+                tc::settle(o);
+            }
+            float x[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e] = empty || n == 0 ? 0.0f : __uint_as_float(o[e]) * inv;
+            stage_columns<BF16>(q_tile + (c / 2) * (128 * 128), tid, (c % 2) * 32, x);
+        }
+        tc::writes_to_async();
+        __syncwarp();
+        if (lane == 0 && i0 + warp * 32 < p.t) {
+            for (int x = 0; x < DP; x += 64)
+                if (x < p.d) tc::tensor_store(&maps.out, x, i0 + warp * 32, h, b, tc::smem_of(q_tile) + x * 256 + warp * 32 * 128);
+            tc::stores_read();
+        }
+        if (p.lse && row < p.t)
+            p.lse[((int64_t)b * p.heads + h) * p.t + row] = empty ? -INFINITY : (m + log2f(l)) * kLn2;
+    }
+    tc::fence_before();
+    __syncthreads();
+    if (warp == 5) tc::tmem_free<256>(tmem);
+}
+
+// ---- gradients ----------------------------------------------------------------------------------------------------
+
+struct GradMaps {
+    CUtensorMap a1, a2;  // the CTA's own rows: boxes of 128 rows.  q, dout | k, v
+    CUtensorMap b1, b2;  // what streams by: boxes of 64 rows.      k, v    | q, dout
+    CUtensorMap o1, o2;  // boxes of 32 rows.                       dq, -   | dk, dv
+};
+
+template <int DP>
+struct GradTile {
+    static constexpr int kStages = 4;
+    static constexpr int kOwn = 128 * DP * 2, kStream = 64 * DP * 2;
+    static constexpr int kNeeded = 2 * kOwn + kStages * 2 * kStream + 1024;
+    static constexpr int kShared = kNeeded > 116 * 1024 ? kNeeded : 116 * 1024;  // one CTA per SM: it takes all tensor memory
+};
+
+// Both gradient kernels keep two tiles of 128 rows (A1, A2) and let pairs of tiles of 64 rows (B1, B2) stream by:
+//     S = A1 B1^T, dP = A2 B2^T,   P = exp(score(S) - lse),   dS = P (dP - delta) inner,
+//     acc1 += dS B1,               acc2 += P B2 (KEYS) or (P inner) B1 (queries)
+// KEYS: rows are keys, acc1 = dk, acc2 = dv, streamed over the query heads that share them; lse and delta belong to columns.
+// Queries: acc1 = dq; lse and delta belong to rows.  delta = sum_j P_ij dP_ij is first taken as dout . out with the rounded out
+// of the forward call; the row sum eps of P (dP - delta) over the walk is exactly what that is off by, so delta + eps goes to
+// the second kernel, and for walks of at most kExact tiles, where few keys share the error, dq is corrected by
+// -eps * sum_j P_ij inner k_j, for which acc2 is kept.
+//
+// Two warpgroups take turns at the tiles (tile n belongs to group n & 1 and its part of tensor memory), so that the products of
+// one run under the arithmetic of the other.  No product waits for arithmetic that has not begun: per pair of tiles the order is
+// acc(n), acc(n+1), S(n+2), S(n+3).
+constexpr int kExact = 1 << 20;
+
+template <bool BF16, int DP, bool MOD, bool KEYS>
+__global__ void __launch_bounds__(320, 1)
+    k30_attention_grad(const AttnParams p, const AttnTensors<typename Element<BF16>::type> a, const __grid_constant__ GradMaps maps)
+{
+    using Tile = GradTile<DP>;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t bars[1 + 2 * Tile::kStages + 6];
+    __shared__ uint32_t tmem_base;
+    __shared__ int dead, junk;
+    __shared__ ReachShared<4> reach_shared;
+    __shared__ float eps_shared[2][128];
+    __shared__ float4 column_stats[KEYS ? 8 : 1][KEYS ? 32 : 1];  // per warp: (lse, delta) of 64 columns
+
+    uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* const a1 = tiles;
+    uint8_t* const a2 = tiles + Tile::kOwn;
+    uint8_t* const stream = tiles + 2 * Tile::kOwn;  // per stage: B1, B2
+    const uint32_t bar0 = tc::smem_of(bars);
+    const uint32_t a_full = bar0, s_full = bar0 + 8, p_full = bar0 + 24, acc_done = bar0 + 40, b_full = bar0 + 56,
+                   b_free = b_full + 8 * Tile::kStages;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int own_heads = KEYS ? p.kv_heads : p.heads;
+    const int own_tiles = (p.t + 127) / 128;
+    const int64_t bh = blockIdx.x % (p.blocks * own_heads);
+    const int turn = (int)(blockIdx.x / (p.blocks * own_heads));
+    const int r0 = (KEYS ? turn : own_tiles - 1 - turn) * 128;  // the longest walks of a long sequence first
+    const int h = (int)(bh % own_heads), b = (int)(bh / own_heads);
+    const int32_t* const pos = p.pos + (int64_t)b * p.t;
+    const int group = warp >> 2, quarter = warp & 3;  // of warps 0 to 7
+    const int row = r0 + quarter * 32 + lane;
+
+    rows::Span span{kNever, -1};
+    if (warp < 8) {
+        span = span_of(p, pos, row, KEYS, lane);
+        if (group == 0) put_reach(reach_shared, quarter, lane, span);
+        if (tid == 0) dead = junk = 0;
+    } else if (warp == 8) {
+        if (lane == 0) {
+            tc::bar_init(a_full, 1);
+            for (int w = 0; w < 2; ++w) {
+                tc::bar_init(s_full + 8 * w, 1);
+                tc::bar_init(p_full + 8 * w, 128);
+                tc::bar_init(acc_done + 8 * w, 1);
+            }
+            for (int s = 0; s < 2 * Tile::kStages; ++s) tc::bar_init(b_full + 8 * s, 1);
+            tc::bar_init_done();
+        }
+    } else {
+        tc::tmem_alloc<512>(tc::smem_of(&tmem_base));
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = tmem_base, acc1_at = tmem, acc2_at = tmem + DP, pairs_at = tmem + 2 * DP;  // S, dP of group w: + 128 w, + 64
+    const Reach reach = get_reach(reach_shared);
+    const int per_head = reach.hi < 0 ? 0 : (reach.hi - reach.lo) / 64 + 1;
+    const int n = KEYS ? per_head * p.group : per_head;
+    const bool second = KEYS || n <= kExact;  // acc2 is kept
+    float eps = 0.0f;
+
+    if (warp == 8) {
+        if (lane == 0 && n > 0) {
+            bool ok = true;
+            tc::bar_expect(a_full, 2 * Tile::kOwn);
+            for (int x = 0; x < DP; x += 64) {
+                tc::tensor_load(tc::smem_of(a1) + x * 256, &maps.a1, x, r0, h, b, a_full);
+                tc::tensor_load(tc::smem_of(a2) + x * 256, &maps.a2, x, r0, h, b, a_full);
+            }
+            int issued = 0;
+            for (int i = 0; i < n; ++i, ++issued) {
+                const int s = i % Tile::kStages;
+                if (!(ok = tc::bar_wait(b_free + 8 * s, (i / Tile::kStages + 1) & 1))) break;
+                const int j0 = reach.lo + (KEYS ? i % per_head : i) * 64, hs = KEYS ? h * p.group + i / per_head : h / p.group;
+                const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream;
+                tc::bar_expect(b_full + 8 * s, 2 * Tile::kStream);
+                for (int x = 0; x < DP; x += 64) {
+                    tc::tensor_load(at + x * 128, &maps.b1, x, j0, hs, b, b_full + 8 * s);
+                    tc::tensor_load(at + Tile::kStream + x * 128, &maps.b2, x, j0, hs, b, b_full + 8 * s);
+                }
+            }
+            if (!ok) {  // copies in flight end before the CTA does
+                dead = 1;
+                tc::bar_wait(a_full, 0);
+                for (int i = max(0, issued - Tile::kStages); i < issued; ++i) tc::bar_wait(b_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
+            }
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && n > 0) {
+            bool ok = tc::bar_wait(a_full, 0);
+            auto scores = [&](int i) {
+                const int w = i & 1;
+                const uint32_t at = tc::smem_of(stream) + (i % Tile::kStages) * 2 * Tile::kStream, to = pairs_at + 128 * w;
+                // they take the place of the group's last P and dS: the products that read those have to be over
+                if (!tc::bar_wait(b_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1) ||
+                    (i > 1 && !tc::bar_wait(acc_done + 8 * w, (i / 2 - 1) & 1)))
+                    return false;
+                tc::fence_after();
+                tc::product_rows<BF16, 64, DP>(to, tc::smem_of(a1), at);
+                tc::product_rows<BF16, 64, DP>(to + 64, tc::smem_of(a2), at + Tile::kStream);
+                tc::products_arrive(s_full + 8 * w);
+                return true;
+            };
+            for (int i = 0; i < 2 && i < n && ok; ++i) ok = scores(i);
+            for (int i0 = 0; i0 < n && ok; i0 += 2) {
+                for (int i = i0; i < i0 + 2 && i < n && ok; ++i) {
+                    const int w = i & 1, s = i % Tile::kStages;
+                    const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream, from = pairs_at + 128 * w;
+                    if (!(ok = tc::bar_wait(p_full + 8 * w, (i / 2) & 1))) break;
+                    tc::fence_after();
+                    tc::product_across<BF16, 64, DP>(acc1_at, from + 64, at, i > 0);
+                    if (second) tc::product_across<BF16, 64, DP>(acc2_at, from, KEYS ? at + Tile::kStream : at, i > 0);
+                    tc::products_arrive(b_free + 8 * s);
+                    tc::products_arrive(acc_done + 8 * w);
+                }
+                for (int i = i0 + 2; i < i0 + 4 && i < n && ok; ++i) ok = scores(i);
+            }
+            if (!ok) {
+                dead = 1;
+                tc::products_arrive(a_full);  // its second phase: products in flight end before the CTA does
+                tc::bar_wait(a_full, 1);
+            }
+        }
+    } else {
+        const uint32_t lanes = (uint32_t)quarter << 21;
+        const uint32_t pair_at = pairs_at + 128 * group + lanes;
+        const int wtid = tid & 127;
+        bool found = false;
+        float lse2 = 0.0f, delta = 0.0f;
+        if (!KEYS && row < p.t) {  // this row's statistics
+            const int64_t at = ((int64_t)b * p.heads + h) * p.t + row;
+            lse2 = p.lse[at];
+            lse2 = lse2 == -INFINITY ? INFINITY : lse2 * kLog2e;
+            const uint4* o = reinterpret_cast<const uint4*>(a.out_in.at(b, row, h));
+            const uint4* g = reinterpret_cast<const uint4*>(a.dout.at(b, row, h));
+            using T2 = typename Element<BF16>::type;
+            for (int c = 0; c < p.d / 8; ++c) {
+                const uint4 x = o[c], y = g[c];
+                const T2* xe = reinterpret_cast<const T2*>(&x);
+                const T2* ye = reinterpret_cast<const T2*>(&y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) delta = fmaf(to_float(xe[e]), to_float(ye[e]), delta);
+            }
+        }
+        for (int i = group; i < n; i += 2) {
+            const int j0 = reach.lo + (KEYS ? i % per_head : i) * 64;
+            const int hq = KEYS ? h * p.group + i / per_head : h;
+            const Modifier modify(p, hq);
+            if (KEYS) {  // statistics of the 64 columns
+                const int64_t base = ((int64_t)b * p.heads + hq) * p.t;
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int c = lane + 32 * k, j = j0 + c;
+                    float2 st = make_float2(0.0f, 0.0f);
+                    if (j < p.t) {
+                        st.x = p.lse[base + j];
+                        st.x = st.x == -INFINITY ? INFINITY : st.x * kLog2e;
+                        st.y = p.delta[base + j];
+                    }
+                    reinterpret_cast<float2*>(column_stats[KEYS ? warp : 0])[c] = st;
+                }
+                __syncwarp();
+            }
+            if (!__all_sync(0xffffffffu, tc::bar_wait(s_full + 8 * group, (i / 2) & 1))) {
+                dead = 1;
+                break;
+            }
+            tc::fence_after();
+            const bool clear = __all_sync(0xffffffffu, span.lo <= j0 && span.hi >= j0 + 63);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t s[32], d[32], pw[16], dw[16];
+                tc::tmem_load(s, pair_at + 32 * c);
+                tc::tmem_load(d, pair_at + 64 + 32 * c);
+                tc::tmem_loaded();
+                tc::settle(s);
+                tc::settle(d);
+                const uint32_t mask = clear ? 0xffffffffu : column_mask(span.lo - j0 - 32 * c, span.hi - j0 - 32 * c);
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    float w[2], g[2];
+                    float4 stats;
+                    if (KEYS) stats = column_stats[KEYS ? warp : 0][KEYS ? 16 * c + e / 2 : 0];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float lse_here = KEYS ? (k ? stats.z : stats.x) : lse2, delta_here = KEYS ? (k ? stats.w : stats.y) : delta;
+                        const float x = __uint_as_float(s[e + k]), dp = __uint_as_float(d[e + k]);
+                        float inner = 1.0f, pe;
+                        if (MOD)
+                            pe = tc::exp2_fast(modify(x, (float)(row - j0 - 32 * c - e - k), inner) - lse_here);
+                        else
+                            pe = tc::exp2_fast(fmaf(x, modify.by, -lse_here));
+                        float ds = pe * (dp - delta_here);
+                        if (!clear) {
+                            const bool seen = (mask >> (e + k)) & 1;
+                            pe = seen ? pe : 0.0f;
+                            ds = seen ? ds : 0.0f;
+                            if (MOD) inner = seen ? inner : 0.0f;
+                        }
+                        if (!KEYS) eps += ds;
+                        g[k] = MOD ? ds * inner : ds;
+                        w[k] = MOD && !KEYS ? pe * inner : pe;
+                    }
+                    pw[e / 2] = tc::pack<BF16>(w[0], w[1]);
+                    dw[e / 2] = tc::pack<BF16>(g[0], g[1]);
+                }
+                if (second) tc::tmem_store16(pair_at + 16 * c, pw);
+                tc::tmem_store16(pair_at + 64 + 16 * c, dw);
+            }
+            if (j0 < reach.all_lo || j0 + 63 > reach.all_hi) {  // hidden from some row: no junk may reach the products
+                const int st = i % Tile::kStages;
+                uint8_t* const at = stream + st * 2 * Tile::kStream;
+                if (!tc::bar_wait(b_full + 8 * st, (i / Tile::kStages) & 1)) dead = 1;
+                found |= scan_tile<BF16, 64, DP, 128>(p, pos, at, j0, wtid);
+                if (KEYS) found |= scan_tile<BF16, 64, DP, 128>(p, pos, at + Tile::kStream, j0, wtid);
+                tc::writes_to_async();
+            }
+            tc::tmem_stored();
+            tc::fence_before();
+            tc::bar_arrive(p_full + 8 * group);
+        }
+        if (found) junk = 1;
+        if (!KEYS) eps_shared[group][quarter * 32 + lane] = eps;
+        if (!KEYS) eps = delta;  // kept for the end
+    }
+    __syncthreads();
+    const bool good = !dead && !junk;
+    if (dead) {
+        if (tid == 0) atomicAdd(&g_timeouts, 1u);
+    } else if (junk) {
+        for (int r = warp; r < 128; r += 10) {
+            if (r0 + r >= p.t) continue;
+            if (KEYS)
+                rows::dkv_row(p, a, b, h, r0 + r, lane);
+            else
+                rows::dq_row(p, a, b, h, r0 + r, lane);
+        }
+    } else if (warp < 8) {
+        const uint32_t lanes = (uint32_t)quarter << 21;
+        const bool empty = span.lo > span.hi;
+        if (n > 0 && !tc::bar_wait(acc_done + 8 * ((n - 1) & 1), ((n - 1) / 2) & 1)) atomicAdd(&g_timeouts, 1u);
+        tc::fence_after();
+        const int own_row = quarter * 32 + lane;
+        if (KEYS) {  // group 0: dk, group 1: dv
+#pragma unroll
+            for (int c = 0; c < DP / 32; ++c) {
+                uint32_t o[32];
+                if (n > 0) {
+                    tc::tmem_load(o, (group ? acc2_at : acc1_at) + lanes + 32 * c);
+                    tc::tmem_loaded();
+                    tc::settle(o);
+                }
+                float x[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = empty || n == 0 ? 0.0f : __uint_as_float(o[e]) * (group ? 1.0f : p.scale);
+                stage_columns<BF16>((group ? a2 : a1) + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
+            }
+        } else {  // each group half of the columns
+            const float delta = eps, off = eps_shared[0][own_row] + eps_shared[1][own_row];
+            if (group == 0 && row < p.t) p.delta[((int64_t)b * p.heads + h) * p.t + row] = empty ? 0.0f : delta + off;
+#pragma unroll
+            for (int k = 0; k < DP / 64; ++k) {
+                const int c = group * (DP / 64) + k;
+                uint32_t o[32], o2[32] = {};
+                if (n > 0) {
+                    tc::tmem_load(o, acc1_at + lanes + 32 * c);
+                    if (second) tc::tmem_load(o2, acc2_at + lanes + 32 * c);
+                    tc::tmem_loaded();
+                    tc::settle(o);
+                    tc::settle(o2);
+                }
+                float x[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    float y = __uint_as_float(o[e]);
+                    if (second) y = fmaf(-off, __uint_as_float(o2[e]), y);
+                    x[e] = empty || n == 0 ? 0.0f : y * p.scale;
+                }
+                stage_columns<BF16>(a1 + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
+            }
+        }
+        tc::writes_to_async();
+    }
+    tc::fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc::tmem_free<512>(tmem);
+    } else if (good && warp < 8 && lane == 0) {
+        // dk, dv: a warp stores the 32 rows it staged; dq: the halves of the columns, or all of them at heads of at most 64
+        const int at_row = r0 + quarter * 32;
+        for (int x = 0; x < DP; x += 64) {
+            if (x >= p.d || at_row >= p.t || (!KEYS && group != x / 64)) continue;
+            tc::tensor_store(KEYS && group ? &maps.o2 : &maps.o1, x, at_row, h, b,
+                             tc::smem_of(KEYS && group ? a2 : a1) + x * 256 + quarter * 32 * 128);
+        }
+        tc::stores_read();
+    }
+}
+
+// ---- launches -----------------------------------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return fn;
+}
+
+// The tensor [block, head, slot, element] with boxes of `box` slots by 64 elements: elements from d on read as zeros and are
+// not written, nor are slots from t on.
+template <typename P>
+bool make_map(CUtensorMap* map, const AttnParams& p, bool bf16, const Heads<P>& x, int heads, int box)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)p.d, (cuuint64_t)p.t, (cuuint64_t)heads, (cuuint64_t)p.blocks};
+    auto bytes = [](int64_t stride) { return (cuuint64_t)(stride ? stride * 2 : 16); };  // (0: a dimension of length one)
+    const cuuint64_t strides[3] = {bytes(x.slot), bytes(x.head), bytes(x.block)};
+    const cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1}, steps[4] = {1, 1, 1, 1};
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+                  const_cast<void*>(static_cast<const void*>(x.data)), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename F>
+cudaError_t with_shared(F* kernel, int bytes)
+{
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+template <bool BF16, int DP, bool MOD>
+cudaError_t forward(const AttnParams& p, const AttnTensors<typename Element<BF16>::type>& a, cudaStream_t st)
+{
+    ForwardMaps m;
+    if (!make_map(&m.q, p, BF16, a.q, p.heads, 128) || !make_map(&m.k, p, BF16, a.k, p.kv_heads, 128) ||
+        !make_map(&m.v, p, BF16, a.v, p.kv_heads, 128) || !make_map(&m.out, p, BF16, a.out, p.heads, 32))
+        return cudaErrorInvalidValue;
+    const int64_t grid = p.blocks * p.heads * ((p.t + 127) / 128);
+    if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+    auto* kernel = k29_attention<BF16, DP, MOD>;
+    static const cudaError_t set = with_shared(kernel, ForwardTile<DP>::kShared);
+    if (set != cudaSuccess) return set;
+    kernel<<<(unsigned)grid, 192, ForwardTile<DP>::kShared, st>>>(p, a, m);
     count_launches(1);
     return cudaGetLastError();
+}
+
+template <bool BF16, int DP, bool MOD, bool KEYS>
+cudaError_t gradient(const AttnParams& p, const AttnTensors<typename Element<BF16>::type>& a, cudaStream_t st)
+{
+    GradMaps m;
+    const int own = KEYS ? p.kv_heads : p.heads, other = KEYS ? p.heads : p.kv_heads;
+    bool ok = make_map(&m.a1, p, BF16, KEYS ? a.k : a.q, own, 128) && make_map(&m.a2, p, BF16, KEYS ? a.v : a.dout, own, 128) &&
+              make_map(&m.b1, p, BF16, KEYS ? a.q : a.k, other, 64) && make_map(&m.b2, p, BF16, KEYS ? a.dout : a.v, other, 64) &&
+              make_map(&m.o1, p, BF16, KEYS ? a.dk : a.dq, own, 32) && make_map(&m.o2, p, BF16, KEYS ? a.dv : a.dq, own, 32);
+    const int64_t grid = p.blocks * own * ((p.t + 127) / 128);
+    if (!ok || grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+    auto* kernel = k30_attention_grad<BF16, DP, MOD, KEYS>;
+    static const cudaError_t set = with_shared(kernel, GradTile<DP>::kShared);
+    if (set != cudaSuccess) return set;
+    kernel<<<(unsigned)grid, 320, GradTile<DP>::kShared, st>>>(p, a, m);
+    count_launches(1);
+    return cudaGetLastError();
+}
+
+template <bool BF16, int DP, bool MOD>
+cudaError_t both(const AttnParams& p, const AttnTensors<typename Element<BF16>::type>& a, cudaStream_t st)
+{
+    const cudaError_t e = gradient<BF16, DP, MOD, false>(p, a, st);
+    return e != cudaSuccess ? e : gradient<BF16, DP, MOD, true>(p, a, st);
 }
 
 }  // namespace
@@ -39,13 +872,18 @@ cudaError_t launch(const AttnParams& p, const AttnTensors<T>& a, cudaStream_t st
 template <typename T>
 cudaError_t launch_attention(const AttnParams& p, const AttnTensors<T>& a, cudaStream_t st)
 {
-    return launch<T, kForward>(p, a, st);
+    constexpr bool kBf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
+    const bool mod = p.cap > 0.0f || p.slopes;
+    if (p.d <= 64) return mod ? forward<kBf16, 64, true>(p, a, st) : forward<kBf16, 64, false>(p, a, st);
+    return mod ? forward<kBf16, 128, true>(p, a, st) : forward<kBf16, 128, false>(p, a, st);
 }
 template <typename T>
 cudaError_t launch_attention_grad(const AttnParams& p, const AttnTensors<T>& a, cudaStream_t st)
 {
-    cudaError_t e = launch<T, kDq>(p, a, st);
-    return e != cudaSuccess ? e : launch<T, kDkv>(p, a, st);
+    constexpr bool kBf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
+    const bool mod = p.cap > 0.0f || p.slopes;
+    if (p.d <= 64) return mod ? both<kBf16, 64, true>(p, a, st) : both<kBf16, 64, false>(p, a, st);
+    return mod ? both<kBf16, 128, true>(p, a, st) : both<kBf16, 128, false>(p, a, st);
 }
 #define BLOAD_INSTANTIATE(T)                                                                          \
     template cudaError_t launch_attention<T>(const AttnParams&, const AttnTensors<T>&, cudaStream_t); \
@@ -53,5 +891,15 @@ cudaError_t launch_attention_grad(const AttnParams& p, const AttnTensors<T>& a, 
 BLOAD_INSTANTIATE(__half)
 BLOAD_INSTANTIATE(__nv_bfloat16)
 #undef BLOAD_INSTANTIATE
+
+int64_t attention_timeouts()
+{
+    unsigned int v = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&v, g_timeouts, sizeof v) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return -1;
+    }
+    return (int64_t)v;
+}
 
 }  // namespace bload

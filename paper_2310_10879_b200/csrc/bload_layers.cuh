@@ -74,6 +74,8 @@ cudaError_t launch_recurrence(const RecurParams& p, const RecurTensors<T>& a, cu
 template <typename T>
 cudaError_t launch_recurrence_grad(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t st);
 
+int64_t attention_timeouts();  // see bload_device_timeouts
+
 #ifdef __CUDACC__
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }

@@ -84,7 +84,8 @@ int check_attention(const bload_attention_t* a, bool gradient)
     if (rc) return rc;
     if (a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->head_dim < 1 || a->window < 0) return BLOAD_ERR_ARG;
     if (!isfinite(a->scale) || !isfinite(a->softcap) || a->softcap < 0.0f) return BLOAD_ERR_ARG;
-    if (a->block_count * a->heads > 0x7fffffffLL) return BLOAD_ERR_ARG;
+    if (a->block_count * a->heads > 0x7fffffffLL || a->block_count * a->heads * ((a->t_block + 127) / 128) > 0x7fffffffLL)
+        return BLOAD_ERR_ARG;
     if (a->dtype == BLOAD_F32 || a->head_dim % 8 || a->head_dim > 128) return BLOAD_ERR_UNSUPPORTED;
     if (a->block_count == 0) return BLOAD_OK;
     auto tensor = [&](const bload_heads_t& x, int heads) {
@@ -254,5 +255,7 @@ int bload_recurrence_grad(const bload_recurrence_t* a, void* stream)
                 : a->dtype == BLOAD_F16 ? launch_recurrence_grad<__half>(p, recurrence_tensors<__half>(a), st)
                                         : launch_recurrence_grad<__nv_bfloat16>(p, recurrence_tensors<__nv_bfloat16>(a), st));
 }
+
+int64_t bload_device_timeouts(void) { return attention_timeouts(); }
 
 }  // extern "C"
