@@ -74,7 +74,8 @@ cudaError_t launch_recurrence(const RecurParams& p, const RecurTensors<T>& a, cu
 template <typename T>
 cudaError_t launch_recurrence_grad(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t st);
 
-int64_t attention_timeouts();  // see bload_device_timeouts
+size_t recurrence_work_bytes(int64_t blocks, int32_t t, int64_t channels);
+int64_t attention_timeouts(), recurrence_timeouts();  // see bload_device_timeouts
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float to_float(float x) { return x; }

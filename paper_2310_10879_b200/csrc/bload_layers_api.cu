@@ -150,7 +150,8 @@ int check_recurrence(const bload_recurrence_t* a, bool gradient)
     if (!a) return BLOAD_ERR_NULL;
     int rc = check_common(a->block_count, a->t_block, a->dtype, a->d_pos);
     if (rc) return rc;
-    if (a->channels < 1 || a->channels > 0x7fffffffLL || a->block_count * a->channels > ((int64_t)1 << 36)) return BLOAD_ERR_ARG;
+    if (a->channels < 1 || a->channels > 0x7fffffffLL || a->block_count * ((a->channels + 63) / 64) * ((a->t_block + 63) / 64) > 0x7fffffffLL)
+        return BLOAD_ERR_ARG;
     if (a->block_count == 0) return BLOAD_OK;
     auto tensor = [&](const bload_channels_t& x, bool zero_ok) {
         if (!x.data) return BLOAD_ERR_NULL;
@@ -230,8 +231,8 @@ int bload_attention_grad(const bload_attention_t* a, void* stream)
 
 size_t bload_recurrence_work_bytes(int64_t block_count, int32_t t_block, int64_t channels)
 {
-    (void)block_count; (void)t_block; (void)channels;
-    return 0;
+    if (block_count < 1 || t_block < 1 || t_block > BLOAD_MAX_T_BLOCK || channels < 1) return 0;
+    return recurrence_work_bytes(block_count, t_block, channels);
 }
 
 int bload_recurrence(const bload_recurrence_t* a, void* stream)
@@ -256,6 +257,10 @@ int bload_recurrence_grad(const bload_recurrence_t* a, void* stream)
                                         : launch_recurrence_grad<__nv_bfloat16>(p, recurrence_tensors<__nv_bfloat16>(a), st));
 }
 
-int64_t bload_device_timeouts(void) { return attention_timeouts(); }
+int64_t bload_device_timeouts(void) 
+{
+    const int64_t a = attention_timeouts(), r = recurrence_timeouts();
+    return a < 0 || r < 0 ? -1 : a + r;
+}
 
 }  // extern "C"
