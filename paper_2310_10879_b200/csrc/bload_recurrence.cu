@@ -1,20 +1,20 @@
 // k27_recurrence: gated linear recurrence along the slots of packed blocks, restarted at every sequence start,
 //     f = sigmoid(gate);  h = f h_prev + (1 - f) x
-// and its gradient, each in one pass over the data.  The work is bytes only: three tensors move forward, five backward.
+// and its gradient.  The work is bytes only: three tensors move forward, five backward.
 //
-// A run of 64 slots by 64 channels is a tile: 8 warps own 8 slots each, a lane 2 channels.  h_out = A h_in + H over any stretch
-// of slots, and stretches compose, so a warp reduces its slots to (A, H), the warps combine theirs through shared memory, and
-// a tile needs only the state that enters it.  That state comes from the tiles before it by looking back: a tile publishes
-// (A, H) as soon as it has them, and the state behind it as soon as it has that; its successor reads back over published (A, H)
-// to the nearest published state.  Positions tell where nothing is needed: no tile looks back that starts with a sequence
-// start or padding, none publishes whose successor does, and a tile with a start inside publishes at once.  A position p > 0
-// in slot s also says that slot s - p starts the sequence, so every look back ends.
+// A CTA owns 64 channels of a block and walks the slots in runs of 64: 8 warps take 8 slots each, a lane 2 channels.  h_out =
+// A h_in + H over any stretch of slots, and stretches compose: a warp reduces its slots to (A, H), every warp then applies those
+// of all eight to the state, which gives its own entering state and the next run's.  One barrier per run; the next runs' data
+// are under way meanwhile.
 //
-// Tiles are taken by ticket, in order of time, so those that a tile waits for were taken before it by CTAs that run or have
-// ended; within a CTA tickets are processed in order.  So the earliest unfinished tile never waits, whatever the scheduling.
+// Where there are too few such walks for the machine, the slots are cut into segments, a CTA each.  A segment that starts inside
+// a sequence needs the state of the one before it, so a segment that ends inside a sequence first reduces itself to (A, H) --
+// only from the last sequence start on, which positions tell without a search -- and publishes that, or the state itself if a
+// sequence starts inside; its successor looks back over published (A, H) to the nearest state.  Segments are taken by ticket, in
+// the order of the walk, so those that one waits for were taken by CTAs that run or have ended, whatever the scheduling.
 //
-// The gradient walks the time backwards: E = f g (0 where a sequence starts) is what a slot hands to the one before it, and
-// E_out = A E_in + E over a stretch.  It rebuilds h from the states the forward call kept at the start of each run.
+// The gradient walks backwards: E = f g (0 where a sequence starts) is what a slot hands to the one before it, and E_out =
+// A E_in + E over a stretch.  It rebuilds h from the states that the forward call kept at the start of each run.
 #include "bload_internal.cuh"
 #include "bload_layers.cuh"
 
@@ -27,17 +27,17 @@ constexpr int kWarps = 8, kRows = kRun / kWarps, kCh = 64;
 
 __device__ unsigned int g_timeouts;  // bounded waits that gave up (bload_device_timeouts)
 
-// Scratch: a ticket, then per tile (group-major within a step of time) a flag, (A, H) and the state.
+// Scratch: a ticket, then per segment (all groups of channels of the first, of the second, ...) a flag, (A, H) and the state.
 struct WorkView2 {
     unsigned int* ticket;
-    unsigned int* flags;  // 0 nothing, 1 (A, H), 2 the state behind the tile as well
-    float4* sums;         // [tiles][32]: A, H of a lane's two channels
-    float2* states;       // [tiles][32]
+    unsigned int* flags;  // 0 nothing, 1 (A, H), 2 the state behind the segment as well
+    float4* sums;         // [parts][32]: A, H of a lane's two channels
+    float2* states;       // [parts][32]
 };
-__host__ __device__ inline size_t work_view(int64_t tiles, void* base, WorkView2* v)
+__host__ __device__ inline size_t work_view(int64_t parts, void* base, WorkView2* v)
 {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    const size_t flags = 256, sums = flags + up(4 * (size_t)tiles), states = sums + 512 * (size_t)tiles;
+    const size_t flags = 256, sums = flags + up(4 * (size_t)parts), states = sums + 512 * (size_t)parts;
     if (v) {
         char* b = static_cast<char*>(base);
         v->ticket = reinterpret_cast<unsigned int*>(b);
@@ -45,18 +45,19 @@ __host__ __device__ inline size_t work_view(int64_t tiles, void* base, WorkView2
         v->sums = reinterpret_cast<float4*>(b + sums);
         v->states = reinterpret_cast<float2*>(b + states);
     }
-    return states + 256 * (size_t)tiles;
+    return states + 256 * (size_t)parts;
 }
 
-// f = sigmoid(g) and 1 - f, each with a small relative error of its own (1 - f must not cancel: it scales the input)
+// f = sigmoid(g) and 1 - f, each with a small relative error of its own (1 - f must not cancel: it scales the input).  With e =
+// exp(-g): f = 1 / (1 + e), 1 - f = e f; e is held at 2^126 (f at 2^-126) so that e f does not become inf * 0.
 __device__ __forceinline__ void gate_of(float g, float& f, float& keep)
 {
-    float e, big;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-1.4426950408889634f * fabsf(g)));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(big) : "f"(1.0f + e));
-    const float small = e * big;
-    f = g >= 0.0f ? big : small;
-    keep = g >= 0.0f ? small : big;
+    float y = -1.4426950408889634f * g, e;
+    asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(y) : "f"(y));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(y));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(1.0f + e));
+    keep = e * f;
+    f -= 1.1754943508222875e-38f;  // 2^-126: a gate held there is 0, others do not change
 }
 
 // A stretch of slots, seen as one: state -> A state + H.  Nothing passes through a stretch in which a sequence starts or that
@@ -80,16 +81,16 @@ __device__ __forceinline__ void set_flag(unsigned int* p, unsigned int v, int la
     if (lane == 0) asm volatile("st.release.gpu.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
 
-// The state that enters a tile, for this lane's two channels, by a whole warp: finds the nearest tile before it whose state
+// The state that enters a segment, for this lane's two channels, by a whole warp: finds the nearest segment before it whose state
 // is published, with (A, H) of all between published too, and applies those in the order of the walk.  That is the same chain
 // of multiply-adds wherever the state was found, so results do not depend on timing.  Gives up after four seconds, which
 // nothing but a hardware failure takes.
-__device__ float2 look_back(const WorkView2& w, int64_t tile, int64_t step, int lane)
+__device__ float2 look_back(const WorkView2& w, int64_t part, int64_t step, int lane)
 {
     uint64_t since = 0;
-    int64_t far = 1;  // how many tiles back the lanes begin to look
+    int64_t far = 1;  // how many segments back the lanes begin to look
     for (;;) {
-        const int64_t mine = tile - (far + lane) * step;
+        const int64_t mine = part - (far + lane) * step;
         const unsigned flag = mine >= 0 ? flag_of(w.flags + mine) : 0;
         const unsigned ready = __ballot_sync(0xffffffffu, flag >= 1), state = __ballot_sync(0xffffffffu, flag == 2);
         const int run = ~ready ? __ffs(~ready) - 1 : 32, stop = state ? __ffs(state) - 1 : 32;
@@ -112,11 +113,11 @@ __device__ float2 look_back(const WorkView2& w, int64_t tile, int64_t step, int 
         __nanosleep(40);
     }
     __threadfence();
-    float2 e = __ldcg(w.states + (tile - far * step) * 32 + lane);
+    float2 e = __ldcg(w.states + (part - far * step) * 32 + lane);
     for (int64_t k = far - 1; k > 0; k -= 8) {  // eight loads at a time
         float4 s[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] = k > j ? __ldcg(w.sums + (tile - (k - j) * step) * 32 + lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int j = 0; j < 8; ++j) s[j] = k > j ? __ldcg(w.sums + (part - (k - j) * step) * 32 + lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (k > j) e = make_float2(fmaf(s[j].x, e.x, s[j].y), fmaf(s[j].z, e.y, s[j].w));
@@ -151,308 +152,346 @@ struct Pair<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat162 put(float a, float b) { return __floats2bfloat162_rn(a, b); }
 };
 
-// STAGED: rows on 16-byte boundaries; tiles are copied to shared memory asynchronously, one ahead, lane l has channels 2l and
-// 2l + 1.  Otherwise elements are loaded one by one, lane l has channels l and l + 32.
-template <typename T, bool GRAD, bool STAGED>
-__global__ void __launch_bounds__(256, GRAD ? 2 : 3) k27_recurrence(const RecurParams p, const RecurTensors<T> a, int64_t tiles, int groups_per_block)
-{
-    constexpr int kTensors = GRAD ? 3 : 2;
-    constexpr int kRowBytes = kCh * sizeof(T), kTensorBytes = kRows * kRowBytes;  // of a warp
-    extern __shared__ __align__(16) uint8_t staged[];  // [2 stages][8 warps][tensors][8 rows][64]
-    __shared__ float4 sums[2][GRAD ? 2 : 1][kWarps][32];
-    __shared__ float2 entering[2][32];
-    __shared__ int64_t tickets[2];
+// One run as a warp and lane see it: 8 slots of 2 channels.
+template <bool GRAD>
+struct Run {
+    float f[kRows][2], x[kRows][2], keep[GRAD ? kRows : 1][2], dh[GRAD ? kRows : 1][2];
+    unsigned cont, valid;  // bit r: slot r continues a sequence, is a frame
+};
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int runs = (p.t + kRun - 1) / kRun;
-    const int64_t groups = p.blocks * groups_per_block;
-    WorkView2 work;
-    work_view(tiles, p.work, &work);
-    const bool by_ticket = runs > 1;
+// Brings runs to a warp, some ahead of their use.  STAGED: rows on 16-byte boundaries, copied to shared memory
+// asynchronously, lane l has channels 2l and 2l + 1.  Otherwise elements are loaded one by one into registers, a run
+// ahead, and lane l has channels l and l + 32.  TENSORS 2: gate and x, or (DH) gate and dh; 3: gate, x, dh.
+template <typename T, int TENSORS, bool DH, bool STAGED>
+struct Feed {
+    static constexpr int kRowBytes = kCh * sizeof(T), kTensorBytes = kRows * kRowBytes, kRunBytes = kWarps * TENSORS * kTensorBytes;
+    static constexpr int kStages = !STAGED ? 2 : kRunBytes <= 16384 ? 4 : kRunBytes <= 32768 ? 3 : 2;  // of up to 96 KB in all
+    static constexpr int kPieces = kRowBytes / 16, kRowsAtOnce = 32 / kPieces;
 
-    // where a tile is
-    int64_t q = 0, ch0 = 0;
-    int run = 0, s0 = 0;
-    auto place = [&](int64_t tile) {
-        const int64_t step = tile / groups, g = tile - step * groups;
-        run = (int)(GRAD ? runs - 1 - step : step);
-        q = g / groups_per_block;
-        ch0 = (g - q * groups_per_block) * kCh;
-        s0 = run * kRun;
-    };
-    // positions of the warp's rows (lanes 0 to 7), the tile's first slot (9), the slot behind the tile (10), its last (11)
-    auto positions = [&]() {
-        const int s = lane < 9 ? s0 + warp * kRows + lane : lane == 9 ? s0 : lane == 10 ? s0 + kRun : s0 + kRun - 1;
-        return s < p.t && lane < 12 ? p.pos[q * p.t + s] : -1;
-    };
-    auto copy_in = [&](int stage) {
-        uint8_t* const to = staged + (stage * kWarps + warp) * kTensors * kTensorBytes;
-        constexpr int kPieces = kRowBytes / 16;
+    const RecurTensors<T>& a;
+    const T* at[TENSORS];  // this lane's first element of the next run to fetch
+    const int32_t* pos;
+    uint8_t* ring;
+    int t, s, bytes, lane;  // s: the warp's first slot of the next run to fetch; bytes: of a row that this lane copies at once
+    int64_t left;           // channels from this lane's first one on
+    int ahead[kStages - 1]; // positions of the runs under way
+    T raw[STAGED ? 1 : TENSORS][STAGED ? 1 : kRows][2];
+
+    __device__ __forceinline__ explicit Feed(const RecurTensors<T>& tensors) : a(tensors) {}
+    __device__ __forceinline__ const Channels<const T>& tensor(int n) const { return n == 0 ? a.gate : n == 2 || DH ? a.dh : a.x; }
+    __device__ __forceinline__ void init(const RecurParams& p, int64_t q, int64_t ch0, int run, uint8_t* shared)
+    {
+        const int warp = threadIdx.x >> 5;
+        lane = threadIdx.x & 31;
+        ring = shared + warp * TENSORS * kTensorBytes;
+        t = p.t;
+        s = run * kRun + warp * kRows;
+        pos = p.pos + q * p.t;
+        const int c = STAGED ? lane % kPieces * (16 / (int)sizeof(T)) : lane, r = STAGED ? lane / kPieces : 0;
+        left = p.channels - ch0 - c;
+        bytes = left <= 0 ? 0 : left * (int64_t)sizeof(T) < 16 ? (int)left * (int)sizeof(T) : 16;
 #pragma unroll
-        for (int n = 0; n < kTensors; ++n) {
-            const Channels<const T>& x = n == 0 ? a.gate : n == 1 ? a.x : a.dh;
+        for (int n = 0; n < TENSORS; ++n) at[n] = tensor(n).data + q * tensor(n).block + (int64_t)(s + r) * tensor(n).slot + ch0 + c;
+    }
+    // begins to fetch the next run into a stage, its positions into ahead[k]; `on`: there is one
+    template <int DIR>
+    __device__ __forceinline__ void fetch(int stage, int k, bool on)
+    {
+        if (on) {
+            ahead[k] = lane < kRows && s + lane < t ? pos[s + lane] : -1;
 #pragma unroll
-            for (int k = lane; k < kRows * kPieces; k += 32) {
-                const int r = k / kPieces, piece = k % kPieces;
-                const int s = s0 + warp * kRows + r;
-                const int64_t c = ch0 + piece * (16 / (int)sizeof(T));
-                const int64_t left = s < p.t ? (p.channels - c) * (int64_t)sizeof(T) : 0;
-                const int bytes = left <= 0 ? 0 : left < 16 ? (int)left : 16;
-                copy16(to + n * kTensorBytes + r * kRowBytes + piece * 16, bytes ? x.at(q, s) + c : x.data, bytes);
+            for (int n = 0; n < TENSORS; ++n) {
+                const int64_t slot = tensor(n).slot;
+                if (STAGED) {
+                    uint8_t* const to = ring + stage * kRunBytes + n * kTensorBytes + lane * 16;
+#pragma unroll
+                    for (int j = 0; j < kRows / kRowsAtOnce; ++j) {
+                        const bool in = s + lane / kPieces + j * kRowsAtOnce < t && bytes > 0;
+                        copy16(to + j * 512, in ? at[n] + j * kRowsAtOnce * slot : tensor(n).data, in ? bytes : 0);
+                    }
+                } else {
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+                            raw[STAGED ? 0 : n][STAGED ? 0 : r][c] = s + r < t && left > 32 * c ? at[n][r * slot + 32 * c] : from_float<T>(0.0f);
+                }
+                at[n] += DIR * kRun * slot;
             }
+            s += DIR * kRun;
         }
-    };
-
-    int64_t tile, next, after = 0;
-    if (by_ticket) {
-        if (tid == 0) {
-            tickets[0] = atomicAdd(work.ticket, 1u);
-            tickets[1] = atomicAdd(work.ticket, 1u);
-        }
-        __syncthreads();
-        tile = tickets[0];
-        next = tickets[1];
-        __syncthreads();
-    } else {
-        tile = blockIdx.x;
-        next = tile + gridDim.x;
+        if (STAGED) asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    int pos_next = -1;
-    if (tile < tiles) {
-        place(tile);
-        pos_next = positions();
-        if (STAGED) copy_in(0);
+    __device__ __forceinline__ float2 get(int stage, int n, int r) const
+    {
+        if (STAGED)
+            return Pair<T>::get(reinterpret_cast<const typename Pair<T>::type*>(ring + stage * kRunBytes + n * kTensorBytes + r * kRowBytes)[lane]);
+        return make_float2(to_float(raw[STAGED ? 0 : n][STAGED ? 0 : r][0]), to_float(raw[STAGED ? 0 : n][STAGED ? 0 : r][1]));
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+};
 
-    for (int turn = 0; tile < tiles; ++turn) {
-        place(tile);
-        const int pos = pos_next;
-        const int64_t q_here = q, ch_here = ch0;
-        const int run_here = run, s_here = s0;
-        const int buffer = turn & 1;
-        if (by_ticket && tid == 0) after = atomicAdd(work.ticket, 1u);  // two tiles ahead: its latency is hidden
-        if (next < tiles) {
-            place(next);
-            pos_next = positions();
-            if (STAGED) copy_in(buffer ^ 1);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+// OUTPUT false: only reduces `count` runs from `run` on (direction of the walk) to (A, state).
+template <typename T, bool GRAD, bool STAGED, bool OUTPUT>
+__device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>& a, int64_t q, int64_t ch0, int run, int count,
+                                     uint8_t* ring, float4 (&sums)[2][GRAD ? 2 : 1][kWarps][32], float2& state, float2& A)
+{
+    constexpr int kTensors = GRAD && OUTPUT ? 3 : 2;
+    constexpr int kDir = GRAD ? -1 : 1;
+    using F = Feed<T, kTensors, GRAD && !OUTPUT, STAGED>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int runs = (p.t + kRun - 1) / kRun;
+    const int64_t c0 = ch0 + (STAGED ? 2 * lane : lane), c1 = STAGED ? c0 + 1 : c0 + 32;
+    const bool on0 = c0 < p.channels, on1 = c1 < p.channels;
 
-        const unsigned cont = __ballot_sync(0xffffffffu, pos > 0), valid = __ballot_sync(0xffffffffu, pos >= 0);
-        const int last_pos = __shfl_sync(0xffffffffu, pos, 11);
-        const bool left = run_here > 0 && (cont >> 9) & 1, right = (cont >> 10) & 1;  // a sequence crosses that edge
-        const bool closed = last_pos < kRun;                                         // one starts inside (or padding): nothing passes through
-        const bool need = GRAD ? right : left, give = GRAD ? left : right;
-        const int64_t c0 = ch_here + (STAGED ? 2 * lane : lane), c1 = STAGED ? c0 + 1 : c0 + 32;
+    F feed(a);
+    feed.init(p, q, ch0, run, ring);
+#pragma unroll
+    for (int k = 0; k < F::kStages - 1; ++k) feed.template fetch<kDir>(k, k, k < count);
 
-        float f[kRows][2], keep[GRAD ? kRows : 1][2], x[kRows][2], dh[GRAD ? kRows : 1][2];
-        float2 carry = make_float2(0.0f, 0.0f);
-        if (GRAD && left) {
-            const float* at = p.carry + (q_here * runs + run_here) * p.channels;
-            if (c0 < p.channels) carry.x = at[c0];
-            if (c1 < p.channels) carry.y = at[c1];
+    T *out0 = nullptr, *out1 = nullptr;  // this lane's first element of the warp's first slot
+    if (OUTPUT) {
+        const Channels<T>& o = GRAD ? a.dgate : a.h;
+        out0 = o.data + q * o.block + (int64_t)(run * kRun + warp * kRows) * o.slot + c0;
+        if (GRAD) out1 = a.dx.data + q * a.dx.block + (int64_t)(run * kRun + warp * kRows) * a.dx.slot + c0;
+    }
+    float* carry_at = OUTPUT && p.carry ? p.carry + (q * runs + run) * p.channels : nullptr;
+
+    int stage = 0;
+    for (int i = 0; i < count; ++i, run += kDir) {
+        const int s_warp = run * kRun + warp * kRows;
+        float2 h_in = make_float2(0.0f, 0.0f);  // (gradient) the state that entered this run forward
+        if (GRAD && OUTPUT) {
+            if (on0) h_in.x = carry_at[c0];
+            if (on1) h_in.y = carry_at[c1];
         }
         if (STAGED) {
-            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(F::kStages - 2) : "memory");
             __syncwarp();
         }
-        // gates and inputs (forward: x is (1 - f) x); zeros on padding
-        {
-            const uint8_t* const from = staged + (buffer * kWarps + warp) * kTensors * kTensorBytes;
-            float raw[kTensors][kRows][2];
+        const int pos = feed.ahead[0];
+        Run<GRAD> w;
+        w.cont = __ballot_sync(0xffffffffu, pos > 0) & ((1u << kRows) - 1);
+        w.valid = __ballot_sync(0xffffffffu, pos >= 0) & ((1u << kRows) - 1);
+        const bool whole = w.cont == (1u << kRows) - 1;  // (uniform) a stretch without a break, the usual case in long sequences
+
+        float fA[2] = {1.0f, 1.0f}, H[2] = {0.0f, 0.0f}, E[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int n = 0; n < kTensors; ++n) {
-                const Channels<const T>& src = n == 0 ? a.gate : n == 1 ? a.x : a.dh;
+        for (int r = 0; r < kRows; ++r) {
+            const float2 g = feed.get(stage, 0, r), v = feed.get(stage, 1, r);
+            const float2 d = kTensors == 3 ? feed.get(stage, kTensors - 1, r) : v;
+            const bool on = (w.cont >> r) & 1, is = (w.valid >> r) & 1;
 #pragma unroll
-                for (int r = 0; r < kRows; ++r) {
-                    if (STAGED) {
-                        const float2 v = Pair<T>::get(reinterpret_cast<const typename Pair<T>::type*>(from + n * kTensorBytes + r * kRowBytes)[lane]);
-                        raw[n][r][0] = v.x;
-                        raw[n][r][1] = v.y;
-                    } else {
-                        const int s = s_here + warp * kRows + r;
-                        const T* at = s < p.t ? src.at(q_here, s) : nullptr;
-                        raw[n][r][0] = at && c0 < p.channels ? to_float(at[c0]) : 0.0f;
-                        raw[n][r][1] = at && c1 < p.channels ? to_float(at[c1]) : 0.0f;
-                    }
+            for (int k = 0; k < 2; ++k) {
+                float f, keep;
+                gate_of(k ? g.y : g.x, f, keep);
+                float x = k ? v.y : v.x, dh = k ? d.y : d.x;
+                if (!whole && !is) f = keep = x = dh = 0.0f;
+                w.f[r][k] = f;
+                if (GRAD) {
+                    w.keep[GRAD ? r : 0][k] = keep;
+                    w.dh[GRAD ? r : 0][k] = dh;
+                    w.x[r][k] = x;
+                } else {
+                    w.x[r][k] = keep * x;
                 }
-            }
-#pragma unroll
-            for (int r = 0; r < kRows; ++r)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    float kp;
-                    gate_of(raw[0][r][k], f[r][k], kp);
-                    const bool is = (valid >> r) & 1;
-                    if (GRAD) {
-                        keep[r][k] = is ? kp : 0.0f;
-                        f[r][k] = is ? f[r][k] : 0.0f;
-                        x[r][k] = is ? raw[1][r][k] : 0.0f;
-                        dh[r][k] = is ? raw[kTensors - 1][r][k] : 0.0f;
-                    } else {
-                        x[r][k] = is ? kp * raw[1][r][k] : 0.0f;
-                    }
+                if (!GRAD || OUTPUT) {
+                    const float add = GRAD ? keep * x : w.x[r][k];
+                    H[k] = whole || on ? fmaf(f, H[k], add) : add;
                 }
-        }
-        // the warp's slots as one step, forward and (gradient) backward
-        {
-            float A[2] = {1.0f, 1.0f}, H[2] = {0.0f, 0.0f}, E[2] = {0.0f, 0.0f};
-#pragma unroll
-            for (int r = 0; r < kRows; ++r)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float add = GRAD ? keep[r][k] * x[r][k] : x[r][k];
-                    H[k] = (cont >> r) & 1 ? fmaf(f[r][k], H[k], add) : add;
-                    A[k] *= f[r][k];
-                }
-            if (~cont & ((1u << kRows) - 1)) A[0] = A[1] = kShut;
-            sums[buffer][0][warp][lane] = make_float4(A[0], H[0], A[1], H[1]);
-            if (GRAD) {
-#pragma unroll
-                for (int r = kRows - 1; r >= 0; --r)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) E[k] = (cont >> r) & 1 ? f[r][k] * (dh[r][k] + E[k]) : 0.0f;
-                sums[buffer][GRAD ? 1 : 0][warp][lane] = make_float4(A[0], E[0], A[1], E[1]);
+                fA[k] *= f;
             }
         }
-        if (by_ticket && tid == 0) tickets[buffer] = after;
+        if (!whole) fA[0] = fA[1] = kShut;
+        const int buffer = i & 1;
+        if (GRAD) {
+#pragma unroll
+            for (int r = kRows - 1; r >= 0; --r)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) E[k] = whole || (w.cont >> r) & 1 ? w.f[r][k] * (w.dh[GRAD ? r : 0][k] + E[k]) : 0.0f;
+            sums[buffer][GRAD ? 1 : 0][warp][lane] = make_float4(fA[0], E[0], fA[1], E[1]);
+        }
+        if (!GRAD || OUTPUT) sums[buffer][0][warp][lane] = make_float4(fA[0], H[0], fA[1], H[1]);
+        // the next run to fetch takes the stage of the run before this one (in registers: this one's)
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k + 1 < F::kStages - 1; ++k) feed.ahead[k] = feed.ahead[k + 1];
+        feed.template fetch<kDir>(stage == 0 ? F::kStages - 1 : stage - 1, F::kStages - 2, i + F::kStages - 1 < count);
+        stage = stage + 1 == F::kStages ? 0 : stage + 1;
         __syncthreads();
-        if (by_ticket) after = tickets[buffer];
 
-        // the stretch between the tile's edge and this warp, and (last warp of the walk) the whole tile
-        float2 in = make_float2(0.0f, 0.0f);
-        float a0 = 1.0f, a1 = 1.0f;
-        {
-            const int first = GRAD ? kWarps - 1 : 0, dir = GRAD ? -1 : 1;
-            const int steps = GRAD ? kWarps - 1 - warp : warp;
-            for (int k = 0; k < steps; ++k) {
-                const float4 s = sums[buffer][GRAD ? 1 : 0][first + dir * k][lane];
-                in.x = through(s.x, in.x, s.y);
-                in.y = through(s.z, in.y, s.w);
-                a0 = both(a0, s.x);
-                a1 = both(a1, s.z);
+        if (OUTPUT && !GRAD && carry_at && warp == 0) {
+            if (on0) carry_at[c0] = state.x;
+            if (on1) carry_at[c1] = state.y;
+        }
+        float2 in = state, mine = state;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) {
+            const int n = GRAD ? kWarps - 1 - k : k;
+            const float4 s = sums[buffer][GRAD ? 1 : 0][n][lane];
+            if (n == warp) mine = in;
+            in.x = through(s.x, in.x, s.y);
+            in.y = through(s.z, in.y, s.w);
+            if (!OUTPUT) {
+                A.x = both(A.x, s.x);
+                A.y = both(A.y, s.z);
             }
         }
-        if (warp == (GRAD ? 0 : kWarps - 1) && (need || give || (!GRAD && p.carry))) {
-            const float4 s = sums[buffer][GRAD ? 1 : 0][warp][lane];
-            const float A0 = both(a0, s.x), A1 = both(a1, s.z), H0 = through(s.x, in.x, s.y), H1 = through(s.z, in.y, s.w);
-            float2 e = make_float2(0.0f, 0.0f);
-            if (give && (!need || closed)) {
-                work.states[tile * 32 + lane] = make_float2(H0, H1);
-                set_flag(work.flags + tile, 2, lane);
-            }
-            if (need) {
-                const bool open = give && !closed;
-                if (open && !__all_sync(0xffffffffu, flag_of(work.flags + tile - groups) == 2)) {
-                    work.sums[tile * 32 + lane] = make_float4(A0, H0, A1, H1);
-                    set_flag(work.flags + tile, 1, lane);
-                }
-                e = look_back(work, tile, groups, lane);
-                if (open) {
-                    work.states[tile * 32 + lane] = make_float2(fmaf(A0, e.x, H0), fmaf(A1, e.y, H1));
-                    set_flag(work.flags + tile, 2, lane);
-                }
-                entering[buffer][lane] = e;
-            }
-            if (!GRAD && p.carry) {
-                float* at = p.carry + (q_here * runs + run_here) * p.channels;
-                if (c0 < p.channels) at[c0] = e.x;
-                if (c1 < p.channels) at[c1] = e.y;
-            }
-        }
-        if (need) {
-            __syncthreads();
-            const float2 e = entering[buffer][lane];
-            in.x = through(a0, e.x, in.x);
-            in.y = through(a1, e.y, in.y);
-        }
+        state = in;
+        if (!OUTPUT) continue;
 
-        auto put = [&](const Channels<T>& to, int r, float v0, float v1) {
-            const int s = s_here + warp * kRows + r;
-            if (s >= p.t) return;
-            T* at = to.at(q_here, s);
-            if (STAGED && c1 < p.channels) {
-                *reinterpret_cast<typename Pair<T>::type*>(at + c0) = Pair<T>::put(v0, v1);
+        auto put = [&](T* at, float v0, float v1) {
+            if (STAGED && on1) {
+                *reinterpret_cast<typename Pair<T>::type*>(at) = Pair<T>::put(v0, v1);
             } else {
-                if (c0 < p.channels) at[c0] = from_float<T>(v0);
-                if (c1 < p.channels) at[c1] = from_float<T>(v1);
+                if (on0) at[0] = from_float<T>(v0);
+                if (on1) at[STAGED ? 1 : 32] = from_float<T>(v1);
             }
         };
         if (!GRAD) {
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
-                const bool on = (cont >> r) & 1;
-                in.x = on ? fmaf(f[r][0], in.x, x[r][0]) : x[r][0];
-                in.y = on ? fmaf(f[r][1], in.y, x[r][1]) : x[r][1];
-                put(a.h, r, in.x, in.y);
+                const bool on = whole || (w.cont >> r) & 1;
+                mine.x = on ? fmaf(w.f[r][0], mine.x, w.x[r][0]) : w.x[r][0];
+                mine.y = on ? fmaf(w.f[r][1], mine.y, w.x[r][1]) : w.x[r][1];
+                if (s_warp + r < p.t) put(out0 + r * a.h.slot, mine.x, mine.y);
             }
+            out0 += kRun * a.h.slot;
+            if (carry_at) carry_at += p.channels;
         } else {
-            // h in front of every slot, less x; then g from the last slot to the first
             for (int k = 0; k < warp; ++k) {
                 const float4 s = sums[buffer][0][k][lane];
-                carry.x = through(s.x, carry.x, s.y);
-                carry.y = through(s.z, carry.y, s.w);
+                h_in.x = through(s.x, h_in.x, s.y);
+                h_in.y = through(s.z, h_in.y, s.w);
             }
-            float h[2] = {carry.x, carry.y};
+            float h[2] = {h_in.x, h_in.y};  // h in front of every slot, less x
 #pragma unroll
             for (int r = 0; r < kRows; ++r)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const float before = (cont >> r) & 1 ? h[k] : 0.0f;
-                    h[k] = fmaf(f[r][k], before, keep[r][k] * x[r][k]);
-                    x[r][k] = before - x[r][k];
+                    const float before = whole || (w.cont >> r) & 1 ? h[k] : 0.0f;
+                    h[k] = fmaf(w.f[r][k], before, w.keep[GRAD ? r : 0][k] * w.x[r][k]);
+                    w.x[r][k] = before - w.x[r][k];
                 }
-            float e[2] = {in.x, in.y};
+            float e[2] = {mine.x, mine.y};  // then g from the last slot to the first
 #pragma unroll
             for (int r = kRows - 1; r >= 0; --r) {
                 float dg[2], dx[2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const float g = (valid >> r) & 1 ? dh[r][k] + e[k] : 0.0f;
-                    dx[k] = keep[r][k] * g;
-                    dg[k] = dx[k] * f[r][k] * x[r][k];
-                    e[k] = (cont >> r) & 1 ? f[r][k] * g : 0.0f;
+                    const float g = whole || (w.valid >> r) & 1 ? w.dh[GRAD ? r : 0][k] + e[k] : 0.0f;
+                    dx[k] = w.keep[GRAD ? r : 0][k] * g;
+                    dg[k] = dx[k] * w.f[r][k] * w.x[r][k];
+                    e[k] = whole || (w.cont >> r) & 1 ? w.f[r][k] * g : 0.0f;
                 }
-                put(a.dgate, r, dg[0], dg[1]);
-                put(a.dx, r, dx[0], dx[1]);
+                if (s_warp + r < p.t) {
+                    put(out0 + r * a.dgate.slot, dg[0], dg[1]);
+                    put(out1 + r * a.dx.slot, dx[0], dx[1]);
+                }
             }
+            out0 -= kRun * a.dgate.slot;
+            out1 -= kRun * a.dx.slot;
+            carry_at -= p.channels;
         }
-        tile = next;
-        next = by_ticket ? after : next + gridDim.x;
     }
+    if (STAGED) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();  // the ring and the sums may be used again
 }
 
-int64_t tiles_of(int64_t blocks, int64_t t, int64_t channels)
+template <typename T, bool GRAD, bool STAGED>
+__global__ void __launch_bounds__(256, GRAD || !STAGED ? 2 : 3)
+    k27_recurrence(const RecurParams p, const RecurTensors<T> a, int groups_per_block, int segments)
 {
-    return blocks * ((channels + kCh - 1) / kCh) * ((t + kRun - 1) / kRun);
+    extern __shared__ __align__(16) uint8_t ring[];  // [stages][8 warps][tensors][8 rows][64]
+    __shared__ float4 sums[2][GRAD ? 2 : 1][kWarps][32];
+    __shared__ float2 entering[32];
+    __shared__ unsigned int drawn;
+
+    const int lane = threadIdx.x & 31;
+    const int runs = (p.t + kRun - 1) / kRun;
+    const int64_t groups = p.blocks * groups_per_block;
+    WorkView2 work;
+    work_view(groups * segments, p.work, &work);
+    int64_t part = blockIdx.x;
+    if (segments > 1) {
+        if (threadIdx.x == 0) drawn = atomicAdd(work.ticket, 1u);
+        __syncthreads();
+        part = drawn;
+    }
+    const int turn = (int)(part / groups);
+    const int64_t group = part - turn * groups, q = group / groups_per_block, ch0 = (group - q * groups_per_block) * kCh;
+    const int segment = GRAD ? segments - 1 - turn : turn;
+    const int first = (int)((int64_t)runs * segment / segments), end = (int)((int64_t)runs * (segment + 1) / segments);
+    float2 state = make_float2(0.0f, 0.0f), A = make_float2(1.0f, 1.0f);
+    if (segments > 1) {
+        const int32_t* const pos = p.pos + q * p.t;
+        const bool left = segment > 0 && pos[first * kRun] > 0;                  // a sequence crosses that edge
+        const bool right = segment < segments - 1 && pos[end * kRun] > 0;
+        const bool need = GRAD ? right : left, give = GRAD ? left : right;
+        bool open = false;
+        if (give) {  // the part of the segment that its successor in the walk hears of
+            int from, count;
+            if (GRAD) {
+                const int stop = min(warp_seq_end(pos, p.t, first * kRun, lane), end * kRun);
+                count = (stop - 1) / kRun - first + 1;
+                from = first + count - 1;
+                open = stop == end * kRun && need;
+            } else {
+                const int start = min(max(end * kRun - pos[end * kRun], 0), end * kRun - 1);
+                from = max(start / kRun, first);
+                count = end - from;
+                open = start < first * kRun && need;
+            }
+            walk<T, GRAD, STAGED, false>(p, a, q, ch0, from, count, ring, sums, state, A);
+        }
+        if (threadIdx.x < 32) {
+            const float2 own = state;
+            if (give && !open) {
+                work.states[part * 32 + lane] = own;
+                set_flag(work.flags + part, 2, lane);
+            } else if (give) {
+                work.sums[part * 32 + lane] = make_float4(A.x, own.x, A.y, own.y);
+                set_flag(work.flags + part, 1, lane);
+            }
+            float2 e = make_float2(0.0f, 0.0f);
+            if (need) e = look_back(work, part, groups, lane);
+            if (open) {
+                work.states[part * 32 + lane] = make_float2(through(A.x, e.x, own.x), through(A.y, e.y, own.y));
+                set_flag(work.flags + part, 2, lane);
+            }
+            entering[lane] = e;
+        }
+        __syncthreads();
+        state = entering[lane];
+    }
+    walk<T, GRAD, STAGED, true>(p, a, q, ch0, GRAD ? end - 1 : first, end - first, ring, sums, state, A);
+}
+
+int64_t groups_of(int64_t blocks, int64_t channels) { return blocks * ((channels + kCh - 1) / kCh); }
+
+// Segments per walk: as many as keep two CTAs on each of the 148 SMs busy, of at least 4 runs each.
+int segments_of(int64_t blocks, int32_t t, int64_t channels)
+{
+    const int64_t runs = (t + kRun - 1) / kRun, groups = groups_of(blocks, channels);
+    const int64_t wanted = groups >= 200 ? 1 : (2 * 148) / groups, most = runs / 4;
+    return (int)(wanted < most ? (wanted < 1 ? 1 : wanted) : (most < 1 ? 1 : most));
 }
 
 template <typename T, bool GRAD, bool STAGED>
 cudaError_t launch(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t st)
 {
-    const int64_t tiles = tiles_of(p.blocks, p.t, p.channels);
-    const int shared = STAGED ? 2 * kRun * kCh * (int)sizeof(T) * (GRAD ? 3 : 2) : 0;
+    using F = Feed<T, GRAD ? 3 : 2, false, STAGED>;
+    constexpr int kShared = STAGED ? F::kStages * F::kRunBytes : 0;
+    static_assert(!GRAD || !STAGED || kShared >= Feed<T, 2, true, STAGED>::kStages * Feed<T, 2, true, STAGED>::kRunBytes, "both walks fit");
+    const int64_t groups = groups_of(p.blocks, p.channels);
+    const int segments = segments_of(p.blocks, p.t, p.channels);
     auto* kernel = k27_recurrence<T, GRAD, STAGED>;
-    struct Fit {
-        cudaError_t error;
-        int ctas;
-    };
-    static const Fit fit = [&] {
-        Fit f{cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared), 0};
-        int device = 0, sms = 0, per = 0;
-        if (f.error == cudaSuccess) f.error = cudaGetDevice(&device);
-        if (f.error == cudaSuccess) f.error = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-        if (f.error == cudaSuccess) f.error = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, 256, shared);
-        f.ctas = sms * per;
-        return f;
-    }();
-    if (fit.error != cudaSuccess) return fit.error;
-    if (p.t > kRun) {  // ticket and flags
-        const cudaError_t e = cudaMemsetAsync(p.work, 0, 256 + 4 * (size_t)tiles, st);
+    static const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+    if (set != cudaSuccess) return set;
+    if (segments > 1) {  // ticket and flags
+        const cudaError_t e = cudaMemsetAsync(p.work, 0, 256 + 4 * (size_t)(groups * segments), st);
         if (e != cudaSuccess) return e;
     }
-    kernel<<<(unsigned)(tiles < fit.ctas ? tiles : fit.ctas), 256, shared, st>>>(p, a, tiles, (int)((p.channels + kCh - 1) / kCh));
+    kernel<<<(unsigned)(groups * segments), 256, kShared, st>>>(p, a, (int)((p.channels + kCh - 1) / kCh), segments);
     count_launches(1);
     return cudaGetLastError();
 }
@@ -467,7 +506,8 @@ bool on_16(const Channels<T>& x)
 
 size_t recurrence_work_bytes(int64_t blocks, int32_t t, int64_t channels)
 {
-    return t > kRun ? work_view(tiles_of(blocks, t, channels), nullptr, nullptr) : 0;
+    const int segments = segments_of(blocks, t, channels);
+    return segments > 1 ? work_view(groups_of(blocks, channels) * segments, nullptr, nullptr) : 0;
 }
 
 template <typename T>
