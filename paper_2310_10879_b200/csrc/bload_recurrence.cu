@@ -15,6 +15,10 @@
 //
 // The gradient walks backwards: E = f g (0 where a sequence starts) is what a slot hands to the one before it, and E_out =
 // A E_in + E over a stretch.  It rebuilds h from the states that the forward call kept at the start of each run.
+#include <math.h>
+
+#include <type_traits>
+
 #include "bload_internal.cuh"
 #include "bload_layers.cuh"
 
@@ -48,16 +52,58 @@ __host__ __device__ inline size_t work_view(int64_t parts, void* base, WorkView2
     return states + 256 * (size_t)parts;
 }
 
-// f = sigmoid(g) and 1 - f, each with a small relative error of its own (1 - f must not cancel: it scales the input).  With e =
-// exp(-g): f = 1 / (1 + e), 1 - f = e f; e is held at 2^126 (f at 2^-126) so that e f does not become inf * 0.
-__device__ __forceinline__ void gate_of(float g, float& f, float& keep)
+// Two channels in one 64-bit register: multiplies and adds of both are one instruction, which matters because the kernels
+// run close to the instruction rate, not only to the memory's.
+struct Two {
+    unsigned long long v;
+};
+__device__ __forceinline__ Two two(float a, float b)
 {
-    float y = -1.4426950408889634f * g, e;
-    asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(y) : "f"(y));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(y));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(1.0f + e));
-    keep = e * f;
-    f -= 1.1754943508222875e-38f;  // 2^-126: a gate held there is 0, others do not change
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 one(Two x)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x.v));
+    return r;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b)
+{
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b)
+{
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c)
+{
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ Two zero() { return {0ull}; }
+
+// f = sigmoid(g) and 1 - f, each with a small relative error of its own (1 - f must not cancel: it scales the input).  With e =
+// exp(-g): f = 1 / (1 + e), 1 - f = e f; g has been held at -87, so that e f does not become inf * 0, and what f is then
+// (some 2^-125.5) is taken off again.
+__device__ __forceinline__ void gate_of(Two g, Two& f, Two& keep)
+{
+    const float2 y = one(g * two(-1.4426950408889634f, -1.4426950408889634f));
+    float2 e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(y.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(y.y));
+    const float2 d = one(two(e.x, e.y) + two(1.0f, 1.0f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(d.y));
+    f = two(r.x, r.y);
+    keep = two(e.x, e.y) * f;
+    f = f + two(-1.6458115e-38f, -1.6458115e-38f);
 }
 
 // A stretch of slots, seen as one: state -> A state + H.  Nothing passes through a stretch in which a sequence starts or that
@@ -65,7 +111,19 @@ __device__ __forceinline__ void gate_of(float g, float& f, float& keep)
 constexpr float kShut = -0.0f;
 __device__ __forceinline__ bool shut(float A) { return __float_as_int(A) < 0; }
 __device__ __forceinline__ float through(float A, float state, float H) { return shut(A) ? H : fmaf(A, state, H); }
-__device__ __forceinline__ float both(float A1, float A2) { return shut(A1) || shut(A2) ? kShut : A1 * A2; }
+// a stretch of two channels: (A, A', H, H')
+struct alignas(16) Stretch {
+    float2 A, H;
+};
+__device__ __forceinline__ Two through(const Stretch& s, Two state)
+{
+    const float2 x = one(state);
+    return two(through(s.A.x, x.x, s.H.x), through(s.A.y, x.y, s.H.y));
+}
+__device__ __forceinline__ Two open_through(const Stretch& s, Two state)  // neither channel's A is -0
+{
+    return fma(two(s.A.x, s.A.y), state, two(s.H.x, s.H.y));
+}
 
 __device__ __forceinline__ unsigned int flag_of(const unsigned int* p)
 {
@@ -125,60 +183,80 @@ __device__ float2 look_back(const WorkView2& w, int64_t part, int64_t step, int 
     return e;
 }
 
-__device__ __forceinline__ void copy16(void* dst, const void* src, int bytes)
+// `bytes` of N bytes are copied, the rest are zeros
+template <int N>
+__device__ __forceinline__ void copy(void* dst, const void* src, int bytes)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes)
-                 : "memory");
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst);
+    if (N == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(src), "r"(bytes) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(src), "r"(bytes) : "memory");
 }
 
 template <typename T>
-struct Pair;  // two neighbouring elements
+struct Pair;  // two neighbouring elements; get_gate holds them at -87 (NaN stays)
 template <>
 struct Pair<float> {
     using type = float2;
-    static __device__ __forceinline__ float2 get(float2 x) { return x; }
-    static __device__ __forceinline__ float2 put(float a, float b) { return make_float2(a, b); }
+    static __device__ __forceinline__ Two get(float2 x) { return two(x.x, x.y); }
+    static __device__ __forceinline__ Two get_gate(float2 x)
+    {
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-87.0f));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-87.0f));
+        return two(x.x, x.y);
+    }
+    static __device__ __forceinline__ float2 put(float2 x) { return x; }
+    static __device__ __forceinline__ float2 join(float a, float b) { return make_float2(a, b); }
 };
 template <>
 struct Pair<__half> {
     using type = __half2;
-    static __device__ __forceinline__ float2 get(__half2 x) { return __half22float2(x); }
-    static __device__ __forceinline__ __half2 put(float a, float b) { return __floats2half2_rn(a, b); }
+    static __device__ __forceinline__ Two get(__half2 x) { return two(__low2float(x), __high2float(x)); }
+    static __device__ __forceinline__ Two get_gate(__half2 x) { return get(__hmax2_nan(x, __float2half2_rn(-87.0f))); }
+    static __device__ __forceinline__ __half2 put(float2 x) { return __floats2half2_rn(x.x, x.y); }
+    static __device__ __forceinline__ __half2 join(__half a, __half b) { return __halves2half2(a, b); }
 };
 template <>
 struct Pair<__nv_bfloat16> {
     using type = __nv_bfloat162;
-    static __device__ __forceinline__ float2 get(__nv_bfloat162 x) { return __bfloat1622float2(x); }
-    static __device__ __forceinline__ __nv_bfloat162 put(float a, float b) { return __floats2bfloat162_rn(a, b); }
+    static __device__ __forceinline__ Two get(__nv_bfloat162 x) { return two(__low2float(x), __high2float(x)); }
+    static __device__ __forceinline__ Two get_gate(__nv_bfloat162 x) { return get(__hmax2_nan(x, __float2bfloat162_rn(-87.0f))); }
+    static __device__ __forceinline__ __nv_bfloat162 put(float2 x) { return __floats2bfloat162_rn(x.x, x.y); }
+    static __device__ __forceinline__ __nv_bfloat162 join(__nv_bfloat16 a, __nv_bfloat16 b) { return __halves2bfloat162(a, b); }
 };
 
-// One run as a warp and lane see it: 8 slots of 2 channels.
-template <bool GRAD>
-struct Run {
-    float f[kRows][2], x[kRows][2], keep[GRAD ? kRows : 1][2], dh[GRAD ? kRows : 1][2];
-    unsigned cont, valid;  // bit r: slot r continues a sequence, is a frame
-};
+// Brings runs to a warp, some ahead of their use.  COPY 16 or 4: rows on boundaries of so many bytes, copied to shared memory
+// asynchronously in pieces of that size.  COPY 0 (16-bit elements in rows that start on any element): loaded one by one into
+// registers, a run ahead.  A lane has two neighbouring channels where these are one aligned word in memory, else (SPLIT)
+// channels l and l + 32, so that its loads and stores stay side by side with its neighbours'.
+// TENSORS 2: gate and x, or (DH) gate and dh; 3: gate, x, dh.
+template <typename T, int COPY>
+constexpr bool kSplit = COPY == 0 || (COPY == 4 && sizeof(T) == 4);
 
-// Brings runs to a warp, some ahead of their use.  STAGED: rows on 16-byte boundaries, copied to shared memory
-// asynchronously, lane l has channels 2l and 2l + 1.  Otherwise elements are loaded one by one into registers, a run
-// ahead, and lane l has channels l and l + 32.  TENSORS 2: gate and x, or (DH) gate and dh; 3: gate, x, dh.
-template <typename T, int TENSORS, bool DH, bool STAGED>
+template <typename T, int TENSORS, bool DH, int COPY>
 struct Feed {
+    static constexpr bool kStaged = COPY > 0;
     static constexpr int kRowBytes = kCh * sizeof(T), kTensorBytes = kRows * kRowBytes, kRunBytes = kWarps * TENSORS * kTensorBytes;
-    static constexpr int kStages = !STAGED ? 2 : kRunBytes <= 16384 ? 4 : kRunBytes <= 32768 ? 3 : 2;  // of up to 96 KB in all
-    static constexpr int kPieces = kRowBytes / 16, kRowsAtOnce = 32 / kPieces;
+    static constexpr int kStages = !kStaged ? 2 : kRunBytes <= 16384 ? 4 : kRunBytes <= 32768 ? 3 : 2;  // of up to 96 KB in all
+    static constexpr int kPieces = kStaged ? kRowBytes / COPY : 32, kCopies = kRows * kPieces / 32;  // per row; per lane and tensor
+    static constexpr int kPer = kStaged ? COPY / (int)sizeof(T) : 1;                                 // elements of a piece
 
     const RecurTensors<T>& a;
     const T* at[TENSORS];  // this lane's first element of the next run to fetch
     const int32_t* pos;
     uint8_t* ring;
-    int t, s, bytes, lane;  // s: the warp's first slot of the next run to fetch; bytes: of a row that this lane copies at once
-    int64_t left;           // channels from this lane's first one on
-    int ahead[kStages - 1]; // positions of the runs under way
-    T raw[STAGED ? 1 : TENSORS][STAGED ? 1 : kRows][2];
+    int t, s, lane;          // s: the warp's first slot of the next run to fetch
+    int left;                // channels from this lane's first one on (at most 64)
+    bool inside;             // (uniform) all 64 channels exist
+    int ahead[kStages - 1];  // positions of the runs under way
+    T raw[kStaged ? 1 : TENSORS][kStaged ? 1 : kRows][2];
 
     __device__ __forceinline__ explicit Feed(const RecurTensors<T>& tensors) : a(tensors) {}
     __device__ __forceinline__ const Channels<const T>& tensor(int n) const { return n == 0 ? a.gate : n == 2 || DH ? a.dh : a.x; }
+    // copy j of a lane: row and channels relative to its first ones
+    static __device__ __forceinline__ int row_of(int j) { return kPieces >= 32 ? j / (kPieces / 32) : j * (32 / kPieces); }
+    static __device__ __forceinline__ int column_of(int j) { return kPieces > 32 ? j % (kPieces / 32) * 32 * kPer : 0; }
     __device__ __forceinline__ void init(const RecurParams& p, int64_t q, int64_t ch0, int run, uint8_t* shared)
     {
         const int warp = threadIdx.x >> 5;
@@ -187,9 +265,9 @@ struct Feed {
         t = p.t;
         s = run * kRun + warp * kRows;
         pos = p.pos + q * p.t;
-        const int c = STAGED ? lane % kPieces * (16 / (int)sizeof(T)) : lane, r = STAGED ? lane / kPieces : 0;
-        left = p.channels - ch0 - c;
-        bytes = left <= 0 ? 0 : left * (int64_t)sizeof(T) < 16 ? (int)left * (int)sizeof(T) : 16;
+        const int c = lane % kPieces * kPer, r = lane / kPieces;
+        left = (int)min(p.channels - ch0, (int64_t)kCh) - c;
+        inside = ch0 + kCh <= p.channels;
 #pragma unroll
         for (int n = 0; n < TENSORS; ++n) at[n] = tensor(n).data + q * tensor(n).block + (int64_t)(s + r) * tensor(n).slot + ch0 + c;
     }
@@ -199,50 +277,61 @@ struct Feed {
     {
         if (on) {
             ahead[k] = lane < kRows && s + lane < t ? pos[s + lane] : -1;
+            const bool full = s + kRows <= t && inside;  // (uniform)
 #pragma unroll
             for (int n = 0; n < TENSORS; ++n) {
                 const int64_t slot = tensor(n).slot;
-                if (STAGED) {
-                    uint8_t* const to = ring + stage * kRunBytes + n * kTensorBytes + lane * 16;
+                if (kStaged) {
+                    uint8_t* const to = ring + stage * kRunBytes + n * kTensorBytes + lane * COPY;
+                    if (full) {
 #pragma unroll
-                    for (int j = 0; j < kRows / kRowsAtOnce; ++j) {
-                        const bool in = s + lane / kPieces + j * kRowsAtOnce < t && bytes > 0;
-                        copy16(to + j * 512, in ? at[n] + j * kRowsAtOnce * slot : tensor(n).data, in ? bytes : 0);
+                        for (int j = 0; j < kCopies; ++j) copy<kStaged ? COPY : 4>(to + j * 32 * COPY, at[n] + row_of(j) * slot + column_of(j), COPY);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < kCopies; ++j) {
+                            const int more = (left - column_of(j)) * (int)sizeof(T);
+                            const int bytes = s + lane / kPieces + row_of(j) >= t || more <= 0 ? 0 : min(more, COPY);
+                            copy<kStaged ? COPY : 4>(to + j * 32 * COPY, bytes ? at[n] + row_of(j) * slot + column_of(j) : tensor(n).data, bytes);
+                        }
                     }
                 } else {
 #pragma unroll
                     for (int r = 0; r < kRows; ++r)
 #pragma unroll
                         for (int c = 0; c < 2; ++c)
-                            raw[STAGED ? 0 : n][STAGED ? 0 : r][c] = s + r < t && left > 32 * c ? at[n][r * slot + 32 * c] : from_float<T>(0.0f);
+                            raw[kStaged ? 0 : n][kStaged ? 0 : r][c] = full || (left > 32 * c && s + r < t) ? at[n][r * slot + 32 * c] : from_float<T>(0.0f);
                 }
                 at[n] += DIR * kRun * slot;
             }
             s += DIR * kRun;
         }
-        if (STAGED) asm volatile("cp.async.commit_group;" ::: "memory");
+        if (kStaged) asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    __device__ __forceinline__ float2 get(int stage, int n, int r) const
+    __device__ __forceinline__ typename Pair<T>::type get(int stage, int n, int r) const
     {
-        if (STAGED)
-            return Pair<T>::get(reinterpret_cast<const typename Pair<T>::type*>(ring + stage * kRunBytes + n * kTensorBytes + r * kRowBytes)[lane]);
-        return make_float2(to_float(raw[STAGED ? 0 : n][STAGED ? 0 : r][0]), to_float(raw[STAGED ? 0 : n][STAGED ? 0 : r][1]));
+        const uint8_t* const row = ring + stage * kRunBytes + n * kTensorBytes + r * kRowBytes;
+        if (!kStaged) return Pair<T>::join(raw[kStaged ? 0 : n][kStaged ? 0 : r][0], raw[kStaged ? 0 : n][kStaged ? 0 : r][1]);
+        if (kSplit<T, COPY>) return Pair<T>::join(reinterpret_cast<const T*>(row)[lane], reinterpret_cast<const T*>(row)[lane + 32]);
+        return reinterpret_cast<const typename Pair<T>::type*>(row)[lane];
     }
 };
 
 // OUTPUT false: only reduces `count` runs from `run` on (direction of the walk) to (A, state).
-template <typename T, bool GRAD, bool STAGED, bool OUTPUT>
+template <typename T, bool GRAD, int COPY, bool OUTPUT>
 __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>& a, int64_t q, int64_t ch0, int run, int count,
-                                     uint8_t* ring, float4 (&sums)[2][GRAD ? 2 : 1][kWarps][32], float2& state, float2& A)
+                                     uint8_t* ring, Stretch (&sums)[2][GRAD ? 2 : 1][kWarps][32], Two (&entering)[2][32], Two& state, float2& A)
 {
     constexpr int kTensors = GRAD && OUTPUT ? 3 : 2;
     constexpr int kDir = GRAD ? -1 : 1;
-    using F = Feed<T, kTensors, GRAD && !OUTPUT, STAGED>;
+    constexpr bool kForward = !GRAD || OUTPUT;  // h is needed
+    using F = Feed<T, kTensors, GRAD && !OUTPUT, COPY>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int runs = (p.t + kRun - 1) / kRun;
-    const int64_t c0 = ch0 + (STAGED ? 2 * lane : lane), c1 = STAGED ? c0 + 1 : c0 + 32;
+    constexpr bool kApart = kSplit<T, COPY>;
+    const int64_t c0 = ch0 + (kApart ? lane : 2 * lane), c1 = kApart ? c0 + 32 : c0 + 1;
     const bool on0 = c0 < p.channels, on1 = c1 < p.channels;
 
+    if (warp == 0) entering[0][lane] = state;
     F feed(a);
     feed.init(p, q, ch0, run, ring);
 #pragma unroll
@@ -259,58 +348,72 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
     int stage = 0;
     for (int i = 0; i < count; ++i, run += kDir) {
         const int s_warp = run * kRun + warp * kRows;
-        float2 h_in = make_float2(0.0f, 0.0f);  // (gradient) the state that entered this run forward
-        if (GRAD && OUTPUT) {
-            if (on0) h_in.x = carry_at[c0];
-            if (on1) h_in.y = carry_at[c1];
-        }
-        if (STAGED) {
+        Two h_in = zero();  // (gradient) the state that entered this run forward
+        if (GRAD && OUTPUT) h_in = two(on0 ? carry_at[c0] : 0.0f, on1 ? carry_at[c1] : 0.0f);
+        if (COPY) {
             asm volatile("cp.async.wait_group %0;" ::"n"(F::kStages - 2) : "memory");
             __syncwarp();
         }
-        const int pos = feed.ahead[0];
-        Run<GRAD> w;
-        w.cont = __ballot_sync(0xffffffffu, pos > 0) & ((1u << kRows) - 1);
-        w.valid = __ballot_sync(0xffffffffu, pos >= 0) & ((1u << kRows) - 1);
-        const bool whole = w.cont == (1u << kRows) - 1;  // (uniform) a stretch without a break, the usual case in long sequences
+        constexpr unsigned kAll = (1u << kRows) - 1;
+        const unsigned cont = __ballot_sync(0xffffffffu, feed.ahead[0] > 0) & kAll;   // bit r: slot r continues a sequence
+        const unsigned valid = __ballot_sync(0xffffffffu, feed.ahead[0] >= 0) & kAll;  // is a frame
 
-        float fA[2] = {1.0f, 1.0f}, H[2] = {0.0f, 0.0f}, E[2] = {0.0f, 0.0f};
+        Two f[kRows], keep[kRows], x[kRows], dh[GRAD ? kRows : 1];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            const float2 g = feed.get(stage, 0, r), v = feed.get(stage, 1, r);
-            const float2 d = kTensors == 3 ? feed.get(stage, kTensors - 1, r) : v;
-            const bool on = (w.cont >> r) & 1, is = (w.valid >> r) & 1;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                float f, keep;
-                gate_of(k ? g.y : g.x, f, keep);
-                float x = k ? v.y : v.x, dh = k ? d.y : d.x;
-                if (!whole && !is) f = keep = x = dh = 0.0f;
-                w.f[r][k] = f;
-                if (GRAD) {
-                    w.keep[GRAD ? r : 0][k] = keep;
-                    w.dh[GRAD ? r : 0][k] = dh;
-                    w.x[r][k] = x;
-                } else {
-                    w.x[r][k] = keep * x;
-                }
-                if (!GRAD || OUTPUT) {
-                    const float add = GRAD ? keep * x : w.x[r][k];
-                    H[k] = whole || on ? fmaf(f, H[k], add) : add;
-                }
-                fA[k] *= f;
-            }
+            gate_of(Pair<T>::get_gate(feed.get(stage, 0, r)), f[r], keep[r]);
+            if (kForward) x[r] = Pair<T>::get(feed.get(stage, 1, r));
+            if (GRAD) dh[GRAD ? r : 0] = Pair<T>::get(feed.get(stage, kTensors - 1, r));
         }
-        if (!whole) fA[0] = fA[1] = kShut;
+        if (valid != kAll) {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+                if (!((valid >> r) & 1)) {
+                    f[r] = keep[r] = x[r] = zero();
+                    if (GRAD) dh[GRAD ? r : 0] = zero();
+                }
+        }
         const int buffer = i & 1;
-        if (GRAD) {
+        Stretch own;
+        own.A = make_float2(kShut, kShut);
+        if (cont == kAll) {
+            Two through_all = f[0];
 #pragma unroll
-            for (int r = kRows - 1; r >= 0; --r)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) E[k] = whole || (w.cont >> r) & 1 ? w.f[r][k] * (w.dh[GRAD ? r : 0][k] + E[k]) : 0.0f;
-            sums[buffer][GRAD ? 1 : 0][warp][lane] = make_float4(fA[0], E[0], fA[1], E[1]);
+            for (int r = 1; r < kRows; ++r) through_all = through_all * f[r];
+            own.A = one(through_all);
         }
-        if (!GRAD || OUTPUT) sums[buffer][0][warp][lane] = make_float4(fA[0], H[0], fA[1], H[1]);
+        if (kForward && !GRAD) {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) x[r] = keep[r] * x[r];
+        }
+        // (a warp without a break, the usual case, takes loops without tests)
+        auto reduce = [&](auto with_breaks) {
+            constexpr bool breaks = decltype(with_breaks)::value;
+            if (kForward) {
+                Two H = zero();
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    if (breaks && !((cont >> r) & 1)) H = zero();
+                    H = fma(f[r], H, GRAD ? keep[r] * x[r] : x[r]);
+                }
+                own.H = one(H);
+                sums[buffer][0][warp][lane] = own;
+            }
+            if (GRAD) {
+                Two E = zero();
+#pragma unroll
+                for (int r = kRows - 1; r >= 0; --r) {
+                    E = f[r] * (dh[GRAD ? r : 0] + E);
+                    if (breaks && !((cont >> r) & 1)) E = zero();
+                }
+                own.H = one(E);
+                sums[buffer][GRAD ? 1 : 0][warp][lane] = own;
+            }
+        };
+        if (cont == kAll)
+            reduce(std::false_type());
+        else
+            reduce(std::true_type());
         // the next run to fetch takes the stage of the run before this one (in registers: this one's)
         __syncwarp();
 #pragma unroll
@@ -320,90 +423,115 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
         __syncthreads();
 
         if (OUTPUT && !GRAD && carry_at && warp == 0) {
-            if (on0) carry_at[c0] = state.x;
-            if (on1) carry_at[c1] = state.y;
+            const float2 e = one(entering[buffer][lane]);
+            if (on0) carry_at[c0] = e.x;
+            if (on1) carry_at[c1] = e.y;
         }
-        float2 in = state, mine = state;
+        // The state that enters this warp: through the warps in front of it.  The last of them goes on to the next run's state and
+        // leaves it for all, read behind the next barrier.  A shut stretch has A = -0, so a multiply-add drops what arrives --
+        // unless that is infinite or NaN, which then shows in the end; only in that case are the stretches gone through again
+        // with a test on each.
+        const int in_front = GRAD ? kWarps - 1 - warp : warp;
+        const Two entered = entering[buffer][lane];
+        Two mine = entered;
 #pragma unroll
-        for (int k = 0; k < kWarps; ++k) {
-            const int n = GRAD ? kWarps - 1 - k : k;
-            const float4 s = sums[buffer][GRAD ? 1 : 0][n][lane];
-            if (n == warp) mine = in;
-            in.x = through(s.x, in.x, s.y);
-            in.y = through(s.z, in.y, s.w);
-            if (!OUTPUT) {
-                A.x = both(A.x, s.x);
-                A.y = both(A.y, s.z);
+        for (int k = 0; k < kWarps - 1; ++k)
+            if (k < in_front) mine = open_through(sums[buffer][GRAD ? 1 : 0][GRAD ? kWarps - 1 - k : k][lane], mine);
+        if (__any_sync(0xffffffffu, !(fabsf(one(mine).x) < INFINITY) || !(fabsf(one(mine).y) < INFINITY))) {
+            mine = entered;
+            for (int k = 0; k < in_front; ++k) mine = through(sums[buffer][GRAD ? 1 : 0][GRAD ? kWarps - 1 - k : k][lane], mine);
+        }
+        if (in_front == kWarps - 1) entering[buffer ^ 1][lane] = through(sums[buffer][GRAD ? 1 : 0][warp][lane], mine);
+        if (!OUTPUT) {
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) {
+                const Stretch s = sums[buffer][GRAD ? 1 : 0][k][lane];
+                A = make_float2(shut(A.x) || shut(s.A.x) ? kShut : A.x * s.A.x, shut(A.y) || shut(s.A.y) ? kShut : A.y * s.A.y);
             }
         }
-        state = in;
         if (!OUTPUT) continue;
 
-        auto put = [&](T* at, float v0, float v1) {
-            if (STAGED && on1) {
-                *reinterpret_cast<typename Pair<T>::type*>(at) = Pair<T>::put(v0, v1);
+        const bool full = s_warp + kRows <= p.t;  // (uniform)
+        auto put = [&](T* at, Two v) {
+            if (!kApart && on1) {
+                *reinterpret_cast<typename Pair<T>::type*>(at) = Pair<T>::put(one(v));
             } else {
-                if (on0) at[0] = from_float<T>(v0);
-                if (on1) at[STAGED ? 1 : 32] = from_float<T>(v1);
+                if (on0) at[0] = from_float<T>(one(v).x);
+                if (on1) at[kApart ? 32 : 1] = from_float<T>(one(v).y);
             }
         };
-        if (!GRAD) {
+        auto finish = [&](auto with_breaks, auto with_edges) {
+            constexpr bool breaks = decltype(with_breaks)::value, edges = decltype(with_edges)::value;
+            auto store = [&](T* at, int r, Two v) {
+                if (!edges && !kApart) {
+                    *reinterpret_cast<typename Pair<T>::type*>(at) = Pair<T>::put(one(v));
+                } else if (!edges) {
+                    at[0] = from_float<T>(one(v).x);
+                    at[32] = from_float<T>(one(v).y);
+                } else if (full || s_warp + r < p.t) {
+                    put(at, v);
+                }
+            };
+            if (!GRAD) {
+                T* at = out0;
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                const bool on = whole || (w.cont >> r) & 1;
-                mine.x = on ? fmaf(w.f[r][0], mine.x, w.x[r][0]) : w.x[r][0];
-                mine.y = on ? fmaf(w.f[r][1], mine.y, w.x[r][1]) : w.x[r][1];
-                if (s_warp + r < p.t) put(out0 + r * a.h.slot, mine.x, mine.y);
+                for (int r = 0; r < kRows; ++r, at += a.h.slot) {
+                    if (breaks && !((cont >> r) & 1)) mine = zero();
+                    mine = fma(f[r], mine, x[r]);
+                    store(at, r, mine);
+                }
+            } else {
+                const Two minus = two(-1.0f, -1.0f);
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {  // h in front of every slot, less x
+                    if (breaks && !((cont >> r) & 1)) h_in = zero();
+                    const Two before = h_in;
+                    h_in = fma(f[r], before, keep[r] * x[r]);
+                    x[r] = fma(x[r], minus, before);
+                }
+                T *at0 = out0 + (kRows - 1) * a.dgate.slot, *at1 = out1 + (kRows - 1) * a.dx.slot;
+#pragma unroll
+                for (int r = kRows - 1; r >= 0; --r, at0 -= a.dgate.slot, at1 -= a.dx.slot) {  // then g, from the last slot to the first
+                    if (breaks && !((valid >> r) & 1)) mine = zero();
+                    const Two g = dh[GRAD ? r : 0] + mine, dx = keep[r] * g;
+                    mine = f[r] * g;
+                    if (breaks && !((cont >> r) & 1)) mine = zero();
+                    store(at0, r, dx * f[r] * x[r]);
+                    store(at1, r, dx);
+                }
             }
+        };
+        if (GRAD)
+            for (int k = 0; k < warp; ++k) h_in = through(sums[buffer][0][k][lane], h_in);
+        if (!(full && feed.inside))
+            finish(std::true_type(), std::true_type());
+        else if (cont == kAll)
+            finish(std::false_type(), std::false_type());
+        else
+            finish(std::true_type(), std::false_type());
+        if (!GRAD) {
             out0 += kRun * a.h.slot;
             if (carry_at) carry_at += p.channels;
         } else {
-            for (int k = 0; k < warp; ++k) {
-                const float4 s = sums[buffer][0][k][lane];
-                h_in.x = through(s.x, h_in.x, s.y);
-                h_in.y = through(s.z, h_in.y, s.w);
-            }
-            float h[2] = {h_in.x, h_in.y};  // h in front of every slot, less x
-#pragma unroll
-            for (int r = 0; r < kRows; ++r)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float before = whole || (w.cont >> r) & 1 ? h[k] : 0.0f;
-                    h[k] = fmaf(w.f[r][k], before, w.keep[GRAD ? r : 0][k] * w.x[r][k]);
-                    w.x[r][k] = before - w.x[r][k];
-                }
-            float e[2] = {mine.x, mine.y};  // then g from the last slot to the first
-#pragma unroll
-            for (int r = kRows - 1; r >= 0; --r) {
-                float dg[2], dx[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float g = whole || (w.valid >> r) & 1 ? w.dh[GRAD ? r : 0][k] + e[k] : 0.0f;
-                    dx[k] = w.keep[GRAD ? r : 0][k] * g;
-                    dg[k] = dx[k] * w.f[r][k] * w.x[r][k];
-                    e[k] = whole || (w.cont >> r) & 1 ? w.f[r][k] * g : 0.0f;
-                }
-                if (s_warp + r < p.t) {
-                    put(out0 + r * a.dgate.slot, dg[0], dg[1]);
-                    put(out1 + r * a.dx.slot, dx[0], dx[1]);
-                }
-            }
             out0 -= kRun * a.dgate.slot;
             out1 -= kRun * a.dx.slot;
             carry_at -= p.channels;
         }
     }
-    if (STAGED) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (COPY) asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();  // the ring and the sums may be used again
+    state = entering[count & 1][lane];
+    __syncthreads();
 }
 
-template <typename T, bool GRAD, bool STAGED>
-__global__ void __launch_bounds__(256, GRAD || !STAGED ? 2 : 3)
+template <typename T, bool GRAD, int COPY>
+__global__ void __launch_bounds__(256, 2)
     k27_recurrence(const RecurParams p, const RecurTensors<T> a, int groups_per_block, int segments)
 {
     extern __shared__ __align__(16) uint8_t ring[];  // [stages][8 warps][tensors][8 rows][64]
-    __shared__ float4 sums[2][GRAD ? 2 : 1][kWarps][32];
-    __shared__ float2 entering[32];
+    __shared__ Stretch sums[2][GRAD ? 2 : 1][kWarps][32];
+    __shared__ Two entering[2][32];
+    __shared__ float2 from_before[32];
     __shared__ unsigned int drawn;
 
     const int lane = threadIdx.x & 31;
@@ -421,7 +549,8 @@ __global__ void __launch_bounds__(256, GRAD || !STAGED ? 2 : 3)
     const int64_t group = part - turn * groups, q = group / groups_per_block, ch0 = (group - q * groups_per_block) * kCh;
     const int segment = GRAD ? segments - 1 - turn : turn;
     const int first = (int)((int64_t)runs * segment / segments), end = (int)((int64_t)runs * (segment + 1) / segments);
-    float2 state = make_float2(0.0f, 0.0f), A = make_float2(1.0f, 1.0f);
+    Two state = zero();
+    float2 A = make_float2(1.0f, 1.0f);
     if (segments > 1) {
         const int32_t* const pos = p.pos + q * p.t;
         const bool left = segment > 0 && pos[first * kRun] > 0;                  // a sequence crosses that edge
@@ -441,10 +570,10 @@ __global__ void __launch_bounds__(256, GRAD || !STAGED ? 2 : 3)
                 count = end - from;
                 open = start < first * kRun && need;
             }
-            walk<T, GRAD, STAGED, false>(p, a, q, ch0, from, count, ring, sums, state, A);
+            walk<T, GRAD, COPY, false>(p, a, q, ch0, from, count, ring, sums, entering, state, A);
         }
         if (threadIdx.x < 32) {
-            const float2 own = state;
+            const float2 own = one(state);
             if (give && !open) {
                 work.states[part * 32 + lane] = own;
                 set_flag(work.flags + part, 2, lane);
@@ -458,12 +587,12 @@ __global__ void __launch_bounds__(256, GRAD || !STAGED ? 2 : 3)
                 work.states[part * 32 + lane] = make_float2(through(A.x, e.x, own.x), through(A.y, e.y, own.y));
                 set_flag(work.flags + part, 2, lane);
             }
-            entering[lane] = e;
+            from_before[lane] = e;
         }
         __syncthreads();
-        state = entering[lane];
+        state = two(from_before[lane].x, from_before[lane].y);
     }
-    walk<T, GRAD, STAGED, true>(p, a, q, ch0, GRAD ? end - 1 : first, end - first, ring, sums, state, A);
+    walk<T, GRAD, COPY, true>(p, a, q, ch0, GRAD ? end - 1 : first, end - first, ring, sums, entering, state, A);
 }
 
 int64_t groups_of(int64_t blocks, int64_t channels) { return blocks * ((channels + kCh - 1) / kCh); }
@@ -476,15 +605,15 @@ int segments_of(int64_t blocks, int32_t t, int64_t channels)
     return (int)(wanted < most ? (wanted < 1 ? 1 : wanted) : (most < 1 ? 1 : most));
 }
 
-template <typename T, bool GRAD, bool STAGED>
+template <typename T, bool GRAD, int COPY>
 cudaError_t launch(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t st)
 {
-    using F = Feed<T, GRAD ? 3 : 2, false, STAGED>;
-    constexpr int kShared = STAGED ? F::kStages * F::kRunBytes : 0;
-    static_assert(!GRAD || !STAGED || kShared >= Feed<T, 2, true, STAGED>::kStages * Feed<T, 2, true, STAGED>::kRunBytes, "both walks fit");
+    using F = Feed<T, GRAD ? 3 : 2, false, COPY>;
+    constexpr int kShared = COPY ? F::kStages * F::kRunBytes : 0;
+    static_assert(!GRAD || !COPY || kShared >= Feed<T, 2, true, COPY>::kStages * Feed<T, 2, true, COPY>::kRunBytes, "both walks fit");
     const int64_t groups = groups_of(p.blocks, p.channels);
     const int segments = segments_of(p.blocks, p.t, p.channels);
-    auto* kernel = k27_recurrence<T, GRAD, STAGED>;
+    auto* kernel = k27_recurrence<T, GRAD, COPY>;
     static const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
     if (set != cudaSuccess) return set;
     if (segments > 1) {  // ticket and flags
@@ -496,10 +625,22 @@ cudaError_t launch(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t 
     return cudaGetLastError();
 }
 
+// rows start on boundaries of n bytes
 template <typename T>
-bool on_16(const Channels<T>& x)
+bool on(const Channels<T>& x, int n)
 {
-    return reinterpret_cast<uintptr_t>(x.data) % 16 == 0 && x.block * sizeof(T) % 16 == 0 && x.slot * sizeof(T) % 16 == 0;
+    return reinterpret_cast<uintptr_t>(x.data) % n == 0 && x.block * sizeof(T) % n == 0 && x.slot * sizeof(T) % n == 0;
+}
+template <typename T, bool GRAD>
+cudaError_t launch_on(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t st)
+{
+    auto all = [&](int n) {
+        return on(a.gate, n) && on(a.x, n) && (GRAD ? on(a.dh, n) && on(a.dgate, n) && on(a.dx, n) : on(a.h, n));
+    };
+    if (all(16)) return launch<T, GRAD, 16>(p, a, st);
+    if (all(4)) return launch<T, GRAD, 4>(p, a, st);
+    if constexpr (sizeof(T) == 2) return launch<T, GRAD, 0>(p, a, st);
+    return cudaErrorInvalidValue;  // (32-bit elements are 4-byte aligned)
 }
 
 }  // namespace
@@ -513,13 +654,12 @@ size_t recurrence_work_bytes(int64_t blocks, int32_t t, int64_t channels)
 template <typename T>
 cudaError_t launch_recurrence(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t st)
 {
-    return on_16(a.gate) && on_16(a.x) && on_16(a.h) ? launch<T, false, true>(p, a, st) : launch<T, false, false>(p, a, st);
+    return launch_on<T, false>(p, a, st);
 }
 template <typename T>
 cudaError_t launch_recurrence_grad(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t st)
 {
-    return on_16(a.gate) && on_16(a.x) && on_16(a.dh) && on_16(a.dgate) && on_16(a.dx) ? launch<T, true, true>(p, a, st)
-                                                                                  : launch<T, true, false>(p, a, st);
+    return launch_on<T, true>(p, a, st);
 }
 #define BLOAD_INSTANTIATE(T)                                                                            \
     template cudaError_t launch_recurrence<T>(const RecurParams&, const RecurTensors<T>&, cudaStream_t); \
