@@ -133,6 +133,9 @@ struct Modifier {
     }
 };
 
+// -lse in units of log2; a row without any weight keeps none
+__device__ __forceinline__ float minus_lse(float lse) { return lse == -INFINITY ? -INFINITY : -lse * kLog2e; }
+
 // Scans a tile [ROWS][DP] in shared memory with THREADS threads for infinities and NaN.  Those on padding (or behind the
 // block's last slot, where copies fill in zeros anyway) are cleared; true if a frame holds one.
 template <bool BF16, int ROWS, int DP, int THREADS>
@@ -321,46 +324,40 @@ __global__ void __launch_bounds__(192, 2)
             tc::tmem_loaded();
 #pragma unroll
             for (int c = 0; c < 4; ++c) tc::settle(s[c]);
+            // The scores in units of log2 are x by (MOD: x itself); hidden ones are -inf.
             const bool clear = __all_sync(0xffffffffu, span.lo <= j0 && span.hi >= j0 + Tile::kKeys - 1);
-            float top = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint32_t mask = clear ? 0xffffffffu : column_mask(span.lo - j0 - 32 * c, span.hi - j0 - 32 * c);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    float x = __uint_as_float(s[c][e]);
-                    if (MOD) {
-                        float inner;
-                        x = modify(x, (float)(row - j0 - 32 * c - e), inner);
-                    }
-                    if (!clear) x = (mask >> e) & 1 ? x : -INFINITY;
-                    s[c][e] = __float_as_uint(x);
-                }
-            }
-            if (!MOD && by < 0.0f) {  // a negative scale turns the order around
+            if (MOD) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const float x = __uint_as_float(s[c][e]);
-                        top = fmaxf(top, x == -INFINITY ? x : x * by);
+                        float inner;
+                        s[c][e] = __float_as_uint(modify(__uint_as_float(s[c][e]), (float)(row - j0 - 32 * c - e), inner));
                     }
-            } else {
-                float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) t4[e & 3] = fmaxf(t4[e & 3], __uint_as_float(s[c][e]));
-                top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
-                if (!MOD) top = top == -INFINITY ? top : top * by;
             }
+            if (!clear) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t mask = column_mask(span.lo - j0 - 32 * c, span.hi - j0 - 32 * c);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) s[c][e] = (mask >> e) & 1 ? s[c][e] : 0xff800000u;
+                }
+            }
+            float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 32; e += 2)
+                    t4[(e / 2) & 3] = fmaxf(t4[(e / 2) & 3], fmaxf(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1])));
+            float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+            if (!MOD) top *= by;
             // The maximum that scales the exponentials may lag behind by a factor of 2^8: the result is the same, and the
             // accumulator in tensor memory is rescaled only when a row has moved further than that.
             constexpr float kLag = 8.0f;
             const bool move = top > m + kLag || (m == -INFINITY && top > m);
             if (__any_sync(0xffffffffu, move)) {
                 const float now = move ? top : m;
-                const float down = m == now || m == -INFINITY ? (m == now ? 1.0f : 0.0f) : tc::exp2_fast(m - now);
+                const float down = m == now ? 1.0f : m == -INFINITY ? 0.0f : tc::exp2_fast(m - now);
                 l *= down;
                 m = now;
                 if (i > 0) {
@@ -376,34 +373,24 @@ __global__ void __launch_bounds__(192, 2)
                     }
                 }
             }
-            const float off = m == -INFINITY ? 0.0f : m;
-            float sum[4] = {};
+            const float off = m == -INFINITY ? 0.0f : -m;
+            const Two by2 = two(by, by), off2 = two(off, off);
+            Two sum[2] = {zero(), zero()};
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t w[32];
+            for (int c = 0; c < 4; ++c) {
+                uint32_t w[16];
 #pragma unroll
-                for (int e = 0; e < 64; e += 2) {
-                    float x0 = __uint_as_float(s[2 * c + e / 32][e % 32]), x1 = __uint_as_float(s[2 * c + e / 32][e % 32 + 1]);
-                    if (!MOD) {
-                        const bool h0 = !clear && x0 == -INFINITY, h1 = !clear && x1 == -INFINITY;
-                        x0 = fmaf(x0, by, -off);
-                        x1 = fmaf(x1, by, -off);
-                        if (by <= 0.0f) {  // (hidden columns stay at -inf)
-                            x0 = h0 ? -INFINITY : x0;
-                            x1 = h1 ? -INFINITY : x1;
-                        }
-                    } else {
-                        x0 -= off;
-                        x1 -= off;
-                    }
-                    const float p0 = tc::exp2_fast(x0), p1 = tc::exp2_fast(x1);
-                    sum[e & 2] += p0;
-                    sum[(e & 2) + 1] += p1;
+                for (int e = 0; e < 32; e += 2) {
+                    const Two raw = two(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1]));
+                    const float2 x = one(MOD ? raw + off2 : fma(raw, by2, off2));
+                    const float p0 = tc::exp2_fast(x.x), p1 = tc::exp2_fast(x.y);
+                    sum[(e / 2) & 1] = sum[(e / 2) & 1] + two(p0, p1);
                     w[e / 2] = tc::pack<BF16>(p0, p1);
                 }
-                tc::tmem_store(s_at + lanes + 32 * c, w);
+                tc::tmem_store16(s_at + lanes + 16 * c, w);
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            const float2 sums = one(sum[0] + sum[1]);
+            l += sums.x + sums.y;
             if (j0 < reach.all_lo || j0 + Tile::kKeys - 1 > reach.all_hi) {  // hidden from some row: no junk may reach the product
                 if (!tc::bar_wait(v_full + 8 * st, (i / Tile::kStages) & 1)) dead = 1;
                 found |= scan_tile<BF16, 128, DP, 128>(p, pos, v_tiles + st * Tile::kTile, j0, tid);
@@ -496,7 +483,7 @@ __global__ void __launch_bounds__(320, 1)
     __shared__ int dead, junk;
     __shared__ ReachShared<4> reach_shared;
     __shared__ float eps_shared[2][128];
-    __shared__ float4 column_stats[KEYS ? 8 : 1][KEYS ? 32 : 1];  // per warp: (lse, delta) of 64 columns
+    __shared__ float4 column_stats[KEYS ? 8 : 1][KEYS ? 32 : 1];  // per warp: -lse (log2 units) and -delta of 32 pairs of columns
 
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* const a1 = tiles;
@@ -613,11 +600,12 @@ __global__ void __launch_bounds__(320, 1)
         const uint32_t pair_at = pairs_at + 128 * group + lanes;
         const int wtid = tid & 127;
         bool found = false;
-        float lse2 = 0.0f, delta = 0.0f;
+        float delta = 0.0f;
+        Two lse2 = zero(), delta2, eps2 = zero();  // of this row, negative
         if (!KEYS && row < p.t) {  // this row's statistics
             const int64_t at = ((int64_t)b * p.heads + h) * p.t + row;
-            lse2 = p.lse[at];
-            lse2 = lse2 == -INFINITY ? INFINITY : lse2 * kLog2e;
+            const float lse = minus_lse(p.lse[at]);
+            lse2 = two(lse, lse);
             const uint4* o = reinterpret_cast<const uint4*>(a.out_in.at(b, row, h));
             const uint4* g = reinterpret_cast<const uint4*>(a.dout.at(b, row, h));
             using T2 = typename Element<BF16>::type;
@@ -629,6 +617,7 @@ __global__ void __launch_bounds__(320, 1)
                 for (int e = 0; e < 8; ++e) delta = fmaf(to_float(xe[e]), to_float(ye[e]), delta);
             }
         }
+        delta2 = two(-delta, -delta);
         for (int i = group; i < n; i += 2) {
             const int j0 = reach.lo + (KEYS ? i % per_head : i) * 64;
             const int hq = KEYS ? h * p.group + i / per_head : h;
@@ -639,13 +628,9 @@ __global__ void __launch_bounds__(320, 1)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int c = lane + 32 * k, j = j0 + c;
-                    float2 st = make_float2(0.0f, 0.0f);
-                    if (j < p.t) {
-                        st.x = p.lse[base + j];
-                        st.x = st.x == -INFINITY ? INFINITY : st.x * kLog2e;
-                        st.y = p.delta[base + j];
-                    }
-                    reinterpret_cast<float2*>(column_stats[KEYS ? warp : 0])[c] = st;
+                    float* const st = reinterpret_cast<float*>(&column_stats[KEYS ? warp : 0][KEYS ? c / 2 : 0]) + (c & 1);
+                    st[0] = j < p.t ? minus_lse(p.lse[base + j]) : 0.0f;
+                    st[2] = j < p.t ? -p.delta[base + j] : 0.0f;
                 }
                 __syncwarp();
             }
@@ -655,6 +640,7 @@ __global__ void __launch_bounds__(320, 1)
             }
             tc::fence_after();
             const bool clear = __all_sync(0xffffffffu, span.lo <= j0 && span.hi >= j0 + 63);
+            const Two by2 = two(modify.by, modify.by);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 uint32_t s[32], d[32], pw[16], dw[16];
@@ -663,35 +649,47 @@ __global__ void __launch_bounds__(320, 1)
                 tc::tmem_loaded();
                 tc::settle(s);
                 tc::settle(d);
-                const uint32_t mask = clear ? 0xffffffffu : column_mask(span.lo - j0 - 32 * c, span.hi - j0 - 32 * c);
+                auto tile = [&](auto masked) {
+                    constexpr bool kMasked = decltype(masked)::value;
+                    const uint32_t mask = kMasked ? column_mask(span.lo - j0 - 32 * c, span.hi - j0 - 32 * c) : 0xffffffffu;
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    float w[2], g[2];
-                    float4 stats;
-                    if (KEYS) stats = column_stats[KEYS ? warp : 0][KEYS ? 16 * c + e / 2 : 0];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const float lse_here = KEYS ? (k ? stats.z : stats.x) : lse2, delta_here = KEYS ? (k ? stats.w : stats.y) : delta;
-                        const float x = __uint_as_float(s[e + k]), dp = __uint_as_float(d[e + k]);
-                        float inner = 1.0f, pe;
-                        if (MOD)
-                            pe = tc::exp2_fast(modify(x, (float)(row - j0 - 32 * c - e - k), inner) - lse_here);
-                        else
-                            pe = tc::exp2_fast(fmaf(x, modify.by, -lse_here));
-                        float ds = pe * (dp - delta_here);
-                        if (!clear) {
-                            const bool seen = (mask >> (e + k)) & 1;
-                            pe = seen ? pe : 0.0f;
-                            ds = seen ? ds : 0.0f;
-                            if (MOD) inner = seen ? inner : 0.0f;
+                    for (int e = 0; e < 32; e += 2) {
+                        Two lse_here = lse2, delta_here = delta2;
+                        if (KEYS) {
+                            const float4 stats = column_stats[KEYS ? warp : 0][KEYS ? 16 * c + e / 2 : 0];
+                            lse_here = two(stats.x, stats.y);
+                            delta_here = two(stats.z, stats.w);
                         }
-                        if (!KEYS) eps += ds;
-                        g[k] = MOD ? ds * inner : ds;
-                        w[k] = MOD && !KEYS ? pe * inner : pe;
+                        const Two raw = two(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+                        float2 x, inner = make_float2(1.0f, 1.0f);
+                        if (MOD) {
+                            x.x = modify(one(raw).x, (float)(row - j0 - 32 * c - e), inner.x);
+                            x.y = modify(one(raw).y, (float)(row - j0 - 32 * c - e - 1), inner.y);
+                            x = one(two(x.x, x.y) + lse_here);
+                        } else {
+                            x = one(fma(raw, by2, lse_here));
+                        }
+                        Two w = two(tc::exp2_fast(x.x), tc::exp2_fast(x.y));
+                        Two g = w * (two(__uint_as_float(d[e]), __uint_as_float(d[e + 1])) + delta_here);
+                        if (kMasked) {
+                            const bool s0 = (mask >> e) & 1, s1 = (mask >> (e + 1)) & 1;
+                            w = two(s0 ? one(w).x : 0.0f, s1 ? one(w).y : 0.0f);
+                            g = two(s0 ? one(g).x : 0.0f, s1 ? one(g).y : 0.0f);
+                            if (MOD) inner = make_float2(s0 ? inner.x : 0.0f, s1 ? inner.y : 0.0f);
+                        }
+                        if (!KEYS) eps2 = eps2 + g;
+                        if (MOD) {
+                            g = g * two(inner.x, inner.y);
+                            if (!KEYS) w = w * two(inner.x, inner.y);
+                        }
+                        pw[e / 2] = tc::pack<BF16>(one(w).x, one(w).y);
+                        dw[e / 2] = tc::pack<BF16>(one(g).x, one(g).y);
                     }
-                    pw[e / 2] = tc::pack<BF16>(w[0], w[1]);
-                    dw[e / 2] = tc::pack<BF16>(g[0], g[1]);
-                }
+                };
+                if (clear)
+                    tile(std::false_type());
+                else
+                    tile(std::true_type());
                 if (second) tc::tmem_store16(pair_at + 16 * c, pw);
                 tc::tmem_store16(pair_at + 64 + 16 * c, dw);
             }
@@ -708,7 +706,7 @@ __global__ void __launch_bounds__(320, 1)
             tc::bar_arrive(p_full + 8 * group);
         }
         if (found) junk = 1;
-        if (!KEYS) eps_shared[group][quarter * 32 + lane] = eps;
+        if (!KEYS) eps_shared[group][quarter * 32 + lane] = one(eps2).x + one(eps2).y;
         if (!KEYS) eps = delta;  // kept for the end
     }
     __syncthreads();
@@ -873,7 +871,7 @@ template <typename T>
 cudaError_t launch_attention(const AttnParams& p, const AttnTensors<T>& a, cudaStream_t st)
 {
     constexpr bool kBf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
-    const bool mod = p.cap > 0.0f || p.slopes;
+    const bool mod = p.cap > 0.0f || p.slopes || p.scale <= 0.0f;  // (without, the largest product has the largest score)
     if (p.d <= 64) return mod ? forward<kBf16, 64, true>(p, a, st) : forward<kBf16, 64, false>(p, a, st);
     return mod ? forward<kBf16, 128, true>(p, a, st) : forward<kBf16, 128, false>(p, a, st);
 }
@@ -881,7 +879,7 @@ template <typename T>
 cudaError_t launch_attention_grad(const AttnParams& p, const AttnTensors<T>& a, cudaStream_t st)
 {
     constexpr bool kBf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
-    const bool mod = p.cap > 0.0f || p.slopes;
+    const bool mod = p.cap > 0.0f || p.slopes || p.scale <= 0.0f;  // (without, the largest product has the largest score)
     if (p.d <= 64) return mod ? both<kBf16, 64, true>(p, a, st) : both<kBf16, 64, false>(p, a, st);
     return mod ? both<kBf16, 128, true>(p, a, st) : both<kBf16, 128, false>(p, a, st);
 }

@@ -90,6 +90,43 @@ __device__ __forceinline__ __half from_float<__half>(float x) { return __float2h
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
+// Two numbers in one 64-bit register: multiplies and adds of both are one instruction, which matters where a kernel runs close
+// to the instruction rate.
+struct Two {
+    unsigned long long v;
+};
+__device__ __forceinline__ Two two(float a, float b)
+{
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 one(Two x)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x.v));
+    return r;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b)
+{
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b)
+{
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c)
+{
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ Two zero() { return {0ull}; }
+
 // First slot behind the sequence that holds slot i (pos[i] >= 0), by a whole warp: pos[s] == s - start holds up to the
 // end of the sequence and nowhere behind it, so 32 probes cut the range by 32 (three rounds for 32,768 slots).
 // Whatever pos holds, the result is in (i, t].

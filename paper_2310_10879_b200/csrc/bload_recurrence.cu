@@ -52,43 +52,6 @@ __host__ __device__ inline size_t work_view(int64_t parts, void* base, WorkView2
     return states + 256 * (size_t)parts;
 }
 
-// Two channels in one 64-bit register: multiplies and adds of both are one instruction, which matters because the kernels
-// run close to the instruction rate, not only to the memory's.
-struct Two {
-    unsigned long long v;
-};
-__device__ __forceinline__ Two two(float a, float b)
-{
-    Two r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float2 one(Two x)
-{
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x.v));
-    return r;
-}
-__device__ __forceinline__ Two operator*(Two a, Two b)
-{
-    Two r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Two operator+(Two a, Two b)
-{
-    Two r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Two fma(Two a, Two b, Two c)
-{
-    Two r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-__device__ __forceinline__ Two zero() { return {0ull}; }
-
 // f = sigmoid(g) and 1 - f, each with a small relative error of its own (1 - f must not cancel: it scales the input).  With e =
 // exp(-g): f = 1 / (1 + e), 1 - f = e f; g has been held at -87, so that e f does not become inf * 0, and what f is then
 // (some 2^-125.5) is taken off again.
