@@ -65,6 +65,9 @@ __device__ __forceinline__ rows::Span span_of(const AttnParams& p, const int32_t
     return s;
 }
 
+// Meeting point of the two warps that share 32 rows.
+__device__ __forceinline__ void pair_barrier(int pair) { asm volatile("bar.sync %0, 64;" ::"r"(1 + pair) : "memory"); }
+
 // columns [lo, hi] of 32
 __device__ __forceinline__ uint32_t column_mask(int lo, int hi)
 {
@@ -193,11 +196,13 @@ struct ForwardTile {
     static constexpr int kShared = kTile * (1 + 2 * kStages) + 1024;
 };
 
-// Warps 0 to 3 own a query row per thread: scores from tensor memory, running maximum and sum, P back to tensor memory over
-// the scores.  Warp 4 copies tiles in, warp 5 issues the products.  256 of the 512 columns of tensor memory and less than half
-// of the shared memory, so that two CTAs share an SM and one's products run under the other's exponentials.
+// Warps 0 to 7 have the queries' arithmetic: warp w and warp w + 4 the same 32 rows, a row per lane, each half of the columns
+// (with one warp per row the tensor cores were busy 31 % of the time: too few warps to hide the latency of their own steps).
+// Scores come from tensor memory, P goes back over them; the two halves of a row agree on its maximum through shared memory,
+// each keeps its own sum.  Warp 8 copies tiles in, warp 9 issues the products.  256 of the 512 columns of tensor memory and less
+// than half of the shared memory, so that two CTAs share an SM and one's products run under the other's exponentials.
 template <bool BF16, int DP, bool MOD>
-__global__ void __launch_bounds__(192, 2)
+__global__ void __launch_bounds__(320, 2)
     k29_attention(const AttnParams p, const AttnTensors<typename Element<BF16>::type> a, const __grid_constant__ ForwardMaps maps)
 {
     using Tile = ForwardTile<DP>;
@@ -206,6 +211,7 @@ __global__ void __launch_bounds__(192, 2)
     __shared__ uint32_t tmem_base;
     __shared__ int dead, junk;
     __shared__ ReachShared<4> reach_shared;
+    __shared__ float halves[2][2][128];  // [turn][half][row]: maxima, and in the end sums
 
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* const q_tile = tiles;
@@ -221,18 +227,19 @@ __global__ void __launch_bounds__(192, 2)
     const int i0 = (q_tiles - 1 - (int)(blockIdx.x / (p.blocks * p.heads))) * 128;  // the longest rows of a long sequence first
     const int h = (int)(bh % p.heads), hk = h / p.group, b = (int)(bh / p.heads);
     const int32_t* const pos = p.pos + (int64_t)b * p.t;
-    const int row = i0 + tid;  // of threads 0 to 127
+    const int half = warp >> 2, quarter = warp & 3;  // of warps 0 to 7
+    const int own_row = quarter * 32 + lane, row = i0 + own_row;
 
     rows::Span span{kNever, -1};
-    if (warp < 4) {
+    if (warp < 8) {
         span = span_of(p, pos, row, false, lane);
-        put_reach(reach_shared, warp, lane, span);
+        if (half == 0) put_reach(reach_shared, quarter, lane, span);
         if (tid == 0) dead = junk = 0;
-    } else if (warp == 4) {
+    } else if (warp == 8) {
         if (lane == 0) {
             tc::bar_init(q_full, 1);
             tc::bar_init(s_full, 1);
-            tc::bar_init(p_full, 128);
+            tc::bar_init(p_full, 256);
             tc::bar_init(o_done, 1);
             for (int s = 0; s < 4 * Tile::kStages; ++s) tc::bar_init(k_full + 8 * s, 1);
             tc::bar_init_done();
@@ -248,7 +255,7 @@ __global__ void __launch_bounds__(192, 2)
     const int n = reach.hi < 0 ? 0 : (reach.hi - reach.lo) / Tile::kKeys + 1;
     float m = -INFINITY, l = 0.0f;  // running maximum (log2 units; may lag by kLag) and sum
 
-    if (warp == 4) {
+    if (warp == 8) {
         if (lane == 0 && n > 0) {
             bool ok = true;
             tc::bar_expect(q_full, Tile::kTile);
@@ -279,7 +286,7 @@ __global__ void __launch_bounds__(192, 2)
                 }
             }
         }
-    } else if (warp == 5) {
+    } else if (warp == 9) {
         if (lane == 0 && n > 0) {
             bool ok = tc::bar_wait(q_full, 0);
             for (int i = 0; i < n && ok; ++i) {
@@ -307,52 +314,53 @@ __global__ void __launch_bounds__(192, 2)
         }
     } else {
         const Modifier modify(p, h);
-        const uint32_t lanes = (uint32_t)warp << 21;  // this warp's 32 lanes of tensor memory
+        const uint32_t lanes = (uint32_t)quarter << 21;  // this warp's 32 lanes of tensor memory
         const float by = modify.by;
-        bool found = false;
+        bool found = false, ok = true;
         for (int i = 0; i < n; ++i) {
             const int st = i % Tile::kStages;
-            const int j0 = reach.lo + i * Tile::kKeys;
-            if (!__all_sync(0xffffffffu, tc::bar_wait(s_full, i & 1))) {
-                dead = 1;
-                break;
-            }
+            const int j0 = reach.lo + i * Tile::kKeys, mine0 = j0 + 64 * half;  // the tile's and this warp's first key
+            // (a warp that gives up goes on without waiting: its partner meets it at a barrier in every turn)
+            if (ok && !(ok = __all_sync(0xffffffffu, tc::bar_wait(s_full, i & 1)))) dead = 1;
             tc::fence_after();
-            uint32_t s[4][32];
+            // The scores in units of log2 are x by (MOD: x itself); hidden ones are -inf.  They are read twice, for the maximum and
+            // for the exponentials: 64 of them would not stay in this thread's registers.  What changes them is written back.
+            const uint32_t own_at = s_at + lanes + 64 * half;
+            const bool clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 63);
+            float top = -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tc::tmem_load(s[c], s_at + lanes + 32 * c);
-            tc::tmem_loaded();
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tc::settle(s[c]);
-            // The scores in units of log2 are x by (MOD: x itself); hidden ones are -inf.
-            const bool clear = __all_sync(0xffffffffu, span.lo <= j0 && span.hi >= j0 + Tile::kKeys - 1);
-            if (MOD) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 2; ++c) {
+                uint32_t s[32];
+                tc::tmem_load(s, own_at + 32 * c);
+                tc::tmem_loaded();
+                tc::settle(s);
+                if (MOD) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
                         float inner;
-                        s[c][e] = __float_as_uint(modify(__uint_as_float(s[c][e]), (float)(row - j0 - 32 * c - e), inner));
+                        s[e] = __float_as_uint(modify(__uint_as_float(s[e]), (float)(row - mine0 - 32 * c - e), inner));
                     }
-            }
-            if (!clear) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint32_t mask = column_mask(span.lo - j0 - 32 * c, span.hi - j0 - 32 * c);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) s[c][e] = (mask >> e) & 1 ? s[c][e] : 0xff800000u;
                 }
-            }
-            float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                if (!clear) {
+                    const uint32_t mask = column_mask(span.lo - mine0 - 32 * c, span.hi - mine0 - 32 * c);
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+                    for (int e = 0; e < 32; ++e) s[e] = (mask >> e) & 1 ? s[e] : 0xff800000u;
+                }
+                if (MOD || !clear) tc::tmem_store(own_at + 32 * c, s);
+                float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int e = 0; e < 32; e += 2)
-                    t4[(e / 2) & 3] = fmaxf(t4[(e / 2) & 3], fmaxf(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1])));
-            float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+                    t4[(e / 2) & 3] = fmaxf(t4[(e / 2) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+                top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
+            }
+            if (MOD || !clear) tc::tmem_stored();
+            halves[i & 1][half][own_row] = top;
+            pair_barrier(quarter);
+            top = fmaxf(top, halves[i & 1][half ^ 1][own_row]);
             if (!MOD) top *= by;
             // The maximum that scales the exponentials may lag behind by a factor of 2^8: the result is the same, and the
-            // accumulator in tensor memory is rescaled only when a row has moved further than that.
+            // accumulator in tensor memory is rescaled only when a row has moved further than that.  (The second half's warp
+            // sees the same maxima and moves with the first's.)
             constexpr float kLag = 8.0f;
             const bool move = top > m + kLag || (m == -INFINITY && top > m);
             if (__any_sync(0xffffffffu, move)) {
@@ -362,14 +370,15 @@ __global__ void __launch_bounds__(192, 2)
                 m = now;
                 if (i > 0) {
 #pragma unroll
-                    for (int c = 0; c < DP / 32; ++c) {
+                    for (int c = 0; c < DP / 64; ++c) {
+                        const uint32_t at = o_at + lanes + half * (DP / 2) + 32 * c;
                         uint32_t o[32];
-                        tc::tmem_load(o, o_at + lanes + 32 * c);
+                        tc::tmem_load(o, at);
                         tc::tmem_loaded();
                         tc::settle(o);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * down);
-                        tc::tmem_store(o_at + lanes + 32 * c, o);
+                        tc::tmem_store(at, o);
                     }
                 }
             }
@@ -377,23 +386,26 @@ __global__ void __launch_bounds__(192, 2)
             const Two by2 = two(by, by), off2 = two(off, off);
             Two sum[2] = {zero(), zero()};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t w[16];
+            for (int c = 0; c < 2; ++c) {
+                uint32_t s[32], w[16];
+                tc::tmem_load(s, own_at + 32 * c);
+                tc::tmem_loaded();
+                tc::settle(s);
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
-                    const Two raw = two(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1]));
+                    const Two raw = two(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
                     const float2 x = one(MOD ? raw + off2 : fma(raw, by2, off2));
                     const float p0 = tc::exp2_fast(x.x), p1 = tc::exp2_fast(x.y);
                     sum[(e / 2) & 1] = sum[(e / 2) & 1] + two(p0, p1);
                     w[e / 2] = tc::pack<BF16>(p0, p1);
                 }
-                tc::tmem_store16(s_at + lanes + 16 * c, w);
+                tc::tmem_store16(own_at + 16 * c, w);  // over scores that this thread is done with
             }
             const float2 sums = one(sum[0] + sum[1]);
             l += sums.x + sums.y;
             if (j0 < reach.all_lo || j0 + Tile::kKeys - 1 > reach.all_hi) {  // hidden from some row: no junk may reach the product
-                if (!tc::bar_wait(v_full + 8 * st, (i / Tile::kStages) & 1)) dead = 1;
-                found |= scan_tile<BF16, 128, DP, 128>(p, pos, v_tiles + st * Tile::kTile, j0, tid);
+                if (ok && !tc::bar_wait(v_full + 8 * st, (i / Tile::kStages) & 1)) dead = 1;
+                found |= scan_tile<BF16, 128, DP, 256>(p, pos, v_tiles + st * Tile::kTile, j0, tid);
                 tc::writes_to_async();
             }
             tc::tmem_stored();
@@ -401,21 +413,24 @@ __global__ void __launch_bounds__(192, 2)
             tc::bar_arrive(p_full);
         }
         if (found) junk = 1;
+        halves[n & 1][half][own_row] = l;
     }
     __syncthreads();
     if (dead) {
         if (tid == 0) atomicAdd(&g_timeouts, 1u);
     } else if (junk) {
-        for (int r = warp; r < 128; r += 6)
+        for (int r = warp; r < 128; r += 10)
             if (i0 + r < p.t) rows::forward_row(p, a, b, h, i0 + r, lane);
-    } else if (warp < 4) {
-        const uint32_t lanes = (uint32_t)warp << 21;
+    } else if (warp < 8) {
+        const uint32_t lanes = (uint32_t)quarter << 21;
+        l += halves[n & 1][half ^ 1][own_row];
         const bool empty = l == 0.0f;
         const float inv = 1.0f / l;
         if (n > 0 && !tc::bar_wait(o_done, (n - 1) & 1)) atomicAdd(&g_timeouts, 1u);
         tc::fence_after();
 #pragma unroll
-        for (int c = 0; c < DP / 32; ++c) {
+        for (int k = 0; k < DP / 64; ++k) {  // each half has half of the columns
+            const int c = half * (DP / 64) + k;
             uint32_t o[32];
             if (n > 0) {
                 tc::tmem_load(o, o_at + lanes + 32 * c);
@@ -425,21 +440,20 @@ __global__ void __launch_bounds__(192, 2)
             float x[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = empty || n == 0 ? 0.0f : __uint_as_float(o[e]) * inv;
-            stage_columns<BF16>(q_tile + (c / 2) * (128 * 128), tid, (c % 2) * 32, x);
+            stage_columns<BF16>(q_tile + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
         }
         tc::writes_to_async();
-        __syncwarp();
-        if (lane == 0 && i0 + warp * 32 < p.t) {
-            for (int x = 0; x < DP; x += 64)
-                if (x < p.d) tc::tensor_store(&maps.out, x, i0 + warp * 32, h, b, tc::smem_of(q_tile) + x * 256 + warp * 32 * 128);
-            tc::stores_read();
-        }
-        if (p.lse && row < p.t)
+        if (half == 0 && p.lse && row < p.t)
             p.lse[((int64_t)b * p.heads + h) * p.t + row] = empty ? -INFINITY : (m + log2f(l)) * kLn2;
     }
     tc::fence_before();
     __syncthreads();
-    if (warp == 5) tc::tmem_free<256>(tmem);
+    if (warp == 9) {
+        tc::tmem_free<256>(tmem);
+    } else if (!dead && !junk && warp < 8 && lane == 0 && half * 64 < DP && half * 64 < p.d && i0 + quarter * 32 < p.t) {
+        tc::tensor_store(&maps.out, half * 64, i0 + quarter * 32, h, b, tc::smem_of(q_tile) + half * (128 * 128) + quarter * 32 * 128);
+        tc::stores_read();
+    }
 }
 
 // ---- gradients ----------------------------------------------------------------------------------------------------
@@ -467,13 +481,14 @@ struct GradTile {
 // the second kernel, and for walks of at most kExact tiles, where few keys share the error, dq is corrected by
 // -eps * sum_j P_ij inner k_j, for which acc2 is kept.
 //
-// Two warpgroups take turns at the tiles (tile n belongs to group n & 1 and its part of tensor memory), so that the products of
-// one run under the arithmetic of the other.  No product waits for arithmetic that has not begun: per pair of tiles the order is
+// Two groups of eight warps take turns at the tiles (tile n belongs to group n & 1 and its part of tensor memory; warps w and
+// w + 4 of a group have the same 32 rows, each half of the columns), so that the products of one run under the arithmetic of the
+// other.  No product waits for arithmetic that has not begun: per pair of tiles the order is
 // acc(n), acc(n+1), S(n+2), S(n+3).
 constexpr int kExact = 1 << 20;
 
 template <bool BF16, int DP, bool MOD, bool KEYS>
-__global__ void __launch_bounds__(320, 1)
+__global__ void __launch_bounds__(576, 1)
     k30_attention_grad(const AttnParams p, const AttnTensors<typename Element<BF16>::type> a, const __grid_constant__ GradMaps maps)
 {
     using Tile = GradTile<DP>;
@@ -482,8 +497,8 @@ __global__ void __launch_bounds__(320, 1)
     __shared__ uint32_t tmem_base;
     __shared__ int dead, junk;
     __shared__ ReachShared<4> reach_shared;
-    __shared__ float eps_shared[2][128];
-    __shared__ float4 column_stats[KEYS ? 8 : 1][KEYS ? 32 : 1];  // per warp: -lse (log2 units) and -delta of 32 pairs of columns
+    __shared__ float eps_shared[4][128];
+    __shared__ float4 column_stats[KEYS ? 16 : 1][KEYS ? 16 : 1];  // per warp: -lse (log2 units) and -delta of 16 pairs of columns
 
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* const a1 = tiles;
@@ -501,20 +516,20 @@ __global__ void __launch_bounds__(320, 1)
     const int r0 = (KEYS ? turn : own_tiles - 1 - turn) * 128;  // the longest walks of a long sequence first
     const int h = (int)(bh % own_heads), b = (int)(bh / own_heads);
     const int32_t* const pos = p.pos + (int64_t)b * p.t;
-    const int group = warp >> 2, quarter = warp & 3;  // of warps 0 to 7
+    const int group = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;  // of warps 0 to 15
     const int row = r0 + quarter * 32 + lane;
 
     rows::Span span{kNever, -1};
-    if (warp < 8) {
+    if (warp < 16) {
         span = span_of(p, pos, row, KEYS, lane);
-        if (group == 0) put_reach(reach_shared, quarter, lane, span);
+        if (group == 0 && half == 0) put_reach(reach_shared, quarter, lane, span);
         if (tid == 0) dead = junk = 0;
-    } else if (warp == 8) {
+    } else if (warp == 16) {
         if (lane == 0) {
             tc::bar_init(a_full, 1);
             for (int w = 0; w < 2; ++w) {
                 tc::bar_init(s_full + 8 * w, 1);
-                tc::bar_init(p_full + 8 * w, 128);
+                tc::bar_init(p_full + 8 * w, 256);
                 tc::bar_init(acc_done + 8 * w, 1);
             }
             for (int s = 0; s < 2 * Tile::kStages; ++s) tc::bar_init(b_full + 8 * s, 1);
@@ -533,7 +548,7 @@ __global__ void __launch_bounds__(320, 1)
     const bool second = KEYS || n <= kExact;  // acc2 is kept
     float eps = 0.0f;
 
-    if (warp == 8) {
+    if (warp == 16) {
         if (lane == 0 && n > 0) {
             bool ok = true;
             tc::bar_expect(a_full, 2 * Tile::kOwn);
@@ -559,7 +574,7 @@ __global__ void __launch_bounds__(320, 1)
                 for (int i = max(0, issued - Tile::kStages); i < issued; ++i) tc::bar_wait(b_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
             }
         }
-    } else if (warp == 9) {
+    } else if (warp == 17) {
         if (lane == 0 && n > 0) {
             bool ok = tc::bar_wait(a_full, 0);
             auto scores = [&](int i) {
@@ -598,7 +613,7 @@ __global__ void __launch_bounds__(320, 1)
     } else {
         const uint32_t lanes = (uint32_t)quarter << 21;
         const uint32_t pair_at = pairs_at + 128 * group + lanes;
-        const int wtid = tid & 127;
+        const int wtid = tid & 255;
         bool found = false;
         float delta = 0.0f;
         Two lse2 = zero(), delta2, eps2 = zero();  // of this row, negative
@@ -622,16 +637,13 @@ __global__ void __launch_bounds__(320, 1)
             const int j0 = reach.lo + (KEYS ? i % per_head : i) * 64;
             const int hq = KEYS ? h * p.group + i / per_head : h;
             const Modifier modify(p, hq);
-            if (KEYS) {  // statistics of the 64 columns
-                const int64_t base = ((int64_t)b * p.heads + hq) * p.t;
+            if (KEYS) {  // statistics of this warp's 32 columns
+                const int64_t at = ((int64_t)b * p.heads + hq) * p.t + j0 + 32 * half + lane;
+                const bool in = j0 + 32 * half + lane < p.t;
                 __syncwarp();
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int c = lane + 32 * k, j = j0 + c;
-                    float* const st = reinterpret_cast<float*>(&column_stats[KEYS ? warp : 0][KEYS ? c / 2 : 0]) + (c & 1);
-                    st[0] = j < p.t ? minus_lse(p.lse[base + j]) : 0.0f;
-                    st[2] = j < p.t ? -p.delta[base + j] : 0.0f;
-                }
+                float* const st = reinterpret_cast<float*>(&column_stats[KEYS ? warp : 0][KEYS ? lane / 2 : 0]) + (lane & 1);
+                st[0] = in ? minus_lse(p.lse[at]) : 0.0f;
+                st[2] = in ? -p.delta[at] : 0.0f;
                 __syncwarp();
             }
             if (!__all_sync(0xffffffffu, tc::bar_wait(s_full + 8 * group, (i / 2) & 1))) {
@@ -639,32 +651,32 @@ __global__ void __launch_bounds__(320, 1)
                 break;
             }
             tc::fence_after();
-            const bool clear = __all_sync(0xffffffffu, span.lo <= j0 && span.hi >= j0 + 63);
+            const int mine0 = j0 + 32 * half;  // this warp's first column
+            const bool clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 31);
             const Two by2 = two(modify.by, modify.by);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            {
                 uint32_t s[32], d[32], pw[16], dw[16];
-                tc::tmem_load(s, pair_at + 32 * c);
-                tc::tmem_load(d, pair_at + 64 + 32 * c);
+                tc::tmem_load(s, pair_at + 32 * half);
+                tc::tmem_load(d, pair_at + 64 + 32 * half);
                 tc::tmem_loaded();
                 tc::settle(s);
                 tc::settle(d);
                 auto tile = [&](auto masked) {
                     constexpr bool kMasked = decltype(masked)::value;
-                    const uint32_t mask = kMasked ? column_mask(span.lo - j0 - 32 * c, span.hi - j0 - 32 * c) : 0xffffffffu;
+                    const uint32_t mask = kMasked ? column_mask(span.lo - mine0, span.hi - mine0) : 0xffffffffu;
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
                         Two lse_here = lse2, delta_here = delta2;
                         if (KEYS) {
-                            const float4 stats = column_stats[KEYS ? warp : 0][KEYS ? 16 * c + e / 2 : 0];
+                            const float4 stats = column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0];
                             lse_here = two(stats.x, stats.y);
                             delta_here = two(stats.z, stats.w);
                         }
                         const Two raw = two(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
                         float2 x, inner = make_float2(1.0f, 1.0f);
                         if (MOD) {
-                            x.x = modify(one(raw).x, (float)(row - j0 - 32 * c - e), inner.x);
-                            x.y = modify(one(raw).y, (float)(row - j0 - 32 * c - e - 1), inner.y);
+                            x.x = modify(one(raw).x, (float)(row - mine0 - e), inner.x);
+                            x.y = modify(one(raw).y, (float)(row - mine0 - e - 1), inner.y);
                             x = one(two(x.x, x.y) + lse_here);
                         } else {
                             x = one(fma(raw, by2, lse_here));
@@ -690,15 +702,15 @@ __global__ void __launch_bounds__(320, 1)
                     tile(std::false_type());
                 else
                     tile(std::true_type());
-                if (second) tc::tmem_store16(pair_at + 16 * c, pw);
-                tc::tmem_store16(pair_at + 64 + 16 * c, dw);
+                if (second) tc::tmem_store16(pair_at + 32 * half, pw);  // over the scores they were made from
+                tc::tmem_store16(pair_at + 64 + 32 * half, dw);
             }
             if (j0 < reach.all_lo || j0 + 63 > reach.all_hi) {  // hidden from some row: no junk may reach the products
                 const int st = i % Tile::kStages;
                 uint8_t* const at = stream + st * 2 * Tile::kStream;
                 if (!tc::bar_wait(b_full + 8 * st, (i / Tile::kStages) & 1)) dead = 1;
-                found |= scan_tile<BF16, 64, DP, 128>(p, pos, at, j0, wtid);
-                if (KEYS) found |= scan_tile<BF16, 64, DP, 128>(p, pos, at + Tile::kStream, j0, wtid);
+                found |= scan_tile<BF16, 64, DP, 256>(p, pos, at, j0, wtid);
+                if (KEYS) found |= scan_tile<BF16, 64, DP, 256>(p, pos, at + Tile::kStream, j0, wtid);
                 tc::writes_to_async();
             }
             tc::tmem_stored();
@@ -706,7 +718,7 @@ __global__ void __launch_bounds__(320, 1)
             tc::bar_arrive(p_full + 8 * group);
         }
         if (found) junk = 1;
-        if (!KEYS) eps_shared[group][quarter * 32 + lane] = one(eps2).x + one(eps2).y;
+        if (!KEYS) eps_shared[warp >> 2][quarter * 32 + lane] = one(eps2).x + one(eps2).y;
         if (!KEYS) eps = delta;  // kept for the end
     }
     __syncthreads();
@@ -714,72 +726,58 @@ __global__ void __launch_bounds__(320, 1)
     if (dead) {
         if (tid == 0) atomicAdd(&g_timeouts, 1u);
     } else if (junk) {
-        for (int r = warp; r < 128; r += 10) {
+        for (int r = warp; r < 128; r += 18) {
             if (r0 + r >= p.t) continue;
             if (KEYS)
                 rows::dkv_row(p, a, b, h, r0 + r, lane);
             else
                 rows::dq_row(p, a, b, h, r0 + r, lane);
         }
-    } else if (warp < 8) {
+    } else if (warp < 16) {
         const uint32_t lanes = (uint32_t)quarter << 21;
         const bool empty = span.lo > span.hi;
         if (n > 0 && !tc::bar_wait(acc_done + 8 * ((n - 1) & 1), ((n - 1) / 2) & 1)) atomicAdd(&g_timeouts, 1u);
         tc::fence_after();
         const int own_row = quarter * 32 + lane;
-        if (KEYS) {  // group 0: dk, group 1: dv
+        float off = 0.0f;
+        if (!KEYS) {
+            const float delta = eps;
+            off = (eps_shared[0][own_row] + eps_shared[1][own_row]) + (eps_shared[2][own_row] + eps_shared[3][own_row]);
+            if (group == 0 && half == 0 && row < p.t) p.delta[((int64_t)b * p.heads + h) * p.t + row] = empty ? 0.0f : delta + off;
+        }
+        // keys: group 0 has dk, group 1 dv, each warp half of the columns; queries: the four warps of a row share dq's columns
 #pragma unroll
-            for (int c = 0; c < DP / 32; ++c) {
-                uint32_t o[32];
-                if (n > 0) {
-                    tc::tmem_load(o, (group ? acc2_at : acc1_at) + lanes + 32 * c);
-                    tc::tmem_loaded();
-                    tc::settle(o);
-                }
-                float x[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = empty || n == 0 ? 0.0f : __uint_as_float(o[e]) * (group ? 1.0f : p.scale);
-                stage_columns<BF16>((group ? a2 : a1) + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
+        for (int c = KEYS ? half : warp >> 2; c < DP / 32; c += KEYS ? 2 : 4) {
+            uint32_t o[32], o2[32] = {};
+            if (n > 0) {
+                tc::tmem_load(o, (KEYS && group ? acc2_at : acc1_at) + lanes + 32 * c);
+                if (!KEYS && second) tc::tmem_load(o2, acc2_at + lanes + 32 * c);
+                tc::tmem_loaded();
+                tc::settle(o);
+                tc::settle(o2);
             }
-        } else {  // each group half of the columns
-            const float delta = eps, off = eps_shared[0][own_row] + eps_shared[1][own_row];
-            if (group == 0 && row < p.t) p.delta[((int64_t)b * p.heads + h) * p.t + row] = empty ? 0.0f : delta + off;
+            float x[32];
 #pragma unroll
-            for (int k = 0; k < DP / 64; ++k) {
-                const int c = group * (DP / 64) + k;
-                uint32_t o[32], o2[32] = {};
-                if (n > 0) {
-                    tc::tmem_load(o, acc1_at + lanes + 32 * c);
-                    if (second) tc::tmem_load(o2, acc2_at + lanes + 32 * c);
-                    tc::tmem_loaded();
-                    tc::settle(o);
-                    tc::settle(o2);
-                }
-                float x[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    float y = __uint_as_float(o[e]);
-                    if (second) y = fmaf(-off, __uint_as_float(o2[e]), y);
-                    x[e] = empty || n == 0 ? 0.0f : y * p.scale;
-                }
-                stage_columns<BF16>(a1 + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
+            for (int e = 0; e < 32; ++e) {
+                float y = __uint_as_float(o[e]);
+                if (!KEYS && second) y = fmaf(-off, __uint_as_float(o2[e]), y);
+                x[e] = empty || n == 0 ? 0.0f : y * (KEYS && group ? 1.0f : p.scale);
             }
+            stage_columns<BF16>((KEYS && group ? a2 : a1) + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
         }
         tc::writes_to_async();
     }
     tc::fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == 17) {
         tc::tmem_free<512>(tmem);
-    } else if (good && warp < 8 && lane == 0) {
-        // dk, dv: a warp stores the 32 rows it staged; dq: the halves of the columns, or all of them at heads of at most 64
-        const int at_row = r0 + quarter * 32;
-        for (int x = 0; x < DP; x += 64) {
-            if (x >= p.d || at_row >= p.t || (!KEYS && group != x / 64)) continue;
+    } else if (good && warp < 16 && lane == 0) {  // keys: group 0 stores dk, group 1 dv; queries: group 0 stores dq
+        const int x = 64 * half, at_row = r0 + quarter * 32;
+        if (x < DP && x < p.d && at_row < p.t && (KEYS || group == 0)) {
             tc::tensor_store(KEYS && group ? &maps.o2 : &maps.o1, x, at_row, h, b,
                              tc::smem_of(KEYS && group ? a2 : a1) + x * 256 + quarter * 32 * 128);
+            tc::stores_read();
         }
-        tc::stores_read();
     }
 }
 
@@ -835,7 +833,7 @@ cudaError_t forward(const AttnParams& p, const AttnTensors<typename Element<BF16
     auto* kernel = k29_attention<BF16, DP, MOD>;
     static const cudaError_t set = with_shared(kernel, ForwardTile<DP>::kShared);
     if (set != cudaSuccess) return set;
-    kernel<<<(unsigned)grid, 192, ForwardTile<DP>::kShared, st>>>(p, a, m);
+    kernel<<<(unsigned)grid, 320, ForwardTile<DP>::kShared, st>>>(p, a, m);
     count_launches(1);
     return cudaGetLastError();
 }
@@ -853,7 +851,7 @@ cudaError_t gradient(const AttnParams& p, const AttnTensors<typename Element<BF1
     auto* kernel = k30_attention_grad<BF16, DP, MOD, KEYS>;
     static const cudaError_t set = with_shared(kernel, GradTile<DP>::kShared);
     if (set != cudaSuccess) return set;
-    kernel<<<(unsigned)grid, 320, GradTile<DP>::kShared, st>>>(p, a, m);
+    kernel<<<(unsigned)grid, 576, GradTile<DP>::kShared, st>>>(p, a, m);
     count_launches(1);
     return cudaGetLastError();
 }
