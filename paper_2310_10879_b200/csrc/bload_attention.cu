@@ -464,12 +464,15 @@ struct GradMaps {
     CUtensorMap o1, o2;  // boxes of 32 rows.                       dq, -   | dk, dv
 };
 
+// Two groups of warps and all of the tensor memory, or, for heads of at most 64 elements, one group and half of it: then two CTAs
+// share an SM, and one's first copies and last stores run under the other's products.
 template <int DP>
 struct GradTile {
+    static constexpr int kGroups = DP == 64 ? 1 : 2;
+    static constexpr int kThreads = 256 * kGroups + 64, kColumns = 256 * kGroups;
     static constexpr int kStages = 4;
     static constexpr int kOwn = 128 * DP * 2, kStream = 64 * DP * 2;
-    static constexpr int kNeeded = 2 * kOwn + kStages * 2 * kStream + 1024;
-    static constexpr int kShared = kNeeded > 116 * 1024 ? kNeeded : 116 * 1024;  // one CTA per SM: it takes all tensor memory
+    static constexpr int kShared = 2 * kOwn + kStages * 2 * kStream + 1024;
 };
 
 // Both gradient kernels keep two tiles of 128 rows (A1, A2) and let pairs of tiles of 64 rows (B1, B2) stream by:
@@ -481,24 +484,24 @@ struct GradTile {
 // the second kernel, and for walks of at most kExact tiles, where few keys share the error, dq is corrected by
 // -eps * sum_j P_ij inner k_j, for which acc2 is kept.
 //
-// Two groups of eight warps take turns at the tiles (tile n belongs to group n & 1 and its part of tensor memory; warps w and
-// w + 4 of a group have the same 32 rows, each half of the columns), so that the products of one run under the arithmetic of the
-// other.  No product waits for arithmetic that has not begun: per pair of tiles the order is
-// acc(n), acc(n+1), S(n+2), S(n+3).
+// A group is eight warps: warps w and w + 4 have the same 32 rows, each half of the columns.  Two groups take turns at the tiles
+// (each with its part of tensor memory), so that the products of one run under the arithmetic of the other: the products are
+// issued in the order acc(n), S(n + 2), acc(n + 1), S(n + 3), ...
 constexpr int kExact = 1 << 20;
 
 template <bool BF16, int DP, bool MOD, bool KEYS>
-__global__ void __launch_bounds__(576, 1)
+__global__ void __launch_bounds__(GradTile<DP>::kThreads, 3 - GradTile<DP>::kGroups)
     k30_attention_grad(const AttnParams p, const AttnTensors<typename Element<BF16>::type> a, const __grid_constant__ GradMaps maps)
 {
     using Tile = GradTile<DP>;
+    constexpr int kGroups = Tile::kGroups, kWarps = 8 * kGroups;  // the warps with the arithmetic; then copies, products
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[1 + 2 * Tile::kStages + 6];
     __shared__ uint32_t tmem_base;
     __shared__ int dead, junk;
     __shared__ ReachShared<4> reach_shared;
-    __shared__ float eps_shared[4][128];
-    __shared__ float4 column_stats[KEYS ? 16 : 1][KEYS ? 16 : 1];  // per warp: -lse (log2 units) and -delta of 16 pairs of columns
+    __shared__ float eps_shared[2 * kGroups][128];
+    __shared__ float4 column_stats[KEYS ? kWarps : 1][KEYS ? 16 : 1];  // per warp: -lse (log2 units) and -delta of 16 pairs of columns
 
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* const a1 = tiles;
@@ -516,18 +519,18 @@ __global__ void __launch_bounds__(576, 1)
     const int r0 = (KEYS ? turn : own_tiles - 1 - turn) * 128;  // the longest walks of a long sequence first
     const int h = (int)(bh % own_heads), b = (int)(bh / own_heads);
     const int32_t* const pos = p.pos + (int64_t)b * p.t;
-    const int group = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;  // of warps 0 to 15
+    const int group = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;  // of the arithmetic's warps
     const int row = r0 + quarter * 32 + lane;
 
     rows::Span span{kNever, -1};
-    if (warp < 16) {
+    if (warp < kWarps) {
         span = span_of(p, pos, row, KEYS, lane);
         if (group == 0 && half == 0) put_reach(reach_shared, quarter, lane, span);
         if (tid == 0) dead = junk = 0;
-    } else if (warp == 16) {
+    } else if (warp == kWarps) {
         if (lane == 0) {
             tc::bar_init(a_full, 1);
-            for (int w = 0; w < 2; ++w) {
+            for (int w = 0; w < kGroups; ++w) {
                 tc::bar_init(s_full + 8 * w, 1);
                 tc::bar_init(p_full + 8 * w, 256);
                 tc::bar_init(acc_done + 8 * w, 1);
@@ -536,7 +539,7 @@ __global__ void __launch_bounds__(576, 1)
             tc::bar_init_done();
         }
     } else {
-        tc::tmem_alloc<512>(tc::smem_of(&tmem_base));
+        tc::tmem_alloc<Tile::kColumns>(tc::smem_of(&tmem_base));
     }
     tc::fence_before();
     __syncthreads();
@@ -548,7 +551,7 @@ __global__ void __launch_bounds__(576, 1)
     const bool second = KEYS || n <= kExact;  // acc2 is kept
     float eps = 0.0f;
 
-    if (warp == 16) {
+    if (warp == kWarps) {
         if (lane == 0 && n > 0) {
             bool ok = true;
             tc::bar_expect(a_full, 2 * Tile::kOwn);
@@ -574,15 +577,15 @@ __global__ void __launch_bounds__(576, 1)
                 for (int i = max(0, issued - Tile::kStages); i < issued; ++i) tc::bar_wait(b_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
             }
         }
-    } else if (warp == 17) {
+    } else if (warp == kWarps + 1) {
         if (lane == 0 && n > 0) {
             bool ok = tc::bar_wait(a_full, 0);
             auto scores = [&](int i) {
-                const int w = i & 1;
+                const int w = i % kGroups;
                 const uint32_t at = tc::smem_of(stream) + (i % Tile::kStages) * 2 * Tile::kStream, to = pairs_at + 128 * w;
                 // they take the place of the group's last P and dS: the products that read those have to be over
                 if (!tc::bar_wait(b_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1) ||
-                    (i > 1 && !tc::bar_wait(acc_done + 8 * w, (i / 2 - 1) & 1)))
+                    (i >= kGroups && !tc::bar_wait(acc_done + 8 * w, (i / kGroups - 1) & 1)))
                     return false;
                 tc::fence_after();
                 tc::product_rows<BF16, 64, DP>(to, tc::smem_of(a1), at);
@@ -590,19 +593,17 @@ __global__ void __launch_bounds__(576, 1)
                 tc::products_arrive(s_full + 8 * w);
                 return true;
             };
-            for (int i = 0; i < 2 && i < n && ok; ++i) ok = scores(i);
-            for (int i0 = 0; i0 < n && ok; i0 += 2) {
-                for (int i = i0; i < i0 + 2 && i < n && ok; ++i) {
-                    const int w = i & 1, s = i % Tile::kStages;
-                    const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream, from = pairs_at + 128 * w;
-                    if (!(ok = tc::bar_wait(p_full + 8 * w, (i / 2) & 1))) break;
-                    tc::fence_after();
-                    tc::product_across<BF16, 64, DP>(acc1_at, from + 64, at, i > 0);
-                    if (second) tc::product_across<BF16, 64, DP>(acc2_at, from, KEYS ? at + Tile::kStream : at, i > 0);
-                    tc::products_arrive(b_free + 8 * s);
-                    tc::products_arrive(acc_done + 8 * w);
-                }
-                for (int i = i0 + 2; i < i0 + 4 && i < n && ok; ++i) ok = scores(i);
+            for (int i = 0; i < kGroups && i < n && ok; ++i) ok = scores(i);
+            for (int i = 0; i < n && ok; ++i) {
+                const int w = i % kGroups, s = i % Tile::kStages;
+                const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream, from = pairs_at + 128 * w;
+                if (!(ok = tc::bar_wait(p_full + 8 * w, (i / kGroups) & 1))) break;
+                tc::fence_after();
+                tc::product_across<BF16, 64, DP>(acc1_at, from + 64, at, i > 0);
+                if (second) tc::product_across<BF16, 64, DP>(acc2_at, from, KEYS ? at + Tile::kStream : at, i > 0);
+                tc::products_arrive(b_free + 8 * s);
+                tc::products_arrive(acc_done + 8 * w);
+                if (i + kGroups < n) ok = scores(i + kGroups);
             }
             if (!ok) {
                 dead = 1;
@@ -633,7 +634,7 @@ __global__ void __launch_bounds__(576, 1)
             }
         }
         delta2 = two(-delta, -delta);
-        for (int i = group; i < n; i += 2) {
+        for (int i = group; i < n; i += kGroups) {
             const int j0 = reach.lo + (KEYS ? i % per_head : i) * 64;
             const int hq = KEYS ? h * p.group + i / per_head : h;
             const Modifier modify(p, hq);
@@ -646,7 +647,7 @@ __global__ void __launch_bounds__(576, 1)
                 st[2] = in ? -p.delta[at] : 0.0f;
                 __syncwarp();
             }
-            if (!__all_sync(0xffffffffu, tc::bar_wait(s_full + 8 * group, (i / 2) & 1))) {
+            if (!__all_sync(0xffffffffu, tc::bar_wait(s_full + 8 * group, (i / kGroups) & 1))) {
                 dead = 1;
                 break;
             }
@@ -726,31 +727,33 @@ __global__ void __launch_bounds__(576, 1)
     if (dead) {
         if (tid == 0) atomicAdd(&g_timeouts, 1u);
     } else if (junk) {
-        for (int r = warp; r < 128; r += 18) {
+        for (int r = warp; r < 128; r += kWarps + 2) {
             if (r0 + r >= p.t) continue;
             if (KEYS)
                 rows::dkv_row(p, a, b, h, r0 + r, lane);
             else
                 rows::dq_row(p, a, b, h, r0 + r, lane);
         }
-    } else if (warp < 16) {
+    } else if (warp < kWarps) {
         const uint32_t lanes = (uint32_t)quarter << 21;
         const bool empty = span.lo > span.hi;
-        if (n > 0 && !tc::bar_wait(acc_done + 8 * ((n - 1) & 1), ((n - 1) / 2) & 1)) atomicAdd(&g_timeouts, 1u);
+        if (n > 0 && !tc::bar_wait(acc_done + 8 * ((n - 1) % kGroups), ((n - 1) / kGroups) & 1)) atomicAdd(&g_timeouts, 1u);
         tc::fence_after();
         const int own_row = quarter * 32 + lane;
         float off = 0.0f;
         if (!KEYS) {
             const float delta = eps;
-            off = (eps_shared[0][own_row] + eps_shared[1][own_row]) + (eps_shared[2][own_row] + eps_shared[3][own_row]);
+            for (int k = 0; k < 2 * kGroups; ++k) off += eps_shared[k][own_row];
             if (group == 0 && half == 0 && row < p.t) p.delta[((int64_t)b * p.heads + h) * p.t + row] = empty ? 0.0f : delta + off;
         }
-        // keys: group 0 has dk, group 1 dv, each warp half of the columns; queries: the four warps of a row share dq's columns
+        // chunks of 32 columns of dq, or of dk and then dv, are shared out among the warps of a row
 #pragma unroll
-        for (int c = KEYS ? half : warp >> 2; c < DP / 32; c += KEYS ? 2 : 4) {
+        for (int k = warp >> 2; k < (KEYS ? 2 : 1) * DP / 32; k += 2 * kGroups) {
+            const bool dv = KEYS && k >= DP / 32;
+            const int c = dv ? k - DP / 32 : k;
             uint32_t o[32], o2[32] = {};
             if (n > 0) {
-                tc::tmem_load(o, (KEYS && group ? acc2_at : acc1_at) + lanes + 32 * c);
+                tc::tmem_load(o, (dv ? acc2_at : acc1_at) + lanes + 32 * c);
                 if (!KEYS && second) tc::tmem_load(o2, acc2_at + lanes + 32 * c);
                 tc::tmem_loaded();
                 tc::settle(o);
@@ -761,21 +764,21 @@ __global__ void __launch_bounds__(576, 1)
             for (int e = 0; e < 32; ++e) {
                 float y = __uint_as_float(o[e]);
                 if (!KEYS && second) y = fmaf(-off, __uint_as_float(o2[e]), y);
-                x[e] = empty || n == 0 ? 0.0f : y * (KEYS && group ? 1.0f : p.scale);
+                x[e] = empty || n == 0 ? 0.0f : y * (dv ? 1.0f : p.scale);
             }
-            stage_columns<BF16>((KEYS && group ? a2 : a1) + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
+            stage_columns<BF16>((dv ? a2 : a1) + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
         }
         tc::writes_to_async();
     }
     tc::fence_before();
     __syncthreads();
-    if (warp == 17) {
-        tc::tmem_free<512>(tmem);
-    } else if (good && warp < 16 && lane == 0) {  // keys: group 0 stores dk, group 1 dv; queries: group 0 stores dq
-        const int x = 64 * half, at_row = r0 + quarter * 32;
-        if (x < DP && x < p.d && at_row < p.t && (KEYS || group == 0)) {
-            tc::tensor_store(KEYS && group ? &maps.o2 : &maps.o1, x, at_row, h, b,
-                             tc::smem_of(KEYS && group ? a2 : a1) + x * 256 + quarter * 32 * 128);
+    if (warp == kWarps + 1) {
+        tc::tmem_free<Tile::kColumns>(tmem);
+    } else if (good && lane == 0 && warp < (KEYS ? 2 : 1) * DP / 16) {  // four warps per 64 columns of dq, or of dk and then dv
+        const int k = warp >> 2, x = k % (DP / 64) * 64, at_row = r0 + quarter * 32;
+        const bool dv = k >= DP / 64;
+        if (x < p.d && at_row < p.t) {
+            tc::tensor_store(dv ? &maps.o2 : &maps.o1, x, at_row, h, b, tc::smem_of(dv ? a2 : a1) + x * 256 + quarter * 32 * 128);
             tc::stores_read();
         }
     }
@@ -851,7 +854,7 @@ cudaError_t gradient(const AttnParams& p, const AttnTensors<typename Element<BF1
     auto* kernel = k30_attention_grad<BF16, DP, MOD, KEYS>;
     static const cudaError_t set = with_shared(kernel, GradTile<DP>::kShared);
     if (set != cudaSuccess) return set;
-    kernel<<<(unsigned)grid, 576, GradTile<DP>::kShared, st>>>(p, a, m);
+    kernel<<<(unsigned)grid, GradTile<DP>::kThreads, GradTile<DP>::kShared, st>>>(p, a, m);
     count_launches(1);
     return cudaGetLastError();
 }
