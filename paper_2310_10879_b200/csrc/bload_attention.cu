@@ -287,28 +287,29 @@ __global__ void __launch_bounds__(320, 2)
             }
         }
     } else if (warp == 9) {
-        if (lane == 0 && n > 0) {
-            bool ok = tc::bar_wait(q_full, 0);
+        if (n > 0) {
+            const uint32_t leader = tc::elect();
+            bool ok = __all_sync(0xffffffffu, tc::bar_wait(q_full, 0));
             for (int i = 0; i < n && ok; ++i) {
                 const int s = i % Tile::kStages;
                 const uint32_t parity = (i / Tile::kStages) & 1;
                 // the scores take the place of the last tile's P: the product that reads it has to be over
-                ok = tc::bar_wait(k_full + 8 * s, parity) && (i == 0 || tc::bar_wait(o_done, (i - 1) & 1));
+                ok = __all_sync(0xffffffffu, tc::bar_wait(k_full + 8 * s, parity) && (i == 0 || tc::bar_wait(o_done, (i - 1) & 1)));
                 if (!ok) break;
                 tc::fence_after();
-                tc::product_rows<BF16, 128, DP>(s_at, tc::smem_of(q_tile), tc::smem_of(k_tiles) + s * Tile::kTile);
-                tc::products_arrive(k_free + 8 * s);
-                tc::products_arrive(s_full);
-                ok = tc::bar_wait(v_full + 8 * s, parity) && tc::bar_wait(p_full, i & 1);
+                tc::product_rows<BF16, 128, DP>(leader, s_at, tc::smem_of(q_tile), tc::smem_of(k_tiles) + s * Tile::kTile);
+                tc::products_arrive(leader, k_free + 8 * s);
+                tc::products_arrive(leader, s_full);
+                ok = __all_sync(0xffffffffu, tc::bar_wait(v_full + 8 * s, parity) && tc::bar_wait(p_full, i & 1));
                 if (!ok) break;
                 tc::fence_after();
-                tc::product_across<BF16, 128, DP>(o_at, s_at, tc::smem_of(v_tiles) + s * Tile::kTile, i > 0);
-                tc::products_arrive(v_free + 8 * s);
-                tc::products_arrive(o_done);
+                tc::product_across<BF16, 128, DP>(leader, o_at, s_at, tc::smem_of(v_tiles) + s * Tile::kTile, i > 0);
+                tc::products_arrive(leader, v_free + 8 * s);
+                tc::products_arrive(leader, o_done);
             }
             if (!ok) {
                 dead = 1;
-                tc::products_arrive(q_full);  // its second phase: products in flight end before the CTA does
+                tc::products_arrive(leader, q_full);  // its second phase: products in flight end before the CTA does
                 tc::bar_wait(q_full, 1);
             }
         }
@@ -578,36 +579,37 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, 3 - GradTile<DP>::kGro
             }
         }
     } else if (warp == kWarps + 1) {
-        if (lane == 0 && n > 0) {
-            bool ok = tc::bar_wait(a_full, 0);
+        if (n > 0) {
+            const uint32_t leader = tc::elect();
+            bool ok = __all_sync(0xffffffffu, tc::bar_wait(a_full, 0));
             auto scores = [&](int i) {
                 const int w = i % kGroups;
                 const uint32_t at = tc::smem_of(stream) + (i % Tile::kStages) * 2 * Tile::kStream, to = pairs_at + 128 * w;
                 // they take the place of the group's last P and dS: the products that read those have to be over
-                if (!tc::bar_wait(b_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1) ||
-                    (i >= kGroups && !tc::bar_wait(acc_done + 8 * w, (i / kGroups - 1) & 1)))
+                if (!__all_sync(0xffffffffu, tc::bar_wait(b_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1) &&
+                                                 (i < kGroups || tc::bar_wait(acc_done + 8 * w, (i / kGroups - 1) & 1))))
                     return false;
                 tc::fence_after();
-                tc::product_rows<BF16, 64, DP>(to, tc::smem_of(a1), at);
-                tc::product_rows<BF16, 64, DP>(to + 64, tc::smem_of(a2), at + Tile::kStream);
-                tc::products_arrive(s_full + 8 * w);
+                tc::product_rows<BF16, 64, DP>(leader, to, tc::smem_of(a1), at);
+                tc::product_rows<BF16, 64, DP>(leader, to + 64, tc::smem_of(a2), at + Tile::kStream);
+                tc::products_arrive(leader, s_full + 8 * w);
                 return true;
             };
             for (int i = 0; i < kGroups && i < n && ok; ++i) ok = scores(i);
             for (int i = 0; i < n && ok; ++i) {
                 const int w = i % kGroups, s = i % Tile::kStages;
                 const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream, from = pairs_at + 128 * w;
-                if (!(ok = tc::bar_wait(p_full + 8 * w, (i / kGroups) & 1))) break;
+                if (!(ok = __all_sync(0xffffffffu, tc::bar_wait(p_full + 8 * w, (i / kGroups) & 1)))) break;
                 tc::fence_after();
-                tc::product_across<BF16, 64, DP>(acc1_at, from + 64, at, i > 0);
-                if (second) tc::product_across<BF16, 64, DP>(acc2_at, from, KEYS ? at + Tile::kStream : at, i > 0);
-                tc::products_arrive(b_free + 8 * s);
-                tc::products_arrive(acc_done + 8 * w);
+                tc::product_across<BF16, 64, DP>(leader, acc1_at, from + 64, at, i > 0);
+                if (second) tc::product_across<BF16, 64, DP>(leader, acc2_at, from, KEYS ? at + Tile::kStream : at, i > 0);
+                tc::products_arrive(leader, b_free + 8 * s);
+                tc::products_arrive(leader, acc_done + 8 * w);
                 if (i + kGroups < n) ok = scores(i + kGroups);
             }
             if (!ok) {
                 dead = 1;
-                tc::products_arrive(a_full);  // its second phase: products in flight end before the CTA does
+                tc::products_arrive(leader, a_full);  // its second phase: products in flight end before the CTA does
                 tc::bar_wait(a_full, 1);
             }
         }

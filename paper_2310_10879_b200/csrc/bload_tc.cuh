@@ -156,44 +156,57 @@ __host__ __device__ constexpr uint32_t product_shape()
     return (1u << 4) | ((BF16 ? 1u : 0u) << 7) | ((BF16 ? 1u : 0u) << 10) | ((ACROSS ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) |
            ((128u >> 4) << 24);
 }
-__device__ __forceinline__ void product(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
+// Products are issued by one thread, but written for a whole converged warp with `leader` set in one lane: descriptors are then
+// uniform values, and a product takes some 20 cycles to issue instead of the 57 it takes from a branch of a single lane (eight
+// of 128 x 64 x 16 then took longer to issue than to run).
+__device__ __forceinline__ uint32_t elect()
+{
+    uint32_t leader;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(leader));
+    return leader;
+}
+__device__ __forceinline__ void product(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add), "r"(leader)
         : "memory");
 }
-__device__ __forceinline__ void product_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add)
+__device__ __forceinline__ void product_tmem(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add), "r"(leader)
         : "memory");
 }
-// arrives on the barrier when every product that this thread issued so far has ended
-__device__ __forceinline__ void products_arrive(uint32_t bar)
+// arrives on the barrier when every product that the leader issued so far has ended
+__device__ __forceinline__ void products_arrive(uint32_t leader, uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader)
+                 : "memory");
 }
 
 // D[128, N] (+)= A[128, DP] B[N, DP]^T, both tiles in shared memory
 template <bool BF16, int N, int DP>
-__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b)
+__device__ __forceinline__ void product_rows(uint32_t leader, uint32_t d, uint32_t a, uint32_t b)
 {
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k)
-        product(d, rows_desc(a + (k / 4) * (128 * 128) + (k % 4) * 32), rows_desc(b + (k / 4) * (N * 128) + (k % 4) * 32),
+        product(leader, d, rows_desc(a + (k / 4) * (128 * 128) + (k % 4) * 32), rows_desc(b + (k / 4) * (N * 128) + (k % 4) * 32),
                 product_shape<BF16, N, false>(), k > 0);
 }
 // D[128, DP] (+)= A[128, K] B[K, DP]: B's K rows in shared memory; A in tensor memory, two elements per column, in two halves
 // that are K / 2 columns apart (each lies at the start of the scores it was made from)
 template <bool BF16, int K, int DP>
-__device__ __forceinline__ void product_across(uint32_t d, uint32_t a, uint32_t b, bool add)
+__device__ __forceinline__ void product_across(uint32_t leader, uint32_t d, uint32_t a, uint32_t b, bool add)
 {
     constexpr int kHalf = K / 32;  // steps of 16 in a half
 #pragma unroll
     for (int k = 0; k < K / 16; ++k)
-        product_tmem(d, a + (k / kHalf) * (K / 2) + (k % kHalf) * 8, across_desc(b + k * (16 * 128), K * 128), product_shape<BF16, DP, true>(),
+        product_tmem(leader, d, a + (k / kHalf) * (K / 2) + (k % kHalf) * 8, across_desc(b + k * (16 * 128), K * 128), product_shape<BF16, DP, true>(),
                      add || k > 0);
 }
 
