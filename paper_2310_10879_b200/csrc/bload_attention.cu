@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(320, 2)
                 ok = __all_sync(0xffffffffu, tc::bar_wait(v_full + 8 * s, parity) && tc::bar_wait(p_full, i & 1));
                 if (!ok) break;
                 tc::fence_after();
-                tc::product_across<BF16, 128, DP>(leader, o_at, s_at, tc::smem_of(v_tiles) + s * Tile::kTile, i > 0);
+                tc::product_across<BF16, 128, DP, 64>(leader, o_at, s_at, tc::smem_of(v_tiles) + s * Tile::kTile, i > 0);
                 tc::products_arrive(leader, v_free + 8 * s);
                 tc::products_arrive(leader, o_done);
             }
@@ -461,47 +461,51 @@ __global__ void __launch_bounds__(320, 2)
 
 struct GradMaps {
     CUtensorMap a1, a2;  // the CTA's own rows: boxes of 128 rows.  q, dout | k, v
-    CUtensorMap b1, b2;  // what streams by: boxes of 64 rows.      k, v    | q, dout
+    CUtensorMap b1, b2;  // what streams by: boxes of kColumns.     k, v    | q, dout
     CUtensorMap o1, o2;  // boxes of 32 rows.                       dq, -   | dk, dv
 };
 
-// Two groups of warps and all of the tensor memory, or, for heads of at most 64 elements, one group and half of it: then two CTAs
+// Tiles of 128 columns and all of the tensor memory; for heads of at most 64 elements, tiles of 64 and half of it: then two CTAs
 // share an SM, and one's first copies and last stores run under the other's products.
 template <int DP>
 struct GradTile {
-    static constexpr int kGroups = DP == 64 ? 1 : 2;
-    static constexpr int kThreads = 256 * kGroups + 64, kColumns = 256 * kGroups;
-    static constexpr int kStages = 4;
-    static constexpr int kOwn = 128 * DP * 2, kStream = 64 * DP * 2;
+    static constexpr int kColumns = DP;                             // of a tile: rows of B1 and B2
+    static constexpr int kWarps = kColumns / 8;                     // with the arithmetic: 32 rows by 32 columns each
+    static constexpr int kThreads = 32 * kWarps + 64;               // then a warp for copies, a warp for products
+    static constexpr int kTmem = 2 * DP + 2 * kColumns;             // two accumulators, S, dP
+    static constexpr int kStages = DP == 64 ? 4 : 2;
+    static constexpr int kOwn = 128 * DP * 2, kStream = kColumns * DP * 2;
     static constexpr int kShared = 2 * kOwn + kStages * 2 * kStream + 1024;
+    static_assert(kTmem == 256 || kTmem == 512, "a power of two");
 };
 
-// Both gradient kernels keep two tiles of 128 rows (A1, A2) and let pairs of tiles of 64 rows (B1, B2) stream by:
+// Both gradient kernels keep two tiles of 128 rows (A1, A2) and let pairs of tiles (B1, B2) stream by:
 //     S = A1 B1^T, dP = A2 B2^T,   P = exp(score(S) - lse),   dS = P (dP - delta) inner,
 //     acc1 += dS B1,               acc2 += P B2 (KEYS) or (P inner) B1 (queries)
 // KEYS: rows are keys, acc1 = dk, acc2 = dv, streamed over the query heads that share them; lse and delta belong to columns.
 // Queries: acc1 = dq; lse and delta belong to rows.  delta = sum_j P_ij dP_ij is first taken as dout . out with the rounded out
 // of the forward call; the row sum eps of P (dP - delta) over the walk is exactly what that is off by, so delta + eps goes to
-// the second kernel, and for walks of at most kExact tiles, where few keys share the error, dq is corrected by
+// the second kernel, and for walks of at most kExact columns, where few keys share the error, dq is corrected by
 // -eps * sum_j P_ij inner k_j, for which acc2 is kept.
 //
-// A group is eight warps: warps w and w + 4 have the same 32 rows, each half of the columns.  Two groups take turns at the tiles
-// (each with its part of tensor memory), so that the products of one run under the arithmetic of the other: the products are
-// issued in the order acc(n), S(n + 2), acc(n + 1), S(n + 3), ...
+// P lies over S and dS over dP, and the products take turns: ..., acc2(n), S(n + 1), acc1(n), dP(n + 1), acc2(n + 1), ...  While
+// acc1(n) and dP(n + 1) run, P(n + 1) is made from S(n + 1); while acc2 and the next S run, dS from dP.  (Two groups of warps with
+// tiles of 64 columns each, taking turns, kept the tensor cores at 41 %: with 64 columns a product reads 192 bytes of shared
+// memory per cycle where there are 128, and what it reads of A serves half as many columns.)
 constexpr int kExact = 1 << 20;
 
 template <bool BF16, int DP, bool MOD, bool KEYS>
-__global__ void __launch_bounds__(GradTile<DP>::kThreads, 3 - GradTile<DP>::kGroups)
+__global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     k30_attention_grad(const AttnParams p, const AttnTensors<typename Element<BF16>::type> a, const __grid_constant__ GradMaps maps)
 {
     using Tile = GradTile<DP>;
-    constexpr int kGroups = Tile::kGroups, kWarps = 8 * kGroups;  // the warps with the arithmetic; then copies, products
+    constexpr int kColumns = Tile::kColumns, kWarps = Tile::kWarps, kStages = Tile::kStages;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[1 + 2 * Tile::kStages + 6];
+    __shared__ uint64_t bars[7 + 4 * kStages];
     __shared__ uint32_t tmem_base;
     __shared__ int dead, junk;
     __shared__ ReachShared<4> reach_shared;
-    __shared__ float eps_shared[2 * kGroups][128];
+    __shared__ float eps_shared[kColumns / 32][128];
     __shared__ float4 column_stats[KEYS ? kWarps : 1][KEYS ? 16 : 1];  // per warp: -lse (log2 units) and -delta of 16 pairs of columns
 
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -509,8 +513,9 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, 3 - GradTile<DP>::kGro
     uint8_t* const a2 = tiles + Tile::kOwn;
     uint8_t* const stream = tiles + 2 * Tile::kOwn;  // per stage: B1, B2
     const uint32_t bar0 = tc::smem_of(bars);
-    const uint32_t a_full = bar0, s_full = bar0 + 8, p_full = bar0 + 24, acc_done = bar0 + 40, b_full = bar0 + 56,
-                   b_free = b_full + 8 * Tile::kStages;
+    const uint32_t a_full = bar0, s_full = bar0 + 8, dp_full = bar0 + 16, p_full = bar0 + 24, ds_full = bar0 + 32, acc1_done = bar0 + 40,
+                   acc2_done = bar0 + 48, b1_full = bar0 + 56, b2_full = b1_full + 8 * kStages, b1_free = b2_full + 8 * kStages,
+                   b2_free = b1_free + 8 * kStages;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int own_heads = KEYS ? p.kv_heads : p.heads;
@@ -520,37 +525,38 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, 3 - GradTile<DP>::kGro
     const int r0 = (KEYS ? turn : own_tiles - 1 - turn) * 128;  // the longest walks of a long sequence first
     const int h = (int)(bh % own_heads), b = (int)(bh / own_heads);
     const int32_t* const pos = p.pos + (int64_t)b * p.t;
-    const int group = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;  // of the arithmetic's warps
-    const int row = r0 + quarter * 32 + lane;
+    const int part = warp >> 2, quarter = warp & 3;  // of the arithmetic's warps: which 32 columns, which 32 rows
+    const int own_row = quarter * 32 + lane, row = r0 + own_row;
 
     rows::Span span{kNever, -1};
     if (warp < kWarps) {
         span = span_of(p, pos, row, KEYS, lane);
-        if (group == 0 && half == 0) put_reach(reach_shared, quarter, lane, span);
+        if (part == 0) put_reach(reach_shared, quarter, lane, span);
         if (tid == 0) dead = junk = 0;
     } else if (warp == kWarps) {
         if (lane == 0) {
             tc::bar_init(a_full, 1);
-            for (int w = 0; w < kGroups; ++w) {
-                tc::bar_init(s_full + 8 * w, 1);
-                tc::bar_init(p_full + 8 * w, 256);
-                tc::bar_init(acc_done + 8 * w, 1);
-            }
-            for (int s = 0; s < 2 * Tile::kStages; ++s) tc::bar_init(b_full + 8 * s, 1);
+            tc::bar_init(s_full, 1);
+            tc::bar_init(dp_full, 1);
+            tc::bar_init(p_full, 32 * kWarps);
+            tc::bar_init(ds_full, 32 * kWarps);
+            tc::bar_init(acc1_done, 1);
+            tc::bar_init(acc2_done, 1);
+            for (int s = 0; s < 4 * kStages; ++s) tc::bar_init(b1_full + 8 * s, 1);
             tc::bar_init_done();
         }
     } else {
-        tc::tmem_alloc<Tile::kColumns>(tc::smem_of(&tmem_base));
+        tc::tmem_alloc<Tile::kTmem>(tc::smem_of(&tmem_base));
     }
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = tmem_base, acc1_at = tmem, acc2_at = tmem + DP, pairs_at = tmem + 2 * DP;  // S, dP of group w: + 128 w, + 64
+    const uint32_t tmem = tmem_base, acc1_at = tmem, acc2_at = tmem + DP, s_at = tmem + 2 * DP, dp_at = s_at + kColumns;
     const Reach reach = get_reach(reach_shared);
-    const int per_head = reach.hi < 0 ? 0 : (reach.hi - reach.lo) / 64 + 1;
+    const int per_head = reach.hi < 0 ? 0 : (reach.hi - reach.lo) / kColumns + 1;
     const int n = KEYS ? per_head * p.group : per_head;
-    const bool second = KEYS || n <= kExact;  // acc2 is kept
-    float eps = 0.0f;
+    const bool second = KEYS || n * kColumns <= kExact;  // acc2 is kept
+    float delta = 0.0f;
 
     if (warp == kWarps) {
         if (lane == 0 && n > 0) {
@@ -560,52 +566,67 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, 3 - GradTile<DP>::kGro
                 tc::tensor_load(tc::smem_of(a1) + x * 256, &maps.a1, x, r0, h, b, a_full);
                 tc::tensor_load(tc::smem_of(a2) + x * 256, &maps.a2, x, r0, h, b, a_full);
             }
-            int issued = 0;
-            for (int i = 0; i < n; ++i, ++issued) {
-                const int s = i % Tile::kStages;
-                if (!(ok = tc::bar_wait(b_free + 8 * s, (i / Tile::kStages + 1) & 1))) break;
-                const int j0 = reach.lo + (KEYS ? i % per_head : i) * 64, hs = KEYS ? h * p.group + i / per_head : h / p.group;
+            int issued1 = 0, issued2 = 0;
+            for (int i = 0; i < n && ok; ++i) {
+                const int s = i % kStages;
+                const uint32_t parity = (i / kStages + 1) & 1;
+                const int j0 = reach.lo + (KEYS ? i % per_head : i) * kColumns, hs = KEYS ? h * p.group + i / per_head : h / p.group;
                 const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream;
-                tc::bar_expect(b_full + 8 * s, 2 * Tile::kStream);
-                for (int x = 0; x < DP; x += 64) {
-                    tc::tensor_load(at + x * 128, &maps.b1, x, j0, hs, b, b_full + 8 * s);
-                    tc::tensor_load(at + Tile::kStream + x * 128, &maps.b2, x, j0, hs, b, b_full + 8 * s);
-                }
+                if (!(ok = tc::bar_wait(b1_free + 8 * s, parity))) break;
+                tc::bar_expect(b1_full + 8 * s, Tile::kStream);
+                for (int x = 0; x < DP; x += 64) tc::tensor_load(at + x * (2 * kColumns), &maps.b1, x, j0, hs, b, b1_full + 8 * s);
+                issued1 = i + 1;
+                if (!(ok = tc::bar_wait(b2_free + 8 * s, parity))) break;
+                tc::bar_expect(b2_full + 8 * s, Tile::kStream);
+                for (int x = 0; x < DP; x += 64)
+                    tc::tensor_load(at + Tile::kStream + x * (2 * kColumns), &maps.b2, x, j0, hs, b, b2_full + 8 * s);
+                issued2 = i + 1;
             }
             if (!ok) {  // copies in flight end before the CTA does
                 dead = 1;
                 tc::bar_wait(a_full, 0);
-                for (int i = max(0, issued - Tile::kStages); i < issued; ++i) tc::bar_wait(b_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
+                for (int i = max(0, issued1 - kStages); i < issued1; ++i) tc::bar_wait(b1_full + 8 * (i % kStages), (i / kStages) & 1);
+                for (int i = max(0, issued2 - kStages); i < issued2; ++i) tc::bar_wait(b2_full + 8 * (i % kStages), (i / kStages) & 1);
             }
         }
     } else if (warp == kWarps + 1) {
         if (n > 0) {
             const uint32_t leader = tc::elect();
-            bool ok = __all_sync(0xffffffffu, tc::bar_wait(a_full, 0));
-            auto scores = [&](int i) {
-                const int w = i % kGroups;
-                const uint32_t at = tc::smem_of(stream) + (i % Tile::kStages) * 2 * Tile::kStream, to = pairs_at + 128 * w;
-                // they take the place of the group's last P and dS: the products that read those have to be over
-                if (!__all_sync(0xffffffffu, tc::bar_wait(b_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1) &&
-                                                 (i < kGroups || tc::bar_wait(acc_done + 8 * w, (i / kGroups - 1) & 1))))
-                    return false;
-                tc::fence_after();
-                tc::product_rows<BF16, 64, DP>(leader, to, tc::smem_of(a1), at);
-                tc::product_rows<BF16, 64, DP>(leader, to + 64, tc::smem_of(a2), at + Tile::kStream);
-                tc::products_arrive(leader, s_full + 8 * w);
-                return true;
-            };
-            for (int i = 0; i < kGroups && i < n && ok; ++i) ok = scores(i);
-            for (int i = 0; i < n && ok; ++i) {
-                const int w = i % kGroups, s = i % Tile::kStages;
-                const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream, from = pairs_at + 128 * w;
-                if (!(ok = __all_sync(0xffffffffu, tc::bar_wait(p_full + 8 * w, (i / kGroups) & 1)))) break;
-                tc::fence_after();
-                tc::product_across<BF16, 64, DP>(leader, acc1_at, from + 64, at, i > 0);
-                if (second) tc::product_across<BF16, 64, DP>(leader, acc2_at, from, KEYS ? at + Tile::kStream : at, i > 0);
-                tc::products_arrive(leader, b_free + 8 * s);
-                tc::products_arrive(leader, acc_done + 8 * w);
-                if (i + kGroups < n) ok = scores(i + kGroups);
+            auto all = [](bool x) { return (bool)__all_sync(0xffffffffu, x); };
+            bool ok = all(tc::bar_wait(a_full, 0));
+            for (int i = 0; i <= n && ok; ++i) {  // acc2(i - 1), S(i), acc1(i - 1), dP(i)
+                const int s = i % kStages, sl = (i + kStages - 1) % kStages;
+                const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream, last = tc::smem_of(stream) + sl * 2 * Tile::kStream;
+                if (i > 0 && second) {
+                    if (!(ok = all(tc::bar_wait(p_full, (i - 1) & 1)))) break;
+                    tc::fence_after();
+                    tc::product_across<BF16, kColumns, DP, 32>(leader, acc2_at, s_at, KEYS ? last + Tile::kStream : last, i > 1);
+                    if (KEYS) tc::products_arrive(leader, b2_free + 8 * sl);
+                    tc::products_arrive(leader, acc2_done);
+                }
+                if (i < n) {
+                    // S's place is free when the product is over that reads the last P there, or when the last S has been read
+                    if (!(ok = all(tc::bar_wait(b1_full + 8 * s, (i / kStages) & 1) &&
+                                   (i == 0 || tc::bar_wait(second ? acc2_done : p_full, (i - 1) & 1)))))
+                        break;
+                    tc::fence_after();
+                    tc::product_rows<BF16, kColumns, DP>(leader, s_at, tc::smem_of(a1), at);
+                    tc::products_arrive(leader, s_full);
+                }
+                if (i > 0) {
+                    if (!(ok = all(tc::bar_wait(ds_full, (i - 1) & 1)))) break;
+                    tc::fence_after();
+                    tc::product_across<BF16, kColumns, DP, 32>(leader, acc1_at, dp_at, last, i > 1);
+                    tc::products_arrive(leader, b1_free + 8 * sl);
+                    tc::products_arrive(leader, acc1_done);
+                }
+                if (i < n) {
+                    if (!(ok = all(tc::bar_wait(b2_full + 8 * s, (i / kStages) & 1) && (i == 0 || tc::bar_wait(acc1_done, (i - 1) & 1))))) break;
+                    tc::fence_after();
+                    tc::product_rows<BF16, kColumns, DP>(leader, dp_at, tc::smem_of(a2), at + Tile::kStream);
+                    if (!KEYS) tc::products_arrive(leader, b2_free + 8 * s);
+                    tc::products_arrive(leader, dp_full);
+                }
             }
             if (!ok) {
                 dead = 1;
@@ -615,12 +636,9 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, 3 - GradTile<DP>::kGro
         }
     } else {
         const uint32_t lanes = (uint32_t)quarter << 21;
-        const uint32_t pair_at = pairs_at + 128 * group + lanes;
-        const int wtid = tid & 255;
         bool found = false;
-        float delta = 0.0f;
-        Two lse2 = zero(), delta2, eps2 = zero();  // of this row, negative
-        if (!KEYS && row < p.t) {  // this row's statistics
+        Two lse2 = zero(), eps2 = zero();  // lse and delta of this row, negative
+        if (!KEYS && row < p.t) {          // this row's statistics
             const int64_t at = ((int64_t)b * p.heads + h) * p.t + row;
             const float lse = minus_lse(p.lse[at]);
             lse2 = two(lse, lse);
@@ -635,94 +653,117 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, 3 - GradTile<DP>::kGro
                 for (int e = 0; e < 8; ++e) delta = fmaf(to_float(xe[e]), to_float(ye[e]), delta);
             }
         }
-        delta2 = two(-delta, -delta);
-        for (int i = group; i < n; i += kGroups) {
-            const int j0 = reach.lo + (KEYS ? i % per_head : i) * 64;
+        const Two delta2 = two(-delta, -delta);
+        // junk in a tile that is hidden from some row must not reach the products
+        auto scan = [&](uint32_t full, int i, int which, int j0) {
+            if (j0 >= reach.all_lo && j0 + kColumns - 1 <= reach.all_hi) return;
+            if (!tc::bar_wait(full + 8 * (i % kStages), (i / kStages) & 1)) dead = 1;
+            found |= scan_tile<BF16, kColumns, DP, 32 * kWarps>(p, pos, stream + ((i % kStages) * 2 + which) * Tile::kStream, j0, tid);
+            tc::writes_to_async();
+        };
+        for (int i = 0; i < n; ++i) {
+            const int j0 = reach.lo + (KEYS ? i % per_head : i) * kColumns, mine0 = j0 + 32 * part;  // the tile's and this warp's first column
             const int hq = KEYS ? h * p.group + i / per_head : h;
             const Modifier modify(p, hq);
             if (KEYS) {  // statistics of this warp's 32 columns
-                const int64_t at = ((int64_t)b * p.heads + hq) * p.t + j0 + 32 * half + lane;
-                const bool in = j0 + 32 * half + lane < p.t;
+                const int64_t at = ((int64_t)b * p.heads + hq) * p.t + mine0 + lane;
+                const bool in = mine0 + lane < p.t;
                 __syncwarp();
                 float* const st = reinterpret_cast<float*>(&column_stats[KEYS ? warp : 0][KEYS ? lane / 2 : 0]) + (lane & 1);
                 st[0] = in ? minus_lse(p.lse[at]) : 0.0f;
                 st[2] = in ? -p.delta[at] : 0.0f;
                 __syncwarp();
             }
-            if (!__all_sync(0xffffffffu, tc::bar_wait(s_full + 8 * group, (i / kGroups) & 1))) {
+            const bool clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 31);
+            const uint32_t mask = clear ? 0xffffffffu : column_mask(span.lo - mine0, span.hi - mine0);
+            if (!__all_sync(0xffffffffu, tc::bar_wait(s_full, i & 1))) {
                 dead = 1;
                 break;
             }
             tc::fence_after();
-            const int mine0 = j0 + 32 * half;  // this warp's first column
-            const bool clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 31);
-            const Two by2 = two(modify.by, modify.by);
+            float w[32], in[MOD ? 32 : 1];  // P, inner
             {
-                uint32_t s[32], d[32], pw[16], dw[16];
-                tc::tmem_load(s, pair_at + 32 * half);
-                tc::tmem_load(d, pair_at + 64 + 32 * half);
+                uint32_t s[32];
+                tc::tmem_load(s, s_at + lanes + 32 * part);
                 tc::tmem_loaded();
                 tc::settle(s);
-                tc::settle(d);
-                auto tile = [&](auto masked) {
-                    constexpr bool kMasked = decltype(masked)::value;
-                    const uint32_t mask = kMasked ? column_mask(span.lo - mine0, span.hi - mine0) : 0xffffffffu;
+                if (!second) {  // S has been read
+                    tc::fence_before();
+                    tc::bar_arrive(p_full);
+                }
+                const Two by2 = two(modify.by, modify.by);
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        Two lse_here = lse2, delta_here = delta2;
-                        if (KEYS) {
-                            const float4 stats = column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0];
-                            lse_here = two(stats.x, stats.y);
-                            delta_here = two(stats.z, stats.w);
-                        }
-                        const Two raw = two(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-                        float2 x, inner = make_float2(1.0f, 1.0f);
-                        if (MOD) {
-                            x.x = modify(one(raw).x, (float)(row - mine0 - e), inner.x);
-                            x.y = modify(one(raw).y, (float)(row - mine0 - e - 1), inner.y);
-                            x = one(two(x.x, x.y) + lse_here);
-                        } else {
-                            x = one(fma(raw, by2, lse_here));
-                        }
-                        Two w = two(tc::exp2_fast(x.x), tc::exp2_fast(x.y));
-                        Two g = w * (two(__uint_as_float(d[e]), __uint_as_float(d[e + 1])) + delta_here);
-                        if (kMasked) {
-                            const bool s0 = (mask >> e) & 1, s1 = (mask >> (e + 1)) & 1;
-                            w = two(s0 ? one(w).x : 0.0f, s1 ? one(w).y : 0.0f);
-                            g = two(s0 ? one(g).x : 0.0f, s1 ? one(g).y : 0.0f);
-                            if (MOD) inner = make_float2(s0 ? inner.x : 0.0f, s1 ? inner.y : 0.0f);
-                        }
-                        if (!KEYS) eps2 = eps2 + g;
-                        if (MOD) {
-                            g = g * two(inner.x, inner.y);
-                            if (!KEYS) w = w * two(inner.x, inner.y);
-                        }
-                        pw[e / 2] = tc::pack<BF16>(one(w).x, one(w).y);
-                        dw[e / 2] = tc::pack<BF16>(one(g).x, one(g).y);
+                for (int e = 0; e < 32; e += 2) {
+                    Two lse_here = lse2;
+                    if (KEYS) {
+                        const float2 l = *reinterpret_cast<const float2*>(&column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0]);
+                        lse_here = two(l.x, l.y);
                     }
-                };
-                if (clear)
-                    tile(std::false_type());
+                    const float s0 = __uint_as_float(s[e]), s1 = __uint_as_float(s[e + 1]);
+                    float2 x;
+                    if (MOD) {
+                        x.x = modify(s0, (float)(row - mine0 - e), in[MOD ? e : 0]);
+                        x.y = modify(s1, (float)(row - mine0 - e - 1), in[MOD ? e + 1 : 0]);
+                        x = one(two(x.x, x.y) + lse_here);
+                    } else {
+                        x = one(fma(two(s0, s1), by2, lse_here));
+                    }
+                    w[e] = tc::exp2_fast(x.x);
+                    w[e + 1] = tc::exp2_fast(x.y);
+                }
+            }
+            if (!clear) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    w[e] = (mask >> e) & 1 ? w[e] : 0.0f;
+                    if (MOD) in[MOD ? e : 0] = (mask >> e) & 1 ? in[MOD ? e : 0] : 0.0f;
+                }
+            }
+            if (second) {
+                uint32_t pw[16];
+#pragma unroll
+                for (int e = 0; e < 32; e += 2)
+                    pw[e / 2] = MOD && !KEYS ? tc::pack<BF16>(w[e] * in[MOD ? e : 0], w[e + 1] * in[MOD ? e + 1 : 0]) : tc::pack<BF16>(w[e], w[e + 1]);
+                tc::tmem_store16(s_at + lanes + 32 * part, pw);  // over the scores they were made from
+                if (KEYS)
+                    scan(b2_full, i, 1, j0);
                 else
-                    tile(std::true_type());
-                if (second) tc::tmem_store16(pair_at + 32 * half, pw);  // over the scores they were made from
-                tc::tmem_store16(pair_at + 64 + 32 * half, dw);
+                    scan(b1_full, i, 0, j0);
+                tc::tmem_stored();
+                tc::fence_before();
+                tc::bar_arrive(p_full);
             }
-            if (j0 < reach.all_lo || j0 + 63 > reach.all_hi) {  // hidden from some row: no junk may reach the products
-                const int st = i % Tile::kStages;
-                uint8_t* const at = stream + st * 2 * Tile::kStream;
-                if (!tc::bar_wait(b_full + 8 * st, (i / Tile::kStages) & 1)) dead = 1;
-                found |= scan_tile<BF16, 64, DP, 256>(p, pos, at, j0, wtid);
-                if (KEYS) found |= scan_tile<BF16, 64, DP, 256>(p, pos, at + Tile::kStream, j0, wtid);
-                tc::writes_to_async();
+            if (!__all_sync(0xffffffffu, tc::bar_wait(dp_full, i & 1))) {
+                dead = 1;
+                break;
             }
+            tc::fence_after();
+            uint32_t d[32], dw[16];
+            tc::tmem_load(d, dp_at + lanes + 32 * part);
+            tc::tmem_loaded();
+            tc::settle(d);
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+                Two delta_here = delta2;
+                if (KEYS) {
+                    const float2 l = *(reinterpret_cast<const float2*>(&column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0]) + 1);
+                    delta_here = two(l.x, l.y);
+                }
+                Two g = two(__uint_as_float(d[e]), __uint_as_float(d[e + 1])) + delta_here;
+                if (!clear) g = two((mask >> e) & 1 ? one(g).x : 0.0f, (mask >> (e + 1)) & 1 ? one(g).y : 0.0f);  // (may be NaN)
+                g = two(w[e], w[e + 1]) * g;
+                if (!KEYS) eps2 = eps2 + g;
+                if (MOD) g = g * two(in[MOD ? e : 0], in[MOD ? e + 1 : 0]);
+                dw[e / 2] = tc::pack<BF16>(one(g).x, one(g).y);
+            }
+            tc::tmem_store16(dp_at + lanes + 32 * part, dw);
+            if (KEYS || !second) scan(b1_full, i, 0, j0);
             tc::tmem_stored();
             tc::fence_before();
-            tc::bar_arrive(p_full + 8 * group);
+            tc::bar_arrive(ds_full);
         }
         if (found) junk = 1;
-        if (!KEYS) eps_shared[warp >> 2][quarter * 32 + lane] = one(eps2).x + one(eps2).y;
-        if (!KEYS) eps = delta;  // kept for the end
+        if (!KEYS) eps_shared[part][own_row] = one(eps2).x + one(eps2).y;
     }
     __syncthreads();
     const bool good = !dead && !junk;
@@ -739,18 +780,16 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, 3 - GradTile<DP>::kGro
     } else if (warp < kWarps) {
         const uint32_t lanes = (uint32_t)quarter << 21;
         const bool empty = span.lo > span.hi;
-        if (n > 0 && !tc::bar_wait(acc_done + 8 * ((n - 1) % kGroups), ((n - 1) / kGroups) & 1)) atomicAdd(&g_timeouts, 1u);
+        if (n > 0 && !tc::bar_wait(acc1_done, (n - 1) & 1)) atomicAdd(&g_timeouts, 1u);
         tc::fence_after();
-        const int own_row = quarter * 32 + lane;
         float off = 0.0f;
         if (!KEYS) {
-            const float delta = eps;
-            for (int k = 0; k < 2 * kGroups; ++k) off += eps_shared[k][own_row];
-            if (group == 0 && half == 0 && row < p.t) p.delta[((int64_t)b * p.heads + h) * p.t + row] = empty ? 0.0f : delta + off;
+            for (int k = 0; k < kColumns / 32; ++k) off += eps_shared[k][own_row];
+            if (part == 0 && row < p.t) p.delta[((int64_t)b * p.heads + h) * p.t + row] = empty ? 0.0f : delta + off;
         }
         // chunks of 32 columns of dq, or of dk and then dv, are shared out among the warps of a row
 #pragma unroll
-        for (int k = warp >> 2; k < (KEYS ? 2 : 1) * DP / 32; k += 2 * kGroups) {
+        for (int k = part; k < (KEYS ? 2 : 1) * DP / 32; k += kColumns / 32) {
             const bool dv = KEYS && k >= DP / 32;
             const int c = dv ? k - DP / 32 : k;
             uint32_t o[32], o2[32] = {};
@@ -775,7 +814,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, 3 - GradTile<DP>::kGro
     tc::fence_before();
     __syncthreads();
     if (warp == kWarps + 1) {
-        tc::tmem_free<Tile::kColumns>(tmem);
+        tc::tmem_free<Tile::kTmem>(tmem);
     } else if (good && lane == 0 && warp < (KEYS ? 2 : 1) * DP / 16) {  // four warps per 64 columns of dq, or of dk and then dv
         const int k = warp >> 2, x = k % (DP / 64) * 64, at_row = r0 + quarter * 32;
         const bool dv = k >= DP / 64;
@@ -849,7 +888,8 @@ cudaError_t gradient(const AttnParams& p, const AttnTensors<typename Element<BF1
     GradMaps m;
     const int own = KEYS ? p.kv_heads : p.heads, other = KEYS ? p.heads : p.kv_heads;
     bool ok = make_map(&m.a1, p, BF16, KEYS ? a.k : a.q, own, 128) && make_map(&m.a2, p, BF16, KEYS ? a.v : a.dout, own, 128) &&
-              make_map(&m.b1, p, BF16, KEYS ? a.q : a.k, other, 64) && make_map(&m.b2, p, BF16, KEYS ? a.dout : a.v, other, 64) &&
+              make_map(&m.b1, p, BF16, KEYS ? a.q : a.k, other, GradTile<DP>::kColumns) &&
+              make_map(&m.b2, p, BF16, KEYS ? a.dout : a.v, other, GradTile<DP>::kColumns) &&
               make_map(&m.o1, p, BF16, KEYS ? a.dk : a.dq, own, 32) && make_map(&m.o2, p, BF16, KEYS ? a.dv : a.dq, own, 32);
     const int64_t grid = p.blocks * own * ((p.t + 127) / 128);
     if (!ok || grid > 0x7fffffffLL) return cudaErrorInvalidValue;

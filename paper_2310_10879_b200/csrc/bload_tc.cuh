@@ -198,16 +198,16 @@ __device__ __forceinline__ void product_rows(uint32_t leader, uint32_t d, uint32
         product(leader, d, rows_desc(a + (k / 4) * (128 * 128) + (k % 4) * 32), rows_desc(b + (k / 4) * (N * 128) + (k % 4) * 32),
                 product_shape<BF16, N, false>(), k > 0);
 }
-// D[128, DP] (+)= A[128, K] B[K, DP]: B's K rows in shared memory; A in tensor memory, two elements per column, in two halves
-// that are K / 2 columns apart (each lies at the start of the scores it was made from)
-template <bool BF16, int K, int DP>
+// D[128, DP] (+)= A[128, K] B[K, DP]: B's K rows in shared memory; A in tensor memory, two elements per column, PIECE elements
+// at the start of every PIECE columns (each piece over the scores it was made from)
+template <bool BF16, int K, int DP, int PIECE>
 __device__ __forceinline__ void product_across(uint32_t leader, uint32_t d, uint32_t a, uint32_t b, bool add)
 {
-    constexpr int kHalf = K / 32;  // steps of 16 in a half
+    constexpr int kSteps = PIECE / 16;
 #pragma unroll
     for (int k = 0; k < K / 16; ++k)
-        product_tmem(leader, d, a + (k / kHalf) * (K / 2) + (k % kHalf) * 8, across_desc(b + k * (16 * 128), K * 128), product_shape<BF16, DP, true>(),
-                     add || k > 0);
+        product_tmem(leader, d, a + (k / kSteps) * PIECE + (k % kSteps) * 8, across_desc(b + k * (16 * 128), K * 128),
+                     product_shape<BF16, DP, true>(), add || k > 0);
 }
 
 // ---- arithmetic ---------------------------------------------------------------------------------------------------
