@@ -492,7 +492,7 @@ struct GradTile {
 // acc1(n) and dP(n + 1) run, P(n + 1) is made from S(n + 1); while acc2 and the next S run, dS from dP.  (Two groups of warps with
 // tiles of 64 columns each, taking turns, kept the tensor cores at 41 %: with 64 columns a product reads 192 bytes of shared
 // memory per cycle where there are 128, and what it reads of A serves half as many columns.)
-constexpr int kExact = 1 << 20;
+constexpr int kExact = 1024;
 
 template <bool BF16, int DP, bool MOD, bool KEYS>
 __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
