@@ -328,9 +328,10 @@ __global__ void __launch_bounds__(320, 2)
             // for the exponentials: 64 of them would not stay in this thread's registers.  What changes them is written back.
             const uint32_t own_at = s_at + lanes + 64 * half;
             const bool clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 63);
+            const bool blind = __all_sync(0xffffffffu, span.lo > mine0 + 63 || span.hi < mine0);  // none of these columns is seen
             float top = -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            for (int c = 0; c < 2 && !blind; ++c) {
                 uint32_t s[32];
                 tc::tmem_load(s, own_at + 32 * c);
                 tc::tmem_loaded();
@@ -386,8 +387,13 @@ __global__ void __launch_bounds__(320, 2)
             const float off = m == -INFINITY ? 0.0f : -m;
             const Two by2 = two(by, by), off2 = two(off, off);
             Two sum[2] = {zero(), zero()};
+            if (blind) {
+                const uint32_t none[16] = {};
+                tc::tmem_store16(own_at, none);
+                tc::tmem_store16(own_at + 16, none);
+            }
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            for (int c = 0; c < 2 && !blind; ++c) {
                 uint32_t s[32], w[16];
                 tc::tmem_load(s, own_at + 32 * c);
                 tc::tmem_loaded();
@@ -505,7 +511,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     __shared__ uint32_t tmem_base;
     __shared__ int dead, junk;
     __shared__ ReachShared<4> reach_shared;
-    __shared__ float eps_shared[kColumns / 32][128];
+    __shared__ float eps_shared[kColumns / 32][128], delta_shared[KEYS ? 1 : kColumns / 32][128];
     __shared__ float4 column_stats[KEYS ? kWarps : 1][KEYS ? 16 : 1];  // per warp: -lse (log2 units) and -delta of 16 pairs of columns
 
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -533,6 +539,28 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         span = span_of(p, pos, row, KEYS, lane);
         if (part == 0) put_reach(reach_shared, quarter, lane, span);
         if (tid == 0) dead = junk = 0;
+        if (!KEYS) {  // dout . out: the warps of a row share out its elements
+            float sum = 0.0f;
+            if (row < p.t) {
+                using E = typename Element<BF16>::type;
+                const E* const o = a.out_in.at(b, row, h);
+                const E* const g = a.dout.at(b, row, h);
+                constexpr int kEach = 4 * DP / kColumns;  // of 16 bytes
+                uint4 x[kEach], y[kEach];
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) {
+                    const int e = (part * kEach + k) * 8;
+                    x[k] = e < p.d ? *reinterpret_cast<const uint4*>(o + e) : make_uint4(0, 0, 0, 0);
+                    y[k] = e < p.d ? *reinterpret_cast<const uint4*>(g + e) : make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int k = 0; k < kEach; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        sum = fmaf(to_float(reinterpret_cast<const E*>(&x[k])[e]), to_float(reinterpret_cast<const E*>(&y[k])[e]), sum);
+            }
+            delta_shared[part][own_row] = sum;
+        }
     } else if (warp == kWarps) {
         if (lane == 0) {
             tc::bar_init(a_full, 1);
@@ -639,19 +667,9 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         bool found = false;
         Two lse2 = zero(), eps2 = zero();  // lse and delta of this row, negative
         if (!KEYS && row < p.t) {          // this row's statistics
-            const int64_t at = ((int64_t)b * p.heads + h) * p.t + row;
-            const float lse = minus_lse(p.lse[at]);
+            const float lse = minus_lse(p.lse[((int64_t)b * p.heads + h) * p.t + row]);
             lse2 = two(lse, lse);
-            const uint4* o = reinterpret_cast<const uint4*>(a.out_in.at(b, row, h));
-            const uint4* g = reinterpret_cast<const uint4*>(a.dout.at(b, row, h));
-            using T2 = typename Element<BF16>::type;
-            for (int c = 0; c < p.d / 8; ++c) {
-                const uint4 x = o[c], y = g[c];
-                const T2* xe = reinterpret_cast<const T2*>(&x);
-                const T2* ye = reinterpret_cast<const T2*>(&y);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) delta = fmaf(to_float(xe[e]), to_float(ye[e]), delta);
-            }
+            for (int k = 0; k < kColumns / 32; ++k) delta += delta_shared[KEYS ? 0 : k][own_row];
         }
         const Two delta2 = two(-delta, -delta);
         // junk in a tile that is hidden from some row must not reach the products
