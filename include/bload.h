@@ -505,7 +505,7 @@ typedef struct {
  * Elements from rot_dim on, and padding slots, are copied.  d_inv_freq (float[n], device) holds base^(-2 i / rot_dim)
  * or any stretched form of it for long contexts; `factor` is the scale some of those apply to the rotated part.
  * bload_rotary_grad is the gradient: it takes dy as `x` and writes dx to `y` (the same turn by -a_i).
- * y may be x itself (same data and strides).  rot_dim is even, 0 <= rot_dim <= head_dim; heads >= 1, head_dim >= 1.
+ * y may be x itself (same data and strides).  rot_dim is even, 0 <= rot_dim <= head_dim; heads and head_dim in [1, 4096].
  * Errors: NULL, ARG (sizes, rot_dim, strides < 0, a broadcast y), ALIGN (data not aligned to the element),
  * UNSUPPORTED (dtype, t_block), CUDA.
  */

@@ -59,7 +59,7 @@ int rotary(const int32_t* d_pos, int64_t block_count, int32_t t_block, int32_t h
     if (!x || !y) return BLOAD_ERR_NULL;
     int rc = check_common(block_count, t_block, dtype, d_pos);
     if (rc) return rc;
-    if (heads < 1 || head_dim < 1 || head_dim > (1 << 20) || rot_dim < 0 || rot_dim > head_dim || (rot_dim & 1) || !isfinite(factor))
+    if (heads < 1 || heads > 4096 || head_dim < 1 || head_dim > 4096 || rot_dim < 0 || rot_dim > head_dim || (rot_dim & 1) || !isfinite(factor))
         return BLOAD_ERR_ARG;
     if (block_count == 0) return BLOAD_OK;
     if (rot_dim && !d_inv_freq) return BLOAD_ERR_NULL;
