@@ -142,7 +142,7 @@ __device__ __forceinline__ float minus_lse(float lse) { return lse == -INFINITY 
 // Scans a tile [ROWS][DP] in shared memory with THREADS threads for infinities and NaN.  Those on padding (or behind the
 // block's last slot, where copies fill in zeros anyway) are cleared; true if a frame holds one.
 template <bool BF16, int ROWS, int DP, int THREADS>
-__device__ __forceinline__ bool scan_tile(const AttnParams& p, const int32_t* pos, uint8_t* tile, int row0, int tid)
+__device__ __noinline__ bool scan_tile(const AttnParams& p, const int32_t* pos, uint8_t* tile, int row0, int tid)
 {
     uint32_t acc = 0;
     constexpr int kChunks = ROWS * DP / 8 / THREADS;
@@ -243,6 +243,8 @@ __global__ void __launch_bounds__(320, 2)
             tc::bar_init(o_done, 1);
             for (int s = 0; s < 4 * Tile::kStages; ++s) tc::bar_init(k_full + 8 * s, 1);
             tc::bar_init_done();
+            tc::bar_expect(q_full, Tile::kTile);  // under way while the rows look for their keys
+            for (int x = 0; x < DP; x += 64) tc::tensor_load(tc::smem_of(q_tile) + x * 256, &maps.q, x, i0, h, b, q_full);
         }
     } else {
         tc::tmem_alloc<256>(tc::smem_of(&tmem_base));
@@ -256,10 +258,9 @@ __global__ void __launch_bounds__(320, 2)
     float m = -INFINITY, l = 0.0f;  // running maximum (log2 units; may lag by kLag) and sum
 
     if (warp == 8) {
-        if (lane == 0 && n > 0) {
+        if (lane == 0) {
             bool ok = true;
-            tc::bar_expect(q_full, Tile::kTile);
-            for (int x = 0; x < DP; x += 64) tc::tensor_load(tc::smem_of(q_tile) + x * 256, &maps.q, x, i0, h, b, q_full);
+            if (n == 0) ok = tc::bar_wait(q_full, 0);  // (its place is written to below)
             int issued = 0;
             for (int i = 0; i < n && ok; ++i, ++issued) {
                 const int s = i % Tile::kStages;
@@ -572,6 +573,11 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
             tc::bar_init(acc2_done, 1);
             for (int s = 0; s < 4 * kStages; ++s) tc::bar_init(b1_full + 8 * s, 1);
             tc::bar_init_done();
+            tc::bar_expect(a_full, 2 * Tile::kOwn);  // under way while the rows look for their columns
+            for (int x = 0; x < DP; x += 64) {
+                tc::tensor_load(tc::smem_of(a1) + x * 256, &maps.a1, x, r0, h, b, a_full);
+                tc::tensor_load(tc::smem_of(a2) + x * 256, &maps.a2, x, r0, h, b, a_full);
+            }
         }
     } else {
         tc::tmem_alloc<Tile::kTmem>(tc::smem_of(&tmem_base));
@@ -587,13 +593,9 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     float delta = 0.0f;
 
     if (warp == kWarps) {
-        if (lane == 0 && n > 0) {
+        if (lane == 0) {
             bool ok = true;
-            tc::bar_expect(a_full, 2 * Tile::kOwn);
-            for (int x = 0; x < DP; x += 64) {
-                tc::tensor_load(tc::smem_of(a1) + x * 256, &maps.a1, x, r0, h, b, a_full);
-                tc::tensor_load(tc::smem_of(a2) + x * 256, &maps.a2, x, r0, h, b, a_full);
-            }
+            if (n == 0) ok = tc::bar_wait(a_full, 0);  // (their place is written to below)
             int issued1 = 0, issued2 = 0;
             for (int i = 0; i < n && ok; ++i) {
                 const int s = i % kStages;
@@ -699,6 +701,27 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 break;
             }
             tc::fence_after();
+            if (__all_sync(0xffffffffu, mask == 0)) {  // nothing of this block of 32 x 32 is seen
+                const uint32_t none[16] = {};
+                if (second) {
+                    tc::tmem_store16(s_at + lanes + 32 * part, none);
+                    scan(KEYS ? b2_full : b1_full, i, KEYS ? 1 : 0, j0);
+                    tc::tmem_stored();
+                    tc::fence_before();
+                }
+                tc::bar_arrive(p_full);
+                if (!__all_sync(0xffffffffu, tc::bar_wait(dp_full, i & 1))) {
+                    dead = 1;
+                    break;
+                }
+                tc::fence_after();
+                tc::tmem_store16(dp_at + lanes + 32 * part, none);
+                if (KEYS || !second) scan(b1_full, i, 0, j0);
+                tc::tmem_stored();
+                tc::fence_before();
+                tc::bar_arrive(ds_full);
+                continue;
+            }
             float w[32], in[MOD ? 32 : 1];  // P, inner
             {
                 uint32_t s[32];
@@ -743,10 +766,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 for (int e = 0; e < 32; e += 2)
                     pw[e / 2] = MOD && !KEYS ? tc::pack<BF16>(w[e] * in[MOD ? e : 0], w[e + 1] * in[MOD ? e + 1 : 0]) : tc::pack<BF16>(w[e], w[e + 1]);
                 tc::tmem_store16(s_at + lanes + 32 * part, pw);  // over the scores they were made from
-                if (KEYS)
-                    scan(b2_full, i, 1, j0);
-                else
-                    scan(b1_full, i, 0, j0);
+                scan(KEYS ? b2_full : b1_full, i, KEYS ? 1 : 0, j0);
                 tc::tmem_stored();
                 tc::fence_before();
                 tc::bar_arrive(p_full);
