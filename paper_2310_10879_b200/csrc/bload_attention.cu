@@ -142,7 +142,7 @@ __device__ __forceinline__ float minus_lse(float lse) { return lse == -INFINITY 
 // Scans a tile [ROWS][DP] in shared memory with THREADS threads for infinities and NaN.  Those on padding (or behind the
 // block's last slot, where copies fill in zeros anyway) are cleared; true if a frame holds one.
 template <bool BF16, int ROWS, int DP, int THREADS>
-__device__ __noinline__ bool scan_tile(const AttnParams& p, const int32_t* pos, uint8_t* tile, int row0, int tid)
+__device__ __forceinline__ bool scan_tile(const AttnParams& p, const int32_t* pos, uint8_t* tile, int row0, int tid)
 {
     uint32_t acc = 0;
     constexpr int kChunks = ROWS * DP / 8 / THREADS;
@@ -167,6 +167,12 @@ __device__ __noinline__ bool scan_tile(const AttnParams& p, const int32_t* pos, 
     return found;
 }
 
+template <bool BF16, int ROWS, int DP, int THREADS>
+__device__ __noinline__ bool scan_tile_apart(const AttnParams& p, const int32_t* pos, uint8_t* tile, int row0, int tid)
+{
+    return scan_tile<BF16, ROWS, DP, THREADS>(p, pos, tile, row0, tid);
+}
+
 // 32 columns of a row in tensor memory, times `by`, to 64 bytes of a staged output tile (128-byte rows, swizzled)
 template <bool BF16>
 __device__ __forceinline__ void stage_columns(uint8_t* tile, int row, int column, const float (&x)[32])
@@ -185,37 +191,42 @@ __device__ __forceinline__ void stage_columns(uint8_t* tile, int row, int column
 // ---- forward ------------------------------------------------------------------------------------------------------
 
 struct ForwardMaps {
-    CUtensorMap q, k, v, out;  // boxes of 128, 128, 128, 32 rows by 64 elements
+    CUtensorMap q, k, v, out;  // boxes of 128, kKeys, kKeys, 32 rows by 64 elements
 };
 
 template <int DP>
 struct ForwardTile {
-    static constexpr int kKeys = 128;
+    static constexpr int kHalves = DP / 64;  // warps that share 32 rows, with 64 columns each
+    static constexpr int kKeys = 64 * kHalves, kWarps = 4 * kHalves, kThreads = 32 * kWarps + 64;
     static constexpr int kStages = DP == 64 ? 2 : 1;
-    static constexpr int kTile = 128 * DP * 2;  // bytes of a tile of 128 rows
-    static constexpr int kShared = kTile * (1 + 2 * kStages) + 1024;
+    static constexpr int kQueries = 128 * DP * 2, kTile = kKeys * DP * 2;  // bytes
+    static constexpr int kShared = kQueries + 2 * kStages * kTile + 1024;
+    static constexpr int kTmem = DP + kKeys, kCtas = 512 / kTmem;  // per SM
 };
 
-// Warps 0 to 7 have the queries' arithmetic: warp w and warp w + 4 the same 32 rows, a row per lane, each half of the columns
-// (with one warp per row the tensor cores were busy 31 % of the time: too few warps to hide the latency of their own steps).
-// Scores come from tensor memory, P goes back over them; the two halves of a row agree on its maximum through shared memory,
-// each keeps its own sum.  Warp 8 copies tiles in, warp 9 issues the products.  256 of the 512 columns of tensor memory and less
-// than half of the shared memory, so that two CTAs share an SM and one's products run under the other's exponentials.
+// Heads of up to 128 elements: tiles of 128 keys, two CTAs per SM.  Warps 0 to 7 have the queries' arithmetic: warp w and warp w + 4
+// the same 32 rows, a row per lane, each half of the columns (with one warp per row the tensor cores were busy 31 % of the time:
+// too few warps to hide the latency of their own steps).  The two halves of a row agree on its maximum through shared memory,
+// each keeps its own sum.  Heads of up to 64: tiles of 64 keys, four warps, four CTAs per SM (short sequences leave a CTA with
+// two or three tiles between its first copies and its last store, so it pays to have more of them).
+// Scores come from tensor memory, P goes back over them.  Two more warps copy tiles in and issue the products.  The CTAs of an SM
+// share its tensor memory evenly, so one's products run under the others' exponentials.
 template <bool BF16, int DP, bool MOD>
-__global__ void __launch_bounds__(320, 2)
+__global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kCtas)
     k29_attention(const AttnParams p, const AttnTensors<typename Element<BF16>::type> a, const __grid_constant__ ForwardMaps maps)
 {
     using Tile = ForwardTile<DP>;
+    constexpr int kHalves = Tile::kHalves, kKeys = Tile::kKeys, kWarps = Tile::kWarps;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[3 + 4 * Tile::kStages + 1];
     __shared__ uint32_t tmem_base;
     __shared__ int dead, junk;
     __shared__ ReachShared<4> reach_shared;
-    __shared__ float halves[2][2][128];  // [turn][half][row]: maxima, and in the end sums
+    __shared__ float halves[2][kHalves][128];  // [turn][half][row]: maxima, and in the end sums
 
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* const q_tile = tiles;
-    uint8_t* const k_tiles = tiles + Tile::kTile;
+    uint8_t* const k_tiles = tiles + Tile::kQueries;
     uint8_t* const v_tiles = k_tiles + Tile::kStages * Tile::kTile;
     const uint32_t bar0 = tc::smem_of(bars);
     const uint32_t q_full = bar0, s_full = bar0 + 8, p_full = bar0 + 16, o_done = bar0 + 24, k_full = bar0 + 32,
@@ -227,37 +238,37 @@ __global__ void __launch_bounds__(320, 2)
     const int i0 = (q_tiles - 1 - (int)(blockIdx.x / (p.blocks * p.heads))) * 128;  // the longest rows of a long sequence first
     const int h = (int)(bh % p.heads), hk = h / p.group, b = (int)(bh / p.heads);
     const int32_t* const pos = p.pos + (int64_t)b * p.t;
-    const int half = warp >> 2, quarter = warp & 3;  // of warps 0 to 7
+    const int half = warp >> 2, quarter = warp & 3;  // of the arithmetic's warps
     const int own_row = quarter * 32 + lane, row = i0 + own_row;
 
     rows::Span span{kNever, -1};
-    if (warp < 8) {
+    if (warp < kWarps) {
         span = span_of(p, pos, row, false, lane);
         if (half == 0) put_reach(reach_shared, quarter, lane, span);
         if (tid == 0) dead = junk = 0;
-    } else if (warp == 8) {
+    } else if (warp == kWarps) {
         if (lane == 0) {
             tc::bar_init(q_full, 1);
             tc::bar_init(s_full, 1);
-            tc::bar_init(p_full, 256);
+            tc::bar_init(p_full, 32 * kWarps);
             tc::bar_init(o_done, 1);
             for (int s = 0; s < 4 * Tile::kStages; ++s) tc::bar_init(k_full + 8 * s, 1);
             tc::bar_init_done();
-            tc::bar_expect(q_full, Tile::kTile);  // under way while the rows look for their keys
+            tc::bar_expect(q_full, Tile::kQueries);  // under way while the rows look for their keys
             for (int x = 0; x < DP; x += 64) tc::tensor_load(tc::smem_of(q_tile) + x * 256, &maps.q, x, i0, h, b, q_full);
         }
     } else {
-        tc::tmem_alloc<256>(tc::smem_of(&tmem_base));
+        tc::tmem_alloc<Tile::kTmem>(tc::smem_of(&tmem_base));
     }
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = tmem_base, o_at = tmem, s_at = tmem + 128;
+    const uint32_t tmem = tmem_base, o_at = tmem, s_at = tmem + DP;
     const Reach reach = get_reach(reach_shared);
-    const int n = reach.hi < 0 ? 0 : (reach.hi - reach.lo) / Tile::kKeys + 1;
+    const int n = reach.hi < 0 ? 0 : (reach.hi - reach.lo) / kKeys + 1;
     float m = -INFINITY, l = 0.0f;  // running maximum (log2 units; may lag by kLag) and sum
 
-    if (warp == 8) {
+    if (warp == kWarps) {
         if (lane == 0) {
             bool ok = true;
             if (n == 0) ok = tc::bar_wait(q_full, 0);  // (its place is written to below)
@@ -265,18 +276,18 @@ __global__ void __launch_bounds__(320, 2)
             for (int i = 0; i < n && ok; ++i, ++issued) {
                 const int s = i % Tile::kStages;
                 const uint32_t parity = (i / Tile::kStages + 1) & 1;
-                const int j0 = reach.lo + i * Tile::kKeys;
+                const int j0 = reach.lo + i * kKeys;
                 if (!(ok = tc::bar_wait(k_free + 8 * s, parity))) break;
                 tc::bar_expect(k_full + 8 * s, Tile::kTile);
                 for (int x = 0; x < DP; x += 64)
-                    tc::tensor_load(tc::smem_of(k_tiles) + s * Tile::kTile + x * 256, &maps.k, x, j0, hk, b, k_full + 8 * s);
+                    tc::tensor_load(tc::smem_of(k_tiles) + s * Tile::kTile + x * (2 * kKeys), &maps.k, x, j0, hk, b, k_full + 8 * s);
                 if (!(ok = tc::bar_wait(v_free + 8 * s, parity))) {
                     tc::bar_wait(k_full + 8 * s, (i / Tile::kStages) & 1);  // a copy in flight ends before the CTA does
                     break;
                 }
                 tc::bar_expect(v_full + 8 * s, Tile::kTile);
                 for (int x = 0; x < DP; x += 64)
-                    tc::tensor_load(tc::smem_of(v_tiles) + s * Tile::kTile + x * 256, &maps.v, x, j0, hk, b, v_full + 8 * s);
+                    tc::tensor_load(tc::smem_of(v_tiles) + s * Tile::kTile + x * (2 * kKeys), &maps.v, x, j0, hk, b, v_full + 8 * s);
             }
             if (!ok) {
                 dead = 1;
@@ -287,7 +298,7 @@ __global__ void __launch_bounds__(320, 2)
                 }
             }
         }
-    } else if (warp == 9) {
+    } else if (warp == kWarps + 1) {
         if (n > 0) {
             const uint32_t leader = tc::elect();
             bool ok = __all_sync(0xffffffffu, tc::bar_wait(q_full, 0));
@@ -298,13 +309,13 @@ __global__ void __launch_bounds__(320, 2)
                 ok = __all_sync(0xffffffffu, tc::bar_wait(k_full + 8 * s, parity) && (i == 0 || tc::bar_wait(o_done, (i - 1) & 1)));
                 if (!ok) break;
                 tc::fence_after();
-                tc::product_rows<BF16, 128, DP>(leader, s_at, tc::smem_of(q_tile), tc::smem_of(k_tiles) + s * Tile::kTile);
+                tc::product_rows<BF16, kKeys, DP>(leader, s_at, tc::smem_of(q_tile), tc::smem_of(k_tiles) + s * Tile::kTile);
                 tc::products_arrive(leader, k_free + 8 * s);
                 tc::products_arrive(leader, s_full);
                 ok = __all_sync(0xffffffffu, tc::bar_wait(v_full + 8 * s, parity) && tc::bar_wait(p_full, i & 1));
                 if (!ok) break;
                 tc::fence_after();
-                tc::product_across<BF16, 128, DP, 64>(leader, o_at, s_at, tc::smem_of(v_tiles) + s * Tile::kTile, i > 0);
+                tc::product_across<BF16, kKeys, DP, 64>(leader, o_at, s_at, tc::smem_of(v_tiles) + s * Tile::kTile, i > 0);
                 tc::products_arrive(leader, v_free + 8 * s);
                 tc::products_arrive(leader, o_done);
             }
@@ -321,7 +332,7 @@ __global__ void __launch_bounds__(320, 2)
         bool found = false, ok = true;
         for (int i = 0; i < n; ++i) {
             const int st = i % Tile::kStages;
-            const int j0 = reach.lo + i * Tile::kKeys, mine0 = j0 + 64 * half;  // the tile's and this warp's first key
+            const int j0 = reach.lo + i * kKeys, mine0 = j0 + 64 * half;  // the tile's and this warp's first key
             // (a warp that gives up goes on without waiting: its partner meets it at a barrier in every turn)
             if (ok && !(ok = __all_sync(0xffffffffu, tc::bar_wait(s_full, i & 1)))) dead = 1;
             tc::fence_after();
@@ -357,9 +368,11 @@ __global__ void __launch_bounds__(320, 2)
                 top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
             }
             if (MOD || !clear) tc::tmem_stored();
-            halves[i & 1][half][own_row] = top;
-            pair_barrier(quarter);
-            top = fmaxf(top, halves[i & 1][half ^ 1][own_row]);
+            if (kHalves == 2) {
+                halves[i & 1][half][own_row] = top;
+                pair_barrier(quarter);
+                top = fmaxf(top, halves[i & 1][kHalves - 1 - half][own_row]);
+            }
             if (!MOD) top *= by;
             // The maximum that scales the exponentials may lag behind by a factor of 2^8: the result is the same, and the
             // accumulator in tensor memory is rescaled only when a row has moved further than that.  (The second half's warp
@@ -373,8 +386,8 @@ __global__ void __launch_bounds__(320, 2)
                 m = now;
                 if (i > 0) {
 #pragma unroll
-                    for (int c = 0; c < DP / 64; ++c) {
-                        const uint32_t at = o_at + lanes + half * (DP / 2) + 32 * c;
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t at = o_at + lanes + half * 64 + 32 * c;
                         uint32_t o[32];
                         tc::tmem_load(o, at);
                         tc::tmem_loaded();
@@ -411,9 +424,9 @@ __global__ void __launch_bounds__(320, 2)
             }
             const float2 sums = one(sum[0] + sum[1]);
             l += sums.x + sums.y;
-            if (j0 < reach.all_lo || j0 + Tile::kKeys - 1 > reach.all_hi) {  // hidden from some row: no junk may reach the product
+            if (j0 < reach.all_lo || j0 + kKeys - 1 > reach.all_hi) {  // hidden from some row: no junk may reach the product
                 if (ok && !tc::bar_wait(v_full + 8 * st, (i / Tile::kStages) & 1)) dead = 1;
-                found |= scan_tile<BF16, 128, DP, 256>(p, pos, v_tiles + st * Tile::kTile, j0, tid);
+                found |= scan_tile<BF16, kKeys, DP, 32 * kWarps>(p, pos, v_tiles + st * Tile::kTile, j0, tid);
                 tc::writes_to_async();
             }
             tc::tmem_stored();
@@ -421,24 +434,24 @@ __global__ void __launch_bounds__(320, 2)
             tc::bar_arrive(p_full);
         }
         if (found) junk = 1;
-        halves[n & 1][half][own_row] = l;
+        if (kHalves == 2) halves[n & 1][half][own_row] = l;
     }
     __syncthreads();
     if (dead) {
         if (tid == 0) atomicAdd(&g_timeouts, 1u);
     } else if (junk) {
-        for (int r = warp; r < 128; r += 10)
+        for (int r = warp; r < 128; r += kWarps + 2)
             if (i0 + r < p.t) rows::forward_row(p, a, b, h, i0 + r, lane);
-    } else if (warp < 8) {
+    } else if (warp < kWarps) {
         const uint32_t lanes = (uint32_t)quarter << 21;
-        l += halves[n & 1][half ^ 1][own_row];
+        if (kHalves == 2) l += halves[n & 1][kHalves - 1 - half][own_row];
         const bool empty = l == 0.0f;
         const float inv = 1.0f / l;
         if (n > 0 && !tc::bar_wait(o_done, (n - 1) & 1)) atomicAdd(&g_timeouts, 1u);
         tc::fence_after();
 #pragma unroll
-        for (int k = 0; k < DP / 64; ++k) {  // each half has half of the columns
-            const int c = half * (DP / 64) + k;
+        for (int k = 0; k < 2; ++k) {  // each half has 64 of the columns
+            const int c = half * 2 + k;
             uint32_t o[32];
             if (n > 0) {
                 tc::tmem_load(o, o_at + lanes + 32 * c);
@@ -456,9 +469,9 @@ __global__ void __launch_bounds__(320, 2)
     }
     tc::fence_before();
     __syncthreads();
-    if (warp == 9) {
-        tc::tmem_free<256>(tmem);
-    } else if (!dead && !junk && warp < 8 && lane == 0 && half * 64 < DP && half * 64 < p.d && i0 + quarter * 32 < p.t) {
+    if (warp == kWarps + 1) {
+        tc::tmem_free<Tile::kTmem>(tmem);
+    } else if (!dead && !junk && warp < kWarps && lane == 0 && half * 64 < p.d && i0 + quarter * 32 < p.t) {
         tc::tensor_store(&maps.out, half * 64, i0 + quarter * 32, h, b, tc::smem_of(q_tile) + half * (128 * 128) + quarter * 32 * 128);
         tc::stores_read();
     }
@@ -678,7 +691,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         auto scan = [&](uint32_t full, int i, int which, int j0) {
             if (j0 >= reach.all_lo && j0 + kColumns - 1 <= reach.all_hi) return;
             if (!tc::bar_wait(full + 8 * (i % kStages), (i / kStages) & 1)) dead = 1;
-            found |= scan_tile<BF16, kColumns, DP, 32 * kWarps>(p, pos, stream + ((i % kStages) * 2 + which) * Tile::kStream, j0, tid);
+            found |= scan_tile_apart<BF16, kColumns, DP, 32 * kWarps>(p, pos, stream + ((i % kStages) * 2 + which) * Tile::kStream, j0, tid);
             tc::writes_to_async();
         };
         for (int i = 0; i < n; ++i) {
@@ -907,15 +920,15 @@ template <bool BF16, int DP, bool MOD>
 cudaError_t forward(const AttnParams& p, const AttnTensors<typename Element<BF16>::type>& a, cudaStream_t st)
 {
     ForwardMaps m;
-    if (!make_map(&m.q, p, BF16, a.q, p.heads, 128) || !make_map(&m.k, p, BF16, a.k, p.kv_heads, 128) ||
-        !make_map(&m.v, p, BF16, a.v, p.kv_heads, 128) || !make_map(&m.out, p, BF16, a.out, p.heads, 32))
+    if (!make_map(&m.q, p, BF16, a.q, p.heads, 128) || !make_map(&m.k, p, BF16, a.k, p.kv_heads, ForwardTile<DP>::kKeys) ||
+        !make_map(&m.v, p, BF16, a.v, p.kv_heads, ForwardTile<DP>::kKeys) || !make_map(&m.out, p, BF16, a.out, p.heads, 32))
         return cudaErrorInvalidValue;
     const int64_t grid = p.blocks * p.heads * ((p.t + 127) / 128);
     if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
     auto* kernel = k29_attention<BF16, DP, MOD>;
     static const cudaError_t set = with_shared(kernel, ForwardTile<DP>::kShared);
     if (set != cudaSuccess) return set;
-    kernel<<<(unsigned)grid, 320, ForwardTile<DP>::kShared, st>>>(p, a, m);
+    kernel<<<(unsigned)grid, ForwardTile<DP>::kThreads, ForwardTile<DP>::kShared, st>>>(p, a, m);
     count_launches(1);
     return cudaGetLastError();
 }
