@@ -910,12 +910,6 @@ bool make_map(CUtensorMap* map, const AttnParams& p, bool bf16, const Heads<P>& 
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename F>
-cudaError_t with_shared(F* kernel, int bytes)
-{
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-}
-
 template <bool BF16, int DP, bool MOD>
 cudaError_t forward(const AttnParams& p, const AttnTensors<typename Element<BF16>::type>& a, cudaStream_t st)
 {
@@ -926,8 +920,9 @@ cudaError_t forward(const AttnParams& p, const AttnTensors<typename Element<BF16
     const int64_t grid = p.blocks * p.heads * ((p.t + 127) / 128);
     if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
     auto* kernel = k29_attention<BF16, DP, MOD>;
-    static const cudaError_t set = with_shared(kernel, ForwardTile<DP>::kShared);
-    if (set != cudaSuccess) return set;
+    static std::atomic<uint64_t> allowed{0};
+    const cudaError_t e = allow_shared(kernel, ForwardTile<DP>::kShared, allowed);
+    if (e != cudaSuccess) return e;
     kernel<<<(unsigned)grid, ForwardTile<DP>::kThreads, ForwardTile<DP>::kShared, st>>>(p, a, m);
     count_launches(1);
     return cudaGetLastError();
@@ -945,8 +940,9 @@ cudaError_t gradient(const AttnParams& p, const AttnTensors<typename Element<BF1
     const int64_t grid = p.blocks * own * ((p.t + 127) / 128);
     if (!ok || grid > 0x7fffffffLL) return cudaErrorInvalidValue;
     auto* kernel = k30_attention_grad<BF16, DP, MOD, KEYS>;
-    static const cudaError_t set = with_shared(kernel, GradTile<DP>::kShared);
-    if (set != cudaSuccess) return set;
+    static std::atomic<uint64_t> allowed{0};
+    const cudaError_t e = allow_shared(kernel, GradTile<DP>::kShared, allowed);
+    if (e != cudaSuccess) return e;
     kernel<<<(unsigned)grid, GradTile<DP>::kThreads, GradTile<DP>::kShared, st>>>(p, a, m);
     count_launches(1);
     return cudaGetLastError();

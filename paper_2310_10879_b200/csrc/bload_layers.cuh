@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "bload.h"
 
 namespace bload {
@@ -62,6 +64,20 @@ struct RecurTensors {
     Channels<const T> gate, x, dh;
     Channels<T> h, dgate, dx;
 };
+
+// Lets a kernel have `bytes` of dynamic shared memory, once per device (`done`: one bit each, of the kernel).
+template <typename F>
+cudaError_t allow_shared(F* kernel, int bytes, std::atomic<uint64_t>& done)
+{
+    int device = 0;
+    const cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = device < 64 ? (uint64_t)1 << device : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    const cudaError_t f = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (f == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return f;
+}
 
 template <typename T>
 cudaError_t launch_rotary(const RotaryParams& p, const Heads<const T>& x, const Heads<T>& y, cudaStream_t st);

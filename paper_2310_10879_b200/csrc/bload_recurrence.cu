@@ -577,8 +577,9 @@ cudaError_t launch(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t 
     const int64_t groups = groups_of(p.blocks, p.channels);
     const int segments = segments_of(p.blocks, p.t, p.channels);
     auto* kernel = k27_recurrence<T, GRAD, COPY>;
-    static const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
-    if (set != cudaSuccess) return set;
+    static std::atomic<uint64_t> allowed{0};
+    const cudaError_t shared = allow_shared(kernel, kShared, allowed);
+    if (shared != cudaSuccess) return shared;
     if (segments > 1) {  // ticket and flags
         const cudaError_t e = cudaMemsetAsync(p.work, 0, 256 + 4 * (size_t)(groups * segments), st);
         if (e != cudaSuccess) return e;
