@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -121,13 +122,12 @@ def load() -> C.CDLL:
     L.bload_epoch.argtypes = [vp, i64, i32, u64, vp, C.c_size_t, vp, C.c_size_t, C.POINTER(EpochIO), vp, vp,
                               C.POINTER(PlanInfo)]
     L.bload_epoch_stage_times.argtypes = [C.POINTER(C.c_float * 5)]
-    L.bload_rotary.argtypes = [vp, i64, i32, i32, i32, i32, C.POINTER(HeadsTensor), C.POINTER(HeadsTensor), vp, i32, i32,
-                               C.c_float, vp]
+    L.bload_rotary.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, vp, i32, i32, C.c_float, vp]
     L.bload_rotary_grad.argtypes = L.bload_rotary.argtypes
-    L.bload_attention.argtypes = [C.POINTER(AttentionArgs), vp]
+    L.bload_attention.argtypes = [vp, vp]
     L.bload_attention_grad.argtypes = L.bload_attention.argtypes
     L.bload_recurrence_work_bytes.argtypes = [i64, i32, i64]
-    L.bload_recurrence.argtypes = [C.POINTER(RecurrenceArgs), vp]
+    L.bload_recurrence.argtypes = [vp, vp]
     L.bload_recurrence_grad.argtypes = L.bload_recurrence.argtypes
     L.bload_set_plan_timing.argtypes = [C.c_int]
     L.bload_plan_stage_times.argtypes = [C.POINTER(C.c_float * 4)]
@@ -570,25 +570,46 @@ class RecurrenceArgs(C.Structure):
                 ("dgate", ChannelsTensor), ("dx", ChannelsTensor)]
 
 
-def _element_type(t, where: str) -> int:
-    import torch
-    code = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}.get(t.dtype)
-    if code is None:
-        raise TypeError("%s: float32, float16 or bfloat16 tensors, not %s" % (where, t.dtype))
-    return code
+# The argument blocks of a call, packed in one step: these calls are made per layer and step, and filling a ctypes structure
+# field by field takes longer than the kernels of a small batch.  (The layouts are those of the structures above.)
+_HEADS = struct.Struct("@4q")
+_ATTENTION = struct.Struct("@q7i2fi2q16qq")
+_ATTENTION_GRAD = struct.Struct("@q7i2fi2q16qq16qq")
+_RECURRENCE = struct.Struct("@2q2iq9q2qQ9q")
 
 
-def _positions(pos, where: str):
-    import torch
-    if pos.dtype != torch.int32 or pos.dim() != 2 or not pos.is_cuda or not pos.is_contiguous():
+def _torch():
+    """(torch, {dtype: code}, int32, float32, raw stream of a device, current device), looked up once."""
+    global _torch_parts
+    if _torch_parts is None:
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _torch_parts = ({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}, torch.int32, torch.float32,
+                        raw or (lambda index: torch.cuda.current_stream(index).cuda_stream), torch.cuda.current_device)
+    return _torch_parts
+
+
+_torch_parts = None
+
+
+def _begin(where: str, pos, x, dims: int, stream):
+    """Checks of the positions and the leading tensor; ((blocks, t_block), element type code, stream)."""
+    codes, int32, _, raw_stream, current_device = _torch()
+    if pos.dtype != int32 or pos.dim() != 2 or not pos.is_cuda or not pos.is_contiguous():
         raise TypeError("%s: pos must be a contiguous CUDA int32 tensor [blocks, t_block], as bload_pack writes it" % where)
-    if pos.device.index != torch.cuda.current_device():
-        raise ValueError("%s: pos is on %s, the current device is cuda:%d" % (where, pos.device, torch.cuda.current_device()))
-    return pos.shape
+    index = pos.device.index
+    if index != current_device():
+        raise ValueError("%s: pos is on %s, the current device is cuda:%d" % (where, pos.device, current_device()))
+    if x.dim() != dims or x.device != pos.device:
+        raise ValueError("%s: tensors are [blocks, t_block, %s] on the device of pos" % (where, "heads, head_dim" if dims == 4 else "channels"))
+    code = codes.get(x.dtype)
+    if code is None:
+        raise TypeError("%s: float32, float16 or bfloat16 tensors, not %s" % (where, x.dtype))
+    return pos.shape, code, raw_stream(index) if stream is None else stream.cuda_stream
 
 
-def _strided(cls, name, t, shape, like, where: str):
-    """A strided tensor argument; the last dimension has to be contiguous."""
+def _strided(where: str, name: str, t, shape, like):
+    """(address, strides but the last) of a strided tensor argument; the last dimension has to be contiguous."""
     if t.dtype != like.dtype or t.device != like.device:
         raise TypeError("%s: %s is %s on %s, expected %s on %s" % (where, name, t.dtype, t.device, like.dtype, like.device))
     if t.shape != shape:
@@ -596,30 +617,26 @@ def _strided(cls, name, t, shape, like, where: str):
     st = t.stride()
     if st[-1] != 1 and shape[-1] > 1:
         raise ValueError("%s: the last dimension of %s must be contiguous" % (where, name))
-    return cls(t.data_ptr(), *st[:-1])
+    return (t.data_ptr(), *st[:-1])
 
 
-def _flat32(name, t, count: int, like, where: str):
-    """A contiguous float32 argument, or None."""
-    import torch
+def _flat32(where: str, name: str, t, count: int, like) -> int:
+    """Address of a contiguous float32 argument, 0 for None."""
     if t is None:
-        return None
-    if t.dtype != torch.float32 or t.device != like.device or not t.is_contiguous() or t.numel() != count:
+        return 0
+    if t.dtype != _torch()[2] or t.device != like.device or not t.is_contiguous() or t.numel() != count:
         raise TypeError("%s: %s must be a contiguous float32 tensor of %d elements on %s" % (where, name, count, like.device))
     return t.data_ptr()
 
 
 def _rotary(fn, where, pos, x, y, inv_freq, interleaved, factor, stream) -> None:
-    b, t = _positions(pos, where)
-    if x.dim() != 4 or x.device != pos.device:
-        raise ValueError("%s: tensors are [blocks, t_block, heads, head_dim] on the device of pos" % where)
+    (b, t), code, stream = _begin(where, pos, x, 4, stream)
     h, d = x.shape[2:]
     shape = (b, t, h, d)
-    xs = _strided(HeadsTensor, "input", x, shape, x, where)
-    ys = _strided(HeadsTensor, "output", y, shape, x, where)
     n = inv_freq.numel()
-    rc = fn(pos.data_ptr(), b, t, h, d, _element_type(x, where), C.byref(xs), C.byref(ys),
-            _flat32("inv_freq", inv_freq, n, x, where), 2 * n, 1 if interleaved else 0, factor, _stream(stream))
+    rc = fn(pos.data_ptr(), b, t, h, d, code, _HEADS.pack(*_strided(where, "input", x, shape, x)),
+            _HEADS.pack(*_strided(where, "output", y, shape, x)), _flat32(where, "inv_freq", inv_freq, n, x), 2 * n,
+            1 if interleaved else 0, factor, stream)
     if rc:
         raise BloadError(rc, where)
 
@@ -635,21 +652,18 @@ def bload_rotary_grad(pos, dy, dx, inv_freq, interleaved: bool = False, factor: 
     _rotary(load().bload_rotary_grad, "bload_rotary_grad", pos, dy, dx, inv_freq, interleaved, factor, stream)
 
 
-def _attention_args(where, pos, q, k, v, out, lse, scale, softcap, slopes, causal, window) -> AttentionArgs:
-    b, t = _positions(pos, where)
-    if q.dim() != 4 or k.dim() != 4 or q.device != pos.device:
-        raise ValueError("%s: tensors are [blocks, t_block, heads, head_dim] on the device of pos" % where)
+def _attention(where, pos, q, k, v, out, lse, scale, softcap, slopes, causal, window, stream):
+    """(packed fields up to d_lse, stream)"""
+    (b, t), code, stream = _begin(where, pos, q, 4, stream)
     h, d = q.shape[2:]
+    if k.dim() != 4:
+        raise ValueError("%s: k and v are [blocks, t_block, kv_heads, head_dim]" % where)
     hk = k.shape[2]
     qs, ks = (b, t, h, d), (b, t, hk, d)
-    a = AttentionArgs(b, t, h, hk, d, _element_type(q, where), 1 if causal else 0, window,
-                      d ** -0.5 if scale is None else scale, softcap, pos.data_ptr(), _flat32("slopes", slopes, h, q, where))
-    a.q = _strided(HeadsTensor, "q", q, qs, q, where)
-    a.k = _strided(HeadsTensor, "k", k, ks, q, where)
-    a.v = _strided(HeadsTensor, "v", v, ks, q, where)
-    a.out = _strided(HeadsTensor, "out", out, qs, q, where)
-    a.d_lse = _flat32("lse", lse, b * h * t, q, where)
-    return a
+    return (b, t, h, hk, d, code, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, softcap, 0,
+            pos.data_ptr(), _flat32(where, "slopes", slopes, h, q), *_strided(where, "q", q, qs, q),
+            *_strided(where, "k", k, ks, q), *_strided(where, "v", v, ks, q), *_strided(where, "out", out, qs, q),
+            _flat32(where, "lse", lse, b * h * t, q)), stream
 
 
 def bload_attention(pos, q, k, v, out, lse=None, scale: float | None = None, softcap: float = 0.0, slopes=None,
@@ -658,8 +672,8 @@ def bload_attention(pos, q, k, v, out, lse=None, scale: float | None = None, sof
     (float16 or bfloat16, strided); pos: int32 [blocks, t_block] from bload_pack; lse: float32 [blocks, heads, t_block] or
     None (needed for the gradient).  scale defaults to head_dim ** -0.5; softcap > 0 caps scores by a tanh; slopes: float32
     [heads], subtracts slope * |i - j|; window > 0 keeps |i - j| < window."""
-    a = _attention_args("bload_attention", pos, q, k, v, out, lse, scale, softcap, slopes, causal, window)
-    rc = load().bload_attention(C.byref(a), _stream(stream))
+    fields, stream = _attention("bload_attention", pos, q, k, v, out, lse, scale, softcap, slopes, causal, window, stream)
+    rc = load().bload_attention(_ATTENTION.pack(*fields), stream)
     if rc:
         raise BloadError(rc, "bload_attention")
 
@@ -669,20 +683,19 @@ def bload_attention_grad(pos, q, k, v, out, lse, dout, dq, dk, dv, delta, scale:
     """dq, dk, dv of bload_attention from dout, with out and lse of the forward call.  delta: float32 [blocks, heads,
     t_block], written (the row sums of dout * out)."""
     where = "bload_attention_grad"
-    a = _attention_args(where, pos, q, k, v, out, lse, scale, softcap, slopes, causal, window)
-    a.dout = _strided(HeadsTensor, "dout", dout, q.shape, q, where)
-    a.dq = _strided(HeadsTensor, "dq", dq, q.shape, q, where)
-    a.dk = _strided(HeadsTensor, "dk", dk, k.shape, q, where)
-    a.dv = _strided(HeadsTensor, "dv", dv, k.shape, q, where)
-    a.d_delta = _flat32("delta", delta, lse.numel(), q, where)
-    rc = load().bload_attention_grad(C.byref(a), _stream(stream))
+    fields, stream = _attention(where, pos, q, k, v, out, lse, scale, softcap, slopes, causal, window, stream)
+    rc = load().bload_attention_grad(_ATTENTION_GRAD.pack(
+        *fields, *_strided(where, "dout", dout, q.shape, q), *_strided(where, "dq", dq, q.shape, q),
+        *_strided(where, "dk", dk, k.shape, q), *_strided(where, "dv", dv, k.shape, q),
+        _flat32(where, "delta", delta, q.shape[0] * q.shape[1] * q.shape[2], q)), stream)
     if rc:
         raise BloadError(rc, where)
 
 
 def bload_recurrence_buffers(pos, x):
     """(carry, work) for bload_recurrence and its gradient on x [blocks, t_block, channels]: the float32 states that the
-    forward call keeps for the gradient, [blocks, ceil(t_block / 64), channels], and scratch (None when none is needed)."""
+    forward call keeps for the gradient, [blocks, ceil(t_block / 64), channels], and scratch (None when none is needed).
+    Calls that may overlap on the GPU need a scratch each."""
     import torch
     b, t = pos.shape
     carry = torch.empty((b, -(-t // RECURRENCE_RUN), x.shape[-1]), dtype=torch.float32, device=x.device)
@@ -690,41 +703,37 @@ def bload_recurrence_buffers(pos, x):
     return carry, torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
 
 
-def _recurrence_args(where, pos, gate, x, carry, work) -> RecurrenceArgs:
-    b, t = _positions(pos, where)
-    if x.dim() != 3 or x.device != pos.device:
-        raise ValueError("%s: tensors are [blocks, t_block, channels] on the device of pos" % where)
+def _recurrence(where, pos, gate, x, carry, work, stream):
+    """(packed fields up to x, of d_carry to work_bytes, stream)"""
+    (b, t), code, stream = _begin(where, pos, x, 3, stream)
     c = x.shape[2]
-    a = RecurrenceArgs(b, c, t, _element_type(x, where), pos.data_ptr())
-    a.gate = _strided(ChannelsTensor, "gate", gate, x.shape, x, where)
-    a.x = _strided(ChannelsTensor, "x", x, (b, t, c), x, where)
-    a.d_carry = _flat32("carry", carry, b * -(-t // RECURRENCE_RUN) * c, x, where)
-    if work is not None:
-        if work.device != x.device or not work.is_contiguous():
-            raise TypeError("%s: work must be a contiguous tensor on %s" % (where, x.device))
-        a.d_work, a.work_bytes = work.data_ptr(), work.numel() * work.element_size()
-    return a
+    head = (b, c, t, code, pos.data_ptr(), *_strided(where, "gate", gate, x.shape, x), *_strided(where, "x", x, (b, t, c), x))
+    at = _flat32(where, "carry", carry, b * -(-t // RECURRENCE_RUN) * c, x)
+    if work is None:
+        return head, (at, 0, 0), stream
+    if work.device != x.device or not work.is_contiguous():
+        raise TypeError("%s: work must be a contiguous tensor on %s" % (where, x.device))
+    return head, (at, work.data_ptr(), work.numel() * work.element_size()), stream
 
 
 def bload_recurrence(pos, gate, x, h, carry=None, work=None, stream=None) -> None:
     """h_s = f_s h_{s-1} + (1 - f_s) x_s with f = sigmoid(gate), restarted at every sequence start.  gate, x, h: [blocks,
     t_block, channels] (float32, float16 or bfloat16, strided); carry, work from bload_recurrence_buffers (carry None:
     no gradient will be asked for)."""
-    a = _recurrence_args("bload_recurrence", pos, gate, x, carry, work)
-    a.h = _strided(ChannelsTensor, "h", h, x.shape, x, "bload_recurrence")
-    rc = load().bload_recurrence(C.byref(a), _stream(stream))
+    where = "bload_recurrence"
+    head, kept, stream = _recurrence(where, pos, gate, x, carry, work, stream)
+    rc = load().bload_recurrence(_RECURRENCE.pack(*head, *_strided(where, "h", h, x.shape, x), *kept, 0, 0, 0, 0, 0, 0, 0, 0, 0), stream)
     if rc:
-        raise BloadError(rc, "bload_recurrence")
+        raise BloadError(rc, where)
 
 
 def bload_recurrence_grad(pos, gate, x, carry, dh, dgate, dx, work=None, stream=None) -> None:
     """dgate and dx of bload_recurrence from dh, the gradient with respect to every h; carry is the forward call's."""
     where = "bload_recurrence_grad"
-    a = _recurrence_args(where, pos, gate, x, carry, work)
-    a.dh = _strided(ChannelsTensor, "dh", dh, x.shape, x, where)
-    a.dgate = _strided(ChannelsTensor, "dgate", dgate, x.shape, x, where)
-    a.dx = _strided(ChannelsTensor, "dx", dx, x.shape, x, where)
-    rc = load().bload_recurrence_grad(C.byref(a), _stream(stream))
+    head, kept, stream = _recurrence(where, pos, gate, x, carry, work, stream)
+    rc = load().bload_recurrence_grad(_RECURRENCE.pack(
+        *head, 0, 0, 0, *kept, *_strided(where, "dh", dh, x.shape, x), *_strided(where, "dgate", dgate, x.shape, x),
+        *_strided(where, "dx", dx, x.shape, x)), stream)
     if rc:
         raise BloadError(rc, where)
 

@@ -114,25 +114,57 @@ __device__ __forceinline__ Reach get_reach(const ReachShared<WARPS>& sh)
 
 // score in units of log2 from q.k, with the cap and the distance bias; `inner` = d score / d (scale q.k)
 struct Modifier {
-    float by, inv_cap2, cap2, slope2;  // scale * log2e; 2 log2e * scale / cap; cap * log2e; slope * log2e
+    enum { kPlain, kNear, kAny };  // no cap; capped and every |scale q.k / cap| of the warp's columns below 1/2; capped
+    float by, unit, cap2, slope2;  // scale * log2e; scale / cap; cap * log2e; slope * log2e
     __device__ __forceinline__ Modifier(const AttnParams& p, int h)
     {
         by = p.scale * kLog2e;
-        inv_cap2 = p.cap > 0.0f ? 2.0f * kLog2e * p.scale / p.cap : 0.0f;
+        unit = p.cap > 0.0f ? p.scale / p.cap : 0.0f;
         cap2 = p.cap * kLog2e;
         slope2 = p.slopes ? p.slopes[h] * kLog2e : 0.0f;
     }
-    // tanh(y) = 1 - 2 / (1 + exp(2 y)): an absolute error of some 2^-23 of the cap, whatever y
-    __device__ __forceinline__ float operator()(float qk, float apart, float& inner) const
+    // which of the three a warp's scores take, so that the usual small ones cost no special functions
+    __device__ __forceinline__ int kind(const uint32_t (&qk)[32]) const
+    {
+        if (!(cap2 > 0.0f)) return kPlain;
+        float top[2] = {};
+#pragma unroll
+        for (int e = 0; e < 32; ++e) top[e & 1] = fmaxf(top[e & 1], fabsf(__uint_as_float(qk[e])));
+        return __all_sync(0xffffffffu, fmaxf(top[0], top[1]) * fabsf(unit) < 0.5f) ? kNear : kAny;
+    }
+    // tanh(y), |y| < 1/2: y (1 + c1 y^2 + ... + c4 y^8), the coefficients of smallest largest relative error (2.8e-8, found by
+    // iteratively reweighted least squares).  Else 1 - 2 / (1 + exp(2 y)), whose absolute error of some 2^-23 is small against
+    // values from 0.46 on, but not against a score much smaller than its cap.
+    template <int KIND>
+    __device__ __forceinline__ float apply(float qk, float apart, float& inner) const
     {
         float x = qk * by;
         inner = 1.0f;
-        if (cap2 > 0.0f) {
-            const float th = fmaf(-2.0f, tc::inverse_fast(1.0f + tc::exp2_fast(qk * inv_cap2)), 1.0f);
+        if (KIND != kPlain) {
+            const float y = qk * unit, z = y * y;
+            float th = fmaf(z, 0.0171350036f, -0.0529860742f);
+            th = fmaf(th, z, 0.133247793f);
+            th = fmaf(th, z, -0.333330691f);
+            th = fmaf(th * z, y, y);
+            if (KIND == kAny) {
+                const float far = fmaf(-2.0f, tc::inverse_fast(1.0f + tc::exp2_fast(y * (2.0f * kLog2e))), 1.0f);
+                th = fabsf(y) < 0.5f ? th : far;  // (NaN goes to far, and stays)
+            }
             x = cap2 * th;
             inner = fmaf(-th, th, 1.0f);
         }
         return fmaf(-slope2, fabsf(apart), x);
+    }
+    // f(kind) with the kind as a constant
+    template <typename F>
+    static __device__ __forceinline__ void with(int kind, F f)
+    {
+        if (kind == kNear)
+            f(std::integral_constant<int, kNear>());
+        else if (kind == kAny)
+            f(std::integral_constant<int, kAny>());
+        else
+            f(std::integral_constant<int, kPlain>());
     }
 };
 
@@ -348,13 +380,15 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
                 tc::tmem_load(s, own_at + 32 * c);
                 tc::tmem_loaded();
                 tc::settle(s);
-                if (MOD) {
+                if (MOD)
+                    Modifier::with(modify.kind(s), [&](auto kind) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        float inner;
-                        s[e] = __float_as_uint(modify(__uint_as_float(s[e]), (float)(row - mine0 - 32 * c - e), inner));
-                    }
-                }
+                        for (int e = 0; e < 32; ++e) {
+                            float inner;
+                            s[e] = __float_as_uint(
+                                modify.apply<decltype(kind)::value>(__uint_as_float(s[e]), (float)(row - mine0 - 32 * c - e), inner));
+                        }
+                    });
                 if (!clear) {
                     const uint32_t mask = column_mask(span.lo - mine0 - 32 * c, span.hi - mine0 - 32 * c);
 #pragma unroll
@@ -746,6 +780,13 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                     tc::bar_arrive(p_full);
                 }
                 const Two by2 = two(modify.by, modify.by);
+                if (MOD)
+                    Modifier::with(modify.kind(s), [&](auto kind) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            s[e] = __float_as_uint(modify.apply<decltype(kind)::value>(__uint_as_float(s[e]), (float)(row - mine0 - e),
+                                                                                      in[MOD ? e : 0]));
+                    });
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
                     Two lse_here = lse2;
@@ -753,15 +794,8 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                         const float2 l = *reinterpret_cast<const float2*>(&column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0]);
                         lse_here = two(l.x, l.y);
                     }
-                    const float s0 = __uint_as_float(s[e]), s1 = __uint_as_float(s[e + 1]);
-                    float2 x;
-                    if (MOD) {
-                        x.x = modify(s0, (float)(row - mine0 - e), in[MOD ? e : 0]);
-                        x.y = modify(s1, (float)(row - mine0 - e - 1), in[MOD ? e + 1 : 0]);
-                        x = one(two(x.x, x.y) + lse_here);
-                    } else {
-                        x = one(fma(two(s0, s1), by2, lse_here));
-                    }
+                    const Two raw = two(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+                    const float2 x = one(MOD ? raw + lse_here : fma(raw, by2, lse_here));
                     w[e] = tc::exp2_fast(x.x);
                     w[e + 1] = tc::exp2_fast(x.y);
                 }

@@ -85,3 +85,16 @@ def test_rotary():
     assert rotary(dtype=-1) == E.ERR_UNSUPPORTED and rotary(t=E.MAX_T_BLOCK + 1) == E.ERR_UNSUPPORTED
     assert rotary(factor=float("nan")) == E.ERR_ARG
     assert rotary(x=heads(P + 1)) == E.ERR_ALIGN and rotary(y=heads(head=0)) == E.ERR_ARG and rotary(x=heads(slot=-1)) == E.ERR_ARG
+
+
+def test_the_packed_argument_blocks_have_the_layout_of_the_structures():
+    assert E._HEADS.size == C.sizeof(E.HeadsTensor)
+    assert E._ATTENTION_GRAD.size == C.sizeof(E.AttentionArgs) and E._RECURRENCE.size == C.sizeof(E.RecurrenceArgs)
+    a = E.AttentionArgs.from_buffer_copy(E._ATTENTION_GRAD.pack(*range(1, 9), 0.5, 0.25, 0, *range(20, 56)))
+    assert (a.block_count, a.t_block, a.heads, a.kv_heads, a.head_dim, a.dtype, a.causal, a.window) == tuple(range(1, 9))
+    assert (a.scale, a.softcap, a.d_pos, a.d_slopes, a.q.data, a.q.head_stride, a.out.data, a.d_lse) == (0.5, 0.25, 20, 21, 22, 25, 34, 38)
+    assert (a.dout.data, a.dv.head_stride, a.d_delta) == (39, 54, 55)
+    assert E._ATTENTION.size == E.AttentionArgs.d_lse.offset + 8
+    r = E.RecurrenceArgs.from_buffer_copy(E._RECURRENCE.pack(*range(1, 27)))
+    assert (r.block_count, r.channels, r.t_block, r.dtype, r.d_pos, r.gate.data, r.h.slot_stride) == (1, 2, 3, 4, 5, 6, 14)
+    assert (r.d_carry, r.d_work, r.work_bytes, r.dh.data, r.dx.slot_stride) == (15, 16, 17, 18, 26)
