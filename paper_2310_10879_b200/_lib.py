@@ -595,12 +595,12 @@ _torch_parts = None
 def _begin(where: str, pos, x, dims: int, stream):
     """Checks of the positions and the leading tensor; ((blocks, t_block), element type code, stream)."""
     codes, int32, _, raw_stream, current_device = _torch()
-    if pos.dtype != int32 or pos.dim() != 2 or not pos.is_cuda or not pos.is_contiguous():
+    index = pos.get_device()
+    if pos.dtype is not int32 or pos.dim() != 2 or index < 0 or not pos.is_contiguous():
         raise TypeError("%s: pos must be a contiguous CUDA int32 tensor [blocks, t_block], as bload_pack writes it" % where)
-    index = pos.device.index
     if index != current_device():
         raise ValueError("%s: pos is on %s, the current device is cuda:%d" % (where, pos.device, current_device()))
-    if x.dim() != dims or x.device != pos.device:
+    if x.dim() != dims or x.get_device() != index:
         raise ValueError("%s: tensors are [blocks, t_block, %s] on the device of pos" % (where, "heads, head_dim" if dims == 4 else "channels"))
     code = codes.get(x.dtype)
     if code is None:
@@ -610,7 +610,7 @@ def _begin(where: str, pos, x, dims: int, stream):
 
 def _strided(where: str, name: str, t, shape, like):
     """(address, strides but the last) of a strided tensor argument; the last dimension has to be contiguous."""
-    if t.dtype != like.dtype or t.device != like.device:
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
         raise TypeError("%s: %s is %s on %s, expected %s on %s" % (where, name, t.dtype, t.device, like.dtype, like.device))
     if t.shape != shape:
         raise ValueError("%s: %s has shape %s, expected %s" % (where, name, tuple(t.shape), tuple(shape)))
@@ -624,7 +624,7 @@ def _flat32(where: str, name: str, t, count: int, like) -> int:
     """Address of a contiguous float32 argument, 0 for None."""
     if t is None:
         return 0
-    if t.dtype != _torch()[2] or t.device != like.device or not t.is_contiguous() or t.numel() != count:
+    if t.dtype is not _torch()[2] or t.get_device() != like.get_device() or not t.is_contiguous() or t.numel() != count:
         raise TypeError("%s: %s must be a contiguous float32 tensor of %d elements on %s" % (where, name, count, like.device))
     return t.data_ptr()
 

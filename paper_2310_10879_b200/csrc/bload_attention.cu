@@ -371,11 +371,20 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
             // The scores in units of log2 are x by (MOD: x itself); hidden ones are -inf.  They are read twice, for the maximum and
             // for the exponentials: 64 of them would not stay in this thread's registers.  What changes them is written back.
             const uint32_t own_at = s_at + lanes + 64 * half;
-            const bool clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 63);
-            const bool blind = __all_sync(0xffffffffu, span.lo > mine0 + 63 || span.hi < mine0);  // none of these columns is seen
+            // All seen by all of the warp's rows, none by any: per 64 columns, or for heads of at most 64 elements, where short walks
+            // are what counts, per 32 (16 x 1000 frames of features 69 -> 65 us, but one sequence of 16,384 304 -> 321 us).
+            constexpr int kFine = kHalves == 1 ? 2 : 1;
+            bool clear[2], blind[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int c0 = mine0 + 32 * c, c1 = c0 + 64 / kFine - 1;
+                clear[c] = c < kFine ? (bool)__all_sync(0xffffffffu, span.lo <= c0 && span.hi >= c1) : clear[0];
+                blind[c] = c < kFine ? (bool)__all_sync(0xffffffffu, span.lo > c1 || span.hi < c0) : blind[0];
+            }
             float top = -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 2 && !blind; ++c) {
+            for (int c = 0; c < 2; ++c) {
+                if (blind[c]) continue;
                 uint32_t s[32];
                 tc::tmem_load(s, own_at + 32 * c);
                 tc::tmem_loaded();
@@ -389,19 +398,19 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
                                 modify.apply<decltype(kind)::value>(__uint_as_float(s[e]), (float)(row - mine0 - 32 * c - e), inner));
                         }
                     });
-                if (!clear) {
+                if (!clear[c]) {
                     const uint32_t mask = column_mask(span.lo - mine0 - 32 * c, span.hi - mine0 - 32 * c);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) s[e] = (mask >> e) & 1 ? s[e] : 0xff800000u;
                 }
-                if (MOD || !clear) tc::tmem_store(own_at + 32 * c, s);
+                if (MOD || !clear[c]) tc::tmem_store(own_at + 32 * c, s);
                 float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int e = 0; e < 32; e += 2)
                     t4[(e / 2) & 3] = fmaxf(t4[(e / 2) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
                 top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
             }
-            if (MOD || !clear) tc::tmem_stored();
+            if (MOD || !clear[0] || !clear[1]) tc::tmem_stored();
             if (kHalves == 2) {
                 halves[i & 1][half][own_row] = top;
                 pair_barrier(quarter);
@@ -435,13 +444,13 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
             const float off = m == -INFINITY ? 0.0f : -m;
             const Two by2 = two(by, by), off2 = two(off, off);
             Two sum[2] = {zero(), zero()};
-            if (blind) {
-                const uint32_t none[16] = {};
-                tc::tmem_store16(own_at, none);
-                tc::tmem_store16(own_at + 16, none);
-            }
 #pragma unroll
-            for (int c = 0; c < 2 && !blind; ++c) {
+            for (int c = 0; c < 2; ++c) {
+                if (blind[c]) {
+                    const uint32_t none[16] = {};
+                    tc::tmem_store16(own_at + 16 * c, none);
+                    continue;
+                }
                 uint32_t s[32], w[16];
                 tc::tmem_load(s, own_at + 32 * c);
                 tc::tmem_loaded();
@@ -498,17 +507,17 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
             stage_columns<BF16>(q_tile + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
         }
         tc::writes_to_async();
+        __syncwarp();
+        if (lane == 0 && half * 64 < p.d && i0 + quarter * 32 < p.t) {  // the 32 rows by 64 columns that this warp has staged
+            tc::tensor_store(&maps.out, half * 64, i0 + quarter * 32, h, b, tc::smem_of(q_tile) + half * (128 * 128) + quarter * 32 * 128);
+            tc::stores_read();
+        }
         if (half == 0 && p.lse && row < p.t)
             p.lse[((int64_t)b * p.heads + h) * p.t + row] = empty ? -INFINITY : (m + log2f(l)) * kLn2;
     }
     tc::fence_before();
     __syncthreads();
-    if (warp == kWarps + 1) {
-        tc::tmem_free<Tile::kTmem>(tmem);
-    } else if (!dead && !junk && warp < kWarps && lane == 0 && half * 64 < p.d && i0 + quarter * 32 < p.t) {
-        tc::tensor_store(&maps.out, half * 64, i0 + quarter * 32, h, b, tc::smem_of(q_tile) + half * (128 * 128) + quarter * 32 * 128);
-        tc::stores_read();
-    }
+    if (warp == kWarps + 1) tc::tmem_free<Tile::kTmem>(tmem);
 }
 
 // ---- gradients ----------------------------------------------------------------------------------------------------

@@ -144,12 +144,24 @@ __device__ __forceinline__ Two fma(Two a, Two b, Two c)
 __device__ __forceinline__ Two zero() { return {0ull}; }
 
 // First slot behind the sequence that holds slot i (pos[i] >= 0), by a whole warp: pos[s] == s - start holds up to the
-// end of the sequence and nowhere behind it, so 32 probes cut the range by 32 (three rounds for 32,768 slots).
-// Whatever pos holds, the result is in (i, t].
+// end of the sequence and nowhere behind it.  The next 128 slots are looked at together, which ends it for short sequences; then 32
+// probes cut the range by 32 (three rounds for 32,768 slots).  Whatever pos holds, the result is in (i, t].
 __device__ __forceinline__ int warp_seq_end(const int32_t* pos, int t, int i, int lane)
 {
     const int start = i - pos[i];
     int lo = i, hi = t;
+    bool near[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int s = i + 1 + 32 * k + lane;
+        near[k] = s < t && pos[s] == s - start;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const unsigned out = ~__ballot_sync(0xffffffffu, near[k]);
+        if (out) return i + 32 * k + __ffs(out);
+    }
+    lo = i + 128;
     while (hi - lo > 1) {
         const int step = (hi - lo - 1 + 31) / 32;
         const int s = lo + step * (lane + 1);
