@@ -579,13 +579,13 @@ _RECURRENCE = struct.Struct("@2q2iq9q2qQ9q")
 
 
 def _torch():
-    """(torch, {dtype: code}, int32, float32, raw stream of a device, current device), looked up once."""
+    """({dtype: code}, int32, float32, raw stream of a device, current device, uint8) of torch, looked up once."""
     global _torch_parts
     if _torch_parts is None:
         import torch
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _torch_parts = ({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}, torch.int32, torch.float32,
-                        raw or (lambda index: torch.cuda.current_stream(index).cuda_stream), torch.cuda.current_device)
+                        raw or (lambda index: torch.cuda.current_stream(index).cuda_stream), torch.cuda.current_device, torch.uint8)
     return _torch_parts
 
 
@@ -594,7 +594,7 @@ _torch_parts = None
 
 def _begin(where: str, pos, x, dims: int, stream):
     """Checks of the positions and the leading tensor; ((blocks, t_block), element type code, stream)."""
-    codes, int32, _, raw_stream, current_device = _torch()
+    codes, int32, _, raw_stream, current_device, _ = _torch()
     index = pos.get_device()
     if pos.dtype is not int32 or pos.dim() != 2 or index < 0 or not pos.is_contiguous():
         raise TypeError("%s: pos must be a contiguous CUDA int32 tensor [blocks, t_block], as bload_pack writes it" % where)
@@ -696,11 +696,12 @@ def bload_recurrence_buffers(pos, x):
     """(carry, work) for bload_recurrence and its gradient on x [blocks, t_block, channels]: the float32 states that the
     forward call keeps for the gradient, [blocks, ceil(t_block / 64), channels], and scratch (None when none is needed).
     Calls that may overlap on the GPU need a scratch each."""
-    import torch
     b, t = pos.shape
-    carry = torch.empty((b, -(-t // RECURRENCE_RUN), x.shape[-1]), dtype=torch.float32, device=x.device)
-    n = load().bload_recurrence_work_bytes(b, t, x.shape[-1])
-    return carry, torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+    c = x.shape[-1]
+    n = load().bload_recurrence_work_bytes(b, t, c)
+    new = x.new_empty
+    return (new((b, -(-t // RECURRENCE_RUN), c), dtype=_torch()[2]),
+            new(n, dtype=_torch()[5]) if n else None)
 
 
 def _recurrence(where, pos, gate, x, carry, work, stream):

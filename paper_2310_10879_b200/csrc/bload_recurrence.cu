@@ -135,12 +135,12 @@ __device__ float2 look_back(const WorkView2& w, int64_t part, int64_t step, int 
     }
     __threadfence();
     float2 e = __ldcg(w.states + (part - far * step) * 32 + lane);
-    for (int64_t k = far - 1; k > 0; k -= 8) {  // eight loads at a time
-        float4 s[8];
+    for (int64_t k = far - 1; k > 0; k -= 16) {  // sixteen loads at a time
+        float4 s[16];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] = k > j ? __ldcg(w.sums + (part - (k - j) * step) * 32 + lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int j = 0; j < 16; ++j) s[j] = k > j ? __ldcg(w.sums + (part - (k - j) * step) * 32 + lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 16; ++j)
             if (k > j) e = make_float2(fmaf(s[j].x, e.x, s[j].y), fmaf(s[j].z, e.y, s[j].w));
     }
     return e;
@@ -280,9 +280,11 @@ struct Feed {
 };
 
 // OUTPUT false: only reduces `count` runs from `run` on (direction of the walk) to (A, state).
-template <typename T, bool GRAD, int COPY, bool OUTPUT>
+// before(state): called when the first runs are under way, brings the state that enters.
+template <typename T, bool GRAD, int COPY, bool OUTPUT, typename Before>
 __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>& a, int64_t q, int64_t ch0, int run, int count,
-                                     uint8_t* ring, Stretch (&sums)[2][GRAD ? 2 : 1][kWarps][32], Two (&entering)[2][32], Two& state, float2& A)
+                                     uint8_t* ring, Stretch (&sums)[2][GRAD ? 2 : 1][kWarps][32], Two (&entering)[2][32], Two& state, float2& A,
+                                     const Before& before)
 {
     constexpr int kTensors = GRAD && OUTPUT ? 3 : 2;
     constexpr int kDir = GRAD ? -1 : 1;
@@ -294,11 +296,12 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
     const int64_t c0 = ch0 + (kApart ? lane : 2 * lane), c1 = kApart ? c0 + 32 : c0 + 1;
     const bool on0 = c0 < p.channels, on1 = c1 < p.channels;
 
-    if (warp == 0) entering[0][lane] = state;
     F feed(a);
     feed.init(p, q, ch0, run, ring);
 #pragma unroll
     for (int k = 0; k < F::kStages - 1; ++k) feed.template fetch<kDir>(k, k, k < count);
+    before(state);
+    if (warp == 0) entering[0][lane] = state;
 
     T *out0 = nullptr, *out1 = nullptr;  // this lane's first element of the warp's first slot
     if (OUTPUT) {
@@ -533,29 +536,32 @@ __global__ void __launch_bounds__(256, 2)
                 count = end - from;
                 open = start < first * kRun && need;
             }
-            walk<T, GRAD, COPY, false>(p, a, q, ch0, from, count, ring, sums, entering, state, A);
+            walk<T, GRAD, COPY, false>(p, a, q, ch0, from, count, ring, sums, entering, state, A, [](Two&) {});
         }
-        if (threadIdx.x < 32) {
-            const float2 own = one(state);
-            if (give && !open) {
-                work.states[part * 32 + lane] = own;
-                set_flag(work.flags + part, 2, lane);
-            } else if (give) {
-                work.sums[part * 32 + lane] = make_float4(A.x, own.x, A.y, own.y);
-                set_flag(work.flags + part, 1, lane);
+        walk<T, GRAD, COPY, true>(p, a, q, ch0, GRAD ? end - 1 : first, end - first, ring, sums, entering, state, A, [&](Two& enters) {
+            if (threadIdx.x < 32) {
+                const float2 own = one(enters);
+                if (give && !open) {
+                    work.states[part * 32 + lane] = own;
+                    set_flag(work.flags + part, 2, lane);
+                } else if (give) {
+                    work.sums[part * 32 + lane] = make_float4(A.x, own.x, A.y, own.y);
+                    set_flag(work.flags + part, 1, lane);
+                }
+                float2 e = make_float2(0.0f, 0.0f);
+                if (need) e = look_back(work, part, groups, lane);
+                if (open) {
+                    work.states[part * 32 + lane] = make_float2(through(A.x, e.x, own.x), through(A.y, e.y, own.y));
+                    set_flag(work.flags + part, 2, lane);
+                }
+                from_before[lane] = e;
             }
-            float2 e = make_float2(0.0f, 0.0f);
-            if (need) e = look_back(work, part, groups, lane);
-            if (open) {
-                work.states[part * 32 + lane] = make_float2(through(A.x, e.x, own.x), through(A.y, e.y, own.y));
-                set_flag(work.flags + part, 2, lane);
-            }
-            from_before[lane] = e;
-        }
-        __syncthreads();
-        state = two(from_before[lane].x, from_before[lane].y);
+            __syncthreads();
+            enters = two(from_before[lane].x, from_before[lane].y);
+        });
+    } else {
+        walk<T, GRAD, COPY, true>(p, a, q, ch0, GRAD ? end - 1 : first, end - first, ring, sums, entering, state, A, [](Two&) {});
     }
-    walk<T, GRAD, COPY, true>(p, a, q, ch0, GRAD ? end - 1 : first, end - first, ring, sums, entering, state, A);
 }
 
 int64_t groups_of(int64_t blocks, int64_t channels) { return blocks * ((channels + kCh - 1) / kCh); }
