@@ -563,13 +563,14 @@ BLOAD_API int bload_attention_grad(const bload_attention_t* a, void* stream);
  *     g_s = dh_s + (f_{s+1} * g_{s+1} if the sequence continues at s + 1);
  *     dx_s = (1 - f_s) g_s;      dgate_s = g_s (h_{s-1} - x_s) f_s (1 - f_s).
  * Padding slots get h = 0, dgate = dx = 0.  gate, x, h, dh, dgate, dx are [block_count, t_block, channels] with
- * contiguous channels, strides in elements; data aligned to the element (16-byte aligned data and strides that are
- * multiples of 16 bytes take the fast path).
+ * contiguous channels, strides in elements; data aligned to the element (rows on 16-byte boundaries are fastest, then rows
+ * on 4-byte boundaries).
  *
  *   d_carry  float [block_count, ceil(t_block / BLOAD_RECURRENCE_RUN), channels]: the state that enters each run of
  *            BLOAD_RECURRENCE_RUN slots, written by the forward call and read by the gradient, which rebuilds h from it
  *            in 32 bits instead of reading the rounded h; 16-byte aligned; NULL in the forward call: not kept
- *   d_work   scratch of bload_recurrence_work_bytes bytes, 256-byte aligned, for both calls (NULL when that is 0)
+ *   d_work   scratch of bload_recurrence_work_bytes bytes, 256-byte aligned, for both calls (NULL when that is 0); calls that
+ *            may overlap on the GPU need one each
  * Errors: NULL, ARG (sizes, strides < 0, a broadcast output), ALIGN, WORKSPACE, UNSUPPORTED (dtype, t_block), CUDA.
  */
 #define BLOAD_RECURRENCE_RUN 64
@@ -592,8 +593,8 @@ BLOAD_API int bload_recurrence(const bload_recurrence_t* a, void* stream);
 BLOAD_API int bload_recurrence_grad(const bload_recurrence_t* a, void* stream);
 
 /*
- * bload_device_timeouts -- number of bounded device-side waits (of the attention kernels: on their own copies, matrix
- * products and arithmetic) that gave up since the library was loaded.  Anything but
+ * bload_device_timeouts -- number of bounded device-side waits (of the attention and recurrence kernels: on their own copies,
+ * matrix products and arithmetic, and on earlier segments of the same call) that gave up since the library was loaded.  Anything but
  * 0 means incomplete outputs.  Synchronises the device; -1 if that fails.
  */
 BLOAD_API int64_t bload_device_timeouts(void);
