@@ -191,7 +191,7 @@ struct Pair<__nv_bfloat16> {
 
 // Brings runs to a warp, some ahead of their use.  COPY 16 or 4: rows on boundaries of so many bytes, copied to shared memory
 // asynchronously in pieces of that size.  COPY 0 (16-bit elements in rows that start on any element): loaded one by one into
-// registers, a run ahead.  A lane has two neighbouring channels where these are one aligned word in memory, else (SPLIT)
+// registers, a run ahead, or for three tensors, which would not fit beside the run's own values, when the run's turn has come.  A lane has two neighbouring channels where these are one aligned word in memory, else (SPLIT)
 // channels l and l + 32, so that its loads and stores stay side by side with its neighbours'.
 // TENSORS 2: gate and x, or (DH) gate and dh; 3: gate, x, dh.
 template <typename T, int COPY>
@@ -199,7 +199,7 @@ constexpr bool kSplit = COPY == 0 || (COPY == 4 && sizeof(T) == 4);
 
 template <typename T, int TENSORS, bool DH, int COPY>
 struct Feed {
-    static constexpr bool kStaged = COPY > 0;
+    static constexpr bool kStaged = COPY > 0, kEarly = kStaged || TENSORS == 2;
     static constexpr int kRowBytes = kCh * sizeof(T), kTensorBytes = kRows * kRowBytes, kRunBytes = kWarps * TENSORS * kTensorBytes;
     static constexpr int kStages = !kStaged ? 2 : kRunBytes <= 16384 ? 4 : kRunBytes <= 32768 ? 3 : 2;  // of up to 96 KB in all
     static constexpr int kPieces = kStaged ? kRowBytes / COPY : 32, kCopies = kRows * kPieces / 32;  // per row; per lane and tensor
@@ -299,7 +299,7 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
     F feed(a);
     feed.init(p, q, ch0, run, ring);
 #pragma unroll
-    for (int k = 0; k < F::kStages - 1; ++k) feed.template fetch<kDir>(k, k, k < count);
+    for (int k = 0; k < F::kStages - 1 && F::kEarly; ++k) feed.template fetch<kDir>(k, k, k < count);
     before(state);
     if (warp == 0) entering[0][lane] = state;
 
@@ -314,6 +314,7 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
     int stage = 0;
     for (int i = 0; i < count; ++i, run += kDir) {
         const int s_warp = run * kRun + warp * kRows;
+        if (!F::kEarly) feed.template fetch<kDir>(0, 0, true);
         Two h_in = zero();  // (gradient) the state that entered this run forward
         if (GRAD && OUTPUT) h_in = two(on0 ? carry_at[c0] : 0.0f, on1 ? carry_at[c1] : 0.0f);
         if (COPY) {
@@ -384,7 +385,7 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
         __syncwarp();
 #pragma unroll
         for (int k = 0; k + 1 < F::kStages - 1; ++k) feed.ahead[k] = feed.ahead[k + 1];
-        feed.template fetch<kDir>(stage == 0 ? F::kStages - 1 : stage - 1, F::kStages - 2, i + F::kStages - 1 < count);
+        if (F::kEarly) feed.template fetch<kDir>(stage == 0 ? F::kStages - 1 : stage - 1, F::kStages - 2, i + F::kStages - 1 < count);
         stage = stage + 1 == F::kStages ? 0 : stage + 1;
         __syncthreads();
 
