@@ -563,8 +563,7 @@ BLOAD_API int bload_attention_grad(const bload_attention_t* a, void* stream);
  *     g_s = dh_s + (f_{s+1} * g_{s+1} if the sequence continues at s + 1);
  *     dx_s = (1 - f_s) g_s;      dgate_s = g_s (h_{s-1} - x_s) f_s (1 - f_s).
  * Padding slots get h = 0, dgate = dx = 0.  gate, x, h, dh, dgate, dx are [block_count, t_block, channels] with
- * contiguous channels, strides in elements; data aligned to the element (rows on 16-byte boundaries are fastest, then rows
- * on 4-byte boundaries).
+ * contiguous channels, strides in elements; data aligned to the element (rows on 16-byte boundaries are faster).
  *
  *   d_carry  float [block_count, ceil(t_block / BLOAD_RECURRENCE_RUN), channels]: the state that enters each run of
  *            BLOAD_RECURRENCE_RUN slots, written by the forward call and read by the gradient, which rebuilds h from it

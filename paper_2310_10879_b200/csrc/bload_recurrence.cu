@@ -146,15 +146,11 @@ __device__ float2 look_back(const WorkView2& w, int64_t part, int64_t step, int 
     return e;
 }
 
-// `bytes` of N bytes are copied, the rest are zeros
-template <int N>
-__device__ __forceinline__ void copy(void* dst, const void* src, int bytes)
+// `bytes` of 16 bytes are copied, the rest are zeros
+__device__ __forceinline__ void copy16(void* dst, const void* src, int bytes)
 {
-    const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst);
-    if (N == 16)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(src), "r"(bytes) : "memory");
-    else
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(src), "r"(bytes) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes)
+                 : "memory");
 }
 
 template <typename T>
@@ -189,21 +185,19 @@ struct Pair<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat162 join(__nv_bfloat16 a, __nv_bfloat16 b) { return __halves2bfloat162(a, b); }
 };
 
-// Brings runs to a warp, some ahead of their use.  COPY 16 or 4: rows on boundaries of so many bytes, copied to shared memory
-// asynchronously in pieces of that size.  COPY 0 (16-bit elements in rows that start on any element): loaded one by one into
-// registers, a run ahead, or for three tensors, which would not fit beside the run's own values, when the run's turn has come.  A lane has two neighbouring channels where these are one aligned word in memory, else (SPLIT)
-// channels l and l + 32, so that its loads and stores stay side by side with its neighbours'.
+// Brings runs to a warp.  STAGED: rows on 16-byte boundaries, copied to shared memory asynchronously, some runs ahead; a lane has
+// channels 2l and 2l + 1.  Otherwise elements are loaded one by one into registers, a run ahead, or for three tensors, which would
+// not fit beside the run's own values, when the run's turn has come; a lane has channels l and l + 32, so that its loads and stores
+// stay side by side with its neighbours'.  (Asynchronous copies of 4 bytes, where rows allow them, were slower: 30,001 x 251 fp32
+// 52 us forward and 76 gradient instead of 42 and 59.)
 // TENSORS 2: gate and x, or (DH) gate and dh; 3: gate, x, dh.
-template <typename T, int COPY>
-constexpr bool kSplit = COPY == 0 || (COPY == 4 && sizeof(T) == 4);
-
-template <typename T, int TENSORS, bool DH, int COPY>
+template <typename T, int TENSORS, bool DH, bool STAGED>
 struct Feed {
-    static constexpr bool kStaged = COPY > 0, kEarly = kStaged || TENSORS == 2;
+    static constexpr bool kStaged = STAGED, kEarly = kStaged || TENSORS == 2;
     static constexpr int kRowBytes = kCh * sizeof(T), kTensorBytes = kRows * kRowBytes, kRunBytes = kWarps * TENSORS * kTensorBytes;
     static constexpr int kStages = !kStaged ? 2 : kRunBytes <= 16384 ? 4 : kRunBytes <= 32768 ? 3 : 2;  // of up to 96 KB in all
-    static constexpr int kPieces = kStaged ? kRowBytes / COPY : 32, kCopies = kRows * kPieces / 32;  // per row; per lane and tensor
-    static constexpr int kPer = kStaged ? COPY / (int)sizeof(T) : 1;                                 // elements of a piece
+    static constexpr int kPieces = kStaged ? kRowBytes / 16 : 32, kRowsAtOnce = 32 / kPieces;  // per row; rows that a warp copies at once
+    static constexpr int kPer = kStaged ? 16 / (int)sizeof(T) : 1;                             // elements of a piece
 
     const RecurTensors<T>& a;
     const T* at[TENSORS];  // this lane's first element of the next run to fetch
@@ -217,9 +211,6 @@ struct Feed {
 
     __device__ __forceinline__ explicit Feed(const RecurTensors<T>& tensors) : a(tensors) {}
     __device__ __forceinline__ const Channels<const T>& tensor(int n) const { return n == 0 ? a.gate : n == 2 || DH ? a.dh : a.x; }
-    // copy j of a lane: row and channels relative to its first ones
-    static __device__ __forceinline__ int row_of(int j) { return kPieces >= 32 ? j / (kPieces / 32) : j * (32 / kPieces); }
-    static __device__ __forceinline__ int column_of(int j) { return kPieces > 32 ? j % (kPieces / 32) * 32 * kPer : 0; }
     __device__ __forceinline__ void init(const RecurParams& p, int64_t q, int64_t ch0, int run, uint8_t* shared)
     {
         const int warp = threadIdx.x >> 5;
@@ -245,16 +236,16 @@ struct Feed {
             for (int n = 0; n < TENSORS; ++n) {
                 const int64_t slot = tensor(n).slot;
                 if (kStaged) {
-                    uint8_t* const to = ring + stage * kRunBytes + n * kTensorBytes + lane * COPY;
+                    uint8_t* const to = ring + stage * kRunBytes + n * kTensorBytes + lane * 16;
+                    const T* from = at[n];
                     if (full) {
 #pragma unroll
-                        for (int j = 0; j < kCopies; ++j) copy<kStaged ? COPY : 4>(to + j * 32 * COPY, at[n] + row_of(j) * slot + column_of(j), COPY);
+                        for (int j = 0; j < kRows / kRowsAtOnce; ++j, from += kRowsAtOnce * slot) copy16(to + j * 512, from, 16);
                     } else {
 #pragma unroll
-                        for (int j = 0; j < kCopies; ++j) {
-                            const int more = (left - column_of(j)) * (int)sizeof(T);
-                            const int bytes = s + lane / kPieces + row_of(j) >= t || more <= 0 ? 0 : min(more, COPY);
-                            copy<kStaged ? COPY : 4>(to + j * 32 * COPY, bytes ? at[n] + row_of(j) * slot + column_of(j) : tensor(n).data, bytes);
+                        for (int j = 0; j < kRows / kRowsAtOnce; ++j, from += kRowsAtOnce * slot) {
+                            const int bytes = s + lane / kPieces + j * kRowsAtOnce >= t ? 0 : min(max(left * (int)sizeof(T), 0), 16);
+                            copy16(to + j * 512, bytes ? from : tensor(n).data, bytes);
                         }
                     }
                 } else {
@@ -274,14 +265,13 @@ struct Feed {
     {
         const uint8_t* const row = ring + stage * kRunBytes + n * kTensorBytes + r * kRowBytes;
         if (!kStaged) return Pair<T>::join(raw[kStaged ? 0 : n][kStaged ? 0 : r][0], raw[kStaged ? 0 : n][kStaged ? 0 : r][1]);
-        if (kSplit<T, COPY>) return Pair<T>::join(reinterpret_cast<const T*>(row)[lane], reinterpret_cast<const T*>(row)[lane + 32]);
         return reinterpret_cast<const typename Pair<T>::type*>(row)[lane];
     }
 };
 
 // OUTPUT false: only reduces `count` runs from `run` on (direction of the walk) to (A, state).
 // before(state): called when the first runs are under way, brings the state that enters.
-template <typename T, bool GRAD, int COPY, bool OUTPUT, typename Before>
+template <typename T, bool GRAD, bool STAGED, bool OUTPUT, typename Before>
 __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>& a, int64_t q, int64_t ch0, int run, int count,
                                      uint8_t* ring, Stretch (&sums)[2][GRAD ? 2 : 1][kWarps][32], Two (&entering)[2][32], Two& state, float2& A,
                                      const Before& before)
@@ -289,10 +279,10 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
     constexpr int kTensors = GRAD && OUTPUT ? 3 : 2;
     constexpr int kDir = GRAD ? -1 : 1;
     constexpr bool kForward = !GRAD || OUTPUT;  // h is needed
-    using F = Feed<T, kTensors, GRAD && !OUTPUT, COPY>;
+    using F = Feed<T, kTensors, GRAD && !OUTPUT, STAGED>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int runs = (p.t + kRun - 1) / kRun;
-    constexpr bool kApart = kSplit<T, COPY>;
+    constexpr bool kApart = !STAGED;
     const int64_t c0 = ch0 + (kApart ? lane : 2 * lane), c1 = kApart ? c0 + 32 : c0 + 1;
     const bool on0 = c0 < p.channels, on1 = c1 < p.channels;
 
@@ -317,7 +307,7 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
         if (!F::kEarly) feed.template fetch<kDir>(0, 0, true);
         Two h_in = zero();  // (gradient) the state that entered this run forward
         if (GRAD && OUTPUT) h_in = two(on0 ? carry_at[c0] : 0.0f, on1 ? carry_at[c1] : 0.0f);
-        if (COPY) {
+        if (STAGED) {
             asm volatile("cp.async.wait_group %0;" ::"n"(F::kStages - 2) : "memory");
             __syncwarp();
         }
@@ -485,13 +475,13 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
             carry_at -= p.channels;
         }
     }
-    if (COPY) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (STAGED) asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();  // the ring and the sums may be used again
     state = entering[count & 1][lane];
     __syncthreads();
 }
 
-template <typename T, bool GRAD, int COPY>
+template <typename T, bool GRAD, bool STAGED>
 __global__ void __launch_bounds__(256, 2)
     k27_recurrence(const RecurParams p, const RecurTensors<T> a, int groups_per_block, int segments)
 {
@@ -537,9 +527,9 @@ __global__ void __launch_bounds__(256, 2)
                 count = end - from;
                 open = start < first * kRun && need;
             }
-            walk<T, GRAD, COPY, false>(p, a, q, ch0, from, count, ring, sums, entering, state, A, [](Two&) {});
+            walk<T, GRAD, STAGED, false>(p, a, q, ch0, from, count, ring, sums, entering, state, A, [](Two&) {});
         }
-        walk<T, GRAD, COPY, true>(p, a, q, ch0, GRAD ? end - 1 : first, end - first, ring, sums, entering, state, A, [&](Two& enters) {
+        walk<T, GRAD, STAGED, true>(p, a, q, ch0, GRAD ? end - 1 : first, end - first, ring, sums, entering, state, A, [&](Two& enters) {
             if (threadIdx.x < 32) {
                 const float2 own = one(enters);
                 if (give && !open) {
@@ -561,7 +551,7 @@ __global__ void __launch_bounds__(256, 2)
             enters = two(from_before[lane].x, from_before[lane].y);
         });
     } else {
-        walk<T, GRAD, COPY, true>(p, a, q, ch0, GRAD ? end - 1 : first, end - first, ring, sums, entering, state, A, [](Two&) {});
+        walk<T, GRAD, STAGED, true>(p, a, q, ch0, GRAD ? end - 1 : first, end - first, ring, sums, entering, state, A, [](Two&) {});
     }
 }
 
@@ -577,15 +567,15 @@ int segments_of(int64_t blocks, int32_t t, int64_t channels)
     return (int)(wanted < most ? (wanted < 1 ? 1 : wanted) : (most < 1 ? 1 : most));
 }
 
-template <typename T, bool GRAD, int COPY>
+template <typename T, bool GRAD, bool STAGED>
 cudaError_t launch(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t st)
 {
-    using F = Feed<T, GRAD ? 3 : 2, false, COPY>;
-    constexpr int kShared = COPY ? F::kStages * F::kRunBytes : 0;
-    static_assert(!GRAD || !COPY || kShared >= Feed<T, 2, true, COPY>::kStages * Feed<T, 2, true, COPY>::kRunBytes, "both walks fit");
+    using F = Feed<T, GRAD ? 3 : 2, false, STAGED>;
+    constexpr int kShared = STAGED ? F::kStages * F::kRunBytes : 0;
+    static_assert(!GRAD || !STAGED || kShared >= Feed<T, 2, true, STAGED>::kStages * Feed<T, 2, true, STAGED>::kRunBytes, "both walks fit");
     const int64_t groups = groups_of(p.blocks, p.channels);
     const int segments = segments_of(p.blocks, p.t, p.channels);
-    auto* kernel = k27_recurrence<T, GRAD, COPY>;
+    auto* kernel = k27_recurrence<T, GRAD, STAGED>;
     static std::atomic<uint64_t> allowed{0};
     const cudaError_t shared = allow_shared(kernel, kShared, allowed);
     if (shared != cudaSuccess) return shared;
@@ -598,22 +588,16 @@ cudaError_t launch(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t 
     return cudaGetLastError();
 }
 
-// rows start on boundaries of n bytes
 template <typename T>
-bool on(const Channels<T>& x, int n)
+bool on_16(const Channels<T>& x)
 {
-    return reinterpret_cast<uintptr_t>(x.data) % n == 0 && x.block * sizeof(T) % n == 0 && x.slot * sizeof(T) % n == 0;
+    return reinterpret_cast<uintptr_t>(x.data) % 16 == 0 && x.block * sizeof(T) % 16 == 0 && x.slot * sizeof(T) % 16 == 0;
 }
 template <typename T, bool GRAD>
 cudaError_t launch_on(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t st)
 {
-    auto all = [&](int n) {
-        return on(a.gate, n) && on(a.x, n) && (GRAD ? on(a.dh, n) && on(a.dgate, n) && on(a.dx, n) : on(a.h, n));
-    };
-    if (all(16)) return launch<T, GRAD, 16>(p, a, st);
-    if (all(4)) return launch<T, GRAD, 4>(p, a, st);
-    if constexpr (sizeof(T) == 2) return launch<T, GRAD, 0>(p, a, st);
-    return cudaErrorInvalidValue;  // (32-bit elements are 4-byte aligned)
+    const bool staged = on_16(a.gate) && on_16(a.x) && (GRAD ? on_16(a.dh) && on_16(a.dgate) && on_16(a.dx) : on_16(a.h));
+    return staged ? launch<T, GRAD, true>(p, a, st) : launch<T, GRAD, false>(p, a, st);
 }
 
 }  // namespace
