@@ -132,28 +132,35 @@ struct Modifier {
         for (int e = 0; e < 32; ++e) top[e & 1] = fmaxf(top[e & 1], fabsf(__uint_as_float(qk[e])));
         return __all_sync(0xffffffffu, fmaxf(top[0], top[1]) * fabsf(unit) < 0.5f) ? kNear : kAny;
     }
+    // Of two neighbouring columns, the first `apart` slots behind (a whole number, exact as float: conversions of integers run at
+    // a quarter of the rate of additions).
     // tanh(y), |y| < 1/2: y (1 + c1 y^2 + ... + c4 y^8), the coefficients of smallest largest relative error (2.8e-8, found by
     // iteratively reweighted least squares).  Else 1 - 2 / (1 + exp(2 y)), whose absolute error of some 2^-23 is small against
     // values from 0.46 on, but not against a score much smaller than its cap.
     template <int KIND>
-    __device__ __forceinline__ float apply(float qk, float apart, float& inner) const
+    __device__ __forceinline__ Two apply(Two qk, float apart, Two& inner) const
     {
-        float x = qk * by;
-        inner = 1.0f;
-        if (KIND != kPlain) {
-            const float y = qk * unit, z = y * y;
-            float th = fmaf(z, 0.0171350036f, -0.0529860742f);
-            th = fmaf(th, z, 0.133247793f);
-            th = fmaf(th, z, -0.333330691f);
-            th = fmaf(th * z, y, y);
+        auto both = [](float c) { return two(c, c); };
+        Two x;
+        if (KIND == kPlain) {
+            x = qk * both(by);
+            inner = both(1.0f);
+        } else {
+            const Two y = qk * both(unit), z = y * y;
+            Two th = fma(z, both(0.0171350036f), both(-0.0529860742f));
+            th = fma(th, z, both(0.133247793f));
+            th = fma(th, z, both(-0.333330691f));
+            th = fma(th * z, y, y);
             if (KIND == kAny) {
-                const float far = fmaf(-2.0f, tc::inverse_fast(1.0f + tc::exp2_fast(y * (2.0f * kLog2e))), 1.0f);
-                th = fabsf(y) < 0.5f ? th : far;  // (NaN goes to far, and stays)
+                const float2 y1 = one(y), t1 = one(th);
+                auto far = [](float v) { return fmaf(-2.0f, tc::inverse_fast(1.0f + tc::exp2_fast(v * (2.0f * kLog2e))), 1.0f); };
+                th = two(fabsf(y1.x) < 0.5f ? t1.x : far(y1.x), fabsf(y1.y) < 0.5f ? t1.y : far(y1.y));  // (NaN goes to far, and stays)
             }
-            x = cap2 * th;
-            inner = fmaf(-th, th, 1.0f);
+            x = both(cap2) * th;
+            inner = fma(th * both(-1.0f), th, both(1.0f));
         }
-        return fmaf(-slope2, fabsf(apart), x);
+        const float2 v = one(x);
+        return two(fmaf(-slope2, fabsf(apart), v.x), fmaf(-slope2, fabsf(apart - 1.0f), v.y));
     }
     // f(kind) with the kind as a constant
     template <typename F>
@@ -371,6 +378,7 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
             // The scores in units of log2 are x by (MOD: x itself); hidden ones are -inf.  They are read twice, for the maximum and
             // for the exponentials: 64 of them would not stay in this thread's registers.  What changes them is written back.
             const uint32_t own_at = s_at + lanes + 64 * half;
+            const float apart = (float)(row - mine0);
             // All seen by all of the warp's rows, none by any: per 64 columns, or for heads of at most 64 elements, where short walks
             // are what counts, per 32 (16 x 1000 frames of features 69 -> 65 us, but one sequence of 16,384 304 -> 321 us).
             constexpr int kFine = kHalves == 1 ? 2 : 1;
@@ -392,10 +400,12 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
                 if (MOD)
                     Modifier::with(modify.kind(s), [&](auto kind) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            float inner;
-                            s[e] = __float_as_uint(
-                                modify.apply<decltype(kind)::value>(__uint_as_float(s[e]), (float)(row - mine0 - 32 * c - e), inner));
+                        for (int e = 0; e < 32; e += 2) {
+                            Two inner;
+                            const float2 x = one(modify.apply<decltype(kind)::value>(two(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
+                                                                                     apart - (float)(32 * c + e), inner));
+                            s[e] = __float_as_uint(x.x);
+                            s[e + 1] = __float_as_uint(x.y);
                         }
                     });
                 if (!clear[c]) {
@@ -789,12 +799,19 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                     tc::bar_arrive(p_full);
                 }
                 const Two by2 = two(modify.by, modify.by);
+                const float apart = (float)(row - mine0);
                 if (MOD)
                     Modifier::with(modify.kind(s), [&](auto kind) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            s[e] = __float_as_uint(modify.apply<decltype(kind)::value>(__uint_as_float(s[e]), (float)(row - mine0 - e),
-                                                                                      in[MOD ? e : 0]));
+                        for (int e = 0; e < 32; e += 2) {
+                            Two inner;
+                            const float2 x = one(modify.apply<decltype(kind)::value>(two(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
+                                                                                     apart - (float)e, inner));
+                            s[e] = __float_as_uint(x.x);
+                            s[e + 1] = __float_as_uint(x.y);
+                            in[MOD ? e : 0] = one(inner).x;
+                            in[MOD ? e + 1 : 0] = one(inner).y;
+                        }
                     });
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
@@ -822,6 +839,9 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 for (int e = 0; e < 32; e += 2)
                     pw[e / 2] = MOD && !KEYS ? tc::pack<BF16>(w[e] * in[MOD ? e : 0], w[e + 1] * in[MOD ? e + 1 : 0]) : tc::pack<BF16>(w[e], w[e + 1]);
                 tc::tmem_store16(s_at + lanes + 32 * part, pw);  // over the scores they were made from
+                if (MOD && KEYS)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) w[e] *= in[MOD ? e : 0];  // (only together from here on)
                 scan(KEYS ? b2_full : b1_full, i, KEYS ? 1 : 0, j0);
                 tc::tmem_stored();
                 tc::fence_before();
@@ -832,23 +852,32 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 break;
             }
             tc::fence_after();
-            uint32_t d[32], dw[16];
-            tc::tmem_load(d, dp_at + lanes + 32 * part);
-            tc::tmem_loaded();
-            tc::settle(d);
+            uint32_t dw[16];
+            // (with a cap and rows of queries, two numbers per column wait for dP already: it is read in halves then, for registers)
+            constexpr int kAtOnce = MOD && !KEYS ? 16 : 32;
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-                Two delta_here = delta2;
-                if (KEYS) {
-                    const float2 l = *(reinterpret_cast<const float2*>(&column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0]) + 1);
-                    delta_here = two(l.x, l.y);
+            for (int c = 0; c < 32; c += kAtOnce) {
+                uint32_t d[kAtOnce];
+                tc::tmem_load(d, dp_at + lanes + 32 * part + c);
+                tc::tmem_loaded();
+                tc::settle(d);
+#pragma unroll
+                for (int k = 0; k < kAtOnce; k += 2) {
+                    const int e = c + k;
+                    Two delta_here = delta2;
+                    if (KEYS) {
+                        const float2 l = *(reinterpret_cast<const float2*>(&column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0]) + 1);
+                        delta_here = two(l.x, l.y);
+                    }
+                    Two g = two(__uint_as_float(d[k]), __uint_as_float(d[k + 1])) + delta_here;
+                    if (!clear) g = two((mask >> e) & 1 ? one(g).x : 0.0f, (mask >> (e + 1)) & 1 ? one(g).y : 0.0f);  // (may be NaN)
+                    g = two(w[e], w[e + 1]) * g;
+                    if (!KEYS) {
+                        eps2 = eps2 + g;
+                        if (MOD) g = g * two(in[MOD ? e : 0], in[MOD ? e + 1 : 0]);
+                    }
+                    dw[e / 2] = tc::pack<BF16>(one(g).x, one(g).y);
                 }
-                Two g = two(__uint_as_float(d[e]), __uint_as_float(d[e + 1])) + delta_here;
-                if (!clear) g = two((mask >> e) & 1 ? one(g).x : 0.0f, (mask >> (e + 1)) & 1 ? one(g).y : 0.0f);  // (may be NaN)
-                g = two(w[e], w[e + 1]) * g;
-                if (!KEYS) eps2 = eps2 + g;
-                if (MOD) g = g * two(in[MOD ? e : 0], in[MOD ? e + 1 : 0]);
-                dw[e / 2] = tc::pack<BF16>(one(g).x, one(g).y);
             }
             tc::tmem_store16(dp_at + lanes + 32 * part, dw);
             if (KEYS || !second) scan(b1_full, i, 0, j0);
