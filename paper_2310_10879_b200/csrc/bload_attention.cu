@@ -112,6 +112,27 @@ __device__ __forceinline__ Reach get_reach(const ReachShared<WARPS>& sh)
     return r;
 }
 
+// A CTA's tiles of COLUMNS columns: tile i starts at first + i * step.  Causal walks start at the CTA's own rows, from where queries go
+// down and keys go up, so that the first tile can be copied in before the positions are known; others at the smallest lo.
+template <int COLUMNS>
+struct Walk {
+    int first, step;
+    static __device__ __forceinline__ int causal_first(const AttnParams& p, int row0, bool keys)
+    {
+        return keys ? row0 : row0 + (min(p.t - row0, 128) - 1) / COLUMNS * COLUMNS;
+    }
+    __device__ __forceinline__ Walk(const AttnParams& p, const Reach& r, int row0, bool keys)
+    {
+        first = p.causal ? causal_first(p, row0, keys) : r.lo;
+        step = p.causal && !keys ? -COLUMNS : COLUMNS;
+    }
+    __device__ __forceinline__ int count(const Reach& r) const
+    {
+        return r.hi < 0 ? 0 : step > 0 ? (r.hi - first) / COLUMNS + 1 : (max(first - r.lo, 0) + COLUMNS - 1) / COLUMNS + 1;
+    }
+    __device__ __forceinline__ int operator()(int i) const { return first + i * step; }
+};
+
 // score in units of log2 from q.k, with the cap and the distance bias; `inner` = d score / d (scale q.k)
 struct Modifier {
     enum { kPlain, kNear, kAny };  // no cap; capped and every |scale q.k / cap| of the warp's columns below 1/2; capped
@@ -280,6 +301,11 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
     const int half = warp >> 2, quarter = warp & 3;  // of the arithmetic's warps
     const int own_row = quarter * 32 + lane, row = i0 + own_row;
 
+    auto load = [&](bool keys, int s, int j0) {  // the tile of keys (or of values) from slot j0 on, to stage s
+        const uint32_t bar = (keys ? k_full : v_full) + 8 * s, to = tc::smem_of(keys ? k_tiles : v_tiles) + s * Tile::kTile;
+        tc::bar_expect(bar, Tile::kTile);
+        for (int x = 0; x < DP; x += 64) tc::tensor_load(to + x * (2 * kKeys), keys ? &maps.k : &maps.v, x, j0, hk, b, bar);
+    };
     rows::Span span{kNever, -1};
     if (warp < kWarps) {
         span = span_of(p, pos, row, false, lane);
@@ -295,6 +321,11 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
             tc::bar_init_done();
             tc::bar_expect(q_full, Tile::kQueries);  // under way while the rows look for their keys
             for (int x = 0; x < DP; x += 64) tc::tensor_load(tc::smem_of(q_tile) + x * 256, &maps.q, x, i0, h, b, q_full);
+            if (p.causal) {
+                const int j0 = Walk<kKeys>::causal_first(p, i0, false);
+                load(true, 0, j0);
+                load(false, 0, j0);
+            }
         }
     } else {
         tc::tmem_alloc<Tile::kTmem>(tc::smem_of(&tmem_base));
@@ -304,29 +335,25 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
     tc::fence_after();
     const uint32_t tmem = tmem_base, o_at = tmem, s_at = tmem + DP;
     const Reach reach = get_reach(reach_shared);
-    const int n = reach.hi < 0 ? 0 : (reach.hi - reach.lo) / kKeys + 1;
+    const Walk<kKeys> walk(p, reach, i0, false);
+    const int n = walk.count(reach);
     float m = -INFINITY, l = 0.0f;  // running maximum (log2 units; may lag by kLag) and sum
 
     if (warp == kWarps) {
         if (lane == 0) {
             bool ok = true;
-            if (n == 0) ok = tc::bar_wait(q_full, 0);  // (its place is written to below)
-            int issued = 0;
-            for (int i = 0; i < n && ok; ++i, ++issued) {
+            if (n == 0) ok = tc::bar_wait(q_full, 0) && (!p.causal || (tc::bar_wait(k_full, 0) && tc::bar_wait(v_full, 0)));  // (copies end)
+            int issued = p.causal;
+            for (int i = issued; i < n && ok; ++i, ++issued) {
                 const int s = i % Tile::kStages;
                 const uint32_t parity = (i / Tile::kStages + 1) & 1;
-                const int j0 = reach.lo + i * kKeys;
                 if (!(ok = tc::bar_wait(k_free + 8 * s, parity))) break;
-                tc::bar_expect(k_full + 8 * s, Tile::kTile);
-                for (int x = 0; x < DP; x += 64)
-                    tc::tensor_load(tc::smem_of(k_tiles) + s * Tile::kTile + x * (2 * kKeys), &maps.k, x, j0, hk, b, k_full + 8 * s);
+                load(true, s, walk(i));
                 if (!(ok = tc::bar_wait(v_free + 8 * s, parity))) {
                     tc::bar_wait(k_full + 8 * s, (i / Tile::kStages) & 1);  // a copy in flight ends before the CTA does
                     break;
                 }
-                tc::bar_expect(v_full + 8 * s, Tile::kTile);
-                for (int x = 0; x < DP; x += 64)
-                    tc::tensor_load(tc::smem_of(v_tiles) + s * Tile::kTile + x * (2 * kKeys), &maps.v, x, j0, hk, b, v_full + 8 * s);
+                load(false, s, walk(i));
             }
             if (!ok) {
                 dead = 1;
@@ -371,7 +398,7 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
         bool found = false, ok = true;
         for (int i = 0; i < n; ++i) {
             const int st = i % Tile::kStages;
-            const int j0 = reach.lo + i * kKeys, mine0 = j0 + 64 * half;  // the tile's and this warp's first key
+            const int j0 = walk(i), mine0 = j0 + 64 * half;  // the tile's and this warp's first key
             // (a warp that gives up goes on without waiting: its partner meets it at a barrier in every turn)
             if (ok && !(ok = __all_sync(0xffffffffu, tc::bar_wait(s_full, i & 1)))) dead = 1;
             tc::fence_after();
@@ -578,7 +605,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     __shared__ uint32_t tmem_base;
     __shared__ int dead, junk;
     __shared__ ReachShared<4> reach_shared;
-    __shared__ float eps_shared[kColumns / 32][128], delta_shared[KEYS ? 1 : kColumns / 32][128];
+    __shared__ float eps_shared[kColumns / 32][128], delta_shared[KEYS ? 1 : 128];
     __shared__ float4 column_stats[KEYS ? kWarps : 1][KEYS ? 16 : 1];  // per warp: -lse (log2 units) and -delta of 16 pairs of columns
 
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -601,32 +628,47 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     const int part = warp >> 2, quarter = warp & 3;  // of the arithmetic's warps: which 32 columns, which 32 rows
     const int own_row = quarter * 32 + lane, row = r0 + own_row;
 
+    // the tile B1 or B2 of head hs from slot j0 on, to stage s
+    auto load = [&](bool one, int s, int j0, int hs) {
+        const uint32_t bar = (one ? b1_full : b2_full) + 8 * s, to = tc::smem_of(stream) + (2 * s + (one ? 0 : 1)) * Tile::kStream;
+        tc::bar_expect(bar, Tile::kStream);
+        for (int x = 0; x < DP; x += 64) tc::tensor_load(to + x * (2 * kColumns), one ? &maps.b1 : &maps.b2, x, j0, hs, b, bar);
+    };
+    const int first_head = KEYS ? h * p.group : h / p.group;  // of the other side
     rows::Span span{kNever, -1};
+    float own_lse = 0.0f;  // queries: of this row
     if (warp < kWarps) {
+        // dout . out of the queries: DP / 8 lanes read a row, 16 bytes each, so that a warp's load touches few lines (with a row per
+        // lane it was 32 each, and the first tile waited 4 us)
+        using E = typename Element<BF16>::type;
+        constexpr int kLanes = DP / 8, kPasses = KEYS ? 1 : 128 * kLanes / (32 * kWarps);
+        uint4 x[kPasses] = {}, y[kPasses] = {};
+        const int sum_row = warp * (32 / kLanes) + lane / kLanes, e0 = lane % kLanes * 8;
+        if (!KEYS) {
+            if (row < p.t) own_lse = p.lse[((int64_t)b * p.heads + h) * p.t + row];
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k) {
+                const int r = r0 + sum_row + k * (32 / kLanes) * kWarps;
+                if (r < p.t && e0 < p.d) {
+                    x[k] = *reinterpret_cast<const uint4*>(a.out_in.at(b, r, h) + e0);
+                    y[k] = *reinterpret_cast<const uint4*>(a.dout.at(b, r, h) + e0);
+                }
+            }
+        }
         span = span_of(p, pos, row, KEYS, lane);
         if (part == 0) put_reach(reach_shared, quarter, lane, span);
         if (tid == 0) dead = junk = 0;
-        if (!KEYS) {  // dout . out: the warps of a row share out its elements
-            float sum = 0.0f;
-            if (row < p.t) {
-                using E = typename Element<BF16>::type;
-                const E* const o = a.out_in.at(b, row, h);
-                const E* const g = a.dout.at(b, row, h);
-                constexpr int kEach = 4 * DP / kColumns;  // of 16 bytes
-                uint4 x[kEach], y[kEach];
+        if (!KEYS) {
 #pragma unroll
-                for (int k = 0; k < kEach; ++k) {
-                    const int e = (part * kEach + k) * 8;
-                    x[k] = e < p.d ? *reinterpret_cast<const uint4*>(o + e) : make_uint4(0, 0, 0, 0);
-                    y[k] = e < p.d ? *reinterpret_cast<const uint4*>(g + e) : make_uint4(0, 0, 0, 0);
-                }
+            for (int k = 0; k < kPasses; ++k) {
+                float sum = 0.0f;
 #pragma unroll
-                for (int k = 0; k < kEach; ++k)
+                for (int e = 0; e < 8; ++e)
+                    sum = fmaf(to_float(reinterpret_cast<const E*>(&x[k])[e]), to_float(reinterpret_cast<const E*>(&y[k])[e]), sum);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        sum = fmaf(to_float(reinterpret_cast<const E*>(&x[k])[e]), to_float(reinterpret_cast<const E*>(&y[k])[e]), sum);
+                for (int o = 1; o < kLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if (e0 == 0) delta_shared[KEYS ? 0 : sum_row + k * (32 / kLanes) * kWarps] = sum;
             }
-            delta_shared[part][own_row] = sum;
         }
     } else if (warp == kWarps) {
         if (lane == 0) {
@@ -644,6 +686,11 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 tc::tensor_load(tc::smem_of(a1) + x * 256, &maps.a1, x, r0, h, b, a_full);
                 tc::tensor_load(tc::smem_of(a2) + x * 256, &maps.a2, x, r0, h, b, a_full);
             }
+            if (p.causal) {
+                const int j0 = Walk<kColumns>::causal_first(p, r0, KEYS);
+                load(true, 0, j0, first_head);
+                load(false, 0, j0, first_head);
+            }
         }
     } else {
         tc::tmem_alloc<Tile::kTmem>(tc::smem_of(&tmem_base));
@@ -653,7 +700,8 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     tc::fence_after();
     const uint32_t tmem = tmem_base, acc1_at = tmem, acc2_at = tmem + DP, s_at = tmem + 2 * DP, dp_at = s_at + kColumns;
     const Reach reach = get_reach(reach_shared);
-    const int per_head = reach.hi < 0 ? 0 : (reach.hi - reach.lo) / kColumns + 1;
+    const Walk<kColumns> walk(p, reach, r0, KEYS);
+    const int per_head = walk.count(reach);
     const int n = KEYS ? per_head * p.group : per_head;
     const bool second = KEYS || n * kColumns <= kExact;  // acc2 is kept
     float delta = 0.0f;
@@ -661,21 +709,17 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     if (warp == kWarps) {
         if (lane == 0) {
             bool ok = true;
-            if (n == 0) ok = tc::bar_wait(a_full, 0);  // (their place is written to below)
-            int issued1 = 0, issued2 = 0;
-            for (int i = 0; i < n && ok; ++i) {
+            if (n == 0) ok = tc::bar_wait(a_full, 0) && (!p.causal || (tc::bar_wait(b1_full, 0) && tc::bar_wait(b2_full, 0)));  // (copies end)
+            int issued1 = p.causal, issued2 = p.causal;
+            for (int i = p.causal; i < n && ok; ++i) {
                 const int s = i % kStages;
                 const uint32_t parity = (i / kStages + 1) & 1;
-                const int j0 = reach.lo + (KEYS ? i % per_head : i) * kColumns, hs = KEYS ? h * p.group + i / per_head : h / p.group;
-                const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream;
+                const int j0 = walk(KEYS ? i % per_head : i), hs = KEYS ? first_head + i / per_head : first_head;
                 if (!(ok = tc::bar_wait(b1_free + 8 * s, parity))) break;
-                tc::bar_expect(b1_full + 8 * s, Tile::kStream);
-                for (int x = 0; x < DP; x += 64) tc::tensor_load(at + x * (2 * kColumns), &maps.b1, x, j0, hs, b, b1_full + 8 * s);
+                load(true, s, j0, hs);
                 issued1 = i + 1;
                 if (!(ok = tc::bar_wait(b2_free + 8 * s, parity))) break;
-                tc::bar_expect(b2_full + 8 * s, Tile::kStream);
-                for (int x = 0; x < DP; x += 64)
-                    tc::tensor_load(at + Tile::kStream + x * (2 * kColumns), &maps.b2, x, j0, hs, b, b2_full + 8 * s);
+                load(false, s, j0, hs);
                 issued2 = i + 1;
             }
             if (!ok) {  // copies in flight end before the CTA does
@@ -735,9 +779,9 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         bool found = false;
         Two lse2 = zero(), eps2 = zero();  // lse and delta of this row, negative
         if (!KEYS && row < p.t) {          // this row's statistics
-            const float lse = minus_lse(p.lse[((int64_t)b * p.heads + h) * p.t + row]);
+            const float lse = minus_lse(own_lse);
             lse2 = two(lse, lse);
-            for (int k = 0; k < kColumns / 32; ++k) delta += delta_shared[KEYS ? 0 : k][own_row];
+            delta = delta_shared[KEYS ? 0 : own_row];
         }
         const Two delta2 = two(-delta, -delta);
         // junk in a tile that is hidden from some row must not reach the products
@@ -747,18 +791,25 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
             found |= scan_tile_apart<BF16, kColumns, DP, 32 * kWarps>(p, pos, stream + ((i % kStages) * 2 + which) * Tile::kStream, j0, tid);
             tc::writes_to_async();
         };
+        // KEYS: statistics of this warp's 32 columns of tile i, a tile ahead
+        float next_lse = 0.0f, next_delta = 0.0f;
+        auto fetch = [&](int i) {
+            const int column = walk(i % per_head) + 32 * part + lane;
+            const int64_t at = ((int64_t)b * p.heads + first_head + i / per_head) * p.t + column;
+            next_lse = column < p.t ? p.lse[at] : 0.0f;
+            next_delta = column < p.t ? p.delta[at] : 0.0f;
+        };
+        if (KEYS && n > 0) fetch(0);
         for (int i = 0; i < n; ++i) {
-            const int j0 = reach.lo + (KEYS ? i % per_head : i) * kColumns, mine0 = j0 + 32 * part;  // the tile's and this warp's first column
-            const int hq = KEYS ? h * p.group + i / per_head : h;
-            const Modifier modify(p, hq);
-            if (KEYS) {  // statistics of this warp's 32 columns
-                const int64_t at = ((int64_t)b * p.heads + hq) * p.t + mine0 + lane;
-                const bool in = mine0 + lane < p.t;
+            const int j0 = walk(KEYS ? i % per_head : i), mine0 = j0 + 32 * part;  // the tile's and this warp's first column
+            const Modifier modify(p, KEYS ? first_head + i / per_head : h);
+            if (KEYS) {
                 __syncwarp();
                 float* const st = reinterpret_cast<float*>(&column_stats[KEYS ? warp : 0][KEYS ? lane / 2 : 0]) + (lane & 1);
-                st[0] = in ? minus_lse(p.lse[at]) : 0.0f;
-                st[2] = in ? -p.delta[at] : 0.0f;
+                st[0] = minus_lse(next_lse);
+                st[2] = -next_delta;
                 __syncwarp();
+                if (i + 1 < n) fetch(i + 1);
             }
             const bool clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 31);
             const uint32_t mask = clear ? 0xffffffffu : column_mask(span.lo - mine0, span.hi - mine0);
