@@ -562,7 +562,6 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
 struct GradMaps {
     CUtensorMap a1, a2;  // the CTA's own rows: boxes of 128 rows.  q, dout | k, v
     CUtensorMap b1, b2;  // what streams by: boxes of kColumns.     k, v    | q, dout
-    CUtensorMap o1, o2;  // boxes of 32 rows.                       dq, -   | dk, dv
 };
 
 // Tiles of 128 columns and all of the tensor memory; for heads of at most 64 elements, tiles of 64 and half of it: then two CTAs
@@ -593,6 +592,25 @@ struct GradTile {
 // tiles of 64 columns each, taking turns, kept the tensor cores at 41 %: with 64 columns a product reads 192 bytes of shared
 // memory per cycle where there are 128, and what it reads of A serves half as many columns.)
 constexpr int kExact = 1024;
+
+// The 32 rows by 32 columns (from `first` on, `column` in the tile) that a warp has staged, to memory: 16 bytes per lane, side by side.
+// At one CTA per SM that is 400 to 600 cycles less than a tensor store, whose reads the CTA has to see the end of; the forward
+// kernel, whose CTAs hide each other's ends, is slower for it (features 65 -> 70 us).
+template <typename T>
+__device__ __forceinline__ void store_staged(const uint8_t* tile, int own_row0, int column, const AttnParams& p, const Heads<T>& out, int b, int h,
+                                             int row0, int first, int lane)
+{
+    const int c = lane % 4;
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = k * 8 + lane / 4;
+        if (first + c * 8 < p.d && row0 + r < p.t)
+            *reinterpret_cast<uint4*>(out.at(b, row0 + r, h) + first + c * 8) =
+                *reinterpret_cast<const uint4*>(tile + (own_row0 + r) * 128 + (((column / 8 + c) ^ (r & 7)) * 16));
+    }
+    __syncwarp();
+}
 
 template <bool BF16, int DP, bool MOD, bool KEYS>
 __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
@@ -637,39 +655,24 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     const int first_head = KEYS ? h * p.group : h / p.group;  // of the other side
     rows::Span span{kNever, -1};
     float own_lse = 0.0f;  // queries: of this row
+    // dout . out of the queries: DP / 8 lanes share a row, 16 bytes each, so that a load of a warp touches few lines (with a row per
+    // lane it was 32 each, and the first tile waited 4 us)
+    using E = typename Element<BF16>::type;
+    constexpr int kSumLanes = DP / 8, kSumRows = kWarps * 32 / kSumLanes, kPasses = KEYS ? 1 : 128 / kSumRows;
+    const int sum_row = warp * (32 / kSumLanes) + lane / kSumLanes, sum_chunk = lane % kSumLanes;
+    uint4 out_part[kPasses] = {};
     if (warp < kWarps) {
-        // dout . out of the queries: DP / 8 lanes read a row, 16 bytes each, so that a warp's load touches few lines (with a row per
-        // lane it was 32 each, and the first tile waited 4 us)
-        using E = typename Element<BF16>::type;
-        constexpr int kLanes = DP / 8, kPasses = KEYS ? 1 : 128 * kLanes / (32 * kWarps);
-        uint4 x[kPasses] = {}, y[kPasses] = {};
-        const int sum_row = warp * (32 / kLanes) + lane / kLanes, e0 = lane % kLanes * 8;
-        if (!KEYS) {
+        if (!KEYS) {  // under way while the rows look for their columns
             if (row < p.t) own_lse = p.lse[((int64_t)b * p.heads + h) * p.t + row];
 #pragma unroll
             for (int k = 0; k < kPasses; ++k) {
-                const int r = r0 + sum_row + k * (32 / kLanes) * kWarps;
-                if (r < p.t && e0 < p.d) {
-                    x[k] = *reinterpret_cast<const uint4*>(a.out_in.at(b, r, h) + e0);
-                    y[k] = *reinterpret_cast<const uint4*>(a.dout.at(b, r, h) + e0);
-                }
+                const int r = r0 + sum_row + k * kSumRows;
+                if (r < p.t && sum_chunk * 8 < p.d) out_part[k] = *reinterpret_cast<const uint4*>(a.out_in.at(b, r, h) + sum_chunk * 8);
             }
         }
         span = span_of(p, pos, row, KEYS, lane);
         if (part == 0) put_reach(reach_shared, quarter, lane, span);
         if (tid == 0) dead = junk = 0;
-        if (!KEYS) {
-#pragma unroll
-            for (int k = 0; k < kPasses; ++k) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    sum = fmaf(to_float(reinterpret_cast<const E*>(&x[k])[e]), to_float(reinterpret_cast<const E*>(&y[k])[e]), sum);
-#pragma unroll
-                for (int o = 1; o < kLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                if (e0 == 0) delta_shared[KEYS ? 0 : sum_row + k * (32 / kLanes) * kWarps] = sum;
-            }
-        }
     } else if (warp == kWarps) {
         if (lane == 0) {
             tc::bar_init(a_full, 1);
@@ -781,6 +784,22 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         if (!KEYS && row < p.t) {          // this row's statistics
             const float lse = minus_lse(own_lse);
             lse2 = two(lse, lse);
+        }
+        if (!KEYS) {
+            if (!tc::bar_wait(a_full, 0)) dead = 1;
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k) {
+                const int r = sum_row + k * kSumRows;
+                const uint4 dout = *reinterpret_cast<const uint4*>(a2 + sum_chunk / 8 * (128 * 128) + r * 128 + ((sum_chunk % 8) ^ (r & 7)) * 16);
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    sum = fmaf(to_float(reinterpret_cast<const E*>(&out_part[k])[e]), to_float(reinterpret_cast<const E*>(&dout)[e]), sum);
+#pragma unroll
+                for (int o = 1; o < kSumLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if (sum_chunk == 0) delta_shared[KEYS ? 0 : r] = sum;
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");  // of the warps with the arithmetic
             delta = delta_shared[KEYS ? 0 : own_row];
         }
         const Two delta2 = two(-delta, -delta);
@@ -940,7 +959,6 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         if (!KEYS) eps_shared[part][own_row] = one(eps2).x + one(eps2).y;
     }
     __syncthreads();
-    const bool good = !dead && !junk;
     if (dead) {
         if (tid == 0) atomicAdd(&g_timeouts, 1u);
     } else if (junk) {
@@ -981,22 +999,14 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 if (!KEYS && second) y = fmaf(-off, __uint_as_float(o2[e]), y);
                 x[e] = empty || n == 0 ? 0.0f : y * (dv ? 1.0f : p.scale);
             }
-            stage_columns<BF16>((dv ? a2 : a1) + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
+            uint8_t* const tile = (dv ? a2 : a1) + (c / 2) * (128 * 128);
+            stage_columns<BF16>(tile, own_row, (c % 2) * 32, x);
+            store_staged(tile, quarter * 32, (c % 2) * 32, p, !KEYS ? a.dq : dv ? a.dv : a.dk, b, h, r0 + quarter * 32, 32 * c, lane);
         }
-        tc::writes_to_async();
     }
     tc::fence_before();
     __syncthreads();
-    if (warp == kWarps + 1) {
-        tc::tmem_free<Tile::kTmem>(tmem);
-    } else if (good && lane == 0 && warp < (KEYS ? 2 : 1) * DP / 16) {  // four warps per 64 columns of dq, or of dk and then dv
-        const int k = warp >> 2, x = k % (DP / 64) * 64, at_row = r0 + quarter * 32;
-        const bool dv = k >= DP / 64;
-        if (x < p.d && at_row < p.t) {
-            tc::tensor_store(dv ? &maps.o2 : &maps.o1, x, at_row, h, b, tc::smem_of(dv ? a2 : a1) + x * 256 + quarter * 32 * 128);
-            tc::stores_read();
-        }
-    }
+    if (warp == kWarps + 1) tc::tmem_free<Tile::kTmem>(tmem);
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------
@@ -1058,8 +1068,7 @@ cudaError_t gradient(const AttnParams& p, const AttnTensors<typename Element<BF1
     const int own = KEYS ? p.kv_heads : p.heads, other = KEYS ? p.heads : p.kv_heads;
     bool ok = make_map(&m.a1, p, BF16, KEYS ? a.k : a.q, own, 128) && make_map(&m.a2, p, BF16, KEYS ? a.v : a.dout, own, 128) &&
               make_map(&m.b1, p, BF16, KEYS ? a.q : a.k, other, GradTile<DP>::kColumns) &&
-              make_map(&m.b2, p, BF16, KEYS ? a.dout : a.v, other, GradTile<DP>::kColumns) &&
-              make_map(&m.o1, p, BF16, KEYS ? a.dk : a.dq, own, 32) && make_map(&m.o2, p, BF16, KEYS ? a.dv : a.dq, own, 32);
+              make_map(&m.b2, p, BF16, KEYS ? a.dout : a.v, other, GradTile<DP>::kColumns);
     const int64_t grid = p.blocks * own * ((p.t + 127) / 128);
     if (!ok || grid > 0x7fffffffLL) return cudaErrorInvalidValue;
     auto* kernel = k30_attention_grad<BF16, DP, MOD, KEYS>;
