@@ -549,6 +549,7 @@ typedef struct {
     const float* d_slopes;
     bload_heads_t q, k, v, out;
     float* d_lse;
+    /* bload_attention reads nothing from here on, and takes a block that ends here */
     bload_heads_t dout, dq, dk, dv; /* gradient only */
     float* d_delta;                 /* gradient only */
 } bload_attention_t;

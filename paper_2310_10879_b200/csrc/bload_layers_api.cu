@@ -109,29 +109,32 @@ int check_attention(const bload_attention_t* a, bool gradient)
     return BLOAD_OK;
 }
 
+// The forward call reads the fields up to d_lse only: its caller's block may end there.
 template <typename T>
-AttnTensors<T> attention_tensors(const bload_attention_t* a)
+AttnTensors<T> attention_tensors(const bload_attention_t* a, bool gradient)
 {
     const int64_t b = a->block_count, t = a->t_block;
-    AttnTensors<T> x;
+    AttnTensors<T> x{};
     x.q = heads_of<const T>(a->q, b, t, a->heads);
     x.k = heads_of<const T>(a->k, b, t, a->kv_heads);
     x.v = heads_of<const T>(a->v, b, t, a->kv_heads);
     x.out = heads_of<T>(a->out, b, t, a->heads);
     x.out_in = heads_of<const T>(a->out, b, t, a->heads);
-    x.dout = heads_of<const T>(a->dout, b, t, a->heads);
-    x.dq = heads_of<T>(a->dq, b, t, a->heads);
-    x.dk = heads_of<T>(a->dk, b, t, a->kv_heads);
-    x.dv = heads_of<T>(a->dv, b, t, a->kv_heads);
+    if (gradient) {
+        x.dout = heads_of<const T>(a->dout, b, t, a->heads);
+        x.dq = heads_of<T>(a->dq, b, t, a->heads);
+        x.dk = heads_of<T>(a->dk, b, t, a->kv_heads);
+        x.dv = heads_of<T>(a->dv, b, t, a->kv_heads);
+    }
     return x;
 }
-AttnParams attention_params(const bload_attention_t* a)
+AttnParams attention_params(const bload_attention_t* a, bool gradient)
 {
     AttnParams p;
     p.pos = a->d_pos;
     p.slopes = a->d_slopes;
     p.lse = a->d_lse;
-    p.delta = a->d_delta;
+    p.delta = gradient ? a->d_delta : nullptr;
     p.blocks = a->block_count;
     p.t = a->t_block;
     p.heads = a->heads;
@@ -214,9 +217,9 @@ int bload_attention(const bload_attention_t* a, void* stream)
     int rc = check_attention(a, false);
     if (rc || a->block_count == 0) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const AttnParams p = attention_params(a);
-    return done(a->dtype == BLOAD_F16 ? launch_attention<__half>(p, attention_tensors<__half>(a), st)
-                                      : launch_attention<__nv_bfloat16>(p, attention_tensors<__nv_bfloat16>(a), st));
+    const AttnParams p = attention_params(a, false);
+    return done(a->dtype == BLOAD_F16 ? launch_attention<__half>(p, attention_tensors<__half>(a, false), st)
+                                      : launch_attention<__nv_bfloat16>(p, attention_tensors<__nv_bfloat16>(a, false), st));
 }
 
 int bload_attention_grad(const bload_attention_t* a, void* stream)
@@ -224,9 +227,9 @@ int bload_attention_grad(const bload_attention_t* a, void* stream)
     int rc = check_attention(a, true);
     if (rc || a->block_count == 0) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const AttnParams p = attention_params(a);
-    return done(a->dtype == BLOAD_F16 ? launch_attention_grad<__half>(p, attention_tensors<__half>(a), st)
-                                      : launch_attention_grad<__nv_bfloat16>(p, attention_tensors<__nv_bfloat16>(a), st));
+    const AttnParams p = attention_params(a, true);
+    return done(a->dtype == BLOAD_F16 ? launch_attention_grad<__half>(p, attention_tensors<__half>(a, true), st)
+                                      : launch_attention_grad<__nv_bfloat16>(p, attention_tensors<__nv_bfloat16>(a, true), st));
 }
 
 size_t bload_recurrence_work_bytes(int64_t block_count, int32_t t_block, int64_t channels)
