@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
     using Tile = ForwardTile<DP>;
     constexpr int kHalves = Tile::kHalves, kKeys = Tile::kKeys, kWarps = Tile::kWarps;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[3 + 4 * Tile::kStages + 1];
+    __shared__ uint64_t bars[5 + 4 * Tile::kStages];
     __shared__ uint32_t tmem_base;
     __shared__ int dead, junk;
     __shared__ ReachShared<4> reach_shared;
@@ -290,7 +290,8 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
     uint8_t* const v_tiles = k_tiles + Tile::kStages * Tile::kTile;
     const uint32_t bar0 = tc::smem_of(bars);
     const uint32_t q_full = bar0, s_full = bar0 + 8, p_full = bar0 + 16, o_done = bar0 + 24, k_full = bar0 + 32,
-                   k_free = k_full + 8 * Tile::kStages, v_full = k_free + 8 * Tile::kStages, v_free = v_full + 8 * Tile::kStages;
+                   k_free = k_full + 8 * Tile::kStages, v_full = k_free + 8 * Tile::kStages, v_free = v_full + 8 * Tile::kStages,
+                   given_up = v_free + 8 * Tile::kStages;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int q_tiles = (p.t + 127) / 128;
@@ -318,6 +319,7 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
             tc::bar_init(p_full, 32 * kWarps);
             tc::bar_init(o_done, 1);
             for (int s = 0; s < 4 * Tile::kStages; ++s) tc::bar_init(k_full + 8 * s, 1);
+            tc::bar_init(given_up, 1);
             tc::bar_init_done();
             tc::bar_expect(q_full, Tile::kQueries);  // under way while the rows look for their keys
             for (int x = 0; x < DP; x += 64) tc::tensor_load(tc::smem_of(q_tile) + x * 256, &maps.q, x, i0, h, b, q_full);
@@ -338,36 +340,31 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
     const Walk<kKeys> walk(p, reach, i0, false);
     const int n = walk.count(reach);
     float m = -INFINITY, l = 0.0f;  // running maximum (log2 units; may lag by kLag) and sum
+    int issued_k = p.causal, issued_v = p.causal;  // (warp of the copies)
+    bool ended = false;                            // (warp of the products) none are under way
 
     if (warp == kWarps) {
         if (lane == 0) {
             bool ok = true;
             if (n == 0) ok = tc::bar_wait(q_full, 0) && (!p.causal || (tc::bar_wait(k_full, 0) && tc::bar_wait(v_full, 0)));  // (copies end)
-            int issued = p.causal;
-            for (int i = issued; i < n && ok; ++i, ++issued) {
+            for (int i = p.causal; i < n; ++i) {
                 const int s = i % Tile::kStages;
                 const uint32_t parity = (i / Tile::kStages + 1) & 1;
                 if (!(ok = tc::bar_wait(k_free + 8 * s, parity))) break;
                 load(true, s, walk(i));
-                if (!(ok = tc::bar_wait(v_free + 8 * s, parity))) {
-                    tc::bar_wait(k_full + 8 * s, (i / Tile::kStages) & 1);  // a copy in flight ends before the CTA does
-                    break;
-                }
+                issued_k = i + 1;
+                if (!(ok = tc::bar_wait(v_free + 8 * s, parity))) break;
                 load(false, s, walk(i));
+                issued_v = i + 1;
             }
-            if (!ok) {
-                dead = 1;
-                tc::bar_wait(q_full, 0);
-                for (int i = max(0, issued - Tile::kStages); i < issued; ++i) {
-                    tc::bar_wait(k_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
-                    tc::bar_wait(v_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
-                }
-            }
+            if (!ok) dead = 1;
         }
     } else if (warp == kWarps + 1) {
+        ended = true;
         if (n > 0) {
             const uint32_t leader = tc::elect();
             bool ok = __all_sync(0xffffffffu, tc::bar_wait(q_full, 0));
+            ended = false;
             for (int i = 0; i < n && ok; ++i) {
                 const int s = i % Tile::kStages;
                 const uint32_t parity = (i / Tile::kStages) & 1;
@@ -376,19 +373,20 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
                 if (!ok) break;
                 tc::fence_after();
                 tc::product_rows<BF16, kKeys, DP>(leader, s_at, tc::smem_of(q_tile), tc::smem_of(k_tiles) + s * Tile::kTile);
-                tc::products_arrive(leader, k_free + 8 * s);
+                if (i + Tile::kStages < n) tc::products_arrive(leader, k_free + 8 * s);  // (nothing arrives that nobody waits for)
                 tc::products_arrive(leader, s_full);
                 ok = __all_sync(0xffffffffu, tc::bar_wait(v_full + 8 * s, parity) && tc::bar_wait(p_full, i & 1));
                 if (!ok) break;
                 tc::fence_after();
                 tc::product_across<BF16, kKeys, DP, 64>(leader, o_at, s_at, tc::smem_of(v_tiles) + s * Tile::kTile, i > 0);
-                tc::products_arrive(leader, v_free + 8 * s);
+                if (i + Tile::kStages < n) tc::products_arrive(leader, v_free + 8 * s);
                 tc::products_arrive(leader, o_done);
             }
             if (!ok) {
                 dead = 1;
-                tc::products_arrive(leader, q_full);  // its second phase: products in flight end before the CTA does
-                tc::bar_wait(q_full, 1);
+                tc::products_arrive(leader, given_up);
+                tc::bar_wait(given_up, 0);
+                ended = true;
             }
         }
     } else {
@@ -517,6 +515,14 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
         if (kHalves == 2) halves[n & 1][half][own_row] = l;
     }
     __syncthreads();
+    // Products and copies under way end before the CTA gives up its memory: the last product's end is waited for here unless the
+    // accumulators are read below, copies that no product has waited for where a wait gave up.
+    if ((dead || junk) && warp == kWarps + 1 && !ended) tc::bar_wait(o_done, (n - 1) & 1);
+    if (dead && warp == kWarps && lane == 0) {
+        tc::bar_wait(q_full, 0);
+        for (int i = max(0, issued_k - Tile::kStages); i < issued_k; ++i) tc::bar_wait(k_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
+        for (int i = max(0, issued_v - Tile::kStages); i < issued_v; ++i) tc::bar_wait(v_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
+    }
     if (dead) {
         if (tid == 0) atomicAdd(&g_timeouts, 1u);
     } else if (junk) {
@@ -619,7 +625,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     using Tile = GradTile<DP>;
     constexpr int kColumns = Tile::kColumns, kWarps = Tile::kWarps, kStages = Tile::kStages;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[7 + 4 * kStages];
+    __shared__ uint64_t bars[8 + 4 * kStages];
     __shared__ uint32_t tmem_base;
     __shared__ int dead, junk;
     __shared__ ReachShared<4> reach_shared;
@@ -633,7 +639,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     const uint32_t bar0 = tc::smem_of(bars);
     const uint32_t a_full = bar0, s_full = bar0 + 8, dp_full = bar0 + 16, p_full = bar0 + 24, ds_full = bar0 + 32, acc1_done = bar0 + 40,
                    acc2_done = bar0 + 48, b1_full = bar0 + 56, b2_full = b1_full + 8 * kStages, b1_free = b2_full + 8 * kStages,
-                   b2_free = b1_free + 8 * kStages;
+                   b2_free = b1_free + 8 * kStages, given_up = b2_free + 8 * kStages;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int own_heads = KEYS ? p.kv_heads : p.heads;
@@ -683,6 +689,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
             tc::bar_init(acc1_done, 1);
             tc::bar_init(acc2_done, 1);
             for (int s = 0; s < 4 * kStages; ++s) tc::bar_init(b1_full + 8 * s, 1);
+            tc::bar_init(given_up, 1);
             tc::bar_init_done();
             tc::bar_expect(a_full, 2 * Tile::kOwn);  // under way while the rows look for their columns
             for (int x = 0; x < DP; x += 64) {
@@ -708,13 +715,14 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     const int n = KEYS ? per_head * p.group : per_head;
     const bool second = KEYS || n * kColumns <= kExact;  // acc2 is kept
     float delta = 0.0f;
+    int issued1 = p.causal, issued2 = p.causal;  // (warp of the copies)
+    bool ended = false;                          // (warp of the products) none are under way
 
     if (warp == kWarps) {
         if (lane == 0) {
             bool ok = true;
             if (n == 0) ok = tc::bar_wait(a_full, 0) && (!p.causal || (tc::bar_wait(b1_full, 0) && tc::bar_wait(b2_full, 0)));  // (copies end)
-            int issued1 = p.causal, issued2 = p.causal;
-            for (int i = p.causal; i < n && ok; ++i) {
+            for (int i = p.causal; i < n; ++i) {
                 const int s = i % kStages;
                 const uint32_t parity = (i / kStages + 1) & 1;
                 const int j0 = walk(KEYS ? i % per_head : i), hs = KEYS ? first_head + i / per_head : first_head;
@@ -725,15 +733,12 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 load(false, s, j0, hs);
                 issued2 = i + 1;
             }
-            if (!ok) {  // copies in flight end before the CTA does
-                dead = 1;
-                tc::bar_wait(a_full, 0);
-                for (int i = max(0, issued1 - kStages); i < issued1; ++i) tc::bar_wait(b1_full + 8 * (i % kStages), (i / kStages) & 1);
-                for (int i = max(0, issued2 - kStages); i < issued2; ++i) tc::bar_wait(b2_full + 8 * (i % kStages), (i / kStages) & 1);
-            }
+            if (!ok) dead = 1;
         }
     } else if (warp == kWarps + 1) {
+        ended = true;
         if (n > 0) {
+            ended = false;
             const uint32_t leader = tc::elect();
             auto all = [](bool x) { return (bool)__all_sync(0xffffffffu, x); };
             bool ok = all(tc::bar_wait(a_full, 0));
@@ -744,8 +749,9 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                     if (!(ok = all(tc::bar_wait(p_full, (i - 1) & 1)))) break;
                     tc::fence_after();
                     tc::product_across<BF16, kColumns, DP, 32>(leader, acc2_at, s_at, KEYS ? last + Tile::kStream : last, i > 1);
-                    if (KEYS) tc::products_arrive(leader, b2_free + 8 * sl);
-                    tc::products_arrive(leader, acc2_done);
+                    // (nothing arrives that nobody waits for: here and below, stages that no copy takes again, ends that no product needs)
+                    if (KEYS && i - 1 + kStages < n) tc::products_arrive(leader, b2_free + 8 * sl);
+                    if (i < n) tc::products_arrive(leader, acc2_done);
                 }
                 if (i < n) {
                     // S's place is free when the product is over that reads the last P there, or when the last S has been read
@@ -760,21 +766,22 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                     if (!(ok = all(tc::bar_wait(ds_full, (i - 1) & 1)))) break;
                     tc::fence_after();
                     tc::product_across<BF16, kColumns, DP, 32>(leader, acc1_at, dp_at, last, i > 1);
-                    tc::products_arrive(leader, b1_free + 8 * sl);
+                    if (i - 1 + kStages < n) tc::products_arrive(leader, b1_free + 8 * sl);
                     tc::products_arrive(leader, acc1_done);
                 }
                 if (i < n) {
                     if (!(ok = all(tc::bar_wait(b2_full + 8 * s, (i / kStages) & 1) && (i == 0 || tc::bar_wait(acc1_done, (i - 1) & 1))))) break;
                     tc::fence_after();
                     tc::product_rows<BF16, kColumns, DP>(leader, dp_at, tc::smem_of(a2), at + Tile::kStream);
-                    if (!KEYS) tc::products_arrive(leader, b2_free + 8 * s);
+                    if (!KEYS && i + kStages < n) tc::products_arrive(leader, b2_free + 8 * s);
                     tc::products_arrive(leader, dp_full);
                 }
             }
             if (!ok) {
                 dead = 1;
-                tc::products_arrive(leader, a_full);  // its second phase: products in flight end before the CTA does
-                tc::bar_wait(a_full, 1);
+                tc::products_arrive(leader, given_up);
+                tc::bar_wait(given_up, 0);
+                ended = true;
             }
         }
     } else {
@@ -959,6 +966,13 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         if (!KEYS) eps_shared[part][own_row] = one(eps2).x + one(eps2).y;
     }
     __syncthreads();
+    // (as in the forward kernel: what is under way ends before the CTA gives up its memory)
+    if ((dead || junk) && warp == kWarps + 1 && !ended) tc::bar_wait(acc1_done, (n - 1) & 1);
+    if (dead && warp == kWarps && lane == 0) {
+        tc::bar_wait(a_full, 0);
+        for (int i = max(0, issued1 - kStages); i < issued1; ++i) tc::bar_wait(b1_full + 8 * (i % kStages), (i / kStages) & 1);
+        for (int i = max(0, issued2 - kStages); i < issued2; ++i) tc::bar_wait(b2_full + 8 * (i % kStages), (i / kStages) & 1);
+    }
     if (dead) {
         if (tid == 0) atomicAdd(&g_timeouts, 1u);
     } else if (junk) {
