@@ -523,9 +523,10 @@ BLOAD_API int bload_rotary_grad(const int32_t* d_pos, int64_t block_count, int32
  *     s_ij = scale * q_i . k_j;   if softcap > 0: s_ij = softcap * tanh(s_ij / softcap);
  *     if d_slopes: s_ij -= d_slopes[h] * |i - j|
  *     out_i = sum_j softmax_j(s_ij) v_j;        lse[q, h, i] = log sum_j exp(s_ij)   (natural logarithm)
- * Query head h reads key and value head h / (heads / kv_heads).  On padding out = 0 and lse = -inf.  A key slot that
- * is not allowed has no influence, whatever it holds (infinities and NaN included).  A row whose allowed scores are
- * all -inf gives zeros and lse = -inf.
+ * Query head h reads key and value head h / (heads / kv_heads).  On padding out = 0 and lse = -inf.  A slot that is not
+ * allowed has no influence on any bit, whatever it holds (infinities and NaN included).  Infinities and NaN of allowed
+ * slots reach what the formulas say: those of v (dout) that element of out (dv), with their sign; all others make NaN.
+ * A row whose allowed scores are all -inf gives zeros and lse = -inf.
  *
  *   q, out, dout, dq  [block_count, t_block, heads, head_dim]          k, v, dk, dv  [.., kv_heads, head_dim]
  *   d_lse             float [block_count, heads, t_block]; NULL in bload_attention: not written

@@ -9,15 +9,18 @@
 // accumulators are held in 32 bits, and P and dS are rounded to the inputs' type as operands of the second product.
 //
 // Hidden slots must have no influence, but a product multiplies them by zero, and 0 * NaN is not 0.  So a tile that is hidden
-// from any row of the CTA is scanned (one multiply-add by zero per pair of elements): infinities and NaN on padding are
-// cleared in shared memory, and if a frame holds any, the CTA's rows are computed once more, one at a time, by the loops of
-// bload_attention_rows.cuh, which never touch a hidden slot.
+// from any row of the CTA is scanned (one multiply-add by zero per pair of elements), and infinities and NaN in it are cleared in
+// shared memory before a product reads across it.  Rows that may see a frame that held some have them added in the end, read
+// from memory once more (add_junk): a clean row's bits do not depend on what a hidden slot holds.  With v and dout infinite
+// everywhere, 8,192 slots of 4 heads on 2 of 128 take 254 us forward and 575 gradient (clean: 155 and 359), 4 x 4096 slots of
+// heavy-tailed lengths 246 and 581 (46 and 124).
 #include <cuda.h>
+#include <math.h>
 
 #include <type_traits>
 
-#include "bload_attention_rows.cuh"
 #include "bload_internal.cuh"
+#include "bload_layers.cuh"
 #include "bload_tc.cuh"
 
 namespace bload {
@@ -38,8 +41,12 @@ struct Element<true> {
     using type = __nv_bfloat16;
 };
 
-// The interval of the other side that row `row` of this warp's rows row0 .. row0 + 31 may see.
-__device__ __forceinline__ rows::Span span_of(const AttnParams& p, const int32_t* pos, int row, bool keys, int lane)
+// The interval of the other side that a row may see: the keys of a query, the queries of a key.  Empty: lo > hi.
+struct Span {
+    int lo, hi;
+};
+// That of row `row`, of this warp's rows row0 .. row0 + 31.
+__device__ __forceinline__ Span span_of(const AttnParams& p, const int32_t* pos, int row, bool keys, int lane)
 {
     const int row0 = row - lane;
     const int here = row < p.t ? pos[row] : -1;
@@ -52,7 +59,7 @@ __device__ __forceinline__ rows::Span span_of(const AttnParams& p, const int32_t
         end = stops ? row0 + __ffs(stops) - 1 : behind;
     }
     if (here < 0) return {kNever, -1};
-    rows::Span s;
+    Span s;
     if (keys) {
         s.lo = p.causal ? row : max(row - here, 0);
         s.hi = end - 1;
@@ -86,7 +93,7 @@ struct ReachShared {
     int lo[WARPS], hi[WARPS], all_lo[WARPS], all_hi[WARPS];
 };
 template <int WARPS>
-__device__ __forceinline__ void put_reach(ReachShared<WARPS>& sh, int warp, int lane, const rows::Span& s)
+__device__ __forceinline__ void put_reach(ReachShared<WARPS>& sh, int warp, int lane, const Span& s)
 {
     const bool some = s.lo <= s.hi;
     const int lo = __reduce_min_sync(0xffffffffu, some ? s.lo : kNever), hi = __reduce_max_sync(0xffffffffu, some ? s.hi : -1);
@@ -199,10 +206,19 @@ struct Modifier {
 // -lse in units of log2; a row without any weight keeps none
 __device__ __forceinline__ float minus_lse(float lse) { return lse == -INFINITY ? -INFINITY : -lse * kLog2e; }
 
-// Scans a tile [ROWS][DP] in shared memory with THREADS threads for infinities and NaN.  Those on padding (or behind the
-// block's last slot, where copies fill in zeros anyway) are cleared; true if a frame holds one.
-template <bool BF16, int ROWS, int DP, int THREADS>
-__device__ __forceinline__ bool scan_tile(const AttnParams& p, const int32_t* pos, uint8_t* tile, int row0, int tid)
+// Junk: which tiles of a CTA's walk held infinities or NaN in a frame, and what its rows may see.
+template <int COLUMNS>
+struct Junk {
+    uint32_t tiles[BLOAD_MAX_T_BLOCK / COLUMNS / 32 + 1];
+    Span spans[128];
+    int any;
+};
+
+// Scans a tile [ROWS][DP] in shared memory, number `turn` of its walk, with THREADS threads for infinities and NaN, and clears them;
+// ready(): called before anything is cleared.  (Behind the block's last slot copies fill in zeros.)
+template <bool BF16, int ROWS, int DP, int THREADS, typename Ready>
+__device__ __forceinline__ void scan_tile(const AttnParams& p, const int32_t* pos, uint8_t* tile, int row0, int tid, Junk<ROWS>& junk, int turn,
+                                          const Ready& ready)
 {
     uint32_t acc = 0;
     constexpr int kChunks = ROWS * DP / 8 / THREADS;
@@ -212,28 +228,80 @@ __device__ __forceinline__ bool scan_tile(const AttnParams& p, const int32_t* po
         acc = tc::probe<BF16>(tc::probe<BF16>(acc, x.x), x.y);
         acc = tc::probe<BF16>(tc::probe<BF16>(acc, x.z), x.w);
     }
-    if (!(acc & 0x7fff7fffu)) return false;
-    bool found = false;
+    if (!(acc & 0x7fff7fffu)) return;
+    ready();
     for (int k = 0; k < kChunks; ++k) {
-        uint4* at = reinterpret_cast<uint4*>(tile + (k * THREADS + tid) * 16);
-        const uint4 x = *at;
-        if (!(tc::probe<BF16>(tc::probe<BF16>(tc::probe<BF16>(tc::probe<BF16>(0u, x.x), x.y), x.z), x.w) & 0x7fff7fffu)) continue;
+        uint32_t* const at = reinterpret_cast<uint32_t*>(tile + (k * THREADS + tid) * 16);
+        bool some = false;
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = at[e], odd = tc::probe<BF16>(0u, x);
+            if (!(odd & 0x7fff7fffu)) continue;
+            some = true;
+            at[e] = x & ((odd & 0x7fff ? 0u : 0xffffu) | (odd & 0x7fff0000u ? 0u : 0xffff0000u));
+        }
         const int row = row0 + (k * THREADS + tid) / 8 % ROWS;
-        if (row >= p.t || pos[row] < 0)
-            *at = make_uint4(0, 0, 0, 0);
-        else
-            found = true;
+        if (some && row < p.t && pos[row] >= 0) {
+            atomicOr(&junk.tiles[turn / 32], 1u << turn % 32);
+            junk.any = 1;
+        }
     }
-    return found;
 }
 
 template <bool BF16, int ROWS, int DP, int THREADS>
-__device__ __noinline__ bool scan_tile_apart(const AttnParams& p, const int32_t* pos, uint8_t* tile, int row0, int tid)
+__device__ __noinline__ void scan_tile_apart(const AttnParams& p, const int32_t* pos, uint8_t* tile, int row0, int tid, Junk<ROWS>& junk, int turn,
+                                             uint32_t after, uint32_t parity, int& dead)
 {
-    return scan_tile<BF16, ROWS, DP, THREADS>(p, pos, tile, row0, tid);
+    scan_tile<BF16, ROWS, DP, THREADS>(p, pos, tile, row0, tid, junk, turn, [&] {
+        if (after && !tc::bar_wait(after, parity)) dead = 1;
+    });
 }
 
-// 32 columns of a row in tensor memory, times `by`, to 64 bytes of a staged output tile (128-byte rows, swizzled)
+// What the cleared elements of x add to the CTA's 128 rows, to add[128][DP]: infinities and NaN of every frame that a row may see
+// in a tile where some were cleared; POISON: NaN for each of them.  A warp has ROWS rows, a lane DP / 32 elements; of a tile that a row
+// sees as far as any row does, the sum is formed once for the warp's rows.
+template <bool POISON, int ROWS, int DP, int COLUMNS, typename T, typename Walk>
+__device__ __noinline__ void add_junk(const AttnParams& p, const Junk<COLUMNS>& junk, const Reach reach, const Walk walk, int tiles, const Heads<const T> x, int b, int head,
+                                      int heads, float* add, int warp, int lane)
+{
+    constexpr int kPer = DP / 32;
+    const bool on = lane * kPer < p.d;
+    for (int r = warp * ROWS; r < (warp + 1) * ROWS; ++r)
+        for (int e = 0; e < kPer; ++e) add[r * DP + lane * kPer + e] = 0.0f;
+    for (int i = 0; i < tiles; ++i) {
+        if (!((junk.tiles[i / 32] >> i % 32) & 1)) continue;
+        const int first = max(walk(i), reach.lo), last = min(walk(i) + COLUMNS - 1, reach.hi);
+        for (int hs = head; hs < head + heads; ++hs) {
+            auto sum = [&](int lo, int hi, float (&s)[kPer]) {
+                for (int e = 0; e < kPer; ++e) s[e] = 0.0f;
+                if (!on) return;
+#pragma unroll 8
+                for (int j = lo; j <= hi; ++j) {
+                    using W = typename std::conditional<kPer == 4, uint2, uint32_t>::type;
+                    const W w = *reinterpret_cast<const W*>(x.at(b, j, hs) + lane * kPer);
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) {
+                        const float v = to_float(reinterpret_cast<const T*>(&w)[e]);
+                        s[e] += POISON ? v * 0.0f : isfinite(v) ? 0.0f : v;
+                    }
+                }
+            };
+            float whole[kPer];
+            bool have = false;
+            for (int r = warp * ROWS; r < (warp + 1) * ROWS; ++r) {
+                const int lo = max(junk.spans[r].lo, first), hi = min(junk.spans[r].hi, last);
+                if (lo > hi) continue;
+                float own[kPer];
+                const bool all = lo == first && hi == last;
+                if (!all) sum(lo, hi, own);
+                if (all && !have) sum(lo, hi, whole);
+                have |= all;
+                for (int e = 0; e < kPer; ++e) add[r * DP + lane * kPer + e] += all ? whole[e] : own[e];
+            }
+        }
+    }
+}
+
+// 32 columns of a row to 64 bytes of a staged output tile (128-byte rows, swizzled)
 template <bool BF16>
 __device__ __forceinline__ void stage_columns(uint8_t* tile, int row, int column, const float (&x)[32])
 {
@@ -280,7 +348,8 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[5 + 4 * Tile::kStages];
     __shared__ uint32_t tmem_base;
-    __shared__ int dead, junk;
+    __shared__ int dead;
+    __shared__ Junk<kKeys> junk;
     __shared__ ReachShared<4> reach_shared;
     __shared__ float halves[2][kHalves][128];  // [turn][half][row]: maxima, and in the end sums
 
@@ -307,11 +376,15 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
         tc::bar_expect(bar, Tile::kTile);
         for (int x = 0; x < DP; x += 64) tc::tensor_load(to + x * (2 * kKeys), keys ? &maps.k : &maps.v, x, j0, hk, b, bar);
     };
-    rows::Span span{kNever, -1};
+    Span span{kNever, -1};
     if (warp < kWarps) {
         span = span_of(p, pos, row, false, lane);
-        if (half == 0) put_reach(reach_shared, quarter, lane, span);
-        if (tid == 0) dead = junk = 0;
+        if (half == 0) {
+            put_reach(reach_shared, quarter, lane, span);
+            junk.spans[own_row] = span;
+            if (tid < (int)(sizeof junk.tiles / 4)) junk.tiles[tid] = 0;
+        }
+        if (tid == 0) dead = junk.any = 0;
     } else if (warp == kWarps) {
         if (lane == 0) {
             tc::bar_init(q_full, 1);
@@ -393,7 +466,7 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
         const Modifier modify(p, h);
         const uint32_t lanes = (uint32_t)quarter << 21;  // this warp's 32 lanes of tensor memory
         const float by = modify.by;
-        bool found = false, ok = true;
+        bool ok = true;
         for (int i = 0; i < n; ++i) {
             const int st = i % Tile::kStages;
             const int j0 = walk(i), mine0 = j0 + 64 * half;  // the tile's and this warp's first key
@@ -504,30 +577,37 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
             l += sums.x + sums.y;
             if (j0 < reach.all_lo || j0 + kKeys - 1 > reach.all_hi) {  // hidden from some row: no junk may reach the product
                 if (ok && !tc::bar_wait(v_full + 8 * st, (i / Tile::kStages) & 1)) dead = 1;
-                found |= scan_tile<BF16, kKeys, DP, 32 * kWarps>(p, pos, v_tiles + st * Tile::kTile, j0, tid);
+                scan_tile<BF16, kKeys, DP, 32 * kWarps>(p, pos, v_tiles + st * Tile::kTile, j0, tid, junk, i, [] {});
+                __syncwarp();
                 tc::writes_to_async();
             }
             tc::tmem_stored();
             tc::fence_before();
             tc::bar_arrive(p_full);
         }
-        if (found) junk = 1;
         if (kHalves == 2) halves[n & 1][half][own_row] = l;
     }
     __syncthreads();
-    // Products and copies under way end before the CTA gives up its memory: the last product's end is waited for here unless the
-    // accumulators are read below, copies that no product has waited for where a wait gave up.
-    if ((dead || junk) && warp == kWarps + 1 && !ended) tc::bar_wait(o_done, (n - 1) & 1);
+    // Products and copies under way end before the CTA gives up its memory.  Where no wait gave up, products have waited for all copies,
+    // and whoever reads the accumulators waits for the last product.
+    if (dead && warp == kWarps + 1 && !ended) tc::bar_wait(o_done, (n - 1) & 1);
     if (dead && warp == kWarps && lane == 0) {
         tc::bar_wait(q_full, 0);
         for (int i = max(0, issued_k - Tile::kStages); i < issued_k; ++i) tc::bar_wait(k_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
         for (int i = max(0, issued_v - Tile::kStages); i < issued_v; ++i) tc::bar_wait(v_full + 8 * (i % Tile::kStages), (i / Tile::kStages) & 1);
     }
+    float* const extra = reinterpret_cast<float*>(k_tiles);  // [128][DP], over the tiles of keys and values
+    static_assert(128 * DP * 4 <= 2 * Tile::kStages * Tile::kTile, "fits");
+    const bool add = junk.any && !dead;
+    if (add) {
+        if (warp < kWarps) {
+            if (!tc::bar_wait(o_done, (n - 1) & 1)) atomicAdd(&g_timeouts, 1u);
+            add_junk<false, 128 / kWarps, DP, kKeys>(p, junk, reach, walk, n, a.v, b, hk, 1, extra, warp, lane);
+        }
+        __syncthreads();
+    }
     if (dead) {
         if (tid == 0) atomicAdd(&g_timeouts, 1u);
-    } else if (junk) {
-        for (int r = warp; r < 128; r += kWarps + 2)
-            if (i0 + r < p.t) rows::forward_row(p, a, b, h, i0 + r, lane);
     } else if (warp < kWarps) {
         const uint32_t lanes = (uint32_t)quarter << 21;
         if (kHalves == 2) l += halves[n & 1][kHalves - 1 - half][own_row];
@@ -547,6 +627,9 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
             float x[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = empty || n == 0 ? 0.0f : __uint_as_float(o[e]) * inv;
+            if (add && !empty)
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] += extra[own_row * DP + 32 * c + e];
             stage_columns<BF16>(q_tile + (c / 2) * (128 * 128), own_row, (c % 2) * 32, x);
         }
         tc::writes_to_async();
@@ -627,7 +710,8 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[8 + 4 * kStages];
     __shared__ uint32_t tmem_base;
-    __shared__ int dead, junk;
+    __shared__ int dead;
+    __shared__ Junk<kColumns> junk;
     __shared__ ReachShared<4> reach_shared;
     __shared__ float eps_shared[kColumns / 32][128], delta_shared[KEYS ? 1 : 128];
     __shared__ float4 column_stats[KEYS ? kWarps : 1][KEYS ? 16 : 1];  // per warp: -lse (log2 units) and -delta of 16 pairs of columns
@@ -659,7 +743,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         for (int x = 0; x < DP; x += 64) tc::tensor_load(to + x * (2 * kColumns), one ? &maps.b1 : &maps.b2, x, j0, hs, b, bar);
     };
     const int first_head = KEYS ? h * p.group : h / p.group;  // of the other side
-    rows::Span span{kNever, -1};
+    Span span{kNever, -1};
     float own_lse = 0.0f;  // queries: of this row
     // dout . out of the queries: DP / 8 lanes share a row, 16 bytes each, so that a load of a warp touches few lines (with a row per
     // lane it was 32 each, and the rows were known after 4 us instead of 1.4)
@@ -677,8 +761,12 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
             }
         }
         span = span_of(p, pos, row, KEYS, lane);
-        if (part == 0) put_reach(reach_shared, quarter, lane, span);
-        if (tid == 0) dead = junk = 0;
+        if (part == 0) {
+            put_reach(reach_shared, quarter, lane, span);
+            junk.spans[own_row] = span;
+            if (tid < (int)(sizeof junk.tiles / 4)) junk.tiles[tid] = 0;
+        }
+        if (tid == 0) dead = junk.any = 0;
     } else if (warp == kWarps) {
         if (lane == 0) {
             tc::bar_init(a_full, 1);
@@ -786,7 +874,6 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         }
     } else {
         const uint32_t lanes = (uint32_t)quarter << 21;
-        bool found = false;
         Two lse2 = zero(), eps2 = zero();  // lse and delta of this row, negative
         if (!KEYS && row < p.t) {          // this row's statistics
             const float lse = minus_lse(own_lse);
@@ -810,11 +897,15 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
             delta = delta_shared[KEYS ? 0 : own_row];
         }
         const Two delta2 = two(-delta, -delta);
-        // junk in a tile that is hidden from some row must not reach the products
+        // Junk in a tile that is hidden from some row must not reach the products across it.  (B1 is scanned when S is done, which reads
+        // it; B2 while dP may still read it, so whoever has something to clear waits for dP's end, which waits for nothing of this turn.
+        // A query with junk in dout has NaN for its delta, so its dS are NaN whatever dP reads.)
         auto scan = [&](uint32_t full, int i, int which, int j0) {
             if (j0 >= reach.all_lo && j0 + kColumns - 1 <= reach.all_hi) return;
             if (!tc::bar_wait(full + 8 * (i % kStages), (i / kStages) & 1)) dead = 1;
-            found |= scan_tile_apart<BF16, kColumns, DP, 32 * kWarps>(p, pos, stream + ((i % kStages) * 2 + which) * Tile::kStream, j0, tid);
+            scan_tile_apart<BF16, kColumns, DP, 32 * kWarps>(p, pos, stream + ((i % kStages) * 2 + which) * Tile::kStream, j0, tid, junk,
+                                                             KEYS ? i % per_head : i, which ? dp_full : 0, i & 1, dead);
+            __syncwarp();
             tc::writes_to_async();
         };
         // KEYS: statistics of this warp's 32 columns of tile i, a tile ahead
@@ -962,27 +1053,30 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
             tc::fence_before();
             tc::bar_arrive(ds_full);
         }
-        if (found) junk = 1;
         if (!KEYS) eps_shared[part][own_row] = one(eps2).x + one(eps2).y;
     }
     __syncthreads();
     // (as in the forward kernel: what is under way ends before the CTA gives up its memory)
-    if ((dead || junk) && warp == kWarps + 1 && !ended) tc::bar_wait(acc1_done, (n - 1) & 1);
+    if (dead && warp == kWarps + 1 && !ended) tc::bar_wait(acc1_done, (n - 1) & 1);
     if (dead && warp == kWarps && lane == 0) {
         tc::bar_wait(a_full, 0);
         for (int i = max(0, issued1 - kStages); i < issued1; ++i) tc::bar_wait(b1_full + 8 * (i % kStages), (i / kStages) & 1);
         for (int i = max(0, issued2 - kStages); i < issued2; ++i) tc::bar_wait(b2_full + 8 * (i % kStages), (i / kStages) & 1);
     }
+    float* const extra = reinterpret_cast<float*>(stream);  // [128][DP], KEYS: of dk, then of dv; over the stream's tiles
+    static_assert((KEYS ? 2 : 1) * 128 * DP * 4 <= kStages * 2 * Tile::kStream, "fits");
+    const bool add = junk.any && !dead;
+    if (add) {  // dS times an infinite element: its sign would be that of dS, and q.k is not finite either; NaN
+        if (warp < kWarps) {
+            if (!tc::bar_wait(acc1_done, (n - 1) & 1)) atomicAdd(&g_timeouts, 1u);
+            add_junk<true, 128 / kWarps, DP, kColumns>(p, junk, reach, walk, per_head, KEYS ? a.q : a.k, b, first_head, KEYS ? p.group : 1, extra, warp, lane);
+            if (KEYS)
+                add_junk<false, 128 / kWarps, DP, kColumns>(p, junk, reach, walk, per_head, a.dout, b, first_head, p.group, extra + 128 * DP, warp, lane);
+        }
+        __syncthreads();
+    }
     if (dead) {
         if (tid == 0) atomicAdd(&g_timeouts, 1u);
-    } else if (junk) {
-        for (int r = warp; r < 128; r += kWarps + 2) {
-            if (r0 + r >= p.t) continue;
-            if (KEYS)
-                rows::dkv_row(p, a, b, h, r0 + r, lane);
-            else
-                rows::dq_row(p, a, b, h, r0 + r, lane);
-        }
     } else if (warp < kWarps) {
         const uint32_t lanes = (uint32_t)quarter << 21;
         const bool empty = span.lo > span.hi;
@@ -1013,6 +1107,9 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 if (!KEYS && second) y = fmaf(-off, __uint_as_float(o2[e]), y);
                 x[e] = empty || n == 0 ? 0.0f : y * (dv ? 1.0f : p.scale);
             }
+            if (add && !empty)
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] += extra[(dv ? 128 * DP : 0) + own_row * DP + 32 * c + e];
             uint8_t* const tile = (dv ? a2 : a1) + (c / 2) * (128 * 128);
             stage_columns<BF16>(tile, own_row, (c % 2) * 32, x);
             store_staged(tile, quarter * 32, (c % 2) * 32, p, !KEYS ? a.dq : dv ? a.dv : a.dk, b, h, r0 + quarter * 32, 32 * c, lane);
