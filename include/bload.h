@@ -530,8 +530,8 @@ BLOAD_API int bload_rotary_grad(const int32_t* d_pos, int64_t block_count, int32
  *
  *   q, out, dout, dq  [block_count, t_block, heads, head_dim]          k, v, dk, dv  [.., kv_heads, head_dim]
  *   d_lse             float [block_count, heads, t_block]; NULL in bload_attention: not written
- *   d_delta           float [block_count, heads, t_block], written by bload_attention_grad: sum over the head of
- *                     dout * out, which both of its kernels need
+ *   d_delta           float [block_count, heads, t_block], written by bload_attention_grad: sum_j P_ij (dout_i . v_j), the
+ *                     sum over the head of dout * out less what the rounding of out put into it; 0 on padding
  * bload_attention_grad takes out and d_lse of the forward call with the same arguments, and dout, and writes dq, dk, dv
  * (gradients of shared key heads are summed over their query heads).
  *

@@ -681,7 +681,7 @@ def bload_attention(pos, q, k, v, out, lse=None, scale: float | None = None, sof
 def bload_attention_grad(pos, q, k, v, out, lse, dout, dq, dk, dv, delta, scale: float | None = None, softcap: float = 0.0,
                          slopes=None, causal: bool = True, window: int = 0, stream=None) -> None:
     """dq, dk, dv of bload_attention from dout, with out and lse of the forward call.  delta: float32 [blocks, heads,
-    t_block], written (the row sums of dout * out)."""
+    t_block], written (the row sums of dout * out, without the rounding of out)."""
     where = "bload_attention_grad"
     fields, stream = _attention(where, pos, q, k, v, out, lse, scale, softcap, slopes, causal, window, stream)
     rc = load().bload_attention_grad(_ATTENTION_GRAD.pack(

@@ -87,10 +87,11 @@ __device__ __forceinline__ uint32_t column_mask(int lo, int hi)
 struct Reach {
     int lo, hi;         // smallest lo, largest hi
     int all_lo, all_hi; // [all_lo, all_hi] is seen by every row that sees anything
+    int least;          // columns that the row sees that sees the fewest
 };
 template <int WARPS>
 struct ReachShared {
-    int lo[WARPS], hi[WARPS], all_lo[WARPS], all_hi[WARPS];
+    int lo[WARPS], hi[WARPS], all_lo[WARPS], all_hi[WARPS], least[WARPS];
 };
 template <int WARPS>
 __device__ __forceinline__ void put_reach(ReachShared<WARPS>& sh, int warp, int lane, const Span& s)
@@ -98,23 +99,26 @@ __device__ __forceinline__ void put_reach(ReachShared<WARPS>& sh, int warp, int 
     const bool some = s.lo <= s.hi;
     const int lo = __reduce_min_sync(0xffffffffu, some ? s.lo : kNever), hi = __reduce_max_sync(0xffffffffu, some ? s.hi : -1);
     const int all_lo = __reduce_max_sync(0xffffffffu, some ? s.lo : -1), all_hi = __reduce_min_sync(0xffffffffu, some ? s.hi : kNever);
+    const int least = __reduce_min_sync(0xffffffffu, some ? s.hi - s.lo + 1 : kNever);
     if (lane == 0) {
         sh.lo[warp] = lo;
         sh.hi[warp] = hi;
         sh.all_lo[warp] = all_lo;
         sh.all_hi[warp] = all_hi;
+        sh.least[warp] = least;
     }
 }
 template <int WARPS>
 __device__ __forceinline__ Reach get_reach(const ReachShared<WARPS>& sh)
 {
-    Reach r{sh.lo[0], sh.hi[0], sh.all_lo[0], sh.all_hi[0]};
+    Reach r{sh.lo[0], sh.hi[0], sh.all_lo[0], sh.all_hi[0], sh.least[0]};
 #pragma unroll
     for (int w = 1; w < WARPS; ++w) {
         r.lo = min(r.lo, sh.lo[w]);
         r.hi = max(r.hi, sh.hi[w]);
         r.all_lo = max(r.all_lo, sh.all_lo[w]);
         r.all_hi = min(r.all_hi, sh.all_hi[w]);
+        r.least = min(r.least, sh.least[w]);
     }
     return r;
 }
@@ -673,8 +677,9 @@ struct GradTile {
 // KEYS: rows are keys, acc1 = dk, acc2 = dv, streamed over the query heads that share them; lse and delta belong to columns.
 // Queries: acc1 = dq; lse and delta belong to rows.  delta = sum_j P_ij dP_ij is first taken as dout . out with the rounded out
 // of the forward call; the row sum eps of P (dP - delta) over the walk is exactly what that is off by, so delta + eps goes to
-// the second kernel, and for walks of at most kExact columns, where few keys share the error, dq is corrected by
-// -eps * sum_j P_ij inner k_j, for which acc2 is kept.
+// the second kernel, and for rows that see at most kExact columns, few of which share the error, dq is corrected by
+// -eps * sum_j P_ij inner k_j.  acc2 holds that sum, over the tiles that such a row of the CTA may reach (a row sees itself, so they
+// lie within kExact of the CTA's rows), if it has one: what a row gets does not depend on what else is in its CTA.
 //
 // P lies over S and dS over dP, and the products take turns: ..., acc2(n), S(n + 1), acc1(n), dP(n + 1), acc2(n + 1), ...  While
 // acc1(n) and dP(n + 1) run, P(n + 1) is made from S(n + 1); while acc2 and the next S run, dS from dP.  (Two groups of warps with
@@ -801,7 +806,10 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     const Walk<kColumns> walk(p, reach, r0, KEYS);
     const int per_head = walk.count(reach);
     const int n = KEYS ? per_head * p.group : per_head;
-    const bool second = KEYS || n * kColumns <= kExact;  // acc2 is kept
+    const bool second = KEYS || reach.least <= kExact;  // acc2 is kept
+    auto kept = [&](int j0) {  // for the tile from column j0 on
+        return KEYS || second && j0 + kColumns > r0 - (kExact - 1) && j0 <= r0 + 127 + (kExact - 1);
+    };
     float delta = 0.0f;
     int issued1 = p.causal, issued2 = p.causal;  // (warp of the copies)
     bool ended = false;                          // (warp of the products) none are under way
@@ -830,13 +838,16 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
             const uint32_t leader = tc::elect();
             auto all = [](bool x) { return (bool)__all_sync(0xffffffffu, x); };
             bool ok = all(tc::bar_wait(a_full, 0));
+            uint32_t turns2 = 0;  // tiles kept so far
             for (int i = 0; i <= n && ok; ++i) {  // acc2(i - 1), S(i), acc1(i - 1), dP(i)
                 const int s = i % kStages, sl = (i + kStages - 1) % kStages;
                 const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream, last = tc::smem_of(stream) + sl * 2 * Tile::kStream;
-                if (i > 0 && second) {
+                const bool last_kept = i > 0 && kept(walk(i - 1));
+                if (last_kept) {
                     if (!(ok = all(tc::bar_wait(p_full, (i - 1) & 1)))) break;
                     tc::fence_after();
-                    tc::product_across<BF16, kColumns, DP, 32>(leader, acc2_at, s_at, KEYS ? last + Tile::kStream : last, i > 1);
+                    tc::product_across<BF16, kColumns, DP, 32>(leader, acc2_at, s_at, KEYS ? last + Tile::kStream : last, KEYS ? i > 1 : turns2 > 0);
+                    ++turns2;
                     // (nothing arrives that nobody waits for: here and below, stages that no copy takes again, ends that no product needs)
                     if (KEYS && i - 1 + kStages < n) tc::products_arrive(leader, b2_free + 8 * sl);
                     if (i < n) tc::products_arrive(leader, acc2_done);
@@ -844,7 +855,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 if (i < n) {
                     // S's place is free when the product is over that reads the last P there, or when the last S has been read
                     if (!(ok = all(tc::bar_wait(b1_full + 8 * s, (i / kStages) & 1) &&
-                                   (i == 0 || tc::bar_wait(second ? acc2_done : p_full, (i - 1) & 1)))))
+                                   (i == 0 || tc::bar_wait(last_kept ? acc2_done : p_full, (last_kept && !KEYS ? turns2 - 1 : i - 1) & 1)))))
                         break;
                     tc::fence_after();
                     tc::product_rows<BF16, kColumns, DP>(leader, s_at, tc::smem_of(a1), at);
@@ -928,7 +939,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 __syncwarp();
                 if (i + 1 < n) fetch(i + 1);
             }
-            const bool clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 31);
+            const bool keep = kept(j0), clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 31);
             const uint32_t mask = clear ? 0xffffffffu : column_mask(span.lo - mine0, span.hi - mine0);
             if (!__all_sync(0xffffffffu, tc::bar_wait(s_full, i & 1))) {
                 dead = 1;
@@ -937,7 +948,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
             tc::fence_after();
             if (__all_sync(0xffffffffu, mask == 0)) {  // nothing of this block of 32 x 32 is seen
                 const uint32_t none[16] = {};
-                if (second) {
+                if (keep) {
                     tc::tmem_store16(s_at + lanes + 32 * part, none);
                     scan(KEYS ? b2_full : b1_full, i, KEYS ? 1 : 0, j0);
                     tc::tmem_stored();
@@ -950,7 +961,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 }
                 tc::fence_after();
                 tc::tmem_store16(dp_at + lanes + 32 * part, none);
-                if (KEYS || !second) scan(b1_full, i, 0, j0);
+                if (KEYS || !keep) scan(b1_full, i, 0, j0);
                 tc::tmem_stored();
                 tc::fence_before();
                 tc::bar_arrive(ds_full);
@@ -962,7 +973,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 tc::tmem_load(s, s_at + lanes + 32 * part);
                 tc::tmem_loaded();
                 tc::settle(s);
-                if (!second) {  // S has been read
+                if (!keep) {  // S has been read
                     tc::fence_before();
                     tc::bar_arrive(p_full);
                 }
@@ -1001,7 +1012,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                     if (MOD) in[MOD ? e : 0] = (mask >> e) & 1 ? in[MOD ? e : 0] : 0.0f;
                 }
             }
-            if (second) {
+            if (keep) {
                 uint32_t pw[16];
 #pragma unroll
                 for (int e = 0; e < 32; e += 2)
@@ -1048,7 +1059,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
                 }
             }
             tc::tmem_store16(dp_at + lanes + 32 * part, dw);
-            if (KEYS || !second) scan(b1_full, i, 0, j0);
+            if (KEYS || !keep) scan(b1_full, i, 0, j0);
             tc::tmem_stored();
             tc::fence_before();
             tc::bar_arrive(ds_full);
@@ -1079,7 +1090,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         if (tid == 0) atomicAdd(&g_timeouts, 1u);
     } else if (warp < kWarps) {
         const uint32_t lanes = (uint32_t)quarter << 21;
-        const bool empty = span.lo > span.hi;
+        const bool empty = span.lo > span.hi, few = !KEYS && second && span.hi - span.lo < kExact;
         if (n > 0 && !tc::bar_wait(acc1_done, (n - 1) & 1)) atomicAdd(&g_timeouts, 1u);
         tc::fence_after();
         float off = 0.0f;
@@ -1104,7 +1115,7 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
                 float y = __uint_as_float(o[e]);
-                if (!KEYS && second) y = fmaf(-off, __uint_as_float(o2[e]), y);
+                if (few) y = fmaf(-off, __uint_as_float(o2[e]), y);
                 x[e] = empty || n == 0 ? 0.0f : y * (dv ? 1.0f : p.scale);
             }
             if (add && !empty)
