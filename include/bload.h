@@ -479,7 +479,8 @@ BLOAD_API int bload_plan_static(const int32_t* d_lengths, int64_t n, int32_t t_b
  *
  * Common rules: block_count >= 0 (0 does nothing), 1 <= t_block <= BLOAD_MAX_T_BLOCK.  Element types are BLOAD_F32,
  * BLOAD_F16 and BLOAD_BF16, one for all tensors of a call; statistics, states and sums are held in 32 bits and every
- * output is rounded once.  Outputs must not overlap inputs or each other, except where a call says so.  Repeated calls
+ * output is rounded once (attention also rounds its weights, and their gradients, to the element type where they enter
+ * its second products; in fp16 scaled so that its range does not matter).  Outputs must not overlap inputs or each other, except where a call says so.  Repeated calls
  * on equal inputs give identical bits: no sum depends on the order in which blocks of threads run.  Asynchronous on
  * `stream`; nothing is allocated; capturable.  Errors: NULL, ARG, ALIGN, UNSUPPORTED, WORKSPACE, CUDA as documented at
  * each call, all before anything is launched.  A device-side wait that expired (it cannot, short of a hardware fault)

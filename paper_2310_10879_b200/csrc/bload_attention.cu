@@ -6,14 +6,16 @@
 // Every row (a query, or a key of the second gradient kernel) may see one interval of slots [lo, hi] -- its sequence, cut by
 // causality and by the window -- so a CTA walks the tiles from the smallest lo of its rows to their largest hi, and a tile's
 // mask is a range of columns per row.  Products run in 16 bits with sums in 32; scores, statistics, probabilities and
-// accumulators are held in 32 bits, and P and dS are rounded to the inputs' type as operands of the second product.
+// accumulators are held in 32 bits, and P and dS are rounded to the inputs' type as operands of the second product.  For
+// fp16 they are scaled by powers of two first, since its smallest step, 2^-24, is one of 16 million keys' even share, and dS is that
+// times whatever dout is: P by a constant, dS row by row by what the row's largest needs (see k30_attention_grad).
 //
 // Hidden slots must have no influence, but a product multiplies them by zero, and 0 * NaN is not 0.  So a tile that is hidden
 // from any row of the CTA is scanned (one multiply-add by zero per pair of elements), and infinities and NaN in it are cleared in
 // shared memory before a product reads across it.  Rows that may see a frame that held some have them added in the end, read
 // from memory once more (add_junk): a clean row's bits do not depend on what a hidden slot holds.  With v and dout infinite
-// everywhere, 8,192 slots of 4 heads on 2 of 128 take 254 us forward and 575 gradient (clean: 155 and 359), 4 x 4096 slots of
-// heavy-tailed lengths 246 and 581 (46 and 124).
+// everywhere, 8,192 slots of 4 heads on 2 of 128 take 254 us forward and 600 gradient (fp16 1,120; clean: 155 and 360), 4 x 4096 slots of
+// heavy-tailed lengths 250 and 610 (fp16 750; clean: 46 and 125).
 #include <cuda.h>
 #include <math.h>
 
@@ -417,6 +419,8 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
     const Walk<kKeys> walk(p, reach, i0, false);
     const int n = walk.count(reach);
     float m = -INFINITY, l = 0.0f;  // running maximum (log2 units; may lag by kLag) and sum
+    // fp16 holds up to 2^16: exponentials of up to 2^kLag are kept 2^kLift times as large, sum and accumulator with them
+    constexpr float kLag = 8.0f, kLift = BF16 ? 0.0f : 7.0f;
     int issued_k = p.causal, issued_v = p.causal;  // (warp of the copies)
     bool ended = false;                            // (warp of the products) none are under way
 
@@ -532,7 +536,6 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
             // The maximum that scales the exponentials may lag behind by a factor of 2^8: the result is the same, and the
             // accumulator in tensor memory is rescaled only when a row has moved further than that.  (The second half's warp
             // sees the same maxima and moves with the first's.)
-            constexpr float kLag = 8.0f;
             const bool move = top > m + kLag || (m == -INFINITY && top > m);
             if (__any_sync(0xffffffffu, move)) {
                 const float now = move ? top : m;
@@ -553,7 +556,7 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
                     }
                 }
             }
-            const float off = m == -INFINITY ? 0.0f : -m;
+            const float off = m == -INFINITY ? 0.0f : kLift - m;
             const Two by2 = two(by, by), off2 = two(off, off);
             Two sum[2] = {zero(), zero()};
 #pragma unroll
@@ -643,7 +646,7 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
             tc::stores_read();
         }
         if (half == 0 && p.lse && row < p.t)
-            p.lse[((int64_t)b * p.heads + h) * p.t + row] = empty ? -INFINITY : (m + log2f(l)) * kLn2;
+            p.lse[((int64_t)b * p.heads + h) * p.t + row] = empty ? -INFINITY : (m + (log2f(l) - kLift)) * kLn2;
     }
     tc::fence_before();
     __syncthreads();
@@ -655,6 +658,7 @@ __global__ void __launch_bounds__(ForwardTile<DP>::kThreads, ForwardTile<DP>::kC
 struct GradMaps {
     CUtensorMap a1, a2;  // the CTA's own rows: boxes of 128 rows.  q, dout | k, v
     CUtensorMap b1, b2;  // what streams by: boxes of kColumns.     k, v    | q, dout
+    CUtensorMap b2_first;  // fp16: b2 in boxes of 128 rows by 8 elements
 };
 
 // Tiles of 128 columns and all of the tensor memory; for heads of at most 64 elements, tiles of 64 and half of it: then two CTAs
@@ -687,6 +691,19 @@ struct GradTile {
 // memory per cycle where there are 128, and what it reads of A serves half as many columns.)
 constexpr int kExact = 1024;
 
+// fp16: P is made 2^14 times as large (its rows' sums are 1, so none is much above 1), and each row of dS is multiplied by 2^14 and a
+// power of two of its own, `lift`, so that 2^14 lift max|dout| max|v| is between 2^9 and 2^10 over the first eight elements of both at the row's
+// own slot (for a key: dout of the first head that shares it): every row sees itself, and vectors of like elements have no dS above
+// 2^15 then.  Terms are off by 2^-34 of that product where they do not have fp16's 11 bits; without a scale a row of 4,000 keys and
+// dout of 1e-2 has dS of 2e-6, which is 32 steps of fp16, and one above 65,504 was infinite.  Where a row's dS do not fit all the
+// same, its acc1 comes out infinite or NaN, and the CTA walks AGAIN, twice: to find such rows' largest dS, and with a lift
+// from that (rows that fit keep theirs, and their bits).  The gradient of 4 x 4096 tokens takes 519 us (without lifts 505), of 16 x 1000
+// frames of features 236 (214); to agree on a row's lift among its warps in every tile took 574 and 257.
+constexpr float kLiftP = 16384.0f;
+constexpr int kOneWalk = 0, kMeasure = 1, kLastWalk = 2;
+__device__ __forceinline__ float power_of_two(int exponent) { return __int_as_float((exponent + 127) << 23); }
+__device__ __forceinline__ int exponent_of(float x) { return (__float_as_int(x) >> 23) - 127; }  // x >= 0; 128 for infinities and NaN
+
 // The 32 rows by 32 columns (from `first` on, `column` in the tile) that a warp has staged, to memory: 16 bytes per lane, side by side.
 // At one CTA per SM that is 400 to 600 cycles less than a tensor store, whose reads the CTA has to see the end of; the forward
 // kernel, whose CTAs hide each other's ends, is slower for it (features 65 -> 70 us).
@@ -706,26 +723,40 @@ __device__ __forceinline__ void store_staged(const uint8_t* tile, int own_row0, 
     __syncwarp();
 }
 
-template <bool BF16, int DP, bool MOD, bool KEYS>
-__global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
-    k30_attention_grad(const AttnParams p, const AttnTensors<typename Element<BF16>::type> a, const __grid_constant__ GradMaps maps)
+template <bool BF16, int DP, bool KEYS>
+struct GradShared {
+    static constexpr int kColumns = GradTile<DP>::kColumns;
+    alignas(128) uint4 b2_first[BF16 ? 1 : 128];  // eight elements of B2's tensor at each row's own slot
+    float4 column_stats[KEYS ? GradTile<DP>::kWarps : 1][KEYS ? 16 : 1];  // per warp: -lse (log2 units) and -delta of 16 pairs of columns
+    uint64_t bars[8 + 4 * GradTile<DP>::kStages];
+    uint32_t tmem_base;
+    int dead, again, stuck;
+    Junk<kColumns> junk;
+    ReachShared<4> reach;
+    float eps[kColumns / 32][128], delta[KEYS ? 1 : 128];
+    float tops[BF16 ? 1 : kColumns / 32][BF16 ? 1 : 128];  // per 32 columns and row: the largest of dS * lift
+};
+
+// All of k30_attention_grad; true if the CTA has to walk AGAIN (fp16: see kLiftP).
+template <bool BF16, int DP, bool MOD, bool KEYS, bool AGAIN>
+__device__ __forceinline__ bool attention_grad(const AttnParams& p, const AttnTensors<typename Element<BF16>::type>& a, const GradMaps& maps,
+                                               GradShared<BF16, DP, KEYS>& sh)
 {
     using Tile = GradTile<DP>;
     constexpr int kColumns = Tile::kColumns, kWarps = Tile::kWarps, kStages = Tile::kStages;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[8 + 4 * kStages];
-    __shared__ uint32_t tmem_base;
-    __shared__ int dead;
-    __shared__ Junk<kColumns> junk;
-    __shared__ ReachShared<4> reach_shared;
-    __shared__ float eps_shared[kColumns / 32][128], delta_shared[KEYS ? 1 : 128];
-    __shared__ float4 column_stats[KEYS ? kWarps : 1][KEYS ? 16 : 1];  // per warp: -lse (log2 units) and -delta of 16 pairs of columns
+    int &dead = sh.dead, &again = sh.again, &stuck = sh.stuck;
+    auto& junk = sh.junk;
+    auto& column_stats = sh.column_stats;
+    auto& eps_shared = sh.eps;
+    auto& delta_shared = sh.delta;
+    auto& tops = sh.tops;
 
     uint8_t* const tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* const a1 = tiles;
     uint8_t* const a2 = tiles + Tile::kOwn;
     uint8_t* const stream = tiles + 2 * Tile::kOwn;  // per stage: B1, B2
-    const uint32_t bar0 = tc::smem_of(bars);
+    const uint32_t bar0 = tc::smem_of(sh.bars);
     const uint32_t a_full = bar0, s_full = bar0 + 8, dp_full = bar0 + 16, p_full = bar0 + 24, ds_full = bar0 + 32, acc1_done = bar0 + 40,
                    acc2_done = bar0 + 48, b1_full = bar0 + 56, b2_full = b1_full + 8 * kStages, b1_free = b2_full + 8 * kStages,
                    b2_free = b1_free + 8 * kStages, given_up = b2_free + 8 * kStages;
@@ -748,6 +779,31 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         for (int x = 0; x < DP; x += 64) tc::tensor_load(to + x * (2 * kColumns), one ? &maps.b1 : &maps.b2, x, j0, hs, b, bar);
     };
     const int first_head = KEYS ? h * p.group : h / p.group;  // of the other side
+    auto begin = [&] {  // by one thread: barriers, and the copies that need no positions
+        if (AGAIN)
+            for (int k = 0; k < 8 + 4 * kStages; ++k) tc::bar_inval(bar0 + 8 * k);
+        tc::bar_init(a_full, 1);
+        tc::bar_init(s_full, 1);
+        tc::bar_init(dp_full, 1);
+        tc::bar_init(p_full, 32 * kWarps);
+        tc::bar_init(ds_full, 32 * kWarps);
+        tc::bar_init(acc1_done, 1);
+        tc::bar_init(acc2_done, 1);
+        for (int s = 0; s < 4 * kStages; ++s) tc::bar_init(b1_full + 8 * s, 1);
+        tc::bar_init(given_up, 1);
+        tc::bar_init_done();
+        tc::bar_expect(a_full, 2 * Tile::kOwn + (BF16 ? 0 : 128 * 16));
+        if (!BF16) tc::tensor_load(tc::smem_of(sh.b2_first), &maps.b2_first, 0, r0, first_head, b, a_full);
+        for (int x = 0; x < DP; x += 64) {
+            tc::tensor_load(tc::smem_of(a1) + x * 256, &maps.a1, x, r0, h, b, a_full);
+            tc::tensor_load(tc::smem_of(a2) + x * 256, &maps.a2, x, r0, h, b, a_full);
+        }
+        if (p.causal) {
+            const int j0 = Walk<kColumns>::causal_first(p, r0, KEYS);
+            load(true, 0, j0, first_head);
+            load(false, 0, j0, first_head);
+        }
+    };
     Span span{kNever, -1};
     float own_lse = 0.0f;  // queries: of this row
     // dout . out of the queries: DP / 8 lanes share a row, 16 bytes each, so that a load of a warp touches few lines (with a row per
@@ -767,42 +823,24 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         }
         span = span_of(p, pos, row, KEYS, lane);
         if (part == 0) {
-            put_reach(reach_shared, quarter, lane, span);
+            put_reach(sh.reach, quarter, lane, span);
             junk.spans[own_row] = span;
             if (tid < (int)(sizeof junk.tiles / 4)) junk.tiles[tid] = 0;
         }
-        if (tid == 0) dead = junk.any = 0;
-    } else if (warp == kWarps) {
-        if (lane == 0) {
-            tc::bar_init(a_full, 1);
-            tc::bar_init(s_full, 1);
-            tc::bar_init(dp_full, 1);
-            tc::bar_init(p_full, 32 * kWarps);
-            tc::bar_init(ds_full, 32 * kWarps);
-            tc::bar_init(acc1_done, 1);
-            tc::bar_init(acc2_done, 1);
-            for (int s = 0; s < 4 * kStages; ++s) tc::bar_init(b1_full + 8 * s, 1);
-            tc::bar_init(given_up, 1);
-            tc::bar_init_done();
-            tc::bar_expect(a_full, 2 * Tile::kOwn);  // under way while the rows look for their columns
-            for (int x = 0; x < DP; x += 64) {
-                tc::tensor_load(tc::smem_of(a1) + x * 256, &maps.a1, x, r0, h, b, a_full);
-                tc::tensor_load(tc::smem_of(a2) + x * 256, &maps.a2, x, r0, h, b, a_full);
-            }
-            if (p.causal) {
-                const int j0 = Walk<kColumns>::causal_first(p, r0, KEYS);
-                load(true, 0, j0, first_head);
-                load(false, 0, j0, first_head);
-            }
+        if (tid == 0) {
+            dead = junk.any = stuck = 0;
+            again = AGAIN;
         }
-    } else {
-        tc::tmem_alloc<Tile::kTmem>(tc::smem_of(&tmem_base));
+    } else if (warp == kWarps) {
+        if (lane == 0) begin();  // under way while the rows look for their columns
+    } else if (!AGAIN) {
+        tc::tmem_alloc<Tile::kTmem>(tc::smem_of(&sh.tmem_base));
     }
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = tmem_base, acc1_at = tmem, acc2_at = tmem + DP, s_at = tmem + 2 * DP, dp_at = s_at + kColumns;
-    const Reach reach = get_reach(reach_shared);
+    const uint32_t tmem = sh.tmem_base, acc1_at = tmem, acc2_at = tmem + DP, s_at = tmem + 2 * DP, dp_at = s_at + kColumns;
+    const Reach reach = get_reach(sh.reach);
     const Walk<kColumns> walk(p, reach, r0, KEYS);
     const int per_head = walk.count(reach);
     const int n = KEYS ? per_head * p.group : per_head;
@@ -810,263 +848,318 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     auto kept = [&](int j0) {  // for the tile from column j0 on
         return KEYS || second && j0 + kColumns > r0 - (kExact - 1) && j0 <= r0 + 127 + (kExact - 1);
     };
-    float delta = 0.0f;
-    int issued1 = p.causal, issued2 = p.causal;  // (warp of the copies)
-    bool ended = false;                          // (warp of the products) none are under way
+    float delta = 0.0f, lift = 1.0f;
+    int issued1, issued2;  // (warp of the copies)
+    bool ended;            // (warp of the products) none are under way
 
-    if (warp == kWarps) {
-        if (lane == 0) {
-            bool ok = true;
-            if (n == 0) ok = tc::bar_wait(a_full, 0) && (!p.causal || (tc::bar_wait(b1_full, 0) && tc::bar_wait(b2_full, 0)));  // (copies end)
-            for (int i = p.causal; i < n; ++i) {
-                const int s = i % kStages;
-                const uint32_t parity = (i / kStages + 1) & 1;
-                const int j0 = walk(KEYS ? i % per_head : i), hs = KEYS ? first_head + i / per_head : first_head;
-                if (!(ok = tc::bar_wait(b1_free + 8 * s, parity))) break;
-                load(true, s, j0, hs);
-                issued1 = i + 1;
-                if (!(ok = tc::bar_wait(b2_free + 8 * s, parity))) break;
-                load(false, s, j0, hs);
-                issued2 = i + 1;
-            }
-            if (!ok) dead = 1;
-        }
-    } else if (warp == kWarps + 1) {
-        ended = true;
-        if (n > 0) {
-            ended = false;
-            const uint32_t leader = tc::elect();
-            auto all = [](bool x) { return (bool)__all_sync(0xffffffffu, x); };
-            bool ok = all(tc::bar_wait(a_full, 0));
-            uint32_t turns2 = 0;  // tiles kept so far
-            for (int i = 0; i <= n && ok; ++i) {  // acc2(i - 1), S(i), acc1(i - 1), dP(i)
-                const int s = i % kStages, sl = (i + kStages - 1) % kStages;
-                const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream, last = tc::smem_of(stream) + sl * 2 * Tile::kStream;
-                const bool last_kept = i > 0 && kept(walk(i - 1));
-                if (last_kept) {
-                    if (!(ok = all(tc::bar_wait(p_full, (i - 1) & 1)))) break;
-                    tc::fence_after();
-                    tc::product_across<BF16, kColumns, DP, 32>(leader, acc2_at, s_at, KEYS ? last + Tile::kStream : last, KEYS ? i > 1 : turns2 > 0);
-                    ++turns2;
-                    // (nothing arrives that nobody waits for: here and below, stages that no copy takes again, ends that no product needs)
-                    if (KEYS && i - 1 + kStages < n) tc::products_arrive(leader, b2_free + 8 * sl);
-                    if (i < n) tc::products_arrive(leader, acc2_done);
+    for (int pass = AGAIN ? kMeasure : kOneWalk;; ++pass) {
+        issued1 = issued2 = p.causal;
+        ended = false;
+        if (warp == kWarps) {
+            if (lane == 0) {
+                bool ok = true;
+                if (n == 0) ok = tc::bar_wait(a_full, 0) && (!p.causal || (tc::bar_wait(b1_full, 0) && tc::bar_wait(b2_full, 0)));  // (copies end)
+                for (int i = p.causal; i < n; ++i) {
+                    const int s = i % kStages;
+                    const uint32_t parity = (i / kStages + 1) & 1;
+                    const int j0 = walk(KEYS ? i % per_head : i), hs = KEYS ? first_head + i / per_head : first_head;
+                    if (!(ok = tc::bar_wait(b1_free + 8 * s, parity))) break;
+                    load(true, s, j0, hs);
+                    issued1 = i + 1;
+                    if (!(ok = tc::bar_wait(b2_free + 8 * s, parity))) break;
+                    load(false, s, j0, hs);
+                    issued2 = i + 1;
                 }
-                if (i < n) {
-                    // S's place is free when the product is over that reads the last P there, or when the last S has been read
-                    if (!(ok = all(tc::bar_wait(b1_full + 8 * s, (i / kStages) & 1) &&
-                                   (i == 0 || tc::bar_wait(last_kept ? acc2_done : p_full, (last_kept && !KEYS ? turns2 - 1 : i - 1) & 1)))))
+                if (!ok) dead = 1;
+            }
+        } else if (warp == kWarps + 1) {
+            ended = true;
+            if (n > 0) {
+                ended = false;
+                const uint32_t leader = tc::elect();
+                auto all = [](bool x) { return (bool)__all_sync(0xffffffffu, x); };
+                bool ok = all(tc::bar_wait(a_full, 0));
+                uint32_t turns2 = 0;  // tiles kept so far
+                for (int i = 0; i <= n && ok; ++i) {  // acc2(i - 1), S(i), acc1(i - 1), dP(i)
+                    const int s = i % kStages, sl = (i + kStages - 1) % kStages;
+                    const uint32_t at = tc::smem_of(stream) + s * 2 * Tile::kStream, last = tc::smem_of(stream) + sl * 2 * Tile::kStream;
+                    const bool last_kept = i > 0 && kept(walk(i - 1));
+                    if (last_kept) {
+                        if (!(ok = all(tc::bar_wait(p_full, (i - 1) & 1)))) break;
+                        tc::fence_after();
+                        tc::product_across<BF16, kColumns, DP, 32>(leader, acc2_at, s_at, KEYS ? last + Tile::kStream : last, KEYS ? i > 1 : turns2 > 0);
+                        ++turns2;
+                        // (nothing arrives that nobody waits for: here and below, stages that no copy takes again, ends that no product needs)
+                        if (KEYS && i - 1 + kStages < n) tc::products_arrive(leader, b2_free + 8 * sl);
+                        if (i < n) tc::products_arrive(leader, acc2_done);
+                    }
+                    if (i < n) {
+                        // S's place is free when the product is over that reads the last P there, or when the last S has been read
+                        if (!(ok = all(tc::bar_wait(b1_full + 8 * s, (i / kStages) & 1) &&
+                                       (i == 0 || tc::bar_wait(last_kept ? acc2_done : p_full, (last_kept && !KEYS ? turns2 - 1 : i - 1) & 1)))))
+                            break;
+                        tc::fence_after();
+                        tc::product_rows<BF16, kColumns, DP>(leader, s_at, tc::smem_of(a1), at);
+                        tc::products_arrive(leader, s_full);
+                    }
+                    if (i > 0) {
+                        if (!(ok = all(tc::bar_wait(ds_full, (i - 1) & 1)))) break;
+                        tc::fence_after();
+                        tc::product_across<BF16, kColumns, DP, 32>(leader, acc1_at, dp_at, last, i > 1);
+                        if (i - 1 + kStages < n) tc::products_arrive(leader, b1_free + 8 * sl);
+                        tc::products_arrive(leader, acc1_done);
+                    }
+                    if (i < n) {
+                        if (!(ok = all(tc::bar_wait(b2_full + 8 * s, (i / kStages) & 1) && (i == 0 || tc::bar_wait(acc1_done, (i - 1) & 1))))) break;
+                        tc::fence_after();
+                        tc::product_rows<BF16, kColumns, DP>(leader, dp_at, tc::smem_of(a2), at + Tile::kStream);
+                        if (!KEYS && i + kStages < n) tc::products_arrive(leader, b2_free + 8 * s);
+                        tc::products_arrive(leader, dp_full);
+                    }
+                }
+                if (!ok) {
+                    dead = 1;
+                    tc::products_arrive(leader, given_up);
+                    tc::bar_wait(given_up, 0);
+                    ended = true;
+                }
+            }
+        } else {
+            const uint32_t lanes = (uint32_t)quarter << 21;
+            Two lse2 = zero(), eps2 = zero();  // lse and delta of this row, negative
+            constexpr float kUp = BF16 ? 0.0f : 14.0f;  // log2 kLiftP
+            if (!KEYS && row < p.t) {          // this row's statistics
+                const float lse = minus_lse(own_lse) + kUp;
+                lse2 = two(lse, lse);
+            }
+            if ((!KEYS || !BF16) && pass != kLastWalk) {
+                if (!tc::bar_wait(a_full, 0)) dead = 1;
+                if (!BF16) {
+                    const uint4 own = *reinterpret_cast<const uint4*>(a2 + own_row * 128 + (own_row & 7) * 16);  // dout, or v
+                    lift = power_of_two(-5 - min(max(exponent_of(tc::largest_of_halves(own) * tc::largest_of_halves(sh.b2_first[BF16 ? 0 : own_row])), -64), 64));
+                }
+            }
+            if (!KEYS && pass != kLastWalk) {
+#pragma unroll
+                for (int k = 0; k < kPasses; ++k) {
+                    const int r = sum_row + k * kSumRows;
+                    const uint4 dout = *reinterpret_cast<const uint4*>(a2 + sum_chunk / 8 * (128 * 128) + r * 128 + ((sum_chunk % 8) ^ (r & 7)) * 16);
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        sum = fmaf(to_float(reinterpret_cast<const E*>(&out_part[k])[e]), to_float(reinterpret_cast<const E*>(&dout)[e]), sum);
+#pragma unroll
+                    for (int o = 1; o < kSumLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                    if (sum_chunk == 0) delta_shared[KEYS ? 0 : r] = sum;
+                }
+                asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");  // of the warps with the arithmetic
+                delta = delta_shared[KEYS ? 0 : own_row];
+            }
+            const Two delta2 = two(-delta, -delta);
+            // Junk in a tile that is hidden from some row must not reach the products across it.  (B1 is scanned when S is done, which reads
+            // it; B2 while dP may still read it, so whoever has something to clear waits for dP's end, which waits for nothing of this turn.
+            // A query with junk in dout has NaN for its delta, so its dS are NaN whatever dP reads.)
+            auto scan = [&](uint32_t full, int i, int which, int j0) {
+                if (j0 >= reach.all_lo && j0 + kColumns - 1 <= reach.all_hi) return;
+                if (!tc::bar_wait(full + 8 * (i % kStages), (i / kStages) & 1)) dead = 1;
+                scan_tile_apart<BF16, kColumns, DP, 32 * kWarps>(p, pos, stream + ((i % kStages) * 2 + which) * Tile::kStream, j0, tid, junk,
+                                                                 KEYS ? i % per_head : i, which ? dp_full : 0, i & 1, dead);
+                __syncwarp();
+                tc::writes_to_async();
+            };
+            // KEYS: statistics of this warp's 32 columns of tile i, a tile ahead
+            float next_lse = 0.0f, next_delta = 0.0f;
+            auto fetch = [&](int i) {
+                const int column = walk(i % per_head) + 32 * part + lane;
+                const int64_t at = ((int64_t)b * p.heads + first_head + i / per_head) * p.t + column;
+                next_lse = column < p.t ? p.lse[at] : 0.0f;
+                next_delta = column < p.t ? p.delta[at] : 0.0f;
+            };
+            if (KEYS && n > 0) fetch(0);
+            float top = 0.0f;  // kMeasure
+            for (int i = 0; i < n; ++i) {
+                const int j0 = walk(KEYS ? i % per_head : i), mine0 = j0 + 32 * part;  // the tile's and this warp's first column
+                const Modifier modify(p, KEYS ? first_head + i / per_head : h);
+                if (KEYS) {
+                    __syncwarp();
+                    float* const st = reinterpret_cast<float*>(&column_stats[KEYS ? warp : 0][KEYS ? lane / 2 : 0]) + (lane & 1);
+                    st[0] = minus_lse(next_lse) + kUp;
+                    st[2] = -next_delta;
+                    __syncwarp();
+                    if (i + 1 < n) fetch(i + 1);
+                }
+                const bool keep = kept(j0), clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 31);
+                const uint32_t mask = clear ? 0xffffffffu : column_mask(span.lo - mine0, span.hi - mine0);
+                if (!__all_sync(0xffffffffu, tc::bar_wait(s_full, i & 1))) {
+                    dead = 1;
+                    break;
+                }
+                tc::fence_after();
+                if (__all_sync(0xffffffffu, mask == 0)) {  // nothing of this block of 32 x 32 is seen
+                    const uint32_t none[16] = {};
+                    if (keep) {
+                        tc::tmem_store16(s_at + lanes + 32 * part, none);
+                        scan(KEYS ? b2_full : b1_full, i, KEYS ? 1 : 0, j0);
+                        tc::tmem_stored();
+                        tc::fence_before();
+                    }
+                    tc::bar_arrive(p_full);
+                    if (!__all_sync(0xffffffffu, tc::bar_wait(dp_full, i & 1))) {
+                        dead = 1;
                         break;
+                    }
                     tc::fence_after();
-                    tc::product_rows<BF16, kColumns, DP>(leader, s_at, tc::smem_of(a1), at);
-                    tc::products_arrive(leader, s_full);
+                    tc::tmem_store16(dp_at + lanes + 32 * part, none);
+                    if (KEYS || !keep) scan(b1_full, i, 0, j0);
+                    tc::tmem_stored();
+                    tc::fence_before();
+                    tc::bar_arrive(ds_full);
+                    continue;
                 }
-                if (i > 0) {
-                    if (!(ok = all(tc::bar_wait(ds_full, (i - 1) & 1)))) break;
-                    tc::fence_after();
-                    tc::product_across<BF16, kColumns, DP, 32>(leader, acc1_at, dp_at, last, i > 1);
-                    if (i - 1 + kStages < n) tc::products_arrive(leader, b1_free + 8 * sl);
-                    tc::products_arrive(leader, acc1_done);
+                float w[32], in[MOD ? 32 : 1];  // P, inner
+                {
+                    uint32_t s[32];
+                    tc::tmem_load(s, s_at + lanes + 32 * part);
+                    tc::tmem_loaded();
+                    tc::settle(s);
+                    if (!keep) {  // S has been read
+                        tc::fence_before();
+                        tc::bar_arrive(p_full);
+                    }
+                    const Two by2 = two(modify.by, modify.by);
+                    const float apart = (float)(row - mine0);
+                    if (MOD)
+                        Modifier::with(modify.kind(s), [&](auto kind) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) {
+                                Two inner;
+                                const float2 x = one(modify.apply<decltype(kind)::value>(two(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
+                                                                                         apart - (float)e, inner));
+                                s[e] = __float_as_uint(x.x);
+                                s[e + 1] = __float_as_uint(x.y);
+                                in[MOD ? e : 0] = one(inner).x;
+                                in[MOD ? e + 1 : 0] = one(inner).y;
+                            }
+                        });
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        Two lse_here = lse2;
+                        if (KEYS) {
+                            const float2 l = *reinterpret_cast<const float2*>(&column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0]);
+                            lse_here = two(l.x, l.y);
+                        }
+                        const Two raw = two(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+                        const float2 x = one(MOD ? raw + lse_here : fma(raw, by2, lse_here));
+                        w[e] = tc::exp2_fast(x.x);
+                        w[e + 1] = tc::exp2_fast(x.y);
+                    }
                 }
-                if (i < n) {
-                    if (!(ok = all(tc::bar_wait(b2_full + 8 * s, (i / kStages) & 1) && (i == 0 || tc::bar_wait(acc1_done, (i - 1) & 1))))) break;
-                    tc::fence_after();
-                    tc::product_rows<BF16, kColumns, DP>(leader, dp_at, tc::smem_of(a2), at + Tile::kStream);
-                    if (!KEYS && i + kStages < n) tc::products_arrive(leader, b2_free + 8 * s);
-                    tc::products_arrive(leader, dp_full);
+                if (!clear) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        w[e] = (mask >> e) & 1 ? w[e] : 0.0f;
+                        if (MOD) in[MOD ? e : 0] = (mask >> e) & 1 ? in[MOD ? e : 0] : 0.0f;
+                    }
                 }
-            }
-            if (!ok) {
-                dead = 1;
-                tc::products_arrive(leader, given_up);
-                tc::bar_wait(given_up, 0);
-                ended = true;
-            }
-        }
-    } else {
-        const uint32_t lanes = (uint32_t)quarter << 21;
-        Two lse2 = zero(), eps2 = zero();  // lse and delta of this row, negative
-        if (!KEYS && row < p.t) {          // this row's statistics
-            const float lse = minus_lse(own_lse);
-            lse2 = two(lse, lse);
-        }
-        if (!KEYS) {
-            if (!tc::bar_wait(a_full, 0)) dead = 1;
-#pragma unroll
-            for (int k = 0; k < kPasses; ++k) {
-                const int r = sum_row + k * kSumRows;
-                const uint4 dout = *reinterpret_cast<const uint4*>(a2 + sum_chunk / 8 * (128 * 128) + r * 128 + ((sum_chunk % 8) ^ (r & 7)) * 16);
-                float sum = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    sum = fmaf(to_float(reinterpret_cast<const E*>(&out_part[k])[e]), to_float(reinterpret_cast<const E*>(&dout)[e]), sum);
-#pragma unroll
-                for (int o = 1; o < kSumLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                if (sum_chunk == 0) delta_shared[KEYS ? 0 : r] = sum;
-            }
-            asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");  // of the warps with the arithmetic
-            delta = delta_shared[KEYS ? 0 : own_row];
-        }
-        const Two delta2 = two(-delta, -delta);
-        // Junk in a tile that is hidden from some row must not reach the products across it.  (B1 is scanned when S is done, which reads
-        // it; B2 while dP may still read it, so whoever has something to clear waits for dP's end, which waits for nothing of this turn.
-        // A query with junk in dout has NaN for its delta, so its dS are NaN whatever dP reads.)
-        auto scan = [&](uint32_t full, int i, int which, int j0) {
-            if (j0 >= reach.all_lo && j0 + kColumns - 1 <= reach.all_hi) return;
-            if (!tc::bar_wait(full + 8 * (i % kStages), (i / kStages) & 1)) dead = 1;
-            scan_tile_apart<BF16, kColumns, DP, 32 * kWarps>(p, pos, stream + ((i % kStages) * 2 + which) * Tile::kStream, j0, tid, junk,
-                                                             KEYS ? i % per_head : i, which ? dp_full : 0, i & 1, dead);
-            __syncwarp();
-            tc::writes_to_async();
-        };
-        // KEYS: statistics of this warp's 32 columns of tile i, a tile ahead
-        float next_lse = 0.0f, next_delta = 0.0f;
-        auto fetch = [&](int i) {
-            const int column = walk(i % per_head) + 32 * part + lane;
-            const int64_t at = ((int64_t)b * p.heads + first_head + i / per_head) * p.t + column;
-            next_lse = column < p.t ? p.lse[at] : 0.0f;
-            next_delta = column < p.t ? p.delta[at] : 0.0f;
-        };
-        if (KEYS && n > 0) fetch(0);
-        for (int i = 0; i < n; ++i) {
-            const int j0 = walk(KEYS ? i % per_head : i), mine0 = j0 + 32 * part;  // the tile's and this warp's first column
-            const Modifier modify(p, KEYS ? first_head + i / per_head : h);
-            if (KEYS) {
-                __syncwarp();
-                float* const st = reinterpret_cast<float*>(&column_stats[KEYS ? warp : 0][KEYS ? lane / 2 : 0]) + (lane & 1);
-                st[0] = minus_lse(next_lse);
-                st[2] = -next_delta;
-                __syncwarp();
-                if (i + 1 < n) fetch(i + 1);
-            }
-            const bool keep = kept(j0), clear = __all_sync(0xffffffffu, span.lo <= mine0 && span.hi >= mine0 + 31);
-            const uint32_t mask = clear ? 0xffffffffu : column_mask(span.lo - mine0, span.hi - mine0);
-            if (!__all_sync(0xffffffffu, tc::bar_wait(s_full, i & 1))) {
-                dead = 1;
-                break;
-            }
-            tc::fence_after();
-            if (__all_sync(0xffffffffu, mask == 0)) {  // nothing of this block of 32 x 32 is seen
-                const uint32_t none[16] = {};
                 if (keep) {
-                    tc::tmem_store16(s_at + lanes + 32 * part, none);
+                    uint32_t pw[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2)
+                        pw[e / 2] = MOD && !KEYS ? tc::pack<BF16>(w[e] * in[MOD ? e : 0], w[e + 1] * in[MOD ? e + 1 : 0]) : tc::pack<BF16>(w[e], w[e + 1]);
+                    tc::tmem_store16(s_at + lanes + 32 * part, pw);  // over the scores they were made from
+                    if (MOD && KEYS)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) w[e] *= in[MOD ? e : 0];  // (only together from here on)
                     scan(KEYS ? b2_full : b1_full, i, KEYS ? 1 : 0, j0);
                     tc::tmem_stored();
                     tc::fence_before();
+                    tc::bar_arrive(p_full);
                 }
-                tc::bar_arrive(p_full);
+                if (!BF16) {  // (while dP is made)
+                    const Two lift2 = two(lift, lift);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        const float2 x = one(two(w[e], w[e + 1]) * lift2);
+                        w[e] = x.x;
+                        w[e + 1] = x.y;
+                    }
+                }
                 if (!__all_sync(0xffffffffu, tc::bar_wait(dp_full, i & 1))) {
                     dead = 1;
                     break;
                 }
                 tc::fence_after();
-                tc::tmem_store16(dp_at + lanes + 32 * part, none);
-                if (KEYS || !keep) scan(b1_full, i, 0, j0);
-                tc::tmem_stored();
-                tc::fence_before();
-                tc::bar_arrive(ds_full);
-                continue;
-            }
-            float w[32], in[MOD ? 32 : 1];  // P, inner
-            {
-                uint32_t s[32];
-                tc::tmem_load(s, s_at + lanes + 32 * part);
-                tc::tmem_loaded();
-                tc::settle(s);
-                if (!keep) {  // S has been read
-                    tc::fence_before();
-                    tc::bar_arrive(p_full);
-                }
-                const Two by2 = two(modify.by, modify.by);
-                const float apart = (float)(row - mine0);
-                if (MOD)
-                    Modifier::with(modify.kind(s), [&](auto kind) {
+                // f(e, dS of columns e and e + 1, before `inner` if that is kept apart)
+                // (with a cap and rows of queries, two numbers per column wait for dP already: it is read in halves then, for registers)
+                constexpr int kAtOnce = MOD && !KEYS ? 16 : 32;
+                auto score_gradients = [&](const auto& f) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            Two inner;
-                            const float2 x = one(modify.apply<decltype(kind)::value>(two(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
-                                                                                     apart - (float)e, inner));
-                            s[e] = __float_as_uint(x.x);
-                            s[e + 1] = __float_as_uint(x.y);
-                            in[MOD ? e : 0] = one(inner).x;
-                            in[MOD ? e + 1 : 0] = one(inner).y;
+                    for (int c = 0; c < 32; c += kAtOnce) {
+                        uint32_t d[kAtOnce];
+                        tc::tmem_load(d, dp_at + lanes + 32 * part + c);
+                        tc::tmem_loaded();
+                        tc::settle(d);
+#pragma unroll
+                        for (int k = 0; k < kAtOnce; k += 2) {
+                            const int e = c + k;
+                            Two delta_here = delta2;
+                            if (KEYS) {
+                                const float2 l = *(reinterpret_cast<const float2*>(&column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0]) + 1);
+                                delta_here = two(l.x, l.y);
+                            }
+                            Two g = two(__uint_as_float(d[k]), __uint_as_float(d[k + 1])) + delta_here;
+                            if (!clear) g = two((mask >> e) & 1 ? one(g).x : 0.0f, (mask >> (e + 1)) & 1 ? one(g).y : 0.0f);  // (may be NaN)
+                            f(e, two(w[e], w[e + 1]) * g);
                         }
+                    }
+                };
+                if (!BF16 && __builtin_expect(pass == kMeasure, 0))
+                    score_gradients([&](int e, Two g) {
+                        if (MOD && !KEYS) g = g * two(in[MOD ? e : 0], in[MOD ? e + 1 : 0]);
+                        const float most = tc::largest(0.0f, one(g).x, one(g).y);
+                        top = most <= 3.0e38f ? fmaxf(top, most) : top;
                     });
-#pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    Two lse_here = lse2;
-                    if (KEYS) {
-                        const float2 l = *reinterpret_cast<const float2*>(&column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0]);
-                        lse_here = two(l.x, l.y);
-                    }
-                    const Two raw = two(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-                    const float2 x = one(MOD ? raw + lse_here : fma(raw, by2, lse_here));
-                    w[e] = tc::exp2_fast(x.x);
-                    w[e + 1] = tc::exp2_fast(x.y);
-                }
-            }
-            if (!clear) {
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    w[e] = (mask >> e) & 1 ? w[e] : 0.0f;
-                    if (MOD) in[MOD ? e : 0] = (mask >> e) & 1 ? in[MOD ? e : 0] : 0.0f;
-                }
-            }
-            if (keep) {
-                uint32_t pw[16];
-#pragma unroll
-                for (int e = 0; e < 32; e += 2)
-                    pw[e / 2] = MOD && !KEYS ? tc::pack<BF16>(w[e] * in[MOD ? e : 0], w[e + 1] * in[MOD ? e + 1 : 0]) : tc::pack<BF16>(w[e], w[e + 1]);
-                tc::tmem_store16(s_at + lanes + 32 * part, pw);  // over the scores they were made from
-                if (MOD && KEYS)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) w[e] *= in[MOD ? e : 0];  // (only together from here on)
-                scan(KEYS ? b2_full : b1_full, i, KEYS ? 1 : 0, j0);
-                tc::tmem_stored();
-                tc::fence_before();
-                tc::bar_arrive(p_full);
-            }
-            if (!__all_sync(0xffffffffu, tc::bar_wait(dp_full, i & 1))) {
-                dead = 1;
-                break;
-            }
-            tc::fence_after();
-            uint32_t dw[16];
-            // (with a cap and rows of queries, two numbers per column wait for dP already: it is read in halves then, for registers)
-            constexpr int kAtOnce = MOD && !KEYS ? 16 : 32;
-#pragma unroll
-            for (int c = 0; c < 32; c += kAtOnce) {
-                uint32_t d[kAtOnce];
-                tc::tmem_load(d, dp_at + lanes + 32 * part + c);
-                tc::tmem_loaded();
-                tc::settle(d);
-#pragma unroll
-                for (int k = 0; k < kAtOnce; k += 2) {
-                    const int e = c + k;
-                    Two delta_here = delta2;
-                    if (KEYS) {
-                        const float2 l = *(reinterpret_cast<const float2*>(&column_stats[KEYS ? warp : 0][KEYS ? e / 2 : 0]) + 1);
-                        delta_here = two(l.x, l.y);
-                    }
-                    Two g = two(__uint_as_float(d[k]), __uint_as_float(d[k + 1])) + delta_here;
-                    if (!clear) g = two((mask >> e) & 1 ? one(g).x : 0.0f, (mask >> (e + 1)) & 1 ? one(g).y : 0.0f);  // (may be NaN)
-                    g = two(w[e], w[e + 1]) * g;
+                uint32_t dw[16];
+                score_gradients([&](int e, Two g) {
                     if (!KEYS) {
                         eps2 = eps2 + g;
                         if (MOD) g = g * two(in[MOD ? e : 0], in[MOD ? e + 1 : 0]);
                     }
                     dw[e / 2] = tc::pack<BF16>(one(g).x, one(g).y);
-                }
+                });
+                tc::tmem_store16(dp_at + lanes + 32 * part, dw);
+                if (KEYS || !keep) scan(b1_full, i, 0, j0);
+                tc::tmem_stored();
+                tc::fence_before();
+                tc::bar_arrive(ds_full);
             }
-            tc::tmem_store16(dp_at + lanes + 32 * part, dw);
-            if (KEYS || !keep) scan(b1_full, i, 0, j0);
-            tc::tmem_stored();
-            tc::fence_before();
-            tc::bar_arrive(ds_full);
+            if (!KEYS) eps_shared[part][own_row] = (one(eps2).x + one(eps2).y) * (1.0f / lift);
+            if (!BF16) tops[BF16 ? 0 : part][BF16 ? 0 : own_row] = top;
         }
-        if (!KEYS) eps_shared[part][own_row] = one(eps2).x + one(eps2).y;
+        __syncthreads();
+        if (BF16 || dead || pass == kLastWalk || n == 0) break;
+        if (warp < kWarps) {
+            if (!tc::bar_wait(acc1_done, (n - 1) & 1)) stuck = 1;  // (the end counts it)
+            tc::fence_after();
+            if (pass == kOneWalk && part == 0) {
+                uint32_t x = tc::tmem_load1(acc1_at + ((uint32_t)quarter << 21));
+                tc::tmem_loaded();
+                tc::settle(x);
+                if (span.lo <= span.hi && (x & 0x7f800000u) == 0x7f800000u && (KEYS || isfinite(delta))) again = 1;
+            } else if (pass == kMeasure) {
+                float most = 0.0f;
+                for (int k = 0; k < kColumns / 32; ++k) most = fmaxf(most, tops[BF16 ? 0 : k][BF16 ? 0 : own_row]);
+                if (most > 65000.0f) lift *= power_of_two(14 - exponent_of(most));
+            }
+            tc::fence_before();
+        }
+        __syncthreads();
+        if (stuck || !again) break;
+        if (!AGAIN) return true;
+        if (warp == kWarps && lane == 0) begin();
+        __syncthreads();
+        tc::fence_after();
     }
-    __syncthreads();
     // (as in the forward kernel: what is under way ends before the CTA gives up its memory)
     if (dead && warp == kWarps + 1 && !ended) tc::bar_wait(acc1_done, (n - 1) & 1);
     if (dead && warp == kWarps && lane == 0) {
@@ -1093,9 +1186,11 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
         const bool empty = span.lo > span.hi, few = !KEYS && second && span.hi - span.lo < kExact;
         if (n > 0 && !tc::bar_wait(acc1_done, (n - 1) & 1)) atomicAdd(&g_timeouts, 1u);
         tc::fence_after();
+        const float undo_p = BF16 ? 1.0f : 1.0f / kLiftP, undo = BF16 ? 1.0f : undo_p / lift;  // powers of two
         float off = 0.0f;
         if (!KEYS) {
             for (int k = 0; k < kColumns / 32; ++k) off += eps_shared[k][own_row];
+            off *= undo_p;
             if (part == 0 && row < p.t) p.delta[((int64_t)b * p.heads + h) * p.t + row] = empty ? 0.0f : delta + off;
         }
         // chunks of 32 columns of dq, or of dk and then dv, are shared out among the warps of a row
@@ -1114,8 +1209,8 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
             float x[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-                float y = __uint_as_float(o[e]);
-                if (few) y = fmaf(-off, __uint_as_float(o2[e]), y);
+                float y = __uint_as_float(o[e]) * (dv ? undo_p : undo);
+                if (few) y = fmaf(-off, __uint_as_float(o2[e]) * undo_p, y);
                 x[e] = empty || n == 0 ? 0.0f : y * (dv ? 1.0f : p.scale);
             }
             if (add && !empty)
@@ -1129,6 +1224,18 @@ __global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
     tc::fence_before();
     __syncthreads();
     if (warp == kWarps + 1) tc::tmem_free<Tile::kTmem>(tmem);
+    return false;
+}
+
+template <bool BF16, int DP, bool MOD, bool KEYS>
+__global__ void __launch_bounds__(GradTile<DP>::kThreads, DP == 64 ? 2 : 1)
+    k30_attention_grad(const __grid_constant__ AttnParams p, const __grid_constant__ AttnTensors<typename Element<BF16>::type> a,
+                       const __grid_constant__ GradMaps maps)
+{
+    __shared__ GradShared<BF16, DP, KEYS> sh;
+    const bool again = attention_grad<BF16, DP, MOD, KEYS, false>(p, a, maps, sh);
+    if constexpr (!BF16)  // (in line: a call here, taken or not, cost every CTA 2 us)
+        if (__builtin_expect(again, 0)) (void)attention_grad<BF16, DP, MOD, KEYS, true>(p, a, maps, sh);
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------
@@ -1152,17 +1259,17 @@ EncodeTiled encode_tiled()
 // The tensor [block, head, slot, element] with boxes of `box` slots by 64 elements: elements from d on read as zeros and are
 // not written, nor are slots from t on.
 template <typename P>
-bool make_map(CUtensorMap* map, const AttnParams& p, bool bf16, const Heads<P>& x, int heads, int box)
+bool make_map(CUtensorMap* map, const AttnParams& p, bool bf16, const Heads<P>& x, int heads, int box, int elements = 64)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)p.d, (cuuint64_t)p.t, (cuuint64_t)heads, (cuuint64_t)p.blocks};
     auto bytes = [](int64_t stride) { return (cuuint64_t)(stride ? stride * 2 : 16); };  // (0: a dimension of length one)
     const cuuint64_t strides[3] = {bytes(x.slot), bytes(x.head), bytes(x.block)};
-    const cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1}, steps[4] = {1, 1, 1, 1};
+    const cuuint32_t boxes[4] = {(cuuint32_t)elements, (cuuint32_t)box, 1, 1}, steps[4] = {1, 1, 1, 1};
     return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
                   const_cast<void*>(static_cast<const void*>(x.data)), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                  elements == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <bool BF16, int DP, bool MOD>
@@ -1188,9 +1295,10 @@ cudaError_t gradient(const AttnParams& p, const AttnTensors<typename Element<BF1
 {
     GradMaps m;
     const int own = KEYS ? p.kv_heads : p.heads, other = KEYS ? p.heads : p.kv_heads;
-    bool ok = make_map(&m.a1, p, BF16, KEYS ? a.k : a.q, own, 128) && make_map(&m.a2, p, BF16, KEYS ? a.v : a.dout, own, 128) &&
+    const bool ok = make_map(&m.a1, p, BF16, KEYS ? a.k : a.q, own, 128) && make_map(&m.a2, p, BF16, KEYS ? a.v : a.dout, own, 128) &&
               make_map(&m.b1, p, BF16, KEYS ? a.q : a.k, other, GradTile<DP>::kColumns) &&
-              make_map(&m.b2, p, BF16, KEYS ? a.dout : a.v, other, GradTile<DP>::kColumns);
+              make_map(&m.b2, p, BF16, KEYS ? a.dout : a.v, other, GradTile<DP>::kColumns) &&
+              (BF16 || make_map(&m.b2_first, p, BF16, KEYS ? a.dout : a.v, other, 128, 8));
     const int64_t grid = p.blocks * own * ((p.t + 127) / 128);
     if (!ok || grid > 0x7fffffffLL) return cudaErrorInvalidValue;
     auto* kernel = k30_attention_grad<BF16, DP, MOD, KEYS>;

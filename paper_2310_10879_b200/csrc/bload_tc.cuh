@@ -2,6 +2,7 @@
 // tensor core products (tcgen05) with their memory (TMEM).
 #pragma once
 #include <cuda.h>
+#include <cuda_fp16.h>
 #include <stdint.h>
 
 namespace bload {
@@ -17,6 +18,10 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
 __device__ __forceinline__ void bar_init_done()
 {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+}
+__device__ __forceinline__ void bar_inval(uint32_t bar)  // its place may be used again
+{
+    asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 {
@@ -103,6 +108,12 @@ __device__ __forceinline__ void tmem_load(uint32_t (&r)[32], uint32_t at)
           "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(at));
 }
+__device__ __forceinline__ uint32_t tmem_load1(uint32_t at)  // one column
+{
+    uint32_t r;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(at));
+    return r;
+}
 __device__ __forceinline__ void tmem_load(uint32_t (&r)[16], uint32_t at)
 {
     asm volatile(
@@ -139,6 +150,7 @@ __device__ __forceinline__ void settle(uint32_t (&r)[32])
                  "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]),
                  "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
+__device__ __forceinline__ void settle(uint32_t& r) { asm volatile("" : "+r"(r)); }
 __device__ __forceinline__ void settle(uint32_t (&r)[16])
 {
     asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
@@ -235,6 +247,24 @@ __device__ __forceinline__ float inverse_fast(float x)
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+__device__ __forceinline__ float largest(float a, float b, float c)  // of the magnitudes
+{
+    float r;
+    asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// of the magnitudes of two pairs in fp16, each
+__device__ __forceinline__ uint32_t largest_halves(uint32_t a, uint32_t b)
+{
+    const __half2 m = __hmax2(__habs2(*reinterpret_cast<const __half2*>(&a)), __habs2(*reinterpret_cast<const __half2*>(&b)));
+    return *reinterpret_cast<const uint32_t*>(&m);
+}
+__device__ __forceinline__ float largest_of_halves(const uint4& x)  // the largest magnitude of eight in fp16
+{
+    const uint32_t m = largest_halves(largest_halves(x.x, x.y), largest_halves(x.z, x.w));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&m));
+    return fmaxf(f.x, f.y);
 }
 // lo in the lower half
 template <bool BF16>
