@@ -53,8 +53,9 @@ __host__ __device__ inline size_t work_view(int64_t parts, void* base, WorkView2
 }
 
 // f = sigmoid(g) and 1 - f, each with a small relative error of its own (1 - f must not cancel: it scales the input).  With e =
-// exp(-g): f = 1 / (1 + e), 1 - f = e f; g has been held at -87, so that e f does not become inf * 0, and what f is then
-// (some 2^-125.5) is taken off again.
+// exp(-g): f = 1 / (1 + e), 1 - f = e f; g has been held at -87, so that e f does not become inf * 0, and all but 7e-6 of what f is
+// then (1.6458e-38) is taken off again: f is above 0 whatever the approximations' last bits (a state that is infinite stays so), and
+// down to g = -75 the difference is below 7e-6 of f, below its rounding down to -70.
 __device__ __forceinline__ void gate_of(Two g, Two& f, Two& keep)
 {
     const float2 y = one(g * two(-1.4426950408889634f, -1.4426950408889634f));
@@ -66,14 +67,21 @@ __device__ __forceinline__ void gate_of(Two g, Two& f, Two& keep)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(d.y));
     f = two(r.x, r.y);
     keep = two(e.x, e.y) * f;
-    f = f + two(-1.6458115e-38f, -1.6458115e-38f);
+    f = f + two(-1.6458e-38f, -1.6458e-38f);
 }
 
 // A stretch of slots, seen as one: state -> A state + H.  Nothing passes through a stretch in which a sequence starts or that
-// holds padding, not even NaN: its A is -0 (gates are not negative, so no product of them is), and what arrives is dropped.
+// holds padding, not even NaN: its A is -0 (gates are above 0, so no product of them is), and what arrives is dropped.  A product of
+// small gates may be 0, though: an infinite state passes all the same, as it does slot by slot.  INFINITE: with that test; where it
+// costs, chains are followed without, and once more with it if their end is not finite.
 constexpr float kShut = -0.0f;
 __device__ __forceinline__ bool shut(float A) { return __float_as_int(A) < 0; }
-__device__ __forceinline__ float through(float A, float state, float H) { return shut(A) ? H : fmaf(A, state, H); }
+template <bool INFINITE>
+__device__ __forceinline__ float open_through(float A, float state, float H)
+{
+    return INFINITE && A == 0.0f && fabsf(state) == INFINITY ? state + H : fmaf(A, state, H);
+}
+__device__ __forceinline__ float through(float A, float state, float H) { return shut(A) ? H : open_through<true>(A, state, H); }
 // a stretch of two channels: (A, A', H, H')
 struct alignas(16) Stretch {
     float2 A, H;
@@ -82,6 +90,10 @@ __device__ __forceinline__ Two through(const Stretch& s, Two state)
 {
     const float2 x = one(state);
     return two(through(s.A.x, x.x, s.H.x), through(s.A.y, x.y, s.H.y));
+}
+__device__ __forceinline__ bool any_infinite(Two x)  // or NaN, in the warp
+{
+    return __any_sync(0xffffffffu, !(fabsf(one(x).x) < INFINITY) || !(fabsf(one(x).y) < INFINITY));
 }
 __device__ __forceinline__ Two open_through(const Stretch& s, Two state)  // neither channel's A is -0
 {
@@ -134,16 +146,22 @@ __device__ float2 look_back(const WorkView2& w, int64_t part, int64_t step, int 
         __nanosleep(40);
     }
     __threadfence();
-    float2 e = __ldcg(w.states + (part - far * step) * 32 + lane);
-    for (int64_t k = far - 1; k > 0; k -= 16) {  // sixteen loads at a time
-        float4 s[16];
+    const float2 from = __ldcg(w.states + (part - far * step) * 32 + lane);
+    auto follow = [&](auto infinite) {
+        constexpr bool kInfinite = decltype(infinite)::value;
+        float2 e = from;
+        for (int64_t k = far - 1; k > 0; k -= 16) {  // sixteen loads at a time
+            float4 s[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = k > j ? __ldcg(w.sums + (part - (k - j) * step) * 32 + lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int j = 0; j < 16; ++j) s[j] = k > j ? __ldcg(w.sums + (part - (k - j) * step) * 32 + lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (k > j) e = make_float2(fmaf(s[j].x, e.x, s[j].y), fmaf(s[j].z, e.y, s[j].w));
-    }
-    return e;
+            for (int j = 0; j < 16; ++j)
+                if (k > j) e = make_float2(open_through<kInfinite>(s[j].x, e.x, s[j].y), open_through<kInfinite>(s[j].z, e.y, s[j].w));
+        }
+        return e;
+    };
+    const float2 e = follow(std::false_type());
+    return any_infinite(two(e.x, e.y)) ? follow(std::true_type()) : e;
 }
 
 // `bytes` of 16 bytes are copied, the rest are zeros
@@ -394,11 +412,13 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
 #pragma unroll
         for (int k = 0; k < kWarps - 1; ++k)
             if (k < in_front) mine = open_through(sums[buffer][GRAD ? 1 : 0][GRAD ? kWarps - 1 - k : k][lane], mine);
-        if (__any_sync(0xffffffffu, !(fabsf(one(mine).x) < INFINITY) || !(fabsf(one(mine).y) < INFINITY))) {
+        if (any_infinite(mine)) {
             mine = entered;
             for (int k = 0; k < in_front; ++k) mine = through(sums[buffer][GRAD ? 1 : 0][GRAD ? kWarps - 1 - k : k][lane], mine);
         }
-        if (in_front == kWarps - 1) entering[buffer ^ 1][lane] = through(sums[buffer][GRAD ? 1 : 0][warp][lane], mine);
+        if (in_front == kWarps - 1) {
+            entering[buffer ^ 1][lane] = through(sums[buffer][GRAD ? 1 : 0][warp][lane], mine);
+        }
         if (!OUTPUT) {
 #pragma unroll
             for (int k = 0; k < kWarps; ++k) {
@@ -458,8 +478,9 @@ __device__ __forceinline__ void walk(const RecurParams& p, const RecurTensors<T>
                 }
             }
         };
-        if (GRAD)
+        if (GRAD) {
             for (int k = 0; k < warp; ++k) h_in = through(sums[buffer][0][k][lane], h_in);
+        }
         if (!(full && feed.inside))
             finish(std::true_type(), std::true_type());
         else if (cont == kAll)
