@@ -573,6 +573,8 @@ BLOAD_API int bload_attention_grad(const bload_attention_t* a, void* stream);
  *            in 32 bits instead of reading the rounded h; 16-byte aligned; NULL in the forward call: not kept
  *   d_work   scratch of bload_recurrence_work_bytes bytes, 256-byte aligned, for both calls (NULL when that is 0); calls that
  *            may overlap on the GPU need one each
+ * block_count * ceil(channels / 64) * ceil(t_block / 64) must be below 2^31 (ARG; bload_recurrence_work_bytes gives 0 for
+ * sizes that the calls refuse).
  * Errors: NULL, ARG (sizes, strides < 0, a broadcast output), ALIGN, WORKSPACE, UNSUPPORTED (dtype, t_block), CUDA.
  */
 #define BLOAD_RECURRENCE_RUN 64

@@ -148,13 +148,18 @@ AttnParams attention_params(const bload_attention_t* a, bool gradient)
     return p;
 }
 
+// at most 2^31 - 1 pieces of 64 slots by 64 channels (a grid holds that many)
+bool recurrence_fits(int64_t blocks, int32_t t, int64_t channels)
+{
+    if (channels < 1 || channels > 0x7fffffffLL) return false;
+    return blocks <= 0x7fffffffLL / (((channels + 63) / 64) * ((t + 63) / 64));
+}
 int check_recurrence(const bload_recurrence_t* a, bool gradient)
 {
     if (!a) return BLOAD_ERR_NULL;
     int rc = check_common(a->block_count, a->t_block, a->dtype, a->d_pos);
     if (rc) return rc;
-    if (a->channels < 1 || a->channels > 0x7fffffffLL || a->block_count * ((a->channels + 63) / 64) * ((a->t_block + 63) / 64) > 0x7fffffffLL)
-        return BLOAD_ERR_ARG;
+    if (!recurrence_fits(a->block_count, a->t_block, a->channels)) return BLOAD_ERR_ARG;
     if (a->block_count == 0) return BLOAD_OK;
     auto tensor = [&](const bload_channels_t& x, bool zero_ok) {
         if (!x.data) return BLOAD_ERR_NULL;
@@ -234,7 +239,7 @@ int bload_attention_grad(const bload_attention_t* a, void* stream)
 
 size_t bload_recurrence_work_bytes(int64_t block_count, int32_t t_block, int64_t channels)
 {
-    if (block_count < 1 || t_block < 1 || t_block > BLOAD_MAX_T_BLOCK || channels < 1) return 0;
+    if (block_count < 1 || t_block < 1 || t_block > BLOAD_MAX_T_BLOCK || !recurrence_fits(block_count, t_block, channels)) return 0;
     return recurrence_work_bytes(block_count, t_block, channels);
 }
 

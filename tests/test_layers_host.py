@@ -52,3 +52,29 @@ assert rc == E.ERR_CUDA, rc  # every argument was taken, and there is no device
                                   "bload_rotary", "bload_rotary_grad"])
 def test_a_call_reads_nothing_behind_its_argument_block(name):
     assert alone("NAME = %r\n%s" % (name, BLOCK_AT_THE_END_OF_A_PAGE)) == 0
+
+
+SIZES_WITHOUT_END = """
+from paper_2310_10879_b200 import _lib as E
+import ctypes as C
+L, P = E.load(), 1 << 20
+for blocks in (1, 1 << 20, (1 << 31) - 1, 1 << 31, 1 << 40, 1 << 58, (1 << 62) + 1, (1 << 63) - 1):
+    for t in (1, 64, 65, 5000, E.MAX_T_BLOCK):
+        for channels in (1, 64, 4096, (1 << 31) - 1, 1 << 31, 1 << 58, (1 << 63) - 1):
+            parts = blocks * -(-channels // 64) * -(-t // 64)  # Python's integers have no end
+            fits = blocks < 1 << 31 and channels < 1 << 31 and parts < 1 << 31
+            need = L.bload_recurrence_work_bytes(blocks, t, channels)
+            assert need < 1 << 42 and (fits or need == 0), (blocks, t, channels, need)
+            a = E.RecurrenceArgs(blocks, channels, t, E.BF16, P)
+            for n in ("gate", "x", "h", "dh", "dgate", "dx"):
+                setattr(a, n, E.ChannelsTensor(P, 1 << 38, 1 << 38))
+            a.d_carry, a.d_work, a.work_bytes = P, P, 1 << 60
+            for call in (L.bload_recurrence, L.bload_recurrence_grad):
+                rc = call(C.byref(a), None)
+                assert rc == (E.ERR_CUDA if fits else E.ERR_ARG), (blocks, t, channels, rc)
+"""
+
+
+def test_sizes_whose_product_has_no_room_are_refused():
+    """(In a process of its own: a wrong product once was a division by zero.)"""
+    assert alone(SIZES_WITHOUT_END) == 0
