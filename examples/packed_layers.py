@@ -14,6 +14,7 @@ import os
 import sys
 
 import torch
+from torch.autograd.function import once_differentiable
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2310_10879_b200 as B  # noqa: E402
@@ -28,6 +29,7 @@ class Rotary(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable  # (the gradient calls have no gradients of their own)
     def backward(ctx, dy):
         dx = torch.empty_like(dy)
         B.bload_rotary_grad(ctx.saved_tensors[0], dy, dx, ctx.saved_tensors[1])
@@ -45,6 +47,7 @@ class Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, pos, out, lse = ctx.saved_tensors
         dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
@@ -62,6 +65,7 @@ class Recurrence(torch.autograd.Function):
         return h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dh):
         gate, x, pos, carry = ctx.saved_tensors
         dgate, dx = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for _ in range(2))
