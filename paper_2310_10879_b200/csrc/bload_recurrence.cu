@@ -578,14 +578,14 @@ __global__ void __launch_bounds__(256, 2)
 
 int64_t groups_of(int64_t blocks, int64_t channels) { return blocks * ((channels + kCh - 1) / kCh); }
 
-// Segments per walk: as many as give each of the 148 SMs two CTAs, of at least 4 runs each.  8 x 2048 bf16 channels (256 walks) of
+// Segments per walk: as many as give each of the 148 SMs two CTAs, of at least 4 runs each; from 149 walks on, one.  8 x 2048 bf16 channels (256 walks) of
 // 10,000 slots take 212 us in one segment each and 253 in two on heavy-tailed lengths (320 on one sequence, whose first segments
 // are read twice); 144 walks of 20,000 slots 305 us in one segment, 222 in two (434 on one sequence).
 int segments_of(int64_t blocks, int32_t t, int64_t channels)
 {
     const int64_t runs = (t + kRun - 1) / kRun, groups = groups_of(blocks, channels);
-    const int64_t wanted = groups >= 200 ? 1 : (2 * 148) / groups, most = runs / 4;
-    return (int)(wanted < most ? (wanted < 1 ? 1 : wanted) : (most < 1 ? 1 : most));
+    const int64_t wanted = (2 * 148) / groups, most = runs / 4, segments = wanted < most ? wanted : most;
+    return (int)(segments < 1 ? 1 : segments);
 }
 
 template <typename T, bool GRAD, bool STAGED>
