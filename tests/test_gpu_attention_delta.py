@@ -96,3 +96,17 @@ def test_a_row_does_not_notice_the_length_of_its_neighbours():
     torch.cuda.synchronize()
     for n in ("out", "dq", "dk", "dv"):
         assert torch.equal(got[n][0, 1600:], got[n][1, 1600:]), n
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_rows_with_a_distance_bias(causal):
+    """They see thousands of keys, and a few have the weight."""
+    blocks, t, d = [[2500], [1300, 1200]], 2500, 112
+    q, dout = L.normal((2, t, 2, d), BF, 1), L.normal((2, t, 2, d), BF, 4)
+    k, v = L.normal((2, t, 1, d), BF, 2, mean=1.0), L.normal((2, t, 1, d), BF, 3, mean=8.0, std=0.25)
+    how = dict(causal=causal, window=0, softcap=0.0, slopes=torch.tensor([0.5, 0.1], device=DEV), scale=d ** -0.5)
+    got = call(L.positions(t, blocks), q, k, v, dout, **how)
+    torch.cuda.synchronize()
+    dq, t_dq, _, _, few = expected(blocks, q, k, v, dout, **how)
+    assert not bool(few.all())
+    L.close(got["dq"], dq, t_dq, "dq")
