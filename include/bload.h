@@ -499,7 +499,7 @@ typedef struct {
 
 /*
  * bload_rotary -- rotary positions that restart with every sequence.  For each head of each frame at position p, with
- * n = rot_dim / 2 and a_i = float(p) * d_inv_freq[i] (one rounding to 32 bits), i < n:
+ * n = rot_dim / 2 and a_i = float(p) * d_inv_freq[i] (one rounding to 32 bits: angles of 10,000 are whole multiples of 2^-10), i < n:
  *     (u, w) = (x[i], x[n + i])          interleaved == 0
  *            = (x[2 i], x[2 i + 1])      interleaved == 1
  *     (u, w) -> factor * (u cos a_i - w sin a_i,  w cos a_i + u sin a_i)
@@ -598,8 +598,8 @@ BLOAD_API int bload_recurrence_grad(const bload_recurrence_t* a, void* stream);
 
 /*
  * bload_device_timeouts -- number of bounded device-side waits (of the attention and recurrence kernels: on their own copies,
- * matrix products and arithmetic, and on earlier segments of the same call) that gave up since the library was loaded.  Anything but
- * 0 means incomplete outputs.  Synchronises the device; -1 if that fails.
+ * matrix products and arithmetic, and on earlier segments of the same call) that gave up on the current device since the library was
+ * loaded.  Anything but 0 means incomplete outputs.  Synchronises that device; -1 if that fails.
  */
 BLOAD_API int64_t bload_device_timeouts(void);
 

@@ -541,6 +541,7 @@ def bload_rank_range(n_blocks: int, world_size: int, rank: int, batch_blocks: in
 
 
 # ---- layers on packed batches: everything below takes the per-slot positions that bload_pack writes ----------------
+# The calls write into the tensors they are given and are not recorded by autograd; each has a gradient call of its own.
 
 F32, F16, BF16 = 0, 1, 2
 RECURRENCE_RUN = 64
@@ -740,5 +741,5 @@ def bload_recurrence_grad(pos, gate, x, carry, dh, dgate, dx, work=None, stream=
 
 
 def bload_device_timeouts() -> int:
-    """Bounded device-side waits of the layers' kernels that gave up (0 unless the hardware failed)."""
+    """Bounded device-side waits of the layers' kernels that gave up on the current device (0 unless the hardware failed)."""
     return int(load().bload_device_timeouts())

@@ -342,7 +342,8 @@ struct ForwardTile {
 // the same 32 rows, a row per lane, each half of the columns (with one warp per row the tensor cores were busy 31 % of the time:
 // too few warps to hide the latency of their own steps).  The two halves of a row agree on its maximum through shared memory,
 // each keeps its own sum.  Heads of up to 64: tiles of 64 keys, four warps, four CTAs per SM (short sequences leave a CTA with
-// two or three tiles between its first copies and its last store, so it pays to have more of them).
+// two or three tiles between its first copies and its last store, so it pays to have more of them: 16 x 1000 frames of features 64 us,
+// in the instance for 128, half zeros, 89; one sequence of 16,384 takes 372 us here and 316 there).
 // Scores come from tensor memory, P goes back over them.  Two more warps copy tiles in and issue the products.  The CTAs of an SM
 // share its tensor memory evenly, so one's products run under the others' exponentials.
 template <bool BF16, int DP, bool MOD>
@@ -662,7 +663,8 @@ struct GradMaps {
 };
 
 // Tiles of 128 columns and all of the tensor memory; for heads of at most 64 elements, tiles of 64 and half of it: then two CTAs
-// share an SM, and one's first copies and last stores run under the other's products.
+// share an SM, and one's first copies and last stores run under the other's products (16 x 1000 frames of features in fp16 236 us,
+// in the instance for 128, half zeros, 333; one sequence of 16,384 in bf16 1,045 here and 806 there).
 template <int DP>
 struct GradTile {
     static constexpr int kColumns = DP;                             // of a tile: rows of B1 and B2
