@@ -701,7 +701,7 @@ constexpr int kExact = 1024;
 // 2^15 then.  Terms are off by 2^-34 of that product where they do not have fp16's 11 bits; without a scale a row of 4,000 keys and
 // dout of 1e-2 has dS of 2e-6, which is 32 steps of fp16, and one above 65,504 was infinite.  Where a row's dS do not fit all the
 // same, its acc1 comes out infinite or NaN, and the CTA walks AGAIN, twice: to find such rows' largest dS, and with a lift
-// from that (rows that fit keep theirs, and their bits).  The gradient of 4 x 4096 tokens takes 519 us (without lifts 505), of 16 x 1000
+// from that (rows that fit keep theirs, and their bits): so do keys whose own slot has no dout at all.  The gradient of 4 x 4096 tokens takes 519 us (without lifts 505), of 16 x 1000
 // frames of features 236 (214); to agree on a row's lift among its warps in every tile took 574 and 257.
 constexpr float kLiftP = 16384.0f;
 constexpr int kOneWalk = 0, kMeasure = 1, kLastWalk = 2;
