@@ -1140,27 +1140,27 @@ __device__ __forceinline__ bool attention_grad(const AttnParams& p, const AttnTe
             }
             if (!KEYS) eps_shared[part][own_row] = (one(eps2).x + one(eps2).y) * (1.0f / lift);
             if (!BF16) tops[BF16 ? 0 : part][BF16 ? 0 : own_row] = top;
-        }
-        __syncthreads();
-        if (BF16 || dead || pass == kLastWalk || n == 0) break;
-        if (warp < kWarps) {
-            if (!tc::bar_wait(acc1_done, (n - 1) & 1)) stuck = 1;  // (the end counts it)
-            tc::fence_after();
-            if (pass == kOneWalk && part == 0) {
-                uint32_t x = tc::tmem_load1(acc1_at + ((uint32_t)quarter << 21));
+            if (!BF16 && !AGAIN && part == 0 && n > 0) {  // one column tells: infinity times anything is not finite
+                if (!tc::bar_wait(acc1_done, (n - 1) & 1)) stuck = 1;  // (the end counts it)
+                tc::fence_after();
+                uint32_t x = tc::tmem_load1(acc1_at + lanes);
                 tc::tmem_loaded();
                 tc::settle(x);
                 if (span.lo <= span.hi && (x & 0x7f800000u) == 0x7f800000u && (KEYS || isfinite(delta))) again = 1;
-            } else if (pass == kMeasure) {
-                float most = 0.0f;
-                for (int k = 0; k < kColumns / 32; ++k) most = fmaxf(most, tops[BF16 ? 0 : k][BF16 ? 0 : own_row]);
-                if (most > 65000.0f) lift *= power_of_two(14 - exponent_of(most));
+                tc::fence_before();
             }
-            tc::fence_before();
         }
         __syncthreads();
-        if (stuck || !again) break;
+        if (BF16 || dead || (!AGAIN && stuck) || !again || pass == kLastWalk) break;
         if (!AGAIN) return true;
+        if (warp < kWarps) {
+            if (!tc::bar_wait(acc1_done, (n - 1) & 1)) stuck = 1;
+            float most = 0.0f;
+            for (int k = 0; k < kColumns / 32; ++k) most = fmaxf(most, tops[BF16 ? 0 : k][BF16 ? 0 : own_row]);
+            if (most > 65000.0f) lift *= power_of_two(14 - exponent_of(most));
+        }
+        __syncthreads();
+        if (stuck) break;
         if (warp == kWarps && lane == 0) begin();
         __syncthreads();
         tc::fence_after();
