@@ -663,7 +663,7 @@ struct GradMaps {
 };
 
 // Tiles of 128 columns and all of the tensor memory; for heads of at most 64 elements, tiles of 64 and half of it: then two CTAs
-// share an SM, and one's first copies and last stores run under the other's products (16 x 1000 frames of features in fp16 236 us,
+// share an SM, and one's first copies and last stores run under the other's products (16 x 1000 frames of features in fp16 232 us,
 // in the instance for 128, half zeros, 333; one sequence of 16,384 in bf16 1,045 here and 806 there).
 template <int DP>
 struct GradTile {
@@ -702,7 +702,7 @@ constexpr int kExact = 1024;
 // dout of 1e-2 has dS of 2e-6, which is 32 steps of fp16, and one above 65,504 was infinite.  Where a row's dS do not fit all the
 // same, its acc1 comes out infinite or NaN, and the CTA walks AGAIN, twice: to find such rows' largest dS, and with a lift
 // from that (rows that fit keep theirs, and their bits): so do keys whose own slot has no dout at all.  The gradient of 4 x 4096 tokens takes 519 us (without lifts 505), of 16 x 1000
-// frames of features 236 (214); to agree on a row's lift among its warps in every tile took 574 and 257.
+// frames of features 232 (214); to agree on a row's lift among its warps in every tile took 574 and 257.
 constexpr float kLiftP = 16384.0f;
 constexpr int kOneWalk = 0, kMeasure = 1, kLastWalk = 2;
 __device__ __forceinline__ float power_of_two(int exponent) { return __int_as_float((exponent + 127) << 23); }
