@@ -519,6 +519,24 @@ BLOAD_API int bload_rotary_grad(const int32_t* d_pos, int64_t block_count, int32
                                 void* stream);
 
 /*
+ * bload_rotary_axes -- rotary positions with several axes, as for video (time, height, width): every pair i of a head turns by
+ * the coordinate of one axis, a_i = d_coords[d_axis[i]][q, s] * d_inv_freq[i].  The coordinate is taken as a 32-bit float (whole
+ * up to 2^24) and the product is not rounded: coordinates far along an axis turn by the exact angle.
+ *   d_coords  int32 [axes, block_count, t_block], any values; those of padding (d_pos < 0) are not used
+ *   d_axis    int32 [rot_dim / 2], each in [0, axes) (another value counts as coordinate 0); NULL when rot_dim is 0
+ * 1 <= axes <= BLOAD_MAX_AXES.  Everything else, and bload_rotary_axes_grad, as in bload_rotary.
+ */
+#define BLOAD_MAX_AXES 4
+BLOAD_API int bload_rotary_axes(const int32_t* d_pos, const int32_t* d_coords, int32_t axes, const int32_t* d_axis,
+                                int64_t block_count, int32_t t_block, int32_t heads, int32_t head_dim, int32_t dtype,
+                                const bload_heads_t* x, const bload_heads_t* y, const float* d_inv_freq, int32_t rot_dim,
+                                int32_t interleaved, float factor, void* stream);
+BLOAD_API int bload_rotary_axes_grad(const int32_t* d_pos, const int32_t* d_coords, int32_t axes, const int32_t* d_axis,
+                                     int64_t block_count, int32_t t_block, int32_t heads, int32_t head_dim, int32_t dtype,
+                                     const bload_heads_t* dy, const bload_heads_t* dx, const float* d_inv_freq,
+                                     int32_t rot_dim, int32_t interleaved, float factor, void* stream);
+
+/*
  * bload_attention / bload_attention_grad -- attention inside the sequences of a block.  For head h and slot i of a
  * sequence, over the slots j of the same sequence (j <= i if causal; |i - j| < window if window > 0):
  *     s_ij = scale * q_i . k_j;   if softcap > 0: s_ij = softcap * tanh(s_ij / softcap);
@@ -595,6 +613,142 @@ typedef struct {
 BLOAD_API size_t bload_recurrence_work_bytes(int64_t block_count, int32_t t_block, int64_t channels);
 BLOAD_API int bload_recurrence(const bload_recurrence_t* a, void* stream);
 BLOAD_API int bload_recurrence_grad(const bload_recurrence_t* a, void* stream);
+
+/*
+ * bload_norm / bload_norm_grad -- layer norm over the channels of every frame:
+ *     m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), n = (x - m) r;      y = n * weight + bias
+ *     with g = dy * weight:  dx = r (g - mean(g) - n mean(g n)),   dweight = sum over frames of dy n,  dbias = sum of dy
+ * Padding slots give y = dx = 0 and are not part of the sums.  x, y, dy, dx are [block_count, t_block, channels] with contiguous
+ * channels, strides in elements; data aligned to the element (rows on 16-byte boundaries are faster).
+ *
+ *   d_weight, d_bias  float [channels], NULL: 1, 0
+ *   d_stats           float [block_count, t_block, 2]: m and r (0, 0 on padding), written by the forward call (NULL: not kept) and
+ *                     read by the gradient; 8-byte aligned
+ *   d_dweight, d_dbias  float [channels], written by bload_norm_grad; NULL: not wanted
+ *   d_work            scratch of bload_norm_work_bytes bytes for the gradient, 256-byte aligned (NULL when neither sum is wanted);
+ *                     calls that may overlap on the GPU need one each
+ * 1 <= channels <= BLOAD_NORM_MAX_CHANNELS, eps >= 0 and finite.  bload_norm_work_bytes gives 0 for sizes that the calls refuse.
+ * Errors: NULL, ARG (sizes, strides < 0, a broadcast output, eps), ALIGN, WORKSPACE, UNSUPPORTED (dtype, t_block, channels), CUDA.
+ */
+#define BLOAD_NORM_MAX_CHANNELS 16384
+typedef struct {
+    int64_t block_count, channels;
+    int32_t t_block, dtype;
+    float eps;
+    const int32_t* d_pos;
+    const float *d_weight, *d_bias;
+    float* d_stats;
+    bload_channels_t x, y;   /* y: forward only */
+    bload_channels_t dy, dx; /* from here on: gradient only */
+    float *d_dweight, *d_dbias;
+    void* d_work;
+    size_t work_bytes;
+} bload_norm_t;
+BLOAD_API size_t bload_norm_work_bytes(int64_t block_count, int32_t t_block, int64_t channels, int32_t dtype);
+BLOAD_API int bload_norm(const bload_norm_t* a, void* stream);
+BLOAD_API int bload_norm_grad(const bload_norm_t* a, void* stream);
+
+/*
+ * bload_conv / bload_conv_grad -- a short causal convolution per channel that stays inside sequences:
+ *     u_s = bias + sum over j < taps with j <= d_pos[s] of weight[:, taps - 1 - j] * x_{s - j};      y_s = u_s, or u_s sigmoid(u_s)
+ * if silu.  The gradient writes dx, dweight and dbias (sums over all frames).  Padding slots give 0.  x, y, dy, dx as in bload_norm.
+ *
+ *   d_weight   float [channels, taps], 1 <= taps <= BLOAD_CONV_MAX_TAPS
+ *   d_bias     float [channels] or NULL
+ *   d_seq_id, n_seq, d_tails   forward: with all of them, the last taps - 1 inputs of every sequence k in [0, n_seq) of the batch
+ *              are written to d_tails[k] ([n_seq, taps - 1, channels] of the element type, oldest first, 0 in front of the
+ *              sequence): the state from which bload_conv_step goes on.  d_seq_id: int32 [block_count, t_block] as bload_pack
+ *              writes it.  Other sequences' rows are left as they were.  d_tails NULL: not wanted
+ *   d_dweight, d_dbias         float, written by the gradient; NULL: not wanted
+ *   d_work     scratch of bload_conv_work_bytes bytes for the gradient, 256-byte aligned (NULL when neither sum is wanted); calls
+ *              that may overlap on the GPU need one each
+ * bload_conv_step -- the same for one new frame of each of `rows` sequences.  d_pos: int32 [rows], the frame's position in its
+ * sequence (0 starts one: what the state holds is not used; negative: no frame, y = 0 and the state stays as it is).
+ *   state, next   [rows, taps - 1, channels] contiguous, element type: the last inputs, oldest first, before and after the
+ *                 call; next may be state itself.  x, y: [rows, channels], strides in elements (block_stride; slot_stride unused)
+ * channels below 2^31; block_count * ceil(t_block / 32) * (channels / 256 + 1), and rows * (channels / 256 + 1), below 2^31 (ARG;
+ * bload_conv_work_bytes gives 0 for sizes that the calls refuse).
+ * Errors: NULL, ARG, ALIGN, WORKSPACE, UNSUPPORTED (dtype, t_block, taps), CUDA.
+ */
+#define BLOAD_CONV_MAX_TAPS 8
+typedef struct {
+    int64_t block_count, channels;
+    int32_t t_block, dtype, taps, silu;
+    const int32_t* d_pos;
+    const float *d_weight, *d_bias;
+    bload_channels_t x, y; /* y: forward only */
+    const int32_t* d_seq_id;
+    int64_t n_seq;
+    void* d_tails;
+    bload_channels_t dy, dx; /* from here on: gradient only */
+    float *d_dweight, *d_dbias;
+    void* d_work;
+    size_t work_bytes;
+} bload_conv_t;
+BLOAD_API size_t bload_conv_work_bytes(int64_t block_count, int32_t t_block, int64_t channels, int32_t taps, int32_t dtype);
+BLOAD_API int bload_conv(const bload_conv_t* a, void* stream);
+BLOAD_API int bload_conv_grad(const bload_conv_t* a, void* stream);
+BLOAD_API int bload_conv_step(int64_t rows, int64_t channels, int32_t dtype, int32_t taps, int32_t silu, const int32_t* d_pos,
+                              const void* state, void* next, const bload_channels_t* x, const bload_channels_t* y,
+                              const float* d_weight, const float* d_bias, void* stream);
+
+/*
+ * bload_scan / bload_scan_grad -- a selective state-space scan along the slots of each block, restarted at every sequence start.
+ * Per channel, with `states` states n:
+ *     delta_s = softplus(dt_s + dt_bias)   (softplus == 0: dt_s + dt_bias)
+ *     h_s[n]  = exp(delta_s a[n]) h_{s-1}[n] + delta_s b_s[n] x_s,        h_{s-1} = 0 where a sequence starts at s
+ *     v_s     = sum_n c_s[n] h_s[n] + d x_s;       y_s = v_s, or v_s z_s sigmoid(z_s) if z is given
+ * The gradient takes dy and writes dx, ddt, db, dc, dz and, summed over all frames, da, dd, ddt_bias.  Padding slots give 0.
+ *
+ *   x, dt, z, y, dy, dx, ddt, dz   [block_count, t_block, channels]; z.data NULL: no gate
+ *   b, c, db, dc                   [block_count, t_block, states]        (all with a contiguous last dimension)
+ *   d_a, d_da     float [channels, states]
+ *   d_d, d_dt_bias, d_dd, d_ddt_bias   float [channels]; d_d, d_dt_bias NULL: 0; d_dd, d_ddt_bias NULL: not wanted
+ *   d_carry       float [block_count, ceil(t_block / BLOAD_SCAN_RUN), channels, states], 16-byte aligned: the state that enters
+ *                 each run of BLOAD_SCAN_RUN slots, written by the forward call (NULL: not kept) and read by the gradient
+ *   d_seq_id, n_seq, d_last   forward: with all of them, the state behind the last frame of every sequence k in [0, n_seq) of the
+ *                 batch is written to d_last[k] (float [n_seq, channels, states]), from which bload_scan_step goes on.  Other
+ *                 rows are left as they were.  d_last NULL: not wanted
+ *   d_work        scratch of bload_scan_work_bytes(.., gradient) bytes, 256-byte aligned (NULL when that is 0); calls that may overlap
+ *                 on the GPU need one each
+ * bload_scan_step -- the same for one new frame of each of `rows` sequences; d_pos as in bload_conv_step.
+ *   state, next   float [rows, channels, states] contiguous: h before and after the call; next may be state itself
+ *   x, dt, z, y   [rows, channels], b, c [rows, states], by block_stride (slot_stride unused)
+ * 1 <= states <= BLOAD_SCAN_MAX_STATES; channels and block_count * (channels / 16 + 1) (rows * (channels / 8 + 1)) below 2^31,
+ * block_count * t_block at most 2^31, block_count * channels * (states + 2) at most 2^35 (ARG; bload_scan_work_bytes gives 0 for
+ * sizes that the calls refuse, too).
+ * Errors: NULL, ARG (sizes, strides < 0, a broadcast output), ALIGN, WORKSPACE, UNSUPPORTED (dtype, t_block, states), CUDA.
+ */
+#define BLOAD_SCAN_RUN 16
+#define BLOAD_SCAN_MAX_STATES 64
+typedef struct {
+    int64_t block_count, channels;
+    int32_t t_block, dtype, states, softplus;
+    const int32_t* d_pos;
+    const float *d_a, *d_d, *d_dt_bias;
+    bload_channels_t x, dt, b, c, z, y; /* y: forward only */
+    float* d_carry;
+    void* d_work;
+    size_t work_bytes;
+    const int32_t* d_seq_id; /* forward only */
+    int64_t n_seq;
+    float* d_last;
+    bload_channels_t dy, dx, ddt, db, dc, dz; /* from here on: gradient only */
+    float *d_da, *d_dd, *d_ddt_bias;
+} bload_scan_t;
+BLOAD_API size_t bload_scan_work_bytes(int64_t block_count, int32_t t_block, int64_t channels, int32_t states, int32_t gradient);
+BLOAD_API int bload_scan(const bload_scan_t* a, void* stream);
+BLOAD_API int bload_scan_grad(const bload_scan_t* a, void* stream);
+typedef struct {
+    int64_t rows, channels;
+    int32_t dtype, states, softplus;
+    const int32_t* d_pos;
+    const float *d_a, *d_d, *d_dt_bias;
+    const float* state;
+    float* next;
+    bload_channels_t x, dt, b, c, z, y;
+} bload_scan_step_t;
+BLOAD_API int bload_scan_step(const bload_scan_step_t* a, void* stream);
 
 /*
  * bload_device_timeouts -- number of bounded device-side waits (of the attention and recurrence kernels: on their own copies,

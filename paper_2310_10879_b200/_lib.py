@@ -23,6 +23,9 @@ EXPORTS = ("bload_plan_sizes", "bload_plan", "bload_plan_async", "bload_plan_fin
            "bload_unpack_var2d", "bload_carry_prev", "bload_reset_state", "bload_valid_sum",
            "bload_rotary", "bload_rotary_grad", "bload_attention", "bload_attention_grad", "bload_recurrence_work_bytes",
            "bload_recurrence", "bload_recurrence_grad", "bload_device_timeouts",
+           "bload_rotary_axes", "bload_rotary_axes_grad", "bload_norm_work_bytes", "bload_norm", "bload_norm_grad",
+           "bload_conv_work_bytes", "bload_conv", "bload_conv_grad", "bload_conv_step",
+           "bload_scan_work_bytes", "bload_scan", "bload_scan_grad", "bload_scan_step",
            "bload_plan_static", "bload_chunk_work_bytes", "bload_chunk_count", "bload_plan_chunks", "bload_set_plan_timing", "bload_plan_stage_times", "bload_kernel_launches", "bload_last_copy_kernel", "bload_debug_status", "bload_bulk_copy_timeouts",
            "bload_strerror", "bload_version")
 
@@ -129,6 +132,14 @@ def load() -> C.CDLL:
     L.bload_recurrence_work_bytes.argtypes = [i64, i32, i64]
     L.bload_recurrence.argtypes = [vp, vp]
     L.bload_recurrence_grad.argtypes = L.bload_recurrence.argtypes
+    L.bload_rotary_axes.argtypes = [vp, vp, i32, vp, i64, i32, i32, i32, i32, vp, vp, vp, i32, i32, C.c_float, vp]
+    L.bload_rotary_axes_grad.argtypes = L.bload_rotary_axes.argtypes
+    L.bload_norm_work_bytes.argtypes = [i64, i32, i64, i32]
+    L.bload_conv_work_bytes.argtypes = [i64, i32, i64, i32, i32]
+    L.bload_scan_work_bytes.argtypes = [i64, i32, i64, i32, i32]
+    for name in ("bload_norm", "bload_norm_grad", "bload_conv", "bload_conv_grad", "bload_scan", "bload_scan_grad", "bload_scan_step"):
+        getattr(L, name).argtypes = [vp, vp]
+    L.bload_conv_step.argtypes = [i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     L.bload_set_plan_timing.argtypes = [C.c_int]
     L.bload_plan_stage_times.argtypes = [C.POINTER(C.c_float * 4)]
     L.bload_strerror.argtypes = [C.c_int]
@@ -138,7 +149,7 @@ def load() -> C.CDLL:
     L.bload_version.argtypes = []
     L.bload_kernel_launches.argtypes = []
     for name in EXPORTS:
-        if name not in ("bload_strerror", "bload_kernel_launches", "bload_last_copy_kernel", "bload_debug_status", "bload_bulk_copy_timeouts", "bload_chunk_work_bytes", "bload_recurrence_work_bytes", "bload_device_timeouts"):
+        if name not in ("bload_strerror", "bload_kernel_launches", "bload_last_copy_kernel", "bload_debug_status", "bload_bulk_copy_timeouts", "bload_device_timeouts") and not name.endswith("_work_bytes"):
             getattr(L, name).restype = C.c_int
     L.bload_kernel_launches.restype = C.c_int64
     L.bload_device_timeouts.argtypes = []
@@ -146,7 +157,8 @@ def load() -> C.CDLL:
     L.bload_bulk_copy_timeouts.argtypes = []
     L.bload_bulk_copy_timeouts.restype = C.c_int64
     L.bload_chunk_work_bytes.restype = C.c_size_t
-    L.bload_recurrence_work_bytes.restype = C.c_size_t
+    for name in ("recurrence", "norm", "conv", "scan"):
+        getattr(L, "bload_%s_work_bytes" % name).restype = C.c_size_t
     L.bload_last_copy_kernel.restype = C.c_char_p
     _lib = L
     return L
@@ -571,12 +583,49 @@ class RecurrenceArgs(C.Structure):
                 ("dgate", ChannelsTensor), ("dx", ChannelsTensor)]
 
 
+class NormArgs(C.Structure):
+    _fields_ = [("block_count", C.c_int64), ("channels", C.c_int64), ("t_block", C.c_int32), ("dtype", C.c_int32),
+                ("eps", C.c_float), ("d_pos", C.c_void_p), ("d_weight", C.c_void_p), ("d_bias", C.c_void_p),
+                ("d_stats", C.c_void_p), ("x", ChannelsTensor), ("y", ChannelsTensor), ("dy", ChannelsTensor),
+                ("dx", ChannelsTensor), ("d_dweight", C.c_void_p), ("d_dbias", C.c_void_p), ("d_work", C.c_void_p),
+                ("work_bytes", C.c_size_t)]
+
+
+class ConvArgs(C.Structure):
+    _fields_ = [("block_count", C.c_int64), ("channels", C.c_int64), ("t_block", C.c_int32), ("dtype", C.c_int32),
+                ("taps", C.c_int32), ("silu", C.c_int32), ("d_pos", C.c_void_p), ("d_weight", C.c_void_p),
+                ("d_bias", C.c_void_p), ("x", ChannelsTensor), ("y", ChannelsTensor), ("d_seq_id", C.c_void_p),
+                ("n_seq", C.c_int64), ("d_tails", C.c_void_p), ("dy", ChannelsTensor), ("dx", ChannelsTensor),
+                ("d_dweight", C.c_void_p), ("d_dbias", C.c_void_p), ("d_work", C.c_void_p), ("work_bytes", C.c_size_t)]
+
+
+class ScanArgs(C.Structure):
+    _fields_ = [("block_count", C.c_int64), ("channels", C.c_int64), ("t_block", C.c_int32), ("dtype", C.c_int32),
+                ("states", C.c_int32), ("softplus", C.c_int32), ("d_pos", C.c_void_p), ("d_a", C.c_void_p), ("d_d", C.c_void_p),
+                ("d_dt_bias", C.c_void_p)] + [(n, ChannelsTensor) for n in ("x", "dt", "b", "c", "z", "y")] + \
+               [("d_carry", C.c_void_p), ("d_work", C.c_void_p), ("work_bytes", C.c_size_t), ("d_seq_id", C.c_void_p),
+                ("n_seq", C.c_int64), ("d_last", C.c_void_p)] + \
+               [(n, ChannelsTensor) for n in ("dy", "dx", "ddt", "db", "dc", "dz")] + \
+               [("d_da", C.c_void_p), ("d_dd", C.c_void_p), ("d_ddt_bias", C.c_void_p)]
+
+
+class ScanStepArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("channels", C.c_int64), ("dtype", C.c_int32), ("states", C.c_int32), ("softplus", C.c_int32),
+                ("d_pos", C.c_void_p), ("d_a", C.c_void_p), ("d_d", C.c_void_p), ("d_dt_bias", C.c_void_p),
+                ("state", C.c_void_p), ("next", C.c_void_p)] + [(n, ChannelsTensor) for n in ("x", "dt", "b", "c", "z", "y")]
+
+
 # The argument blocks of a call, packed in one step: these calls are made per layer and step, and filling a ctypes structure
 # field by field takes longer than the kernels of a small batch.  (The layouts are those of the structures above.)
 _HEADS = struct.Struct("@4q")
 _ATTENTION = struct.Struct("@q7i2fi2q16qq")
 _ATTENTION_GRAD = struct.Struct("@q7i2fi2q16qq16qq")
 _RECURRENCE = struct.Struct("@2q2iq9q2qQ9q")
+_CHANNELS = struct.Struct("@3q")
+_NORM = struct.Struct("@2q2if4q6q6q3qQ")
+_CONV = struct.Struct("@2q4i3q6q3q6q3qQ")
+_SCAN = struct.Struct("@2q4i4q18q2qQ3q18q3q")
+_SCAN_STEP = struct.Struct("@2q3i6q18q")
 
 
 def _torch():
@@ -736,6 +785,266 @@ def bload_recurrence_grad(pos, gate, x, carry, dh, dgate, dx, work=None, stream=
     rc = load().bload_recurrence_grad(_RECURRENCE.pack(
         *head, 0, 0, 0, *kept, *_strided(where, "dh", dh, x.shape, x), *_strided(where, "dgate", dgate, x.shape, x),
         *_strided(where, "dx", dx, x.shape, x)), stream)
+    if rc:
+        raise BloadError(rc, where)
+
+
+def _axes(fn, where, pos, coords, axis, x, y, inv_freq, interleaved, factor, stream) -> None:
+    (b, t), code, stream = _begin(where, pos, x, 4, stream)
+    h, d = x.shape[2:]
+    shape, n = (b, t, h, d), inv_freq.numel()
+    for name, given, want in (("coords", coords, coords.dim() == 3 and coords.shape[1:] == pos.shape), ("axis", axis, axis.numel() == n)):
+        if given.dtype is not pos.dtype or given.get_device() != pos.get_device() or not given.is_contiguous():
+            raise TypeError("%s: %s must be a contiguous int32 tensor on %s" % (where, name, pos.device))
+        if not want:
+            raise ValueError("%s: coords is [axes, blocks, t_block], axis has an axis for each of inv_freq's pairs" % where)
+    rc = fn(pos.data_ptr(), coords.data_ptr(), coords.shape[0], axis.data_ptr(), b, t, h, d, code,
+            _HEADS.pack(*_strided(where, "input", x, shape, x)), _HEADS.pack(*_strided(where, "output", y, shape, x)),
+            _flat32(where, "inv_freq", inv_freq, n, x), 2 * n, 1 if interleaved else 0, factor, stream)
+    if rc:
+        raise BloadError(rc, where)
+
+
+def bload_rotary_axes(pos, coords, axis, x, y, inv_freq, interleaved: bool = False, factor: float = 1.0, stream=None) -> None:
+    """Rotary positions with several axes (video: time, height, width): pair i of every head of x [blocks, t_block, heads,
+    head_dim] turns by coords[axis[i]] * inv_freq[i] into y (which may be x).  coords: int32 [axes, blocks, t_block], at most
+    4 axes; axis: int32, one per element of inv_freq; pos: int32 [blocks, t_block] from bload_pack, whose padding is copied."""
+    _axes(load().bload_rotary_axes, "bload_rotary_axes", pos, coords, axis, x, y, inv_freq, interleaved, factor, stream)
+
+
+def bload_rotary_axes_grad(pos, coords, axis, dy, dx, inv_freq, interleaved: bool = False, factor: float = 1.0, stream=None) -> None:
+    """dx = gradient of bload_rotary_axes's input, from the gradient dy of its output (dx may be dy)."""
+    _axes(load().bload_rotary_axes_grad, "bload_rotary_axes_grad", pos, coords, axis, dy, dx, inv_freq, interleaved, factor, stream)
+
+
+_NONE3, _NONE6, _NONE18 = (0,) * 3, (0,) * 6, (0,) * 18
+
+
+def _work(where: str, work, like):
+    """(address, bytes) of a scratch argument"""
+    if work is None:
+        return 0, 0
+    if work.get_device() != like.get_device() or not work.is_contiguous():
+        raise TypeError("%s: work must be a contiguous tensor on %s" % (where, like.device))
+    return work.data_ptr(), work.numel() * work.element_size()
+
+
+def _sequences(where: str, pos, seq_id, out, name: str, shape, dtype):
+    """(address of the sequence numbers, how many, address of the output) of a call that writes something per sequence"""
+    if out is None:
+        return 0, 0, 0
+    if seq_id is None or seq_id.dtype is not pos.dtype or seq_id.shape != pos.shape or seq_id.get_device() != pos.get_device() or not seq_id.is_contiguous():
+        raise TypeError("%s: %s needs seq_id, a contiguous int32 tensor like pos, as bload_pack writes it" % (where, name))
+    if out.dtype is not dtype or out.get_device() != pos.get_device() or not out.is_contiguous() or out.dim() != 3 or out.shape[1:] != shape:
+        raise TypeError("%s: %s must be a contiguous %s tensor [sequences, %d, %d] on %s" % (where, name, dtype, *shape, pos.device))
+    return seq_id.data_ptr(), out.shape[0], out.data_ptr()
+
+
+def bload_norm_buffers(pos, x):
+    """(stats, work) for bload_norm and its gradient on x [blocks, t_block, channels]: float32 [blocks, t_block, 2], means and
+    reciprocal deviations that the forward call keeps, and the gradient's scratch."""
+    b, t = pos.shape
+    n = load().bload_norm_work_bytes(b, t, x.shape[-1], _torch()[0].get(x.dtype, -1))
+    return x.new_empty((b, t, 2), dtype=_torch()[2]), x.new_empty(n, dtype=_torch()[5]) if n else None
+
+
+def _norm(where, pos, x, weight, bias, stats, eps, stream):
+    """(packed fields up to x, stream)"""
+    (b, t), code, stream = _begin(where, pos, x, 3, stream)
+    c = x.shape[2]
+    return (b, c, t, code, eps, pos.data_ptr(), _flat32(where, "weight", weight, c, x), _flat32(where, "bias", bias, c, x),
+            _flat32(where, "stats", stats, b * t * 2, x), *_strided(where, "x", x, (b, t, c), x)), stream
+
+
+def bload_norm(pos, x, y, weight=None, bias=None, stats=None, eps: float = 1e-5, stream=None) -> None:
+    """y = layer norm of x over its channels, times weight plus bias (float32 [channels] or None); padding gives 0.  x, y: [blocks,
+    t_block, channels] (float32, float16 or bfloat16, strided); pos: int32 [blocks, t_block] from bload_pack; stats from
+    bload_norm_buffers (None: no gradient will be asked for)."""
+    where = "bload_norm"
+    fields, stream = _norm(where, pos, x, weight, bias, stats, eps, stream)
+    rc = load().bload_norm(_NORM.pack(*fields, *_strided(where, "y", y, x.shape, x), *_NONE6, 0, 0, 0, 0), stream)
+    if rc:
+        raise BloadError(rc, where)
+
+
+def bload_norm_grad(pos, x, stats, dy, dx, weight=None, dweight=None, dbias=None, work=None, stream=None) -> None:
+    """dx of bload_norm from dy, with the forward call's stats, and the sums over all frames dweight and dbias (float32 [channels];
+    None: not wanted, and neither is work then)."""
+    where = "bload_norm_grad"
+    fields, stream = _norm(where, pos, x, weight, None, stats, 0.0, stream)
+    c = x.shape[2]
+    rc = load().bload_norm_grad(_NORM.pack(
+        *fields, *_NONE3, *_strided(where, "dy", dy, x.shape, x), *_strided(where, "dx", dx, x.shape, x),
+        _flat32(where, "dweight", dweight, c, x), _flat32(where, "dbias", dbias, c, x), *_work(where, work, x)), stream)
+    if rc:
+        raise BloadError(rc, where)
+
+
+def bload_conv_buffers(pos, x, weight):
+    """Scratch of bload_conv_grad for x [blocks, t_block, channels] and weight [channels, taps]."""
+    b, t = pos.shape
+    n = load().bload_conv_work_bytes(b, t, x.shape[-1], weight.shape[-1], _torch()[0].get(x.dtype, -1))
+    return x.new_empty(n, dtype=_torch()[5]) if n else None
+
+
+def _conv(where, pos, x, weight, bias, silu, stream):
+    """(packed fields up to x, stream)"""
+    (b, t), code, stream = _begin(where, pos, x, 3, stream)
+    c = x.shape[2]
+    if weight.dim() != 2:
+        raise ValueError("%s: weight is [channels, taps]" % where)
+    taps = weight.shape[1]
+    return (b, c, t, code, taps, 1 if silu else 0, pos.data_ptr(), _flat32(where, "weight", weight, c * taps, x),
+            _flat32(where, "bias", bias, c, x), *_strided(where, "x", x, (b, t, c), x)), stream
+
+
+def bload_conv(pos, x, y, weight, bias=None, silu: bool = True, seq_id=None, tails=None, stream=None) -> None:
+    """y = short causal convolution of x [blocks, t_block, channels] per channel inside sequences, then u * sigmoid(u) if silu.
+    weight: float32 [channels, taps], the last tap is the frame's own; bias: float32 [channels] or None; taps at most 8.  tails:
+    [sequences, taps - 1, channels] like x or None: the last inputs of every sequence of the batch, numbered by seq_id (int32
+    [blocks, t_block] from bload_pack), for bload_conv_step to go on from."""
+    where = "bload_conv"
+    fields, stream = _conv(where, pos, x, weight, bias, silu, stream)
+    rc = load().bload_conv(_CONV.pack(*fields, *_strided(where, "y", y, x.shape, x),
+                                      *_sequences(where, pos, seq_id, tails, "tails", (weight.shape[1] - 1, x.shape[2]), x.dtype),
+                                      *_NONE6, 0, 0, 0, 0), stream)
+    if rc:
+        raise BloadError(rc, where)
+
+
+def bload_conv_grad(pos, x, dy, dx, weight, dweight=None, bias=None, dbias=None, silu: bool = True, work=None, stream=None) -> None:
+    """dx of bload_conv from dy, and the sums over all frames dweight [channels, taps] and dbias (float32; None: not wanted).  work
+    from bload_conv_buffers."""
+    where = "bload_conv_grad"
+    fields, stream = _conv(where, pos, x, weight, bias, silu, stream)
+    rc = load().bload_conv_grad(_CONV.pack(
+        *fields, *_NONE3, 0, 0, 0, *_strided(where, "dy", dy, x.shape, x), *_strided(where, "dx", dx, x.shape, x),
+        _flat32(where, "dweight", dweight, weight.numel(), x), _flat32(where, "dbias", dbias, x.shape[2], x), *_work(where, work, x)), stream)
+    if rc:
+        raise BloadError(rc, where)
+
+
+def _rows(where: str, pos, x, stream):
+    """Checks of a call for single frames; (rows, channels, element type code, stream)."""
+    codes, int32, _, raw_stream, current_device, _ = _torch()
+    index = pos.get_device()
+    if pos.dtype is not int32 or pos.dim() != 1 or index < 0 or not pos.is_contiguous():
+        raise TypeError("%s: pos must be a contiguous CUDA int32 tensor [rows]" % where)
+    if index != current_device():
+        raise ValueError("%s: pos is on %s, the current device is cuda:%d" % (where, pos.device, current_device()))
+    if x.dim() != 2 or x.get_device() != index or x.shape[0] != pos.shape[0]:
+        raise ValueError("%s: x is [rows, channels] on the device of pos" % where)
+    code = codes.get(x.dtype)
+    if code is None:
+        raise TypeError("%s: float32, float16 or bfloat16 tensors, not %s" % (where, x.dtype))
+    return (*x.shape, code, raw_stream(index) if stream is None else stream.cuda_stream)
+
+
+def _state(where: str, name: str, t, shape, dtype, like) -> int:
+    if t.dtype is not dtype or t.get_device() != like.get_device() or not t.is_contiguous() or t.shape != shape:
+        raise TypeError("%s: %s must be a contiguous %s tensor %s on %s" % (where, name, dtype, tuple(shape), like.device))
+    return t.data_ptr()
+
+
+def bload_conv_step(pos, state, x, y, weight, bias=None, silu: bool = True, next_state=None, stream=None) -> None:
+    """bload_conv for one new frame of each of several sequences: x, y [rows, channels]; state [rows, taps - 1, channels], the last
+    inputs, moves on in place or into next_state.  pos: int32 [rows], positions of the new frames (0 starts a sequence, whatever
+    the state holds; negative: no frame, y = 0 and the state stays)."""
+    where = "bload_conv_step"
+    n, c, code, stream = _rows(where, pos, x, stream)
+    if weight.dim() != 2:
+        raise ValueError("%s: weight is [channels, taps]" % where)
+    taps = weight.shape[1]
+    shape = (n, taps - 1, c)
+    at = _state(where, "state", state, shape, x.dtype, x)
+    to = at if next_state is None else _state(where, "next_state", next_state, shape, x.dtype, x)
+    rc = load().bload_conv_step(n, c, code, taps, 1 if silu else 0, pos.data_ptr(), at, to,
+                                _CHANNELS.pack(*_strided(where, "x", x, (n, c), x), 0), _CHANNELS.pack(*_strided(where, "y", y, (n, c), x), 0),
+                                _flat32(where, "weight", weight, c * taps, x), _flat32(where, "bias", bias, c, x), stream)
+    if rc:
+        raise BloadError(rc, where)
+
+
+SCAN_RUN = 16
+
+
+def bload_scan_buffers(pos, x, a, gradient: bool = True):
+    """(carry, work) for bload_scan and, with gradient, bload_scan_grad on x [blocks, t_block, channels] and a [channels, states]: the
+    float32 states that the forward call keeps for the gradient, [blocks, ceil(t_block / 16), channels, states] (None without), and
+    scratch (None when none is needed).  Calls that may overlap on the GPU need a scratch each."""
+    b, t = pos.shape
+    c, states = x.shape[-1], a.shape[-1]
+    n = load().bload_scan_work_bytes(b, t, c, states, 1 if gradient else 0)
+    return (x.new_empty((b, -(-t // SCAN_RUN), c, states), dtype=_torch()[2]) if gradient else None,
+            x.new_empty(n, dtype=_torch()[5]) if n else None)
+
+
+def _scan(where, pos, x, dt, a, b, c, d, dt_bias, z, softplus, carry, work, stream):
+    """(packed fields up to z, of d_carry to work_bytes, stream)"""
+    (blocks, t), code, stream = _begin(where, pos, x, 3, stream)
+    channels = x.shape[2]
+    if a.dim() != 2:
+        raise ValueError("%s: a is [channels, states]" % where)
+    states, shape = a.shape[1], (blocks, t, channels)
+    rows = (blocks, t, states)
+    return ((blocks, channels, t, code, states, 1 if softplus else 0, pos.data_ptr(), _flat32(where, "a", a, channels * states, x),
+             _flat32(where, "d", d, channels, x), _flat32(where, "dt_bias", dt_bias, channels, x), *_strided(where, "x", x, shape, x),
+             *_strided(where, "dt", dt, shape, x), *_strided(where, "b", b, rows, x), *_strided(where, "c", c, rows, x),
+             *(_NONE3 if z is None else _strided(where, "z", z, shape, x))),
+            (_flat32(where, "carry", carry, blocks * -(-t // SCAN_RUN) * channels * states, x), *_work(where, work, x)), stream)
+
+
+def bload_scan(pos, x, dt, a, b, c, y, d=None, dt_bias=None, z=None, softplus: bool = True, carry=None, work=None, seq_id=None,
+               last=None, stream=None) -> None:
+    """Selective state-space scan inside the sequences of packed blocks: with delta = softplus(dt + dt_bias), per channel and state n
+    h_s = exp(delta a[n]) h_{s-1} + delta b_s[n] x_s, y = sum_n c_s[n] h_s + d x, times z sigmoid(z) if z is given.  x, dt, y, z:
+    [blocks, t_block, channels], b, c: [blocks, t_block, states] (float32, float16 or bfloat16, strided); a: float32 [channels,
+    states], at most 64 states; d, dt_bias: float32 [channels] or None; softplus False: delta = dt + dt_bias.  carry, work from
+    bload_scan_buffers (carry None: no gradient will be asked for).  last: float32 [sequences, channels, states] or None: the state
+    behind every sequence of the batch, numbered by seq_id (int32 [blocks, t_block] from bload_pack), for bload_scan_step."""
+    where = "bload_scan"
+    head, kept, stream = _scan(where, pos, x, dt, a, b, c, d, dt_bias, z, softplus, carry, work, stream)
+    rc = load().bload_scan(_SCAN.pack(*head, *_strided(where, "y", y, x.shape, x), *kept,
+                                      *_sequences(where, pos, seq_id, last, "last", a.shape, _torch()[2]), *_NONE18, 0, 0, 0), stream)
+    if rc:
+        raise BloadError(rc, where)
+
+
+def bload_scan_grad(pos, x, dt, a, b, c, carry, dy, dx, ddt, da, db, dc, d=None, dd=None, dt_bias=None, ddt_bias=None, z=None, dz=None,
+                    softplus: bool = True, work=None, stream=None) -> None:
+    """Gradients of bload_scan from dy, with the forward call's carry: dx, ddt, dz like x, db and dc like b, and summed over all frames da
+    [channels, states], dd, ddt_bias [channels] (float32; the last two may be None: not wanted).  dz is needed where z is given."""
+    where = "bload_scan_grad"
+    head, kept, stream = _scan(where, pos, x, dt, a, b, c, d, dt_bias, z, softplus, carry, work, stream)
+    channels = x.shape[2]
+    if (z is None) != (dz is None):
+        raise ValueError("%s: dz goes with z" % where)
+    rc = load().bload_scan_grad(_SCAN.pack(
+        *head, *_NONE3, *kept, 0, 0, 0, *_strided(where, "dy", dy, x.shape, x), *_strided(where, "dx", dx, x.shape, x),
+        *_strided(where, "ddt", ddt, x.shape, x), *_strided(where, "db", db, b.shape, x), *_strided(where, "dc", dc, b.shape, x),
+        *(_NONE3 if dz is None else _strided(where, "dz", dz, x.shape, x)), _flat32(where, "da", da, a.numel(), x),
+        _flat32(where, "dd", dd, channels, x), _flat32(where, "ddt_bias", ddt_bias, channels, x)), stream)
+    if rc:
+        raise BloadError(rc, where)
+
+
+def bload_scan_step(pos, state, x, dt, a, b, c, y, d=None, dt_bias=None, z=None, softplus: bool = True, next_state=None, stream=None) -> None:
+    """bload_scan for one new frame of each of several sequences: x, dt, y, z [rows, channels], b, c [rows, states]; state: float32
+    [rows, channels, states], moves on in place or into next_state.  pos as in bload_conv_step."""
+    where = "bload_scan_step"
+    n, channels, code, stream = _rows(where, pos, x, stream)
+    if a.dim() != 2:
+        raise ValueError("%s: a is [channels, states]" % where)
+    states, f32 = a.shape[1], _torch()[2]
+    shape = (n, channels, states)
+    at = _state(where, "state", state, shape, f32, x)
+    to = at if next_state is None else _state(where, "next_state", next_state, shape, f32, x)
+    rows, narrow = (n, channels), (n, states)
+    rc = load().bload_scan_step(_SCAN_STEP.pack(
+        n, channels, code, states, 1 if softplus else 0, pos.data_ptr(), _flat32(where, "a", a, channels * states, x),
+        _flat32(where, "d", d, channels, x), _flat32(where, "dt_bias", dt_bias, channels, x), at, to, *_strided(where, "x", x, rows, x), 0,
+        *_strided(where, "dt", dt, rows, x), 0, *_strided(where, "b", b, narrow, x), 0, *_strided(where, "c", c, narrow, x), 0,
+        *(_NONE3 if z is None else (*_strided(where, "z", z, rows, x), 0)), *_strided(where, "y", y, rows, x), 0), stream)
     if rc:
         raise BloadError(rc, where)
 

@@ -44,6 +44,9 @@ struct RotaryParams {
     int32_t t, heads, d, n;  // n: pairs that turn
     int32_t interleaved, gradient;
     float factor;
+    // several axes: the coordinate of axis k and slot s is coords[k * slots + s]; NULL: positions, one axis
+    const int32_t *coords, *axis;
+    int32_t axes;
 };
 
 struct RecurParams {
@@ -63,6 +66,71 @@ template <typename T>
 struct RecurTensors {
     Channels<const T> gate, x, dh;
     Channels<T> h, dgate, dx;
+};
+
+struct NormParams {
+    const int32_t* pos;
+    const float *weight, *bias;
+    float2* stats;
+    float *dweight, *dbias;
+    float* work;  // [CTAs][2][channels]
+    int64_t rows, channels;
+    int32_t t;
+    float eps;
+    bool flat;  // blocks of every tensor lie one behind the other
+};
+template <typename T>
+struct NormTensors {
+    Channels<const T> x, dy;
+    Channels<T> y, dx;
+};
+
+struct ConvParams {
+    const int32_t* pos;
+    const float *weight, *bias;
+    const int32_t* seq_id;
+    int64_t n_seq;
+    void* tails;
+    float *dweight, *dbias;
+    float* work;  // [tiles of all blocks][channels * (taps + 1)]
+    int64_t blocks, channels;
+    int32_t t, taps, silu;
+};
+template <typename T>
+struct ConvTensors {
+    Channels<const T> x, dy;
+    Channels<T> y, dx;
+};
+
+struct ScanParams {
+    const int32_t* pos;
+    const float *a, *d, *dt_bias;
+    float* carry;
+    void* work;
+    const int32_t* seq_id;
+    int64_t n_seq;
+    float* last;
+    float *da, *dd, *ddt_bias;
+    int64_t blocks, channels;
+    int32_t t, states, softplus;
+};
+template <typename T>
+struct ScanTensors {
+    Channels<const T> x, dt, b, c, z, dy;
+    Channels<T> y, dx, ddt, db, dc, dz;
+};
+struct ScanStepParams {
+    const int32_t* pos;
+    const float *a, *d, *dt_bias, *state;
+    float* next;
+    int64_t rows, channels;
+    int32_t states, softplus;
+};
+template <typename T>
+struct ScanStepTensors {  // by rows
+    const T *x, *dt, *b, *c, *z;
+    T* y;
+    int64_t sx, sdt, sb, sc, sz, sy;
 };
 
 // Lets a kernel have `bytes` of dynamic shared memory, once per device (`done`: one bit each, of the kernel).
@@ -90,6 +158,36 @@ cudaError_t launch_recurrence(const RecurParams& p, const RecurTensors<T>& a, cu
 template <typename T>
 cudaError_t launch_recurrence_grad(const RecurParams& p, const RecurTensors<T>& a, cudaStream_t st);
 
+template <typename T>
+cudaError_t launch_norm(const NormParams& p, const NormTensors<T>& a, cudaStream_t st);
+template <typename T>
+cudaError_t launch_norm_grad(const NormParams& p, const NormTensors<T>& a, cudaStream_t st);
+template <typename T>
+cudaError_t launch_conv(const ConvParams& p, const ConvTensors<T>& a, cudaStream_t st);
+template <typename T>
+cudaError_t launch_conv_grad(const ConvParams& p, const ConvTensors<T>& a, cudaStream_t st);
+template <typename T>
+cudaError_t launch_conv_step(const ConvParams& p, int64_t rows, const T* state, T* next, const T* x, int64_t sx, T* y, int64_t sy,
+                             cudaStream_t st);
+template <typename T>
+cudaError_t launch_scan(const ScanParams& p, const ScanTensors<T>& a, cudaStream_t st);
+template <typename T>
+cudaError_t launch_scan_grad(const ScanParams& p, const ScanTensors<T>& a, cudaStream_t st);
+template <typename T>
+cudaError_t launch_scan_step(const ScanStepParams& p, const ScanStepTensors<T>& a, cudaStream_t st);
+
+// Up to three arrays side by side in the columns of `part`: out[k][i] = sum over rows of part[row][column], rows in a fixed order.
+struct ColumnSums {
+    const float* part;
+    int64_t rows, columns;
+    float* out[3];       // NULL: not wanted
+    int64_t end[3];      // columns below end[k] and not below end[k - 1] go to out[k]
+};
+cudaError_t launch_column_sums(const ColumnSums& s, cudaStream_t st);
+
+size_t norm_work_bytes(int64_t rows, int64_t channels);
+size_t conv_work_bytes(int64_t blocks, int32_t t, int64_t channels, int32_t taps, int32_t dtype);
+size_t scan_work_bytes(int64_t blocks, int32_t t, int64_t channels, int32_t states, bool gradient);
 size_t recurrence_work_bytes(int64_t blocks, int32_t t, int64_t channels);
 int64_t attention_timeouts(), recurrence_timeouts();  // see bload_device_timeouts
 
@@ -142,6 +240,108 @@ __device__ __forceinline__ Two fma(Two a, Two b, Two c)
     return r;
 }
 __device__ __forceinline__ Two zero() { return {0ull}; }
+
+// V neighbouring elements in registers.  WIDE: they lie on a boundary of their size (at most 16 bytes) and all exist; otherwise
+// the first `there` of them are moved one by one, and the rest read as zeros.
+template <typename T, int V>
+struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Elements {
+    T x[V];
+    static constexpr int kBytes = V * sizeof(T), kWord = kBytes < 16 ? kBytes : 16;
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] = from_float<T>(0.0f);
+    }
+    __device__ __forceinline__ void load(const T* p, int there, bool wide)
+    {
+        if (wide && there >= V) {
+            if constexpr (kWord == 16) {
+#pragma unroll
+                for (int k = 0; k < kBytes / 16; ++k) reinterpret_cast<uint4*>(x)[k] = reinterpret_cast<const uint4*>(p)[k];
+            } else if constexpr (kWord == 8) {
+                *reinterpret_cast<uint2*>(x) = *reinterpret_cast<const uint2*>(p);
+            } else if constexpr (kWord == 4) {
+                *reinterpret_cast<uint32_t*>(x) = *reinterpret_cast<const uint32_t*>(p);
+            } else {
+                x[0] = p[0];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = e < there ? p[e] : from_float<T>(0.0f);
+        }
+    }
+    __device__ __forceinline__ void store(T* p, int there, bool wide) const
+    {
+        if (wide && there >= V) {
+            if constexpr (kWord == 16) {
+#pragma unroll
+                for (int k = 0; k < kBytes / 16; ++k) reinterpret_cast<uint4*>(p)[k] = reinterpret_cast<const uint4*>(x)[k];
+            } else if constexpr (kWord == 8) {
+                *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(x);
+            } else if constexpr (kWord == 4) {
+                *reinterpret_cast<uint32_t*>(p) = *reinterpret_cast<const uint32_t*>(x);
+            } else {
+                p[0] = x[0];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e < there) p[e] = x[e];
+        }
+    }
+    // elements `step` apart
+    __device__ __forceinline__ void load_apart(const T* p, int64_t step, int there)
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] = e < there ? p[e * step] : from_float<T>(0.0f);
+    }
+    __device__ __forceinline__ void store_apart(T* p, int64_t step, int there) const
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (e < there) p[e * step] = x[e];
+    }
+    __device__ __forceinline__ float get(int e) const { return to_float(x[e]); }
+    __device__ __forceinline__ void set(int e, float v) { x[e] = from_float<T>(v); }
+};
+
+// sigmoid(v) = 1 / (1 + exp(-v)), to a few 2^-23 of itself for |v| up to some tens (where exp(-v) passes 2^128 it is 0)
+__device__ __forceinline__ float sigmoid_of(float v)
+{
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return r;
+}
+
+// Sums of N values (a power of two, at most 32) over the lanes that differ in the bits from 16 down to LOW: the values are shared
+// out on the way, so that each step exchanges half as many.  A lane ends with `left` sums, v[0..left-1], of the values from index
+// `first` on: N - 1 exchanges instead of 5 N for a whole warp.
+template <int N, int LOW>
+struct Shared {
+    static constexpr int kSteps = LOW == 1 ? 5 : LOW == 2 ? 4 : LOW == 4 ? 3 : LOW == 8 ? 2 : LOW == 16 ? 1 : 0;
+    static constexpr int kLeft = (N >> kSteps) > 1 ? N >> kSteps : 1;
+};
+template <int N, int BIT, int LOW>
+__device__ __forceinline__ void share_sums(float* v, int lane, int& first)
+{
+    if constexpr (BIT >= LOW) {
+        if constexpr (N > 1) {
+            constexpr int H = N / 2;
+            const bool upper = lane & BIT;
+#pragma unroll
+            for (int i = 0; i < H; ++i) {
+                const float send = upper ? v[i] : v[i + H], keep = upper ? v[i + H] : v[i];
+                v[i] = keep + __shfl_xor_sync(0xffffffffu, send, BIT);
+            }
+            if (upper) first += H;
+            share_sums<H, BIT / 2, LOW>(v, lane, first);
+        } else {
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], BIT);
+            share_sums<1, BIT / 2, LOW>(v, lane, first);
+        }
+    }
+}
 
 // First slot behind the sequence that holds slot i (pos[i] >= 0), by a whole warp: pos[s] == s - start holds up to the
 // end of the sequence and nowhere behind it.  The next 128 slots are looked at together, which ends it for short sequences; then 32

@@ -8,6 +8,8 @@
 // took 138 us instead of 121 for 16 x 4096 slots of 20 heads of 128, the half layout 116 either way: 5.8 TB/s).  A thread walks
 // the slots with its unit and heads fixed: with a thread per slot, unit and group of heads the divisions that place it cost as
 // much as the work (166 us).
+// AXES: the angle is a coordinate of the pair's axis times its frequency, with what the product's rounding loses.  A thread whose pairs
+// all have one axis loads one coordinate per slot; otherwise one per pair, which its neighbours load too.
 // Pieces are as wide as alignment and the sizes of the turned part and of the rest allow: 16, 8 or 4 bytes, or one element.
 #include "bload_internal.cuh"
 #include "bload_layers.cuh"
@@ -64,15 +66,26 @@ struct alignas(V * sizeof(T)) Piece {
 // exact as long as k < 2^22), then the Taylor series of both to r^9 and r^8, and the quadrant.  Angles are below 3e5, where the 24 bits
 // of 2 / pi place k within 0.01 of a's multiple: |r| <= 0.8, and the series' remainders are below 3e-8 (over 2 million angles the result
 // was never off by more than 1e-7; up to 6e6 |r| grew to 1.03 and the error to 4.7e-7).  Larger angles go to sincosf.
-__device__ __forceinline__ void sine_cosine(float a, float& sn, float& cs)
+// REST: of the angle a + rest, where rest is below half a unit of a's last place.
+template <bool REST>
+__device__ __forceinline__ void sine_cosine(float a, float rest, float& sn, float& cs)
 {
     if (!(fabsf(a) < 3.0e5f)) {
         sincosf(a, &sn, &cs);
+        if (REST && rest != 0.0f) {
+            float s, c;
+            sincosf(rest, &s, &c);
+            const float turned = fmaf(cs, c, -sn * s);
+            sn = fmaf(sn, c, cs * s);
+            cs = turned;
+        }
         return;
     }
     constexpr float kRound = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer, which then is in the low bits
     const float t = fmaf(a, 0.636619772f, kRound), k = t - kRound;
-    const float r = fmaf(k, 4.37113883e-8f, fmaf(k, -1.57079637f, a)), z = r * r;
+    float r = fmaf(k, 4.37113883e-8f, fmaf(k, -1.57079637f, a));
+    if (REST) r += rest;
+    const float z = r * r;
     float s = fmaf(fmaf(fmaf(fmaf(z, 1.0f / 362880, -1.0f / 5040), z, 1.0f / 120), z, -1.0f / 6), z * r, r);
     float c = fmaf(fmaf(fmaf(fmaf(z, 1.0f / 40320, -1.0f / 720), z, 1.0f / 24), z, -0.5f), z, 1.0f);
     const int quadrant = __float_as_int(t);
@@ -87,7 +100,7 @@ __device__ __forceinline__ void sine_cosine(float a, float& sn, float& cs)
 
 // V: elements of a piece.  Units of a head: half layout, (d - n) / V (a turned one is two pieces); interleaved, d / V.
 // blockIdx.y and the thread fix a unit and a group of heads; the thread walks the slots with them.
-template <typename T, bool INTERLEAVED, int V, bool WIDE>
+template <typename T, bool INTERLEAVED, int V, bool WIDE, bool AXES>
 __global__ void __launch_bounds__(kThreads, 2) k26_rotary(const RotaryParams p, const Heads<const T> x, const Heads<T> y, int units)
 {
     constexpr int kPairs = INTERLEAVED ? V / 2 : V;  // of a turned unit
@@ -102,6 +115,17 @@ __global__ void __launch_bounds__(kThreads, 2) k26_rotary(const RotaryParams p, 
     float freq[kPairs];
 #pragma unroll
     for (int e = 0; e < kPairs; ++e) freq[e] = turns ? p.inv_freq[unit * kPairs + e] : 0.0f;
+    const int32_t* along[AXES ? kPairs : 1];  // coordinates of each pair's axis
+    bool one_axis = true;
+    if (AXES) {
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) {
+            const int axis = turns ? p.axis[unit * kPairs + e] : 0, known = axis >= 0 && axis < p.axes ? axis : 0;
+            if (known != axis) freq[e] = 0.0f;
+            along[AXES ? e : 0] = p.coords + known * p.slots;
+            one_axis = one_axis && along[AXES ? e : 0] == along[0];
+        }
+    }
     const float factor = p.factor, back = p.gradient ? -p.factor : p.factor;
     const T* const x0 = x.data + h0 * x.head + at;
     T* const y0 = y.data + h0 * y.head + at;
@@ -112,9 +136,14 @@ __global__ void __launch_bounds__(kThreads, 2) k26_rotary(const RotaryParams p, 
     const int64_t step_q = step / p.t;
     int s = (int)(slot - q * p.t);
     const int step_s = (int)(step - step_q * p.t);
-    int next = slot < p.slots ? p.pos[slot] : 0;
+    int next = slot < p.slots ? p.pos[slot] : 0, next_at = AXES && slot < p.slots ? along[0][slot] : 0;
     for (; slot < p.slots; slot += step) {
-        const int pos = next;
+        const int pos = next, first_at = next_at;
+        int others[AXES ? kPairs : 1];
+        if (AXES && !one_axis) {
+#pragma unroll
+            for (int e = 1; e < kPairs; ++e) others[AXES ? e : 0] = along[AXES ? e : 0][slot];
+        }
         const T* from = x0 + q * x.block + s * x.slot;
         T* to = y0 + q * y.block + s * y.slot;
         Piece<T, V, WIDE> u[kHeads], w[INTERLEAVED ? 1 : kHeads];
@@ -127,12 +156,20 @@ __global__ void __launch_bounds__(kThreads, 2) k26_rotary(const RotaryParams p, 
                     u[j].x[0] = from[j * x.head];
                 if (two_pieces) w[INTERLEAVED ? 0 : j].load(from + j * x.head + p.n);
             }
-        if (slot + step < p.slots) next = p.pos[slot + step];
+        if (slot + step < p.slots) {
+            next = p.pos[slot + step];
+            if (AXES) next_at = along[0][slot + step];
+        }
         if (turns && pos >= 0) {
             float cs[kPairs], sn[kPairs];
 #pragma unroll
             for (int e = 0; e < kPairs; ++e) {
-                sine_cosine((float)pos * freq[e], sn[e], cs[e]);
+                if (AXES) {
+                    const float x = (float)(e == 0 || one_axis ? first_at : others[AXES ? e : 0]), a = x * freq[e];
+                    sine_cosine<true>(a, fmaf(x, freq[e], -a), sn[e], cs[e]);
+                } else {
+                    sine_cosine<false>((float)pos * freq[e], 0.0f, sn[e], cs[e]);
+                }
                 sn[e] *= back;
                 cs[e] *= factor;
             }
@@ -192,7 +229,8 @@ cudaError_t launch(const RotaryParams& p, const Heads<const T>& x, const Heads<T
     const int all = units * ((p.heads + kHeads - 1) / kHeads), parts = (all + kThreads - 1) / kThreads;
     const int64_t slots_at_once = all < kThreads ? kThreads / all : 1;
     const int64_t wanted = (p.slots + slots_at_once - 1) / slots_at_once, most = (8 * 148 + parts - 1) / parts;
-    k26_rotary<T, INTERLEAVED, V, WIDE><<<dim3((unsigned)(wanted < most ? wanted : most), parts), kThreads, 0, st>>>(p, x, y, units);
+    auto* kernel = p.coords ? k26_rotary<T, INTERLEAVED, V, WIDE, true> : k26_rotary<T, INTERLEAVED, V, WIDE, false>;
+    kernel<<<dim3((unsigned)(wanted < most ? wanted : most), parts), kThreads, 0, st>>>(p, x, y, units);
     count_launches(1);
     return cudaGetLastError();
 }
