@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "bload.h"
 
@@ -113,6 +114,7 @@ struct ScanParams {
     float *da, *dd, *ddt_bias;
     int64_t blocks, channels;
     int32_t t, states, softplus;
+    bool rows_wide;  // rows of b and c are whole pieces of 16 bytes
 };
 template <typename T>
 struct ScanTensors {
@@ -303,6 +305,31 @@ struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Elements {
     }
     __device__ __forceinline__ float get(int e) const { return to_float(x[e]); }
     __device__ __forceinline__ void set(int e, float v) { x[e] = from_float<T>(v); }
+    // elements e and e + 1, e even
+    __device__ __forceinline__ Two pair(int e) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            return two(x[e], x[e + 1]);
+        } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(x + e);  // (its halves are the upper halves of 32-bit numbers)
+            return two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        } else {
+            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(x + e));
+            return two(v.x, v.y);
+        }
+    }
+    __device__ __forceinline__ void set_pair(int e, Two v)
+    {
+        const float2 f = one(v);
+        if constexpr (sizeof(T) == 4) {
+            x[e] = f.x;
+            x[e + 1] = f.y;
+        } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+            *reinterpret_cast<__nv_bfloat162*>(x + e) = __floats2bfloat162_rn(f.x, f.y);
+        } else {
+            *reinterpret_cast<__half2*>(x + e) = __floats2half2_rn(f.x, f.y);
+        }
+    }
 };
 
 // sigmoid(v) = 1 / (1 + exp(-v)), to a few 2^-23 of itself for |v| up to some tens (where exp(-v) passes 2^128 it is 0)
@@ -312,6 +339,18 @@ __device__ __forceinline__ float sigmoid_of(float v)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v * -1.4426950408889634f));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
     return r;
+}
+
+__device__ __forceinline__ Two sigmoid_of(Two v)
+{
+    const float2 x = one(v * two(-1.4426950408889634f, -1.4426950408889634f));
+    float2 e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(x.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(x.y));
+    e = one(two(e.x, e.y) + two(1.0f, 1.0f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(e.y));
+    return two(r.x, r.y);
 }
 
 // Sums of N values (a power of two, at most 32) over the lanes that differ in the bits from 16 down to LOW: the values are shared

@@ -16,6 +16,7 @@
 // run's states into shared memory (each thread its own), then goes through them from the last slot to the first.  Sums over
 // channels (db, dc) are shared out over the lanes of a warp, then over the CTA's warps, and written once per CTA; k40 adds the CTAs'.
 #include <math.h>
+#include <stddef.h>
 
 #include <type_traits>
 
@@ -36,7 +37,8 @@ struct Split {
     static constexpr int kChannels = 256 / LANES;   // of a CTA
     static constexpr int kV = kChannels / 8;        // of a thread, where a run lies as in memory: 8 threads per slot
     static constexpr int kPerWarp = 64 / LANES;
-    static constexpr int kGroup = LANES < 4 ? LANES : 4;  // slots whose sums over states are taken together
+    static constexpr int kGroup = 2;                // slots whose sums over states are taken together
+    static constexpr int kRow = kChannels + 8;      // of an array by slots and channels, so that slots two apart lie in other banks
 };
 
 // Scratch: per boundary between segments and block what crosses it (0 nothing, 1 a state that nothing before the segment
@@ -67,61 +69,107 @@ __device__ __forceinline__ Two decay(Two delta, Two a)
     return two(ex2(x.x), ex2(x.y));
 }
 
-// softplus(v) = max(v, 0) + log1p(e) and sigmoid(v) from e = exp(-|v|), which is in (0, 1].  The product with log2(e) keeps what its
-// rounding loses (without: up to 1e-6 of e for v = -10).  log1p(e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by its series to s^15: the
-// rest is below 2e-9 of it.
-__device__ __forceinline__ void softplus_of(float v, float& value, float& slope)
+// softplus(v) = max(v, 0) + log1p(e) of two values, e = exp(-|v|), which is in (0, 1].  The product with log2(e) keeps what its rounding
+// loses (without: up to 1e-6 of e for v = -10).  log1p(e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by its series to s^15: the rest is
+// below 2e-9 of it.
+__device__ __forceinline__ Two softplus_of(Two v)
 {
-    const float x = fabsf(v) * -kLog2E, rest = fmaf(fabsf(v), -kLog2E, -x) + fabsf(v) * -1.925963033e-8f;
-    float e = ex2(x);
-    e = e > 0.0f ? fmaf(e, rest * kLn2, e) : e;
-    float r, q;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(2.0f + e));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(1.0f + e));
-    const float s = e * r, z = s * s;
-    float p = fmaf(z, 1.0f / 15, 1.0f / 13);
-    p = fmaf(z, p, 1.0f / 11);
-    p = fmaf(z, p, 1.0f / 9);
-    p = fmaf(z, p, 1.0f / 7);
-    p = fmaf(z, p, 1.0f / 5);
-    p = fmaf(z, p, 1.0f / 3);
-    const float l = 2.0f * fmaf(s * z, p, s);
-    value = v != v ? v : fmaxf(v, 0.0f) + l;
-    slope = v < 0.0f ? e * q : q;
-}
-__device__ __forceinline__ void delta_of(const ScanParams& p, float v, float& value, float& slope)
-{
-    value = v;
-    slope = 1.0f;
-    if (p.softplus) softplus_of(v, value, slope);
+    const float v0 = one(v).x, v1 = one(v).y;
+    const Two a = two(fminf(fabsf(v0), 126.0f), fminf(fabsf(v1), 126.0f)), x = a * two(kLog2E, kLog2E);
+    const Two rest = fma(a, two(-1.925963033e-8f, -1.925963033e-8f), fma(a, two(-kLog2E, -kLog2E), x));
+    Two e = two(ex2(-one(x).x), ex2(-one(x).y));
+    e = fma(e, rest * two(kLn2, kLn2), e);
+    const float2 d = one(e + two(2.0f, 2.0f));
+    float r0, r1;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(d.y));
+    const Two s = e * two(r0, r1), z = s * s;
+    auto c = [](float k) { return two(2.0f / k, 2.0f / k); };
+    Two p = fma(z, c(15.0f), c(13.0f));
+    p = fma(z, p, c(11.0f));
+    p = fma(z, p, c(9.0f));
+    p = fma(z, p, c(7.0f));
+    p = fma(z, p, c(5.0f));
+    p = fma(z, p, c(3.0f));
+    float m0, m1;  // (NaN stays)
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m0) : "f"(v0), "f"(0.0f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m1) : "f"(v1), "f"(0.0f));
+    return fma(s * z, p, fma(s, two(2.0f, 2.0f), two(m0, m1)));
 }
 
-// Where a thread stands: as the lanes hold states, and as a run lies in memory.
+// The first slot from `from` on, but before `end`, where a sequence starts or padding lies, by a whole warp; `from` if there is none.
+__device__ __forceinline__ int warp_start_from(const int32_t* pos, int from, int end, int lane)
+{
+    for (int s = from; s < end; s += 128) {
+        bool starts[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) starts[k] = s + 32 * k + lane < end && pos[s + 32 * k + lane] <= 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const unsigned any = __ballot_sync(0xffffffffu, starts[k]);
+            if (any) return s + 32 * k + __ffs(any) - 1;
+        }
+    }
+    return from;
+}
+
+// Where a thread stands: as the lanes hold states, and as a run lies in memory.  In shared memory channel e of the kV that a thread
+// has in memory order lies at e * 8 + its place among the slot's 8 threads, so that neighbouring threads write side by side.
+// A segment ends at a sequence start where there is one in the half segment behind its share of the runs: then nothing crosses.
 template <typename S>
 struct Place {
-    int lane, warp, part;    // part: which of the states
-    int c_lane;              // first of the lane's two channels in the CTA
-    int slot, c_mem;         // of the run, first of kV channels in the CTA
-    int64_t c0;              // first channel of the CTA
-    int there;               // of the kV channels
-    int64_t q;               // block
-    int segment, first, end; // runs of the segment
+    int lane, warp, part;  // part: which of the states
+    int ch[2], at[2];      // the lane's two channels, of the CTA and in shared memory; every other lane has them the other way round
+    int slot, m;           // of the run, and which 8th of its channels
+    int64_t c0;            // first channel of the CTA
+    int there;             // of the kV channels
+    int64_t q;             // block
+    int segment;
+    int begin, stop;       // slots of the segment
+    bool enters, leaves;   // a sequence crosses its first slot, its last
     __device__ __forceinline__ Place(const ScanParams& p, const ScanCuts& cuts)
     {
         lane = threadIdx.x & 31;
         warp = threadIdx.x >> 5;
         part = lane % S::kLanes;
-        c_lane = warp * S::kPerWarp + lane / S::kLanes * 2;
+        const int pair = warp * (S::kPerWarp / 2) + lane / S::kLanes, e = pair / 8 * 2, odd = part & 1;
+        ch[0] = pair % 8 * S::kV + e + odd;
+        ch[1] = pair % 8 * S::kV + e + 1 - odd;
+        at[0] = (e + odd) * 8 + pair % 8;
+        at[1] = (e + 1 - odd) * 8 + pair % 8;
         slot = threadIdx.x >> 3;
-        c_mem = (threadIdx.x & 7) * S::kV;
-        const int64_t at = blockIdx.x / cuts.groups;
-        c0 = (int64_t)(blockIdx.x - at * cuts.groups) * S::kChannels;
-        there = (int)max((int64_t)0, min(p.channels - c0 - c_mem, (int64_t)S::kV));
-        segment = (int)(at / p.blocks);
-        q = at - segment * p.blocks;
-        const int runs = (p.t + kRun - 1) / kRun;
-        first = (int)((int64_t)runs * segment / cuts.segments);
-        end = (int)((int64_t)runs * (segment + 1) / cuts.segments);
+        m = threadIdx.x & 7;
+        const int64_t i = blockIdx.x / cuts.groups;
+        c0 = (int64_t)(blockIdx.x - i * cuts.groups) * S::kChannels;
+        there = (int)max((int64_t)0, min(p.channels - c0 - m * S::kV, (int64_t)S::kV));
+        segment = (int)(i / p.blocks);
+        q = i - segment * p.blocks;
+        begin = 0;
+        stop = p.t;
+        enters = leaves = false;
+        if (cuts.segments > 1) {
+            const int runs = (p.t + kRun - 1) / kRun, room = runs / cuts.segments * (kRun / 2);
+            const int32_t* const pos = p.pos + q * p.t;
+            if (segment > 0) {
+                const int edge = (int)((int64_t)runs * segment / cuts.segments) * kRun;
+                begin = warp_start_from(pos, edge, min(edge + room, p.t), lane);
+                enters = pos[begin] > 0;
+            }
+            if (segment + 1 < cuts.segments) {
+                const int edge = (int)((int64_t)runs * (segment + 1) / cuts.segments) * kRun;
+                stop = warp_start_from(pos, edge, min(edge + room, p.t), lane);
+                leaves = pos[stop] > 0;
+            }
+        }
+    }
+    // bit s of `valid`: slot s of the run is a frame of the segment, of `starts`: it starts a sequence (or is none), of `ends`:
+    // its sequence ends with it
+    __device__ __forceinline__ void masks(const int32_t* pos, int t, int s0, unsigned& valid, unsigned& starts, unsigned* ends = nullptr) const
+    {
+        const int s = s0 + lane, here = lane < kRun && s >= begin && s < stop ? pos[s] : -1;
+        valid = __ballot_sync(0xffffffffu, here >= 0);
+        starts = __ballot_sync(0xffffffffu, here <= 0);
+        if (ends) *ends = __ballot_sync(0xffffffffu, here >= 0 && (s + 1 >= t || pos[s + 1] <= 0));
     }
 };
 
@@ -133,7 +181,7 @@ __device__ __forceinline__ void load_a(const ScanParams& p, const Place<S>& at, 
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int k = 0; k < S::kPairs; ++k) {
-            const int64_t ch = at.c0 + at.c_lane + c;
+            const int64_t ch = at.c0 + at.ch[c];
             const int n = at.part * S::kStates + 2 * k;
             const float* const from = p.a + ch * p.states + n;
             const bool on = ch < p.channels;
@@ -141,69 +189,123 @@ __device__ __forceinline__ void load_a(const ScanParams& p, const Place<S>& at, 
         }
 }
 
-// states [channel][state] in memory, from `base` of the CTA's block (or sequence) on
+// States [channel][state] in memory, from `base` of the CTA's first channel on
+template <typename S>
+__device__ __forceinline__ bool states_wide(const ScanParams& p, const float* base)
+{
+    return S::kStates == 4 && p.states % 4 == 0 && reinterpret_cast<uintptr_t>(base) % 16 == 0;
+}
 template <typename S>
 __device__ __forceinline__ void load_states(const ScanParams& p, const Place<S>& at, const float* base, Two (&h)[2][S::kPairs])
 {
+    const int n = at.part * S::kStates;
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < 2; ++c) {
+        const float* const from = base + ((uint32_t)at.ch[c] * (uint32_t)p.states + (uint32_t)n);
+        const int there = at.c0 + at.ch[c] < p.channels ? p.states - n : 0;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (states_wide<S>(p, base)) {
+            if (there > 0) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(from);
+        } else {
 #pragma unroll
-        for (int k = 0; k < S::kPairs; ++k) {
-            const int64_t ch = at.c0 + at.c_lane + c;
-            const int n = at.part * S::kStates + 2 * k;
-            const float* const from = base + ch * p.states + n;
-            const bool on = ch < p.channels;
-            h[c][k] = two(on && n < p.states ? from[0] : 0.0f, on && n + 1 < p.states ? from[1] : 0.0f);
+            for (int k = 0; k < S::kStates; ++k) v[k] = k < there ? from[k] : 0.0f;
         }
+#pragma unroll
+        for (int k = 0; k < S::kPairs; ++k) h[c][k] = two(v[2 * k], v[2 * k + 1]);
+    }
 }
 template <typename S>
 __device__ __forceinline__ void store_states(const ScanParams& p, const Place<S>& at, float* base, const Two (&h)[2][S::kPairs])
 {
+    const int n = at.part * S::kStates;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-        const int64_t ch = at.c0 + at.c_lane + c;
-        if (ch >= p.channels) continue;
-        const int n0 = at.part * S::kStates;
-        float* const to = base + ch * p.states + n0;
-        if (S::kStates == 4 && p.states % 4 == 0 && reinterpret_cast<uintptr_t>(base) % 16 == 0) {
-            if (n0 < p.states) {
-                const float2 x = one(h[c][0]), y = one(h[c][S::kPairs - 1]);
-                *reinterpret_cast<float4*>(to) = make_float4(x.x, x.y, y.x, y.y);
-            }
-            continue;
-        }
+        float* const to = base + ((uint32_t)at.ch[c] * (uint32_t)p.states + (uint32_t)n);
+        const int there = at.c0 + at.ch[c] < p.channels ? p.states - n : 0;
+        if (states_wide<S>(p, base)) {
+            const float2 x = one(h[c][0]), y = one(h[c][S::kPairs - 1]);
+            if (there > 0) *reinterpret_cast<float4*>(to) = make_float4(x.x, x.y, y.x, y.y);
+        } else {
 #pragma unroll
-        for (int k = 0; k < S::kPairs; ++k) {
-            const float2 x = one(h[c][k]);
-            if (n0 + 2 * k < p.states) to[2 * k] = x.x;
-            if (n0 + 2 * k + 1 < p.states) to[2 * k + 1] = x.y;
+            for (int k = 0; k < S::kPairs; ++k) {
+                if (2 * k < there) to[2 * k] = one(h[c][k]).x;
+                if (2 * k + 1 < there) to[2 * k + 1] = one(h[c][k]).y;
+            }
         }
     }
 }
 
-// b and c of a run, [slot][b, c][kAll] in shared memory; 0 on padding
-template <typename T, typename S, bool B, bool C>
-struct Rows {
-    static constexpr int kEach = kRun * S::kAll / kThreads;
-    T b[B ? kEach : 1], c[C ? kEach : 1];
-    __device__ __forceinline__ void load(const ScanParams& p, const ScanTensors<T>& a, int64_t q, int s0, unsigned valid)
+// Elements of a run in the order of memory.  WIDE: pieces lie on boundaries of their size, channels are a multiple of them, and a
+// block of a tensor spans less than 2^32 bytes, so that an address is a base that the CTA shares and a 32-bit offset.
+template <typename T, typename S, bool WIDE>
+struct Frames {
+    using Piece = Elements<T, S::kV>;
+    template <typename P>
+    static __device__ __forceinline__ P* at_slot(const Channels<P>& x, const Place<S>& at, int s0)
     {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int at = threadIdx.x + i * kThreads, slot = at / S::kAll, n = at % S::kAll;
-            const bool on = ((valid >> slot) & 1) && n < p.states;
-            const int64_t s = s0 + slot;
-            if (B) b[i] = on ? a.b.at(q, s)[n] : from_float<T>(0.0f);
-            if (C) c[i] = on ? a.c.at(q, s)[n] : from_float<T>(0.0f);
+        if constexpr (WIDE) {
+            using Byte = std::conditional_t<std::is_const<P>::value, const char, char>;
+            Byte* const base = reinterpret_cast<Byte*>(x.data + at.q * x.block + at.c0);
+            return reinterpret_cast<P*>(base + ((uint32_t)(s0 + at.slot) * ((uint32_t)x.slot * (uint32_t)sizeof(T)) + (uint32_t)(at.m * S::kV * (int)sizeof(T))));
+        } else {
+            return x.at(at.q, s0 + at.slot) + at.c0 + at.m * S::kV;
         }
     }
-    __device__ __forceinline__ void store(float (*to)[2][S::kAll]) const
+    static __device__ __forceinline__ void load(Piece& v, const Channels<const T>& x, const Place<S>& at, int s0, bool on)
+    {
+        if (WIDE && on && at.there)
+            v.load(at_slot(x, at, s0), S::kV, true);
+        else if (!WIDE && on)
+            v.load(at_slot(x, at, s0), at.there, false);
+        else
+            v.clear();
+    }
+    static __device__ __forceinline__ void store(const Piece& v, const Channels<T>& x, const Place<S>& at, int s0)
+    {
+        if (!WIDE)
+            v.store(at_slot(x, at, s0), at.there, false);
+        else if (at.there)
+            v.store(at_slot(x, at, s0), S::kV, true);
+    }
+};
+
+// b and c of a run, [slot][b, c][kAll] in shared memory; 0 on padding and where there is no state.  In pieces of 16 bytes where rows
+// allow it (p.rows_wide), element by element otherwise.
+template <typename T, typename S, bool B, bool C>
+struct Rows {
+    static constexpr int kV = 16 / sizeof(T) < S::kAll ? 16 / sizeof(T) : S::kAll, kPieces = kRun * S::kAll / kV;
+    static constexpr int kEach = (kPieces + kThreads - 1) / kThreads;
+    Elements<T, kV> b[B ? kEach : 1], c[C ? kEach : 1];
+    __device__ __forceinline__ void load(const ScanParams& p, const ScanTensors<T>& a, int64_t q, int s0, unsigned valid)
+    {
+        const T *const b0 = a.b.data + q * a.b.block, *const c0 = a.c.data + q * a.c.block;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int at = threadIdx.x + i * kThreads, slot = at / (S::kAll / kV), n = at % (S::kAll / kV) * kV;
+            const int there = slot < kRun && ((valid >> slot) & 1) ? p.states - n : 0;
+            b[B ? i : 0].clear();
+            c[C ? i : 0].clear();
+            if (there > 0 && p.rows_wide) {  // (blocks of less than 2^32 elements, too)
+                if (B) b[B ? i : 0].load(b0 + ((uint32_t)(s0 + slot) * (uint32_t)a.b.slot + (uint32_t)n), kV, true);
+                if (C) c[C ? i : 0].load(c0 + ((uint32_t)(s0 + slot) * (uint32_t)a.c.slot + (uint32_t)n), kV, true);
+            } else if (there > 0) {
+                if (B) b[B ? i : 0].load(b0 + (s0 + slot) * a.b.slot + n, there, false);
+                if (C) c[C ? i : 0].load(c0 + (s0 + slot) * a.c.slot + n, there, false);
+            }
+        }
+    }
+    // `turn` 2: with the pairs of every four states the other way round
+    __device__ __forceinline__ void store(float (*to)[2][S::kAll], int turn = 0) const
     {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int at = threadIdx.x + i * kThreads, slot = at / S::kAll, n = at % S::kAll;
-            if (B) to[slot][0][n] = to_float(b[i]);
-            if (C) to[slot][1][n] = to_float(c[i]);
+            const int at = threadIdx.x + i * kThreads, slot = at / (S::kAll / kV), n = at % (S::kAll / kV) * kV;
+            if (slot >= kRun) break;
+#pragma unroll
+            for (int e = 0; e < kV; e += 2) {
+                if (B) *reinterpret_cast<float2*>(&to[slot][0][n + (e ^ turn)]) = make_float2(b[B ? i : 0].get(e), b[B ? i : 0].get(e + 1));
+                if (C) *reinterpret_cast<float2*>(&to[slot][1][n + (e ^ turn)]) = make_float2(c[C ? i : 0].get(e), c[C ? i : 0].get(e + 1));
+            }
         }
     }
 };
@@ -220,36 +322,63 @@ __device__ __forceinline__ void pairs_of(const float* from, Two (&x)[S::kPairs])
     }
 }
 
-// positions of a run: bit s of `valid`: slot s is a frame, of `starts`: it starts a sequence (or is none)
-__device__ __forceinline__ void run_masks(const int32_t* pos, int t, int s0, int lane, unsigned& valid, unsigned& starts)
+// dt_bias or d of a thread's channels, 0 where there is none
+template <int V>
+__device__ __forceinline__ Elements<float, V> of_channels(const float* from, int64_t c, int there)
 {
-    const int here = lane < kRun && s0 + lane < t ? pos[s0 + lane] : -1;
-    valid = __ballot_sync(0xffffffffu, here >= 0) & ((1u << kRun) - 1);
-    starts = __ballot_sync(0xffffffffu, here <= 0) & ((1u << kRun) - 1);
+    Elements<float, V> v;
+    v.clear();
+    if (from) v.load(from + c, there, reinterpret_cast<uintptr_t>(from) % 16 == 0);
+    return v;
+}
+
+// Sums over a channel's lanes of what each has for kGroup slots and its two channels.  The lanes that share a channel have the two in
+// turned order, so the first step hands over one channel without choosing; then the slots are shared out.  A lane ends with its first
+// channel's sum for slot `first`, in v[0][0] (beyond four lanes, several have the same).
+template <typename S>
+__device__ __forceinline__ void lane_sums(float (&v)[2][S::kGroup], int lane, int& first)
+{
+    first = 0;
+#pragma unroll
+    for (int i = 0; i < S::kGroup; ++i) v[0][i] += __shfl_xor_sync(0xffffffffu, v[1][i], 1);
+#pragma unroll
+    for (int bit = 2, n = S::kGroup; bit < S::kLanes; bit *= 2) {
+        if (n > 1) {
+            n /= 2;
+            const bool upper = lane & bit;
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                const float send = upper ? v[0][i] : v[0][i + n], keep = upper ? v[0][i + n] : v[0][i];
+                v[0][i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
+            }
+            if (upper) first += n;
+        } else {
+            v[0][0] += __shfl_xor_sync(0xffffffffu, v[0][0], bit);
+        }
+    }
 }
 
 // OUTPUT false: leaves what crosses the segment's end (kind, delta, state of ScanWork).
-template <typename T, typename S, bool OUTPUT>
-__global__ void __launch_bounds__(kThreads) k37_scan(const ScanParams p, const ScanTensors<T> a, const ScanCuts cuts, const ScanWork work, bool wide)
+template <typename T, typename S, bool WIDE, bool OUTPUT>
+__global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, const ScanTensors<T> a, const ScanCuts cuts, const ScanWork work)
 {
-    __shared__ __align__(16) float2 prepared[kRun][S::kChannels];  // delta, delta x
+    __shared__ __align__(16) float4 prepared[kRun][S::kChannels];  // delta, delta, delta x, delta x
     __shared__ __align__(16) float rows[kRun][2][S::kAll];
-    __shared__ __align__(8) float sums[OUTPUT ? kRun : 1][OUTPUT ? S::kChannels : 2];
+    __shared__ float sums[OUTPUT ? kRun : 1][OUTPUT ? S::kRow : 1];
 
     const Place<S> at(p, cuts);
     const int32_t* const pos = p.pos + at.q * p.t;
-    const int runs = (p.t + kRun - 1) / kRun;
-    int run = at.first;
-    const int64_t cell = (int64_t)at.segment * p.blocks + at.q, per = p.channels * p.states;
+    const int runs = (p.t + kRun - 1) / kRun, end = (at.stop + kRun - 1) / kRun;
+    int run = at.begin / kRun;
+    const int64_t cell = (int64_t)at.segment * p.blocks + at.q, per = p.channels * p.states, first_state = at.c0 * p.states;
     if (!OUTPUT) {
-        const int edge = at.end * kRun;  // of a segment that is not the last: below t
-        if (at.segment == cuts.segments - 1 || at.first == at.end || pos[edge] <= 0) {
+        if (!at.leaves || at.stop <= at.begin) {
             if (threadIdx.x == 0) work.kind[cell] = 0;
             return;
         }
-        const int start = edge - min(pos[edge], edge);
-        run = max(at.first, min(start / kRun, at.end - 1));
-        if (threadIdx.x == 0) work.kind[cell] = start < at.first * kRun ? 2 : 1;
+        const int start = at.stop - min(pos[at.stop], at.stop);  // of the sequence
+        run = max(run, min(start / kRun, end - 1));
+        if (threadIdx.x == 0) work.kind[cell] = start < at.begin ? 2 : 1;
     }
     Two A[2][S::kPairs], h[2][S::kPairs];
     load_a(p, at, kLog2E, A);
@@ -257,68 +386,62 @@ __global__ void __launch_bounds__(kThreads) k37_scan(const ScanParams p, const S
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int k = 0; k < S::kPairs; ++k) h[c][k] = zero();
-    if (OUTPUT && at.segment > 0 && at.first < at.end && pos[at.first * kRun] > 0)
-        load_states(p, at, work.state + (cell - p.blocks) * per, h);
+    if (OUTPUT && at.enters && at.begin < at.stop) load_states(p, at, work.state + (cell - p.blocks) * per + first_state, h);
 
-    float bias[S::kV], skip[S::kV], passed[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int e = 0; e < S::kV; ++e) {
-        const int64_t c = at.c0 + at.c_mem + e;
-        bias[e] = p.dt_bias && e < at.there ? p.dt_bias[c] : 0.0f;
-        skip[e] = OUTPUT && p.d && e < at.there ? p.d[c] : 0.0f;
-    }
-    const bool gated = OUTPUT && a.z.data;
+    float passed[2] = {0.0f, 0.0f};
+    const int64_t c_mem = at.c0 + at.m * S::kV;
+    const bool gated = OUTPUT && a.z.data, softplus = p.softplus;
 
+    using F = Frames<T, S, WIDE>;
     Elements<T, S::kV> x, dt, z;
+    z.clear();
     Rows<T, S, true, OUTPUT> bc;
-    unsigned valid, starts;
+    unsigned valid, starts, ends = 0;
     auto fetch = [&](int r) {
         const int s0 = r * kRun;
-        run_masks(pos, p.t, s0, at.lane, valid, starts);
+        at.masks(pos, p.t, s0, valid, starts, OUTPUT && p.last ? &ends : nullptr);
         const bool on = (valid >> at.slot) & 1;
-        const int64_t s = s0 + at.slot, c = at.c0 + at.c_mem;
-        x.clear();
-        dt.clear();
-        z.clear();
-        if (on) {
-            x.load(a.x.at(at.q, s) + c, at.there, wide);
-            dt.load(a.dt.at(at.q, s) + c, at.there, wide);
-            if (gated) z.load(a.z.at(at.q, s) + c, at.there, wide);
-        }
+        F::load(x, a.x, at, s0, on);
+        F::load(dt, a.dt, at, s0, on);
+        if (gated) F::load(z, a.z, at, s0, on);
         bc.load(p, a, at.q, s0, valid);
     };
-    if (run < at.end) fetch(run);
-    for (; run < at.end; ++run) {
+    if (run < end) fetch(run);
+    for (; run < end; ++run) {
         const int s0 = run * kRun;
-        const unsigned now_valid = valid, now_starts = starts;
+        const unsigned now_starts = starts, now_ends = ends;
         const Elements<T, S::kV> now_x = x, now_z = z;
-        {
-            const bool on = (valid >> at.slot) & 1;
+        const bool on = (valid >> at.slot) & 1;
+        if (on) {
+            const auto bias = of_channels<S::kV>(p.dt_bias, c_mem, at.there);
 #pragma unroll
-            for (int e = 0; e < S::kV; ++e) {
-                float delta, slope;
-                delta_of(p, dt.get(e) + bias[e], delta, slope);
-                if (!on || e >= at.there) delta = 0.0f;
-                prepared[at.slot][at.c_mem + e] = make_float2(delta, delta * x.get(e));
+            for (int e = 0; e < S::kV; e += 2) {
+                Two delta = dt.pair(e) + bias.pair(e);
+                if (softplus) delta = softplus_of(delta);
+                if (!WIDE) delta = two(e < at.there ? one(delta).x : 0.0f, e + 1 < at.there ? one(delta).y : 0.0f);
+                const float2 d = one(delta), u = one(delta * x.pair(e));
+                prepared[at.slot][e * 8 + at.m] = make_float4(d.x, d.x, u.x, u.x);
+                prepared[at.slot][e * 8 + 8 + at.m] = make_float4(d.y, d.y, u.y, u.y);
             }
+        } else {
+#pragma unroll
+            for (int e = 0; e < S::kV; ++e) prepared[at.slot][e * 8 + at.m] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
         bc.store(rows);
-        if (OUTPUT && p.carry) store_states(p, at, p.carry + (at.q * runs + run) * per, h);
+        if (OUTPUT && p.carry && s0 >= at.begin) store_states(p, at, p.carry + (at.q * runs + run) * per + first_state, h);
         __syncthreads();
-        if (run + 1 < at.end) fetch(run + 1);
+        if (run + 1 < end) fetch(run + 1);
 
-#pragma unroll 1
-        for (int g = 0; g < kRun; g += S::kGroup) {
+        auto group = [&](int g, auto with_breaks) {
+            constexpr bool breaks = decltype(with_breaks)::value;
             float y[2][S::kGroup];
 #pragma unroll
             for (int i = 0; i < S::kGroup; ++i) {
                 const int s = g + i;
-                const float4 d = *reinterpret_cast<const float4*>(&prepared[s][at.c_lane]);
                 Two B[S::kPairs], C[S::kPairs];
                 pairs_of<S>(&rows[s][0][at.part * S::kStates], B);
                 if (OUTPUT) pairs_of<S>(&rows[s][1][at.part * S::kStates], C);
-                const Two delta[2] = {two(d.x, d.x), two(d.z, d.z)}, u[2] = {two(d.y, d.y), two(d.w, d.w)};
-                if ((now_starts >> s) & 1) {
+                if (breaks && ((now_starts >> s) & 1)) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -326,70 +449,61 @@ __global__ void __launch_bounds__(kThreads) k37_scan(const ScanParams p, const S
                 }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
+                    const float4 d = prepared[s][at.at[c]];
+                    const Two delta = two(d.x, d.y), u = two(d.z, d.w);
                     Two sum = zero();
 #pragma unroll
                     for (int k = 0; k < S::kPairs; ++k) {
-                        h[c][k] = fma(decay(delta[c], A[c][k]), h[c][k], u[c] * B[k]);
+                        h[c][k] = fma(decay(delta, A[c][k]), h[c][k], u * B[k]);
                         if (OUTPUT) sum = k ? fma(h[c][k], C[k], sum) : h[c][k] * C[k];
                     }
                     y[c][i] = one(sum).x + one(sum).y;
+                    if (!OUTPUT) passed[c] += d.x;
                 }
-                if (!OUTPUT) {
-                    passed[0] += d.x;
-                    passed[1] += d.z;
-                }
-                if (OUTPUT && p.last && ((now_valid >> s) & 1)) {
-                    const int here = s0 + s;
-                    if (here + 1 >= p.t || pos[here + 1] <= 0) {  // the sequence ends (uniform)
-                        const int64_t id = p.seq_id[at.q * p.t + here];
-                        if (id >= 0 && id < p.n_seq) store_states(p, at, p.last + id * per, h);
-                    }
+                if (OUTPUT && breaks && ((now_ends >> s) & 1)) {
+                    const int64_t id = p.seq_id[at.q * p.t + s0 + s];
+                    if (id >= 0 && id < p.n_seq) store_states(p, at, p.last + id * per + first_state, h);
                 }
             }
             if (OUTPUT) {
-                // over the channel's lanes: they end with a slot each (beyond four lanes, with copies of four)
-                int which[2] = {0, 0};
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-#pragma unroll
-                    for (int bit = S::kLanes / 2, n = S::kGroup; bit; bit /= 2) {
-                        if (n > 1) {
-                            n /= 2;
-                            const bool upper = at.lane & bit;
-#pragma unroll
-                            for (int i = 0; i < n; ++i) {
-                                const float send = upper ? y[c][i] : y[c][i + n], keep = upper ? y[c][i + n] : y[c][i];
-                                y[c][i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
-                            }
-                            if (upper) which[c] += n;
-                        } else {
-                            y[c][0] += __shfl_xor_sync(0xffffffffu, y[c][0], bit);
-                        }
-                    }
-                }
-                if (S::kLanes <= S::kGroup || at.part % (S::kLanes / S::kGroup) == 0)
-                    *reinterpret_cast<float2*>(&sums[g + which[0]][at.c_lane]) = make_float2(y[0][0], y[1][0]);
+                int first;
+                lane_sums<S>(y, at.lane, first);
+                sums[g + first][at.at[0]] = y[0][0];
+            }
+        };
+#pragma unroll 1
+        for (int g = 0; g < kRun; g += 2 * S::kGroup) {
+            if (((now_starts | now_ends) >> g) & ((1 << 2 * S::kGroup) - 1)) {
+                group(g, std::true_type());
+                group(g + S::kGroup, std::true_type());
+            } else {
+                group(g, std::false_type());
+                group(g + S::kGroup, std::false_type());
             }
         }
         __syncthreads();
-        if (OUTPUT && s0 + at.slot < p.t) {
-            const bool on = (now_valid >> at.slot) & 1;
+        if (OUTPUT && s0 + at.slot >= at.begin && s0 + at.slot < at.stop) {
             Elements<T, S::kV> out;
+            if (on) {
+                const auto skip = of_channels<S::kV>(p.d, c_mem, at.there);
 #pragma unroll
-            for (int e = 0; e < S::kV; ++e) {
-                float v = fmaf(skip[e], now_x.get(e), sums[at.slot][at.c_mem + e]);
-                if (gated) v *= now_z.get(e) * sigmoid_of(now_z.get(e));
-                out.set(e, on ? v : 0.0f);
+                for (int e = 0; e < S::kV; e += 2) {
+                    Two v = fma(skip.pair(e), now_x.pair(e), two(sums[at.slot][e * 8 + at.m], sums[at.slot][e * 8 + 8 + at.m]));
+                    if (gated) v = v * (now_z.pair(e) * sigmoid_of(now_z.pair(e)));
+                    out.set_pair(e, v);
+                }
+            } else {
+                out.clear();
             }
-            out.store(a.y.at(at.q, s0 + at.slot) + at.c0 + at.c_mem, at.there, wide);
+            F::store(out, a.y, at, s0);
         }
     }
     if (!OUTPUT) {
-        store_states(p, at, work.state + cell * per, h);
+        store_states(p, at, work.state + cell * per + first_state, h);
         if (at.part == 0) {
 #pragma unroll
             for (int c = 0; c < 2; ++c)
-                if (at.c0 + at.c_lane + c < p.channels) work.delta[cell * p.channels + at.c0 + at.c_lane + c] = passed[c];
+                if (at.c0 + at.ch[c] < p.channels) work.delta[cell * p.channels + at.c0 + at.ch[c]] = passed[c];
         }
     }
 }
@@ -403,286 +517,371 @@ __global__ void __launch_bounds__(256) k38_scan_join(const ScanParams p, const S
     const int64_t q = i / per, c = (i - q * per) / p.states;
     const float a = p.a[i - q * per] * kLog2E;
     float state = 0.0f;
-    for (int k = 0; k < cuts.segments; ++k) {
-        const int64_t cell = (int64_t)(backwards ? cuts.segments - 1 - k : k) * p.blocks + q;
-        const int kind = work.kind[cell];
-        if (kind == 0) {
-            state = 0.0f;
-            continue;
+    constexpr int kAhead = 8;  // segments whose values are loaded together
+    for (int k0 = 0; k0 < cuts.segments; k0 += kAhead) {
+        int kind[kAhead];
+        float delta[kAhead], own[kAhead];
+        auto cell = [&](int j) { return (int64_t)(backwards ? cuts.segments - 1 - k0 - j : k0 + j) * p.blocks + q; };
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            kind[j] = k0 + j < cuts.segments ? work.kind[cell(j)] : 0;
+            delta[j] = k0 + j < cuts.segments ? work.delta[cell(j) * p.channels + c] : 0.0f;
+            own[j] = k0 + j < cuts.segments ? work.state[cell(j) * per + (i - q * per)] : 0.0f;
         }
-        float* const at = work.state + cell * per + (i - q * per);
-        state = kind == 2 ? fmaf(ex2(work.delta[cell * p.channels + c] * a), state, *at) : *at;
-        *at = state;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            // (kind 0: nothing was written)
+            state = kind[j] == 0 ? 0.0f : kind[j] == 2 ? fmaf(ex2(delta[j] * a), state, own[j]) : own[j];
+            if (kind[j] == 2) work.state[cell(j) * per + (i - q * per)] = state;
+        }
     }
 }
 
-// dy times the gate, and what the gate's gradient needs
-__device__ __forceinline__ float silu_slope(float z, float sig) { return sig * fmaf(z, 1.0f - sig, 1.0f); }
-
 template <typename S>
 struct GradShared {
-    float4 kept[kRun][S::kPairs][kThreads];     // exp(delta a) h of the slot before, of a thread's states: pair by pair, both channels
-    float4 prepared[kRun][S::kChannels];        // delta, delta x, gated dy; then sums over states: g b, g a h, h c (w stays: delta)
-    float rows[kRun][2][S::kAll];
-    float across[kWarps][kRun][2 * S::kAll];    // db, dc of a warp's channels
+    float4 prepared[kRun][S::kChannels];  // delta, delta, delta x, delta x; then sums over states: g b, g a h, h c, and delta
+    float dv[kRun][S::kChannels];         // dy times the gate
+    float rows[2][kRun][2][S::kAll];      // b, c as they are, and with the pairs of each lane's states the other way round
+    // The states that enter every other slot, of a thread: pair by pair, both channels.  Where a warp has read those of two slots, it
+    // leaves their db and dc, of its channels.
+    float4 kept[kRun / 2][S::kPairs][kThreads];
+    __device__ float* across(int warp, int slot)
+    {
+        constexpr bool two_planes = S::kPairs == 2;
+        return reinterpret_cast<float*>(&kept[slot / 2][two_planes ? slot & 1 : 0][warp * 32]) + (two_planes ? 0 : (slot & 1) * 2 * S::kAll);
+    }
 };
+template <typename S>
+constexpr int kPartShared = offsetof(GradShared<S>, kept);  // without output
 
 // OUTPUT false: leaves what crosses the segment's first slot, backwards.
-template <typename T, typename S, bool OUTPUT>
-__global__ void __launch_bounds__(kThreads) k39_scan_grad(const ScanParams p, const ScanTensors<T> a, const ScanCuts cuts, const ScanWork work, bool wide)
+template <typename T, typename S, bool WIDE, bool OUTPUT>
+__global__ void __launch_bounds__(kThreads, 4)
+    k39_scan_grad(const ScanParams p, const ScanTensors<T> a, const ScanCuts cuts, const ScanWork work)
 {
     extern __shared__ __align__(16) uint8_t shared_bytes[];
     GradShared<S>& sh = *reinterpret_cast<GradShared<S>*>(shared_bytes);
 
     const Place<S> at(p, cuts);
     const int32_t* const pos = p.pos + at.q * p.t;
-    const int runs = (p.t + kRun - 1) / kRun;
-    const int64_t cell = (int64_t)at.segment * p.blocks + at.q, per = p.channels * p.states;
-    int run = at.end - 1;
+    const int runs = (p.t + kRun - 1) / kRun, first = at.begin / kRun;
+    const int64_t cell = (int64_t)at.segment * p.blocks + at.q, per = p.channels * p.states, first_state = at.c0 * p.states;
+    int run = at.begin < at.stop ? (at.stop - 1) / kRun : first - 1;
     if (!OUTPUT) {
-        const int edge = at.first * kRun;
-        if (at.segment == 0 || at.first == at.end || pos[edge] <= 0) {
+        if (!at.enters || at.stop <= at.begin) {
             if (threadIdx.x == 0) work.kind[cell] = 0;
             return;
         }
-        const int stop = warp_seq_end(pos, p.t, edge, at.lane);  // in (edge, t]
-        run = min((stop - 1) / kRun, at.end - 1);
-        // (the sequence goes on into the next segment: what enters there is handed on)
-        if (threadIdx.x == 0) work.kind[cell] = stop > at.end * kRun && at.end < runs ? 2 : 1;
+        const int end = warp_seq_end(pos, p.t, at.begin, at.lane);  // of the sequence
+        run = min((end - 1) / kRun, run);
+        // (it goes on into the next segment: what enters there is handed on)
+        if (threadIdx.x == 0) work.kind[cell] = at.leaves && end > at.stop ? 2 : 1;
     }
+    // The state pairs of the lanes of a warp's upper half are the other way round, so that the first step of the sums over channels
+    // hands over one of them without choosing.
+    const int turned = S::kPairs == 2 && (at.lane & 16) ? 1 : 0;
+    const float* const b_rows = &sh.rows[turned][0][0][at.part * S::kStates];
     Two A[2][S::kPairs], e[2][S::kPairs], dA[2][S::kPairs];  // e: exp(delta a) g of the slot behind
+    auto turn = [&](Two (&v)[2][S::kPairs]) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const Two x = v[c][0], y = v[c][S::kPairs - 1];
+            v[c][0].v = turned ? y.v : x.v;
+            v[c][S::kPairs - 1].v = turned ? x.v : y.v;
+        }
+    };
     load_a(p, at, kLog2E, A);
+    turn(A);
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int k = 0; k < S::kPairs; ++k) e[c][k] = dA[c][k] = zero();
-    if (OUTPUT && at.segment + 1 < cuts.segments && at.first < at.end && pos[at.end * kRun] > 0)
-        load_states(p, at, work.state + (cell + p.blocks) * per, e);
-
-    float bias[S::kV], skip[S::kV], d_skip[S::kV], d_bias[S::kV], passed[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < S::kV; ++i) {
-        const int64_t c = at.c0 + at.c_mem + i;
-        bias[i] = p.dt_bias && i < at.there ? p.dt_bias[c] : 0.0f;
-        skip[i] = p.d && i < at.there ? p.d[c] : 0.0f;
-        d_skip[i] = d_bias[i] = 0.0f;
+    if (OUTPUT && at.leaves && at.begin < at.stop) {
+        load_states(p, at, work.state + (cell + p.blocks) * per + first_state, e);
+        turn(e);
     }
-    const bool gated = a.z.data != nullptr;
 
-    for (; run >= at.first; --run) {
+    Two d_skip[S::kV / 2], d_bias[S::kV / 2];
+    float passed[2] = {0.0f, 0.0f};
+    const int64_t c_mem = at.c0 + at.m * S::kV;
+#pragma unroll
+    for (int i = 0; i < S::kV / 2; ++i) d_skip[i] = d_bias[i] = zero();
+    const bool gated = a.z.data != nullptr, softplus = p.softplus;
+    using F = Frames<T, S, WIDE>;
+
+    for (; run >= first; --run) {
         const int s0 = run * kRun;
         unsigned valid, starts;
-        run_masks(pos, p.t, s0, at.lane, valid, starts);
+        at.masks(pos, p.t, s0, valid, starts);
         const bool on = (valid >> at.slot) & 1;
-        const int64_t s_mem = s0 + at.slot, c_mem = at.c0 + at.c_mem;
-        Elements<T, S::kV> x, dt, z, dy;
-        x.clear();
-        dt.clear();
-        z.clear();
-        dy.clear();
-        if (on) {
-            if (OUTPUT) x.load(a.x.at(at.q, s_mem) + c_mem, at.there, wide);
-            dt.load(a.dt.at(at.q, s_mem) + c_mem, at.there, wide);
-            dy.load(a.dy.at(at.q, s_mem) + c_mem, at.there, wide);
-            if (gated) z.load(a.z.at(at.q, s_mem) + c_mem, at.there, wide);
-        }
-        Rows<T, S, OUTPUT, true> bc;
-        bc.load(p, a, at.q, s0, valid);
         Two h[2][S::kPairs];
-        if (OUTPUT) load_states(p, at, p.carry + (at.q * runs + run) * per, h);
+        {
+            Elements<T, S::kV> x, dt, z, dy;
+            x.clear();
+            z.clear();
+            if (OUTPUT) F::load(x, a.x, at, s0, on);
+            F::load(dt, a.dt, at, s0, on);
+            F::load(dy, a.dy, at, s0, on);
+            if (gated) F::load(z, a.z, at, s0, on);
+            Rows<T, S, OUTPUT, true> bc;
+            bc.load(p, a, at.q, s0, valid);
+            if (OUTPUT) {
+                load_states(p, at, p.carry + (at.q * runs + run) * per + first_state, h);
+                turn(h);
+            }
+            if (on) {
+                const auto bias = of_channels<S::kV>(p.dt_bias, c_mem, at.there);
 #pragma unroll
-        for (int i = 0; i < S::kV; ++i) {
-            float delta, slope, g = dy.get(i);
-            delta_of(p, dt.get(i) + bias[i], delta, slope);
-            if (!on || i >= at.there) delta = 0.0f;
-            if (gated) g *= z.get(i) * sigmoid_of(z.get(i));
-            sh.prepared[at.slot][at.c_mem + i] = make_float4(delta, delta * x.get(i), g, delta);
+                for (int i = 0; i < S::kV; i += 2) {
+                    Two delta = dt.pair(i) + bias.pair(i), g = dy.pair(i);
+                    if (softplus) delta = softplus_of(delta);
+                    if (!WIDE) delta = two(i < at.there ? one(delta).x : 0.0f, i + 1 < at.there ? one(delta).y : 0.0f);
+                    if (gated) g = g * (z.pair(i) * sigmoid_of(z.pair(i)));
+                    const float2 d = one(delta), u = one(delta * x.pair(i)), dv = one(g);
+                    sh.prepared[at.slot][i * 8 + at.m] = make_float4(d.x, d.x, u.x, u.x);
+                    sh.prepared[at.slot][i * 8 + 8 + at.m] = make_float4(d.y, d.y, u.y, u.y);
+                    sh.dv[at.slot][i * 8 + at.m] = dv.x;
+                    sh.dv[at.slot][i * 8 + 8 + at.m] = dv.y;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < S::kV; ++i) {
+                    sh.prepared[at.slot][i * 8 + at.m] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    sh.dv[at.slot][i * 8 + at.m] = 0.0f;
+                }
+            }
+            bc.store(sh.rows[0]);
+            if (S::kPairs == 2) bc.store(sh.rows[1], 2);
         }
-        bc.store(sh.rows);
         __syncthreads();
 
-        if (OUTPUT) {
-#pragma unroll 4
-            for (int s = 0; s < kRun; ++s) {
-                const float2 d0 = *reinterpret_cast<const float2*>(&sh.prepared[s][at.c_lane]), d1 = *reinterpret_cast<const float2*>(&sh.prepared[s][at.c_lane + 1]);
-                Two B[S::kPairs];
-                pairs_of<S>(&sh.rows[s][0][at.part * S::kStates], B);
-                const Two delta[2] = {two(d0.x, d0.x), two(d1.x, d1.x)}, u[2] = {two(d0.y, d0.y), two(d1.y, d1.y)};
-                const bool start = (starts >> s) & 1;
+        if (OUTPUT) {  // the states that enter the even slots
+            auto forward = [&](int g, auto with_breaks) {
+                constexpr bool breaks = decltype(with_breaks)::value;
 #pragma unroll
-                for (int k = 0; k < S::kPairs; ++k) {
-                    float2 w[2];
+                for (int i = 0; i < 4; ++i) {
+                    const int s = g + i;
+                    if (i % 2 == 0)
+#pragma unroll
+                        for (int k = 0; k < S::kPairs; ++k) {
+                            const float2 x = one(h[0][k]), y = one(h[1][k]);
+                            sh.kept[s / 2][k][threadIdx.x] = make_float4(x.x, x.y, y.x, y.y);
+                        }
+                    Two B[S::kPairs];
+                    pairs_of<S>(b_rows + s * 2 * S::kAll, B);
+                    const bool start = breaks && ((starts >> s) & 1);
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const Two v = start ? zero() : decay(delta[c], A[c][k]) * h[c][k];
-                        w[c] = one(v);
-                        h[c][k] = fma(u[c], B[k], v);
+                        const float4 d = sh.prepared[s][at.at[c]];
+#pragma unroll
+                        for (int k = 0; k < S::kPairs; ++k) {
+                            const Two push = two(d.z, d.w) * B[k];
+                            h[c][k] = start ? push : fma(decay(two(d.x, d.y), A[c][k]), h[c][k], push);
+                        }
                     }
-                    sh.kept[s][k][threadIdx.x] = make_float4(w[0].x, w[0].y, w[1].x, w[1].y);
                 }
+            };
+#pragma unroll 1
+            for (int g = 0; g < kRun; g += 4) {
+                if ((starts >> g) & 15)
+                    forward(g, std::true_type());
+                else
+                    forward(g, std::false_type());
             }
         }
 
-#pragma unroll 1
-        for (int g0 = kRun - S::kGroup; g0 >= 0; g0 -= S::kGroup) {
+        auto backward = [&](int g0, auto with_breaks) {
+            constexpr bool breaks = decltype(with_breaks)::value;
             float sum[3][2][S::kGroup];  // over states: g b, g a h, h c
+            {
+                constexpr int i0 = 0;
+                Two decays[2][2][S::kPairs], w[2][2][S::kPairs], now[2][2][S::kPairs];  // exp(delta a), exp(delta a) h before, h
 #pragma unroll
-            for (int i = S::kGroup - 1; i >= 0; --i) {
-                const int s = g0 + i;
-                const float4 d0 = sh.prepared[s][at.c_lane], d1 = sh.prepared[s][at.c_lane + 1];
-                Two B[S::kPairs], C[S::kPairs];
-                if (OUTPUT) pairs_of<S>(&sh.rows[s][0][at.part * S::kStates], B);
-                pairs_of<S>(&sh.rows[s][1][at.part * S::kStates], C);
-                const Two delta[2] = {two(d0.x, d0.x), two(d1.x, d1.x)}, u[2] = {two(d0.y, d0.y), two(d1.y, d1.y)},
-                          dv[2] = {two(d0.z, d0.z), two(d1.z, d1.z)};
-                const bool start = (starts >> s) & 1;
-                Two gb[2], gah[2], hc[2];
-                float v[4 * S::kPairs];
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int k = 0; k < S::kPairs; ++k) {
-                    Two w[2], db, dc;
-                    if (OUTPUT) {
-                        const float4 kept = sh.kept[s][k][threadIdx.x];
-                        w[0] = two(kept.x, kept.y);
-                        w[1] = two(kept.z, kept.w);
-                    }
+                    for (int i = 0; i < 2; ++i) {
+                        const int s = g0 + i0 + i;
+                        const float4 d = sh.prepared[s][at.at[c]];
+                        Two B[S::kPairs];
+                        if (OUTPUT) pairs_of<S>(b_rows + s * 2 * S::kAll, B);
+                        const bool start = breaks && ((starts >> s) & 1);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const Two g = fma(dv[c], C[k], e[c][k]);
-                        if (OUTPUT) {
-                            const Two now = fma(u[c], B[k], w[c]), gw = g * w[c];
-                            hc[c] = k ? fma(now, C[k], hc[c]) : now * C[k];
-                            dc = c ? fma(dv[c], now, dc) : dv[c] * now;
-                            db = c ? fma(u[c], g, db) : u[c] * g;
-                            gb[c] = k ? fma(g, B[k], gb[c]) : g * B[k];
-                            gah[c] = k ? fma(gw, A[c][k], gah[c]) : gw * A[c][k];
-                            dA[c][k] = fma(gw, delta[c], dA[c][k]);
+                        for (int k = 0; k < S::kPairs; ++k) {
+                            decays[i][c][k] = decay(two(d.x, d.y), A[c][k]);
+                            if (OUTPUT) {
+                                Two before;
+                                if (i) {
+                                    before = now[0][c][k];
+                                } else {
+                                    const float2 x = reinterpret_cast<const float2*>(&sh.kept[s / 2][k][threadIdx.x])[c];
+                                    before = two(x.x, x.y);
+                                }
+                                w[i][c][k] = decays[i][c][k] * before;
+                                if (start) w[i][c][k] = zero();
+                                now[i][c][k] = fma(two(d.z, d.w), B[k], w[i][c][k]);
+                            }
+                            if (start) decays[i][c][k] = zero();
                         }
-                        e[c][k] = start ? zero() : decay(delta[c], A[c][k]) * g;
+                        if (!OUTPUT) passed[c] += d.x;
                     }
-                    if (OUTPUT) {
-                        v[2 * k] = one(db).x;
-                        v[2 * k + 1] = one(db).y;
-                        v[2 * S::kPairs + 2 * k] = one(dc).x;
-                        v[2 * S::kPairs + 2 * k + 1] = one(dc).y;
-                    }
-                }
-                if (OUTPUT) {
+#pragma unroll
+                for (int i = 1; i >= 0; --i) {
+                    const int s = g0 + i0 + i;
+                    Two B[S::kPairs], C[S::kPairs], db[S::kPairs], dc[S::kPairs];
+                    if (OUTPUT) pairs_of<S>(b_rows + s * 2 * S::kAll, B);
+                    pairs_of<S>(b_rows + s * 2 * S::kAll + S::kAll, C);
+                    const bool start = breaks && ((starts >> s) & 1);
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        sum[0][c][i] = one(gb[c]).x + one(gb[c]).y;
-                        sum[1][c][i] = one(gah[c]).x + one(gah[c]).y;
-                        sum[2][c][i] = one(hc[c]).x + one(hc[c]).y;
-                    }
-                    int first = 0;
-                    share_sums<4 * S::kPairs, 16, S::kLanes>(v, at.lane, first);
-                    constexpr int kLeft = Shared<4 * S::kPairs, S::kLanes>::kLeft;
-                    // (where the warp has more lanes for a state than values, copies write the same)
+                        const float4 d = sh.prepared[s][at.at[c]];
+                        const float dv1 = sh.dv[s][at.at[c]];
+                        const Two dv = two(dv1, dv1), u = two(d.z, d.w), delta = two(d.x, d.y);
+                        Two gb, gah, hc;
 #pragma unroll
-                    for (int j = 0; j < kLeft; ++j) {
-                        const int n = first + j, of_c = n >= 2 * S::kPairs;
-                        sh.across[at.warp][s][of_c * S::kAll + at.part * S::kStates + n - of_c * 2 * S::kPairs] = v[j];
+                        for (int k = 0; k < S::kPairs; ++k) {
+                            const Two g = fma(dv, C[k], e[c][k]);
+                            if (OUTPUT) {
+                                const Two h1 = now[i][c][k], gw = g * w[i][c][k];
+                                hc = k ? fma(h1, C[k], hc) : h1 * C[k];
+                                dc[k] = c ? fma(dv, h1, dc[k]) : dv * h1;
+                                db[k] = c ? fma(u, g, db[k]) : u * g;
+                                gb = k ? fma(g, B[k], gb) : g * B[k];
+                                gah = k ? fma(gw, A[c][k], gah) : gw * A[c][k];
+                                dA[c][k] = fma(gw, delta, dA[c][k]);
+                            }
+                            e[c][k] = decays[i][c][k] * g;
+                            if (start) e[c][k] = zero();
+                        }
+                        if (OUTPUT) {
+                            sum[0][c][i0 + i] = one(gb).x + one(gb).y;
+                            sum[1][c][i0 + i] = one(gah).x + one(gah).y;
+                            sum[2][c][i0 + i] = one(hc).x + one(hc).y;
+                        }
                     }
-                } else {
-                    passed[0] += d0.x;
-                    passed[1] += d1.x;
+                    if (OUTPUT) {
+                        float v[4];  // of one pair of states: db, dc
+                        if (S::kPairs == 2) {
+                            const float2 b1 = one(db[S::kPairs - 1]), c1 = one(dc[S::kPairs - 1]);
+                            const Two b2 = two(__shfl_xor_sync(0xffffffffu, b1.x, 16), __shfl_xor_sync(0xffffffffu, b1.y, 16));
+                            const Two c2 = two(__shfl_xor_sync(0xffffffffu, c1.x, 16), __shfl_xor_sync(0xffffffffu, c1.y, 16));
+                            const float2 b0 = one(db[0] + b2), c0 = one(dc[0] + c2);
+                            v[0] = b0.x;
+                            v[1] = b0.y;
+                            v[2] = c0.x;
+                            v[3] = c0.y;
+                        } else {
+                            v[0] = one(db[0]).x;
+                            v[1] = one(db[0]).y;
+                            v[2] = one(dc[0]).x;
+                            v[3] = one(dc[0]).y;
+                        }
+                        constexpr int kTop = S::kPairs == 2 ? 8 : 16;  // the highest lane bit that is left
+                        constexpr int kSteps = S::kLanes == 4 ? (kTop == 8 ? 2 : 3) : S::kLanes == 8 ? 1 : 0, kLeft = 4 >> kSteps ? 4 >> kSteps : 1;
+                        int from = 0;
+                        share_sums<4, kTop, S::kLanes>(v, at.lane, from);
+                        if (i == 1) __syncwarp();  // all lanes have read the states of both slots
+                        // (where the warp has more lanes for a state than values, copies write the same)
+#pragma unroll
+                        for (int j = 0; j < kLeft; ++j) {
+                            const int n = from + j;
+                            sh.across(at.warp, s)[(n >> 1) * S::kAll + at.part * S::kStates + 2 * turned + (n & 1)] = v[j];
+                        }
+                    }
                 }
             }
             if (OUTPUT) {
-                int which = 0;
+                int slot = 0;
 #pragma unroll
-                for (int m = 0; m < 3; ++m)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        which = 0;
-#pragma unroll
-                        for (int bit = S::kLanes / 2, n = S::kGroup; bit; bit /= 2) {
-                            float* const y = sum[m][c];
-                            if (n > 1) {
-                                n /= 2;
-                                const bool upper = at.lane & bit;
-#pragma unroll
-                                for (int i = 0; i < n; ++i) {
-                                    const float send = upper ? y[i] : y[i + n], keep = upper ? y[i + n] : y[i];
-                                    y[i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
-                                }
-                                if (upper) which += n;
-                            } else {
-                                y[0] += __shfl_xor_sync(0xffffffffu, y[0], bit);
-                            }
-                        }
-                    }
+                for (int m = 0; m < 3; ++m) lane_sums<S>(sum[m], at.lane, slot);
                 __syncwarp();  // all lanes have read these slots
-                if (S::kLanes <= S::kGroup || at.part % (S::kLanes / S::kGroup) == 0) {
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        float4& to = sh.prepared[g0 + which][at.c_lane + c];
-                        *reinterpret_cast<float2*>(&to) = make_float2(sum[0][c][0], sum[1][c][0]);
-                        to.z = sum[2][c][0];
-                    }
-                }
+                float4& to = sh.prepared[g0 + slot][at.at[0]];
+                const float delta = to.x;
+                if (S::kLanes > 4) __syncwarp();  // (lanes with the same)
+                to = make_float4(sum[0][0][0], sum[1][0][0], sum[2][0][0], delta);
             }
+        };
+#pragma unroll 1
+        for (int g0 = kRun - S::kGroup; g0 >= 0; g0 -= S::kGroup) {
+            if ((starts >> g0) & ((1 << S::kGroup) - 1))
+                backward(g0, std::true_type());
+            else
+                backward(g0, std::false_type());
         }
         __syncthreads();
-        if (OUTPUT && s_mem < p.t) {
-            Elements<T, S::kV> dx, ddt, dz;
-#pragma unroll
-            for (int i = 0; i < S::kV; ++i) {
-                const float4 r = sh.prepared[at.slot][at.c_mem + i];
-                float value, slope, dv = dy.get(i);
-                delta_of(p, dt.get(i) + bias[i], value, slope);
-                const float xi = x.get(i);
-                if (gated) {
-                    const float zi = z.get(i), sig = sigmoid_of(zi);
-                    dz.set(i, on ? dv * fmaf(skip[i], xi, r.z) * silu_slope(zi, sig) : 0.0f);
-                    dv *= zi * sig;
-                }
-                const float dd = on ? fmaf(xi, r.x, r.y * kLn2) * slope : 0.0f;
-                ddt.set(i, dd);
-                dx.set(i, on ? fmaf(r.w, r.x, skip[i] * dv) : 0.0f);
-                d_bias[i] += dd;
-                if (on) d_skip[i] = fmaf(dv, xi, d_skip[i]);
-            }
-            dx.store(a.dx.at(at.q, s_mem) + c_mem, at.there, wide);
-            ddt.store(a.ddt.at(at.q, s_mem) + c_mem, at.there, wide);
-            if (gated) dz.store(a.dz.at(at.q, s_mem) + c_mem, at.there, wide);
-        }
         if (OUTPUT) {
-            const int n2 = 2 * S::kAll;
-            float* const to = work.across + (((blockIdx.x % cuts.groups) * p.blocks + at.q) * (int64_t)p.t + s0) * n2;
-            for (int i = threadIdx.x; i < min(kRun, p.t - s0) * n2; i += kThreads) {
-                float v = 0.0f;
+            if (s0 + at.slot >= at.begin && s0 + at.slot < at.stop) {
+                Elements<T, S::kV> x, dt, z, dy;  // (once more: in registers meanwhile they would cost more)
+                x.clear();
+                dt.clear();
+                z.clear();
+                if (on) {
+                    F::load(x, a.x, at, s0, true);
+                    F::load(dt, a.dt, at, s0, true);
+                    F::load(dy, a.dy, at, s0, true);
+                    if (gated) F::load(z, a.z, at, s0, true);
+                    const auto bias = of_channels<S::kV>(p.dt_bias, c_mem, at.there), skips = of_channels<S::kV>(p.d, c_mem, at.there);
+                    const Two ones = two(1.0f, 1.0f), minus = two(-1.0f, -1.0f), ln2 = two(kLn2, kLn2);
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) v += (&sh.across[w][0][0])[i];
-                to[i] = v;
+                    for (int i = 0; i < S::kV; i += 2) {
+                        const float4 r0 = sh.prepared[at.slot][i * 8 + at.m], r1 = sh.prepared[at.slot][i * 8 + 8 + at.m];
+                        const Two xi = x.pair(i), skip = skips.pair(i), gb = two(r0.x, r1.x), gah = two(r0.y, r1.y);
+                        Two dv = dy.pair(i);
+                        if (gated) {
+                            const Two zi = z.pair(i), sig = sigmoid_of(zi), gate = zi * sig;
+                            // d(z sig) = sig (1 + z (1 - sig)) = sig + gate (1 - sig)
+                            z.set_pair(i, dv * fma(skip, xi, two(r0.z, r1.z)) * fma(gate, fma(sig, minus, ones), sig));
+                            dv = dv * gate;
+                        }
+                        Two dd = fma(xi, gb, gah * ln2);
+                        if (softplus) dd = dd * sigmoid_of(dt.pair(i) + bias.pair(i));
+                        const Two dx = fma(two(r0.w, r1.w), gb, skip * dv);
+                        d_bias[i / 2] = d_bias[i / 2] + dd;
+                        d_skip[i / 2] = fma(dv, xi, d_skip[i / 2]);
+                        x.set_pair(i, dx);
+                        dt.set_pair(i, dd);
+                    }
+                }
+                F::store(x, a.dx, at, s0);
+                F::store(dt, a.ddt, at, s0);
+                if (gated) F::store(z, a.dz, at, s0);
+            }
+            constexpr int n2 = 2 * S::kAll;
+            float* const to = work.across + (((blockIdx.x % cuts.groups) * p.blocks + at.q) * (int64_t)p.t + s0) * n2;
+#pragma unroll
+            for (int i = threadIdx.x; i < kRun * n2 / 4; i += kThreads) {
+                const int slot = i / (n2 / 4), n = i % (n2 / 4) * 4;
+                float4 v = *reinterpret_cast<const float4*>(sh.across(0, slot) + n);
+#pragma unroll
+                for (int w = 1; w < kWarps; ++w) {
+                    const float4 u = *reinterpret_cast<const float4*>(sh.across(w, slot) + n);
+                    v = make_float4(v.x + u.x, v.y + u.y, v.z + u.z, v.w + u.w);
+                }
+                if (s0 + slot >= at.begin && s0 + slot < at.stop) *reinterpret_cast<float4*>(to + i * 4) = v;
             }
         }
         __syncthreads();
     }
     if (!OUTPUT) {
-        store_states(p, at, work.state + cell * per, e);
+        turn(e);
+        store_states(p, at, work.state + cell * per + first_state, e);
         if (at.part == 0) {
 #pragma unroll
             for (int c = 0; c < 2; ++c)
-                if (at.c0 + at.c_lane + c < p.channels) work.delta[cell * p.channels + at.c0 + at.c_lane + c] = passed[c];
+                if (at.c0 + at.ch[c] < p.channels) work.delta[cell * p.channels + at.c0 + at.ch[c]] = passed[c];
         }
         return;
     }
     float* const frames = work.frames + cell * (per + 2 * p.channels);
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int k = 0; k < S::kPairs; ++k) {
-            const int64_t ch = at.c0 + at.c_lane + c;
-            const int n = at.part * S::kStates + 2 * k;
-            if (ch >= p.channels) continue;
-            if (n < p.states) frames[ch * p.states + n] = one(dA[c][k]).x;
-            if (n + 1 < p.states) frames[ch * p.states + n + 1] = one(dA[c][k]).y;
-        }
+    turn(dA);
+    store_states(p, at, frames + first_state, dA);
     // the sixteen slots' threads of a channel, in their order
     float2* const both = reinterpret_cast<float2*>(&sh.kept[0][0][0]);
 #pragma unroll
-    for (int i = 0; i < S::kV; ++i) both[at.slot * S::kChannels + at.c_mem + i] = make_float2(d_skip[i], d_bias[i]);
+    for (int i = 0; i < S::kV; i += 2) {
+        const float2 d = one(d_skip[i / 2]), b = one(d_bias[i / 2]);
+        both[at.slot * S::kChannels + at.m * S::kV + i] = make_float2(d.x, b.x);
+        both[at.slot * S::kChannels + at.m * S::kV + i + 1] = make_float2(d.y, b.y);
+    }
     __syncthreads();
     for (int c = threadIdx.x; c < S::kChannels; c += kThreads) {
         if (at.c0 + c >= p.channels) break;
@@ -763,8 +962,8 @@ __global__ void __launch_bounds__(kThreads) k41_scan_step(const ScanStepParams p
     for (int r = 0; r < kStepRows; ++r) {
         const int64_t row = row0 + r;
         if (row >= p.rows) break;
-        float delta = dt[r] + bias, slope, y = 0.0f;
-        if (p.softplus) softplus_of(delta, delta, slope);
+        float delta = dt[r] + bias, y = 0.0f;
+        if (p.softplus) delta = one(softplus_of(two(delta, delta))).x;
         const float u = delta * x[r];
         if (here[r] >= 0) {
 #pragma unroll
@@ -841,15 +1040,19 @@ ScanWork work_of(void* base, const ScanCuts& cuts, int64_t blocks, int32_t t, in
     return w;
 }
 
+// Tensors whose pieces of `n` bytes lie on boundaries of their size (at most 16), with blocks of t slots that span less than 2^32 bytes
 template <typename T>
-bool on(const Channels<T>& x, size_t n)
+bool on(const Channels<T>& x, size_t n, int32_t t)
 {
-    return !x.data || (reinterpret_cast<uintptr_t>(x.data) % n == 0 && x.block * sizeof(T) % n == 0 && x.slot * sizeof(T) % n == 0);
+    const size_t m = n < 16 ? n : 16;
+    return !x.data || (reinterpret_cast<uintptr_t>(x.data) % m == 0 && x.block * sizeof(T) % m == 0 && x.slot * sizeof(T) % m == 0 &&
+                       (uint64_t)x.slot * sizeof(T) < ((uint64_t)1 << 32) / ((uint64_t)t + 2 * kRun));
 }
-template <typename T, typename S>
-size_t piece()
+template <typename T>
+ScanParams with_rows(ScanParams p, const ScanTensors<T>& a)
 {
-    return S::kV * sizeof(T) < 16 ? S::kV * sizeof(T) : 16;
+    p.rows_wide = on(a.b, 16, p.t) && on(a.c, 16, p.t) && p.states * sizeof(T) % 16 == 0;
+    return p;
 }
 
 cudaError_t join(const ScanParams& p, const ScanCuts& cuts, const ScanWork& work, bool backwards, cudaStream_t st)
@@ -868,51 +1071,58 @@ size_t scan_work_bytes(int64_t blocks, int32_t t, int64_t channels, int32_t stat
 }
 
 template <typename T>
-cudaError_t launch_scan(const ScanParams& p, const ScanTensors<T>& a, cudaStream_t st)
+cudaError_t launch_scan(const ScanParams& params, const ScanTensors<T>& a, cudaStream_t st)
 {
+    const ScanParams p = with_rows(params, a);
     return with_split(p.states, [&](auto s) {
         using S = decltype(s);
         const ScanCuts cuts = cuts_of(p.blocks, p.t, p.channels, p.states);
         const ScanWork work = work_of(p.work, cuts, p.blocks, p.t, p.channels, p.states, false);
-        const size_t n = piece<T, S>();
-        const bool wide = on(a.x, n) && on(a.dt, n) && on(a.z, n) && on(a.y, n);
+        constexpr size_t n = S::kV * sizeof(T);
+        const bool wide = on(a.x, n, p.t) && on(a.dt, n, p.t) && on(a.z, n, p.t) && on(a.y, n, p.t) && p.channels % S::kV == 0;
         const unsigned grid = (unsigned)(cuts.segments * p.blocks * cuts.groups);
         if (cuts.segments > 1) {
-            k37_scan<T, S, false><<<grid, kThreads, 0, st>>>(p, a, cuts, work, wide);
+            auto* part = wide ? k37_scan<T, S, true, false> : k37_scan<T, S, false, false>;
+            part<<<grid, kThreads, 0, st>>>(p, a, cuts, work);
             count_launches(1);
             cudaError_t e = cudaGetLastError();
             if (e == cudaSuccess) e = join(p, cuts, work, false, st);
             if (e != cudaSuccess) return e;
         }
-        k37_scan<T, S, true><<<grid, kThreads, 0, st>>>(p, a, cuts, work, wide);
+        auto* kernel = wide ? k37_scan<T, S, true, true> : k37_scan<T, S, false, true>;
+        kernel<<<grid, kThreads, 0, st>>>(p, a, cuts, work);
         count_launches(1);
         return cudaGetLastError();
     });
 }
 
 template <typename T>
-cudaError_t launch_scan_grad(const ScanParams& p, const ScanTensors<T>& a, cudaStream_t st)
+cudaError_t launch_scan_grad(const ScanParams& params, const ScanTensors<T>& a, cudaStream_t st)
 {
+    const ScanParams p = with_rows(params, a);
     return with_split(p.states, [&](auto s) {
         using S = decltype(s);
         const ScanCuts cuts = cuts_of(p.blocks, p.t, p.channels, p.states);
         const ScanWork work = work_of(p.work, cuts, p.blocks, p.t, p.channels, p.states, true);
-        const size_t n = piece<T, S>();
-        const bool wide = on(a.x, n) && on(a.dt, n) && on(a.z, n) && on(a.dy, n) && on(a.dx, n) && on(a.ddt, n) && on(a.dz, n);
+        constexpr size_t n = S::kV * sizeof(T);
+        const bool wide = on(a.x, n, p.t) && on(a.dt, n, p.t) && on(a.z, n, p.t) && on(a.dy, n, p.t) && on(a.dx, n, p.t) && on(a.ddt, n, p.t) && on(a.dz, n, p.t) &&
+                          p.channels % S::kV == 0;
         const unsigned grid = (unsigned)(cuts.segments * p.blocks * cuts.groups);
         constexpr int kShared = sizeof(GradShared<S>);
-        static std::atomic<uint64_t> allowed[2] = {};
-        cudaError_t e = allow_shared(k39_scan_grad<T, S, true>, kShared, allowed[0]);
-        if (e == cudaSuccess) e = allow_shared(k39_scan_grad<T, S, false>, kShared, allowed[1]);
+        static std::atomic<uint64_t> allowed[4] = {};
+        auto *part = wide ? k39_scan_grad<T, S, true, false> : k39_scan_grad<T, S, false, false>,
+             *kernel = wide ? k39_scan_grad<T, S, true, true> : k39_scan_grad<T, S, false, true>;
+        cudaError_t e = allow_shared(kernel, kShared, allowed[wide]);
+        if (e == cudaSuccess) e = allow_shared(part, kPartShared<S>, allowed[2 + wide]);
         if (e != cudaSuccess) return e;
         if (cuts.segments > 1) {
-            k39_scan_grad<T, S, false><<<grid, kThreads, kShared, st>>>(p, a, cuts, work, wide);
+            part<<<grid, kThreads, kPartShared<S>, st>>>(p, a, cuts, work);
             count_launches(1);
             e = cudaGetLastError();
             if (e == cudaSuccess) e = join(p, cuts, work, true, st);
             if (e != cudaSuccess) return e;
         }
-        k39_scan_grad<T, S, true><<<grid, kThreads, kShared, st>>>(p, a, cuts, work, wide);
+        kernel<<<grid, kThreads, kShared, st>>>(p, a, cuts, work);
         count_launches(1);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         const int64_t sums = p.blocks * p.t * 2 * S::kAll, per = p.channels * p.states;
