@@ -18,7 +18,7 @@ namespace bload {
 
 namespace {
 
-constexpr int kThreads = 128, kAhead = 4;  // slots that are loaded together
+constexpr int kThreads = 128;
 
 // What a tile of a call is: CTAs are [block][tile][group of channels].
 struct ConvTiles {
@@ -52,13 +52,17 @@ struct Columns {
         else
             x.store_apart(row + c0, step, there);
     }
-    __device__ __forceinline__ void weights(const ConvParams& p, float (&w)[K][V], float (&bias)[V]) const
+    __device__ __forceinline__ void weights(const ConvParams& p, Two (&w)[K][V / 2], Two (&bias)[V / 2]) const
     {
+        auto of = [&](const float* from, int64_t each, int e) { return e < there ? from[(c0 + e * step) * each] : 0.0f; };
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            bias[e] = p.bias && e < there ? p.bias[c0 + e * step] : 0.0f;
+        for (int e = 0; e < V; e += 2) {
+            bias[e / 2] = p.bias ? two(of(p.bias, 1, e), of(p.bias, 1, e + 1)) : zero();
 #pragma unroll
-            for (int j = 0; j < K; ++j) w[j][e] = j < p.taps && e < there ? p.weight[(c0 + e * step) * p.taps + p.taps - 1 - j] : 0.0f;
+            for (int j = 0; j < K; ++j) {
+                const float* const from = p.weight + p.taps - 1 - j;
+                w[j][e / 2] = j < p.taps ? two(of(from, p.taps, e), of(from, p.taps, e + 1)) : zero();
+            }
         }
     }
 };
@@ -70,202 +74,313 @@ __device__ __forceinline__ int taps_of(const ConvParams& p, int pos)
     return min(pos + 1, K <= 4 ? K : p.taps);
 }
 
-// u = bias + sum of the first `taps` (x is that of the slot itself, win[j - 1] of j slots back)
-template <int V, int K>
-__device__ __forceinline__ void convolve(float (&u)[V], const float (&bias)[V], const float (&w)[K][V], const float (&x)[V],
-                                         const float (&win)[K - 1][V], int taps)
+// Slots that are worked on together: a multiple of the taps, so that the window of the last K inputs turns in place.
+template <int K>
+constexpr int kChunk = K <= 3 ? 2 * K : K;
+
+// Brings chunks of slots to a thread, its channels of TENSORS tensors.  WIDE: by asynchronous copies into shared memory, each thread's
+// own (no barrier), three chunks ahead; otherwise into registers when their turn has come.
+template <typename T, int V, int K, bool WIDE, int TENSORS>
+struct Slots {
+    static constexpr int U = kChunk<K>, kStages = 4, kBytes = V * sizeof(T);
+    static constexpr int kShared = WIDE ? kStages * U * TENSORS * kBytes * kThreads : 0;
+    const Columns<T, V, K, WIDE>& col;
+    const Channels<const T>* tensors[TENSORS];
+    const T* at[TENSORS];  // the block's first slot
+    const int32_t* pos;
+    uint32_t ring;
+    int t, stage;
+    int next[U + 1];  // positions of the next chunk, and the slot behind
+    Elements<T, V> raw[WIDE ? 1 : U][TENSORS];
+
+    __device__ __forceinline__ Slots(const Columns<T, V, K, WIDE>& c) : col(c) {}
+    __device__ __forceinline__ void init(const ConvParams& p, int64_t q, uint8_t* shared)
+    {
+        pos = p.pos + q * p.t;
+        t = p.t;
+        stage = 0;
+        ring = (uint32_t)__cvta_generic_to_shared(shared) + threadIdx.x * kBytes;
+#pragma unroll
+        for (int n = 0; n < TENSORS; ++n) at[n] = tensors[n]->data + q * tensors[n]->block + col.c0;
+    }
+    __device__ __forceinline__ void look(int s)
+    {
+#pragma unroll
+        for (int i = 0; i <= U; ++i) next[i] = s + i < t ? pos[s + i] : -1;
+    }
+    // begins to copy a chunk; slots from `end` on are not touched
+    __device__ __forceinline__ void fetch(int s, int end, int to)
+    {
+        if constexpr (WIDE) {
+            if (col.there) {
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    if (s + i >= end) break;
+#pragma unroll
+                    for (int n = 0; n < TENSORS; ++n) {
+                        const uint32_t dst = ring + (uint32_t)(((to * U + i) * TENSORS + n) * kBytes * kThreads);
+                        const T* const src = at[n] + (int64_t)(s + i) * tensors[n]->slot;
+                        if constexpr (kBytes == 16)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+                        else
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(kBytes) : "memory");
+                    }
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    }
+    __device__ __forceinline__ void start(int s, int end)
+    {
+        look(s);
+#pragma unroll
+        for (int k = 0; k < kStages - 1; ++k) fetch(s + k * U, end, k);
+    }
+    // The chunk of slot s has come: here[i] are its positions, changed by `which` (those below 0 are not loaded).
+    template <typename Which>
+    __device__ __forceinline__ void arrive(int s, int end, int (&here)[U + 1], const Which& which)
+    {
+#pragma unroll
+        for (int i = 0; i <= U; ++i) here[i] = which(s + i, next[i]);
+        fetch(s + (kStages - 1) * U, end, stage ? stage - 1 : kStages - 1);
+        look(s + U);
+        if constexpr (WIDE) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        } else {
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+#pragma unroll
+                for (int n = 0; n < TENSORS; ++n) {
+                    raw[WIDE ? 0 : i][n].clear();
+                    if (here[i] >= 0 && s + i < end) raw[WIDE ? 0 : i][n].load_apart(at[n] + (int64_t)(s + i) * tensors[n]->slot, col.step, col.there);
+                }
+        }
+    }
+    // slot i of the chunk, 0 where it is not `on`
+    __device__ __forceinline__ void get(int i, int n, bool on, Two (&x)[V / 2]) const
+    {
+        Elements<T, V> e;
+        e.clear();
+        if constexpr (WIDE) {
+            if (on && col.there) {
+                const uint32_t src = ring + (uint32_t)(((stage * U + i) * TENSORS + n) * kBytes * kThreads);
+                if constexpr (kBytes == 16) {
+                    uint4 w;
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(src) : "memory");
+                    *reinterpret_cast<uint4*>(e.x) = w;
+                } else if constexpr (kBytes == 8) {
+                    uint2 w;
+                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w.x), "=r"(w.y) : "r"(src) : "memory");
+                    *reinterpret_cast<uint2*>(e.x) = w;
+                } else {
+                    uint32_t w;
+                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(src) : "memory");
+                    *reinterpret_cast<uint32_t*>(e.x) = w;
+                }
+            }
+        } else {
+            e = raw[WIDE ? 0 : i][n];
+        }
+#pragma unroll
+        for (int k = 0; k < V; k += 2) x[k / 2] = e.pair(k);
+    }
+    __device__ __forceinline__ void leave() { stage = stage + 1 == kStages ? 0 : stage + 1; }
+    __device__ __forceinline__ void finish() const
+    {
+        if (WIDE) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    // the inputs in front of slot s0 that it sees, into the window: slot s lies at s % K, counted from s0
+    __device__ __forceinline__ void behind(const ConvParams& p, int s0, Two (&win)[K][V / 2])
+    {
+        const int back = taps_of<K>(p, pos[s0]) - 1;  // (whatever positions hold: inside the block)
+#pragma unroll
+        for (int j = 1; j < K; ++j) {
+            Elements<T, V> x;
+            x.clear();
+            if (j <= back && j <= s0) {
+                const T* const from = at[0] + (int64_t)(s0 - j) * tensors[0]->slot;
+                if (WIDE)
+                    x.load(from, col.there, true);
+                else
+                    x.load_apart(from, col.step, col.there);
+            }
+#pragma unroll
+            for (int k = 0; k < V; k += 2) win[K - j][k / 2] = x.pair(k);
+        }
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k) win[0][k] = zero();
+    }
+};
+
+// calls go(j) for the first n taps; where n is K, without a test on each
+template <int K, typename Go>
+__device__ __forceinline__ void for_taps(int n, const Go& go)
 {
+    if (n == K) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) u[e] = fmaf(w[0][e], x[e], bias[e]);
-    if (taps == K) {
-#pragma unroll
-        for (int j = 1; j < K; ++j)
-#pragma unroll
-            for (int e = 0; e < V; ++e) u[e] = fmaf(w[j][e], win[j - 1][e], u[e]);
+        for (int j = 0; j < K; ++j) go(j);
     } else {
 #pragma unroll
-        for (int j = 1; j < K; ++j)
-            if (j < taps)
-#pragma unroll
-                for (int e = 0; e < V; ++e) u[e] = fmaf(w[j][e], win[j - 1][e], u[e]);
+        for (int j = 0; j < K; ++j)
+            if (j < n) go(j);
     }
 }
 
 template <typename T, int V, int K, bool WIDE>
 __global__ void __launch_bounds__(kThreads) k34_conv(const ConvParams p, const ConvTensors<T> a, const ConvTiles tiles)
 {
+    extern __shared__ __align__(16) uint8_t shared_bytes[];
+    using S = Slots<T, V, K, WIDE, 1>;
+    constexpr int U = S::U, H = V / 2;
     const int64_t at = blockIdx.x / tiles.groups, q = at / tiles.tiles;
     const Columns<T, V, K, WIDE> col(p.channels, (int)(blockIdx.x - at * tiles.groups));
     const int s0 = (int)(at - q * tiles.tiles) * tiles.slots, s1 = min(s0 + tiles.slots, p.t);
     if (s0 >= p.t) return;
-    float w[K][V], bias[V], win[K - 1][V];
+    S slots(col);
+    slots.tensors[0] = &a.x;
+    slots.init(p, q, shared_bytes);
+    slots.start(s0, s1);
+    Two w[K][H], bias[H], win[K][H];  // win: the last K inputs, slot s0 + i at i % K
     col.weights(p, w, bias);
-    const int32_t* const pos = p.pos + q * p.t;
-    const T* const x0 = a.x.data + q * a.x.block;
-    T* const y0 = a.y.data + q * a.y.block;
-    const int back = taps_of<K>(p, pos[s0]) - 1;  // inputs in front of the tile that its first slot sees (garbage positions: of this block)
-#pragma unroll
-    for (int j = 1; j < K; ++j) {
-        Elements<T, V> x;
-        x.clear();
-        if (j <= back && j <= s0) col.load(x, x0 + (s0 - j) * a.x.slot);
-#pragma unroll
-        for (int e = 0; e < V; ++e) win[j - 1][e] = x.get(e);
-    }
+    slots.behind(p, s0, win);
+    T* y0 = a.y.data + q * a.y.block + (int64_t)s0 * a.y.slot;
     const int64_t keep = p.taps - 1;
-    for (int s = s0; s < s1; s += kAhead) {
-        Elements<T, V> x[kAhead];
-        int here[kAhead + 1];
+    for (int s = s0; s < s1; s += U) {
+        int here[U + 1];
+        slots.arrive(s, s1, here, [](int, int pos) { return pos; });
 #pragma unroll
-        for (int i = 0; i <= kAhead; ++i) here[i] = s + i < p.t ? pos[s + i] : -1;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            x[i].clear();
-            if (s + i < s1 && here[i] >= 0) col.load(x[i], x0 + (int64_t)(s + i) * a.x.slot);
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int i = 0; i < U; ++i) {
             if (s + i >= s1) break;
-            float v[V], u[V];
+            const bool on = here[i] >= 0;
+            Two(&now)[H] = win[i % K];
+            slots.get(i, 0, on, now);
+            Elements<T, V> out;
+            if (on) {
+                Two u[H];
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = x[i].get(e);
-            convolve<V, K>(u, bias, w, v, win, taps_of<K>(p, here[i]));
-            if (p.tails && here[i] >= 0 && here[i + 1] != here[i] + 1) {  // the sequence ends
-                const int64_t id = p.seq_id[q * p.t + s + i];
-                if (id >= 0 && id < p.n_seq) {
-                    T* const to = static_cast<T*>(p.tails) + id * keep * p.channels;
+                for (int k = 0; k < H; ++k) u[k] = bias[k];
+                for_taps<K>(taps_of<K>(p, here[i]), [&](int j) {
 #pragma unroll
-                    for (int j = 0; j < K - 1; ++j)
-                        if (j < keep) {
-                            Elements<T, V> old;
+                    for (int k = 0; k < H; ++k) u[k] = fma(w[j][k], win[(i + K - j) % K][k], u[k]);
+                });
 #pragma unroll
-                            for (int e = 0; e < V; ++e) old.set(e, j > here[i] ? 0.0f : j == 0 ? v[e] : win[j > 0 ? j - 1 : 0][e]);
+                for (int k = 0; k < H; ++k) out.set_pair(2 * k, p.silu ? u[k] * sigmoid_of(u[k]) : u[k]);
+                if (p.tails && here[i + 1] != here[i] + 1) {  // the sequence ends
+                    const int64_t id = p.seq_id[q * p.t + s + i];
+                    if (id >= 0 && id < p.n_seq) {
+                        T* const to = static_cast<T*>(p.tails) + id * keep * p.channels + col.c0;
 #pragma unroll
-                            for (int e = 0; e < V; ++e)
-                                if (e < col.there) to[(keep - 1 - j) * p.channels + col.c0 + e * col.step] = old.x[e];
-                        }
+                        for (int j = 0; j < K - 1; ++j)
+                            if (j < keep) {
+#pragma unroll
+                                for (int e = 0; e < V; ++e) {
+                                    const float2 x = one(win[(i + K - j) % K][e / 2]);
+                                    if (e < col.there) to[(keep - 1 - j) * p.channels + e * col.step] = from_float<T>(j > here[i] ? 0.0f : e & 1 ? x.y : x.x);
+                                }
+                            }
+                    }
                 }
+            } else {
+                out.clear();
             }
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float y = p.silu ? u[e] * sigmoid_of(u[e]) : u[e];
-                x[i].set(e, here[i] >= 0 ? y : 0.0f);
-            }
-            col.store(x[i], y0 + (int64_t)(s + i) * a.y.slot);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-#pragma unroll
-                for (int j = K - 2; j > 0; --j) win[j][e] = win[j - 1][e];
-                win[0][e] = v[e];
-            }
+            col.store(out, y0 + (int64_t)i * a.y.slot);
         }
+        y0 += U * a.y.slot;
+        slots.leave();
     }
+    slots.finish();
 }
 
 template <typename T, int V, int K, bool WIDE>
 __global__ void __launch_bounds__(kThreads) k35_conv_grad(const ConvParams p, const ConvTensors<T> a, const ConvTiles tiles)
 {
+    extern __shared__ __align__(16) uint8_t shared_bytes[];
+    using S = Slots<T, V, K, WIDE, 2>;
+    constexpr int U = S::U, H = V / 2;
     const int64_t at = blockIdx.x / tiles.groups, q = at / tiles.tiles;
     const Columns<T, V, K, WIDE> col(p.channels, (int)(blockIdx.x - at * tiles.groups));
     const int s0 = (int)(at - q * tiles.tiles) * tiles.slots, s1 = min(s0 + tiles.slots, p.t);
     const int taps = K <= 4 ? K : p.taps;
-    float w[K][V], bias[V], win[K - 1][V], dw[K][V], db[V], dx[K][V];  // dx[j]: of j slots back, so far
-    col.weights(p, w, bias);
+    Two w[K][H], bias[H], win[K][H], dw[K][H], db[H], dx[K][H];  // dx: of the last K slots, so far; slot s0 + i at i % K
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        db[e] = 0.0f;
+    for (int k = 0; k < H; ++k) {
+        db[k] = zero();
 #pragma unroll
-        for (int j = 0; j < K; ++j) dw[j][e] = dx[j][e] = 0.0f;
+        for (int j = 0; j < K; ++j) dw[j][k] = dx[j][k] = zero();
     }
     if (s0 < p.t) {
-        const int32_t* const pos = p.pos + q * p.t;
-        const T *const x0 = a.x.data + q * a.x.block, *const dy0 = a.dy.data + q * a.dy.block;
+        const int end = min(s1 + taps - 1, p.t);
+        S slots(col);
+        slots.tensors[0] = &a.x;
+        slots.tensors[1] = &a.dy;
+        slots.init(p, q, shared_bytes);
+        slots.start(s0, end);
+        col.weights(p, w, bias);
+        slots.behind(p, s0, win);
         T* const dx0 = a.dx.data + q * a.dx.block;
-        const int back = taps_of<K>(p, pos[s0]) - 1;
+        for (int s = s0; s < s1 + taps - 1; s += U) {
+            int here[U + 1];
+            // a slot behind the tile counts where it reaches into it
+            slots.arrive(s, end, here, [&](int slot, int pos) { return slot >= s1 && pos < slot - s1 + 1 ? -1 : pos; });
 #pragma unroll
-        for (int j = 1; j < K; ++j) {
-            Elements<T, V> x;
-            x.clear();
-            if (j <= back && j <= s0) col.load(x, x0 + (s0 - j) * a.x.slot);
+            for (int i = 0; i < U; ++i) {
+                if (s + i >= s1 + taps - 1) break;
+                const bool on = here[i] >= 0 && s + i < end, mine = s + i < s1;
+                Two(&now)[H] = win[i % K];
+                Two du[H];
+                slots.get(i, 0, on, now);
+                slots.get(i, 1, on, du);
 #pragma unroll
-            for (int e = 0; e < V; ++e) win[j - 1][e] = x.get(e);
-        }
-        const int end = s1 + taps - 1;
-        for (int s = s0; s < end; s += kAhead) {
-            Elements<T, V> x[kAhead], dy[kAhead];
-            int here[kAhead];
+                for (int k = 0; k < H; ++k) dx[i % K][k] = zero();
+                if (on) {
+                    const int n = taps_of<K>(p, here[i]);
+                    if (p.silu) {
+                        Two u[H];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {  // a slot behind the tile counts where it reaches into it
-                here[i] = s + i < p.t ? pos[s + i] : -1;
-                if (s + i >= s1 && here[i] < s + i - s1 + 1) here[i] = -1;
-            }
+                        for (int k = 0; k < H; ++k) u[k] = bias[k];
+                        for_taps<K>(n, [&](int j) {
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                x[i].clear();
-                dy[i].clear();
-                if (here[i] >= 0 && s + i < end) {
-                    col.load(x[i], x0 + (int64_t)(s + i) * a.x.slot);
-                    col.load(dy[i], dy0 + (int64_t)(s + i) * a.dy.slot);
-                }
-            }
+                            for (int k = 0; k < H; ++k) u[k] = fma(w[j][k], win[(i + K - j) % K][k], u[k]);
+                        });
+                        // d(u sig) = sig + u sig (1 - sig)
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                if (s + i >= end) break;
-                float v[V], du[V];
-                const int n = taps_of<K>(p, here[i]);
+                        for (int k = 0; k < H; ++k) {
+                            const Two sig = sigmoid_of(u[k]);
+                            du[k] = du[k] * fma(u[k] * sig, fma(sig, two(-1.0f, -1.0f), two(1.0f, 1.0f)), sig);
+                        }
+                    }
+                    for_taps<K>(n, [&](int j) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    v[e] = x[i].get(e);
-                    du[e] = dy[i].get(e);
-                }
-                if (p.silu) {
-                    float u[V];
-                    convolve<V, K>(u, bias, w, v, win, n);
+                        for (int k = 0; k < H; ++k) dx[(i + K - j) % K][k] = fma(w[j][k], du[k], dx[(i + K - j) % K][k]);
+                    });
+                    if (mine) {
+                        for_taps<K>(n, [&](int j) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float g = sigmoid_of(u[e]);
-                        du[e] = here[i] >= 0 ? du[e] * fmaf(u[e] * g, 1.0f - g, g) : 0.0f;
+                            for (int k = 0; k < H; ++k) dw[j][k] = fma(du[k], win[(i + K - j) % K][k], dw[j][k]);
+                        });
+#pragma unroll
+                        for (int k = 0; k < H; ++k) db[k] = db[k] + du[k];
                     }
                 }
-                const bool mine = s + i < s1;
-#pragma unroll
-                for (int j = 0; j < K; ++j)
-                    if (j < n) {
-#pragma unroll
-                        for (int e = 0; e < V; ++e) dx[j][e] = fmaf(w[j][e], du[e], dx[j][e]);
-                        if (mine)
-#pragma unroll
-                            for (int e = 0; e < V; ++e) dw[j][e] = fmaf(du[e], j == 0 ? v[e] : win[j > 0 ? j - 1 : 0][e], dw[j][e]);
-                    }
-                if (mine)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) db[e] += du[e];
                 // slot s + i - (taps - 1) has all of its own
                 const int done = s + i - (taps - 1);
                 if (done >= s0) {
                     Elements<T, V> out;
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        float last = dx[K - 1][e];
+                    for (int k = 0; k < H; ++k) {
+                        Two v = dx[(i + 1) % K][k];
                         if (K > 4) {
 #pragma unroll
-                            for (int j = 0; j < K; ++j) last = j == taps - 1 ? dx[j][e] : last;
+                            for (int j = 0; j < K; ++j) v.v = j == taps - 1 ? dx[(i + K - j) % K][k].v : v.v;
                         }
-                        out.set(e, last);
+                        out.set_pair(2 * k, v);
                     }
                     col.store(out, dx0 + (int64_t)done * a.dx.slot);
                 }
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-#pragma unroll
-                    for (int j = K - 1; j > 0; --j) dx[j][e] = dx[j - 1][e];
-                    dx[0][e] = 0.0f;
-#pragma unroll
-                    for (int j = K - 2; j > 0; --j) win[j][e] = win[j - 1][e];
-                    win[0][e] = v[e];
-                }
             }
+            slots.leave();
         }
+        slots.finish();
     }
     if (p.work) {
         float* const to = p.work + at * p.channels * (taps + 1);
@@ -273,10 +388,11 @@ __global__ void __launch_bounds__(kThreads) k35_conv_grad(const ConvParams p, co
         for (int e = 0; e < V; ++e)
             if (e < col.there) {
                 const int64_t c = col.c0 + e * col.step;
+                auto half = [&](Two x) { return e & 1 ? one(x).y : one(x).x; };
 #pragma unroll
                 for (int j = 0; j < K; ++j)
-                    if (j < taps) to[c * taps + taps - 1 - j] = dw[j][e];
-                to[p.channels * taps + c] = db[e];
+                    if (j < taps) to[c * taps + taps - 1 - j] = half(dw[j][e / 2]);
+                to[p.channels * taps + c] = half(db[e / 2]);
             }
     }
 }
@@ -305,22 +421,23 @@ __global__ void __launch_bounds__(kThreads) k36_conv_step(const ConvParams p, in
             if (on && j <= keep && (here[r] < 0 || j <= here[r])) col.load(old[r][j - 1], state + (row0 + r) * size + (keep - j) * p.channels);
         }
     }
-    float w[K][V], bias[V];
+    Two w[K][V / 2], bias[V / 2];
     col.weights(p, w, bias);
 #pragma unroll
     for (int r = 0; r < kRowsAtOnce; ++r) {
         if (row0 + r >= rows) break;
-        float v[V], u[V], win[K - 1][V];
+        Two u[V / 2];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            v[e] = now[r].get(e);
+        for (int k = 0; k < V / 2; ++k) u[k] = bias[k];
+        for_taps<K>(taps_of<K>(p, here[r]), [&](int j) {
 #pragma unroll
-            for (int j = 1; j < K; ++j) win[j - 1][e] = old[r][j - 1].get(e);
-        }
-        convolve<V, K>(u, bias, w, v, win, taps_of<K>(p, here[r]));
+            for (int k = 0; k < V / 2; ++k) u[k] = fma(w[j][k], (j ? old[r][j > 0 ? j - 1 : 0] : now[r]).pair(2 * k), u[k]);
+        });
         Elements<T, V> out;
+        out.clear();
+        if (here[r] >= 0)
 #pragma unroll
-        for (int e = 0; e < V; ++e) out.set(e, here[r] < 0 ? 0.0f : p.silu ? u[e] * sigmoid_of(u[e]) : u[e]);
+            for (int k = 0; k < V / 2; ++k) out.set_pair(2 * k, p.silu ? u[k] * sigmoid_of(u[k]) : u[k]);
         col.store(out, y + (row0 + r) * sy);
         T* const to = next + (row0 + r) * size;
         if (here[r] >= 0) {
@@ -390,7 +507,11 @@ cudaError_t launch_conv(const ConvParams& p, const ConvTensors<T>& a, cudaStream
         const ConvTiles x = tiles_of(p.blocks, p.t, p.channels, V);
         const bool wide = on<const T, V>(a.x) && on<T, V>(a.y) && p.channels % V == 0;
         auto* kernel = wide ? k34_conv<T, V, K, true> : k34_conv<T, V, K, false>;
-        kernel<<<(unsigned)(p.blocks * x.tiles * x.groups), x.threads, 0, st>>>(p, a, x);
+        constexpr int kShared = Slots<T, V, K, true, 1>::kShared;
+        static std::atomic<uint64_t> allowed{0};
+        const cudaError_t e = allow_shared(k34_conv<T, V, K, true>, kShared, allowed);
+        if (e != cudaSuccess) return e;
+        kernel<<<(unsigned)(p.blocks * x.tiles * x.groups), x.threads, wide ? kShared : 0, st>>>(p, a, x);
         count_launches(1);
         return cudaGetLastError();
     });
@@ -405,7 +526,11 @@ cudaError_t launch_conv_grad(const ConvParams& p, const ConvTensors<T>& a, cudaS
         x = tiles_of(p.blocks, p.t, p.channels, V);
         const bool wide = on<const T, V>(a.x) && on<const T, V>(a.dy) && on<T, V>(a.dx) && p.channels % V == 0;
         auto* kernel = wide ? k35_conv_grad<T, V, K, true> : k35_conv_grad<T, V, K, false>;
-        kernel<<<(unsigned)(p.blocks * x.tiles * x.groups), x.threads, 0, st>>>(p, a, x);
+        constexpr int kShared = Slots<T, V, K, true, 2>::kShared;
+        static std::atomic<uint64_t> allowed{0};
+        const cudaError_t e = allow_shared(k35_conv_grad<T, V, K, true>, kShared, allowed);
+        if (e != cudaSuccess) return e;
+        kernel<<<(unsigned)(p.blocks * x.tiles * x.groups), x.threads, wide ? kShared : 0, st>>>(p, a, x);
         count_launches(1);
         return cudaGetLastError();
     });

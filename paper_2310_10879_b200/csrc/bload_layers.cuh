@@ -78,7 +78,9 @@ struct NormParams {
     int64_t rows, channels;
     int32_t t;
     float eps;
-    bool flat;  // blocks of every tensor lie one behind the other
+    bool flat;    // blocks of every tensor lie one behind the other
+    int32_t stages, params_at;  // groups of frames in shared memory, and where weight and bias begin there
+    uintptr_t end[2];  // where x and dy end
 };
 template <typename T>
 struct NormTensors {
