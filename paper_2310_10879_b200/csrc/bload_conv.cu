@@ -52,6 +52,14 @@ struct Columns {
         else
             x.store_apart(row + c0, step, there);
     }
+    // slot s of the block that begins at `first` (WIDE: a block spans less than 2^32 bytes)
+    __device__ __forceinline__ void store_slot(const Elements<T, V>& x, T* first, int64_t slot, int s) const
+    {
+        if (WIDE)
+            x.store(reinterpret_cast<T*>(reinterpret_cast<char*>(first) + ((uint32_t)s * ((uint32_t)slot * (uint32_t)sizeof(T)) + (uint32_t)c0 * (uint32_t)sizeof(T))), there, true);
+        else
+            store(x, first + s * slot);
+    }
     __device__ __forceinline__ void weights(const ConvParams& p, Two (&w)[K][V / 2], Two (&bias)[V / 2]) const
     {
         auto of = [&](const float* from, int64_t each, int e) { return e < there ? from[(c0 + e * step) * each] : 0.0f; };
@@ -86,7 +94,8 @@ struct Slots {
     static constexpr int kShared = WIDE ? kStages * U * TENSORS * kBytes * kThreads : 0;
     const Columns<T, V, K, WIDE>& col;
     const Channels<const T>* tensors[TENSORS];
-    const T* at[TENSORS];  // the block's first slot
+    const T* at[TENSORS];  // the block's first slot (WIDE: the CTA's; a block spans less than 2^32 bytes)
+    uint32_t mine;         // WIDE: bytes from there to the thread's channels
     const int32_t* pos;
     uint32_t ring;
     int t, stage;
@@ -101,7 +110,13 @@ struct Slots {
         stage = 0;
         ring = (uint32_t)__cvta_generic_to_shared(shared) + threadIdx.x * kBytes;
 #pragma unroll
-        for (int n = 0; n < TENSORS; ++n) at[n] = tensors[n]->data + q * tensors[n]->block + col.c0;
+        for (int n = 0; n < TENSORS; ++n) at[n] = tensors[n]->data + q * tensors[n]->block + (WIDE ? 0 : col.c0);
+        mine = (uint32_t)col.c0 * (uint32_t)sizeof(T);
+    }
+    // WIDE: slot s of a tensor of this block
+    __device__ __forceinline__ const T* slot_of(int n, int s) const
+    {
+        return reinterpret_cast<const T*>(reinterpret_cast<const char*>(at[n]) + ((uint32_t)s * ((uint32_t)tensors[n]->slot * (uint32_t)sizeof(T)) + mine));
     }
     __device__ __forceinline__ void look(int s)
     {
@@ -119,7 +134,7 @@ struct Slots {
 #pragma unroll
                     for (int n = 0; n < TENSORS; ++n) {
                         const uint32_t dst = ring + (uint32_t)(((to * U + i) * TENSORS + n) * kBytes * kThreads);
-                        const T* const src = at[n] + (int64_t)(s + i) * tensors[n]->slot;
+                        const T* const src = slot_of(n, s + i);
                         if constexpr (kBytes == 16)
                             asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
                         else
@@ -198,11 +213,10 @@ struct Slots {
             Elements<T, V> x;
             x.clear();
             if (j <= back && j <= s0) {
-                const T* const from = at[0] + (int64_t)(s0 - j) * tensors[0]->slot;
                 if (WIDE)
-                    x.load(from, col.there, true);
+                    x.load(slot_of(0, s0 - j), col.there, true);
                 else
-                    x.load_apart(from, col.step, col.there);
+                    x.load_apart(at[0] + (int64_t)(s0 - j) * tensors[0]->slot, col.step, col.there);
             }
 #pragma unroll
             for (int k = 0; k < V; k += 2) win[K - j][k / 2] = x.pair(k);
@@ -232,9 +246,9 @@ __global__ void __launch_bounds__(kThreads) k34_conv(const ConvParams p, const C
     extern __shared__ __align__(16) uint8_t shared_bytes[];
     using S = Slots<T, V, K, WIDE, 1>;
     constexpr int U = S::U, H = V / 2;
-    const int64_t at = blockIdx.x / tiles.groups, q = at / tiles.tiles;
-    const Columns<T, V, K, WIDE> col(p.channels, (int)(blockIdx.x - at * tiles.groups));
-    const int s0 = (int)(at - q * tiles.tiles) * tiles.slots, s1 = min(s0 + tiles.slots, p.t);
+    const unsigned at = blockIdx.x / (unsigned)tiles.groups, q = at / (unsigned)tiles.tiles;
+    const Columns<T, V, K, WIDE> col(p.channels, (int)(blockIdx.x - at * (unsigned)tiles.groups));
+    const int s0 = (int)(at - q * (unsigned)tiles.tiles) * tiles.slots, s1 = min(s0 + tiles.slots, p.t);
     if (s0 >= p.t) return;
     S slots(col);
     slots.tensors[0] = &a.x;
@@ -243,49 +257,60 @@ __global__ void __launch_bounds__(kThreads) k34_conv(const ConvParams p, const C
     Two w[K][H], bias[H], win[K][H];  // win: the last K inputs, slot s0 + i at i % K
     col.weights(p, w, bias);
     slots.behind(p, s0, win);
-    T* y0 = a.y.data + q * a.y.block + (int64_t)s0 * a.y.slot;
+    T* const y0 = a.y.data + q * a.y.block;
     const int64_t keep = p.taps - 1;
+    const int full = K <= 4 ? K - 1 : p.taps - 1;
     for (int s = s0; s < s1; s += U) {
         int here[U + 1];
         slots.arrive(s, s1, here, [](int, int pos) { return pos; });
+        auto chunk = [&](auto with_tests) {
+            constexpr bool tests = decltype(with_tests)::value;
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            if (s + i >= s1) break;
-            const bool on = here[i] >= 0;
-            Two(&now)[H] = win[i % K];
-            slots.get(i, 0, on, now);
-            Elements<T, V> out;
-            if (on) {
-                Two u[H];
+            for (int i = 0; i < U; ++i) {
+                if (tests && s + i >= s1) break;
+                const bool on = !tests || here[i] >= 0;
+                Two(&now)[H] = win[i % K];
+                slots.get(i, 0, on, now);
+                Elements<T, V> out;
+                if (on) {
+                    Two u[H];
 #pragma unroll
-                for (int k = 0; k < H; ++k) u[k] = bias[k];
-                for_taps<K>(taps_of<K>(p, here[i]), [&](int j) {
+                    for (int k = 0; k < H; ++k) u[k] = bias[k];
+                    for_taps<K>(!tests && K <= 4 ? K : taps_of<K>(p, here[i]), [&](int j) {
 #pragma unroll
-                    for (int k = 0; k < H; ++k) u[k] = fma(w[j][k], win[(i + K - j) % K][k], u[k]);
-                });
+                        for (int k = 0; k < H; ++k) u[k] = fma(w[j][k], win[(i + K - j) % K][k], u[k]);
+                    });
 #pragma unroll
-                for (int k = 0; k < H; ++k) out.set_pair(2 * k, p.silu ? u[k] * sigmoid_of(u[k]) : u[k]);
-                if (p.tails && here[i + 1] != here[i] + 1) {  // the sequence ends
-                    const int64_t id = p.seq_id[q * p.t + s + i];
-                    if (id >= 0 && id < p.n_seq) {
-                        T* const to = static_cast<T*>(p.tails) + id * keep * p.channels + col.c0;
+                    for (int k = 0; k < H; ++k) out.set_pair(2 * k, p.silu ? u[k] * sigmoid_of(u[k]) : u[k]);
+                    if (tests && p.tails && here[i + 1] != here[i] + 1) {  // the sequence ends
+                        const int64_t id = p.seq_id[(int64_t)q * p.t + s + i];
+                        if (id >= 0 && id < p.n_seq) {
+                            T* const to = static_cast<T*>(p.tails) + id * keep * p.channels + col.c0;
 #pragma unroll
-                        for (int j = 0; j < K - 1; ++j)
-                            if (j < keep) {
+                            for (int j = 0; j < K - 1; ++j)
+                                if (j < keep) {
 #pragma unroll
-                                for (int e = 0; e < V; ++e) {
-                                    const float2 x = one(win[(i + K - j) % K][e / 2]);
-                                    if (e < col.there) to[(keep - 1 - j) * p.channels + e * col.step] = from_float<T>(j > here[i] ? 0.0f : e & 1 ? x.y : x.x);
+                                    for (int e = 0; e < V; ++e) {
+                                        const float2 x = one(win[(i + K - j) % K][e / 2]);
+                                        if (e < col.there) to[(keep - 1 - j) * p.channels + e * col.step] = from_float<T>(j > here[i] ? 0.0f : e & 1 ? x.y : x.x);
+                                    }
                                 }
-                            }
+                        }
                     }
+                } else {
+                    out.clear();
                 }
-            } else {
-                out.clear();
+                col.store_slot(out, y0, a.y.slot, s + i);
             }
-            col.store(out, y0 + (int64_t)i * a.y.slot);
-        }
-        y0 += U * a.y.slot;
+        };
+        // whole chunks in which no sequence begins or ends need no tests
+        bool plain = s + U <= s1;
+#pragma unroll
+        for (int i = 0; i < U; ++i) plain = plain && here[i] >= full && (i + 1 < U || !p.tails || here[U] > 0);
+        if (plain)
+            chunk(std::false_type());
+        else
+            chunk(std::true_type());
         slots.leave();
     }
     slots.finish();
@@ -297,9 +322,9 @@ __global__ void __launch_bounds__(kThreads) k35_conv_grad(const ConvParams p, co
     extern __shared__ __align__(16) uint8_t shared_bytes[];
     using S = Slots<T, V, K, WIDE, 2>;
     constexpr int U = S::U, H = V / 2;
-    const int64_t at = blockIdx.x / tiles.groups, q = at / tiles.tiles;
-    const Columns<T, V, K, WIDE> col(p.channels, (int)(blockIdx.x - at * tiles.groups));
-    const int s0 = (int)(at - q * tiles.tiles) * tiles.slots, s1 = min(s0 + tiles.slots, p.t);
+    const unsigned at = blockIdx.x / (unsigned)tiles.groups, q = at / (unsigned)tiles.tiles;
+    const Columns<T, V, K, WIDE> col(p.channels, (int)(blockIdx.x - at * (unsigned)tiles.groups));
+    const int s0 = (int)(at - q * (unsigned)tiles.tiles) * tiles.slots, s1 = min(s0 + tiles.slots, p.t);
     const int taps = K <= 4 ? K : p.taps;
     Two w[K][H], bias[H], win[K][H], dw[K][H], db[H], dx[K][H];  // dx: of the last K slots, so far; slot s0 + i at i % K
 #pragma unroll
@@ -322,68 +347,78 @@ __global__ void __launch_bounds__(kThreads) k35_conv_grad(const ConvParams p, co
             int here[U + 1];
             // a slot behind the tile counts where it reaches into it
             slots.arrive(s, end, here, [&](int slot, int pos) { return slot >= s1 && pos < slot - s1 + 1 ? -1 : pos; });
+            auto chunk = [&](auto with_tests) {
+                constexpr bool tests = decltype(with_tests)::value;
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                if (s + i >= s1 + taps - 1) break;
-                const bool on = here[i] >= 0 && s + i < end, mine = s + i < s1;
-                Two(&now)[H] = win[i % K];
-                Two du[H];
-                slots.get(i, 0, on, now);
-                slots.get(i, 1, on, du);
+                for (int i = 0; i < U; ++i) {
+                    if (tests && s + i >= s1 + taps - 1) break;
+                    const bool on = !tests || (here[i] >= 0 && s + i < end), mine = !tests || s + i < s1;
+                    Two(&now)[H] = win[i % K];
+                    Two du[H];
+                    slots.get(i, 0, on, now);
+                    slots.get(i, 1, on, du);
 #pragma unroll
-                for (int k = 0; k < H; ++k) dx[i % K][k] = zero();
-                if (on) {
-                    const int n = taps_of<K>(p, here[i]);
-                    if (p.silu) {
-                        Two u[H];
+                    for (int k = 0; k < H; ++k) dx[i % K][k] = zero();
+                    if (on) {
+                        const int n = !tests && K <= 4 ? K : taps_of<K>(p, here[i]);
+                        if (p.silu) {
+                            Two u[H];
 #pragma unroll
-                        for (int k = 0; k < H; ++k) u[k] = bias[k];
+                            for (int k = 0; k < H; ++k) u[k] = bias[k];
+                            for_taps<K>(n, [&](int j) {
+#pragma unroll
+                                for (int k = 0; k < H; ++k) u[k] = fma(w[j][k], win[(i + K - j) % K][k], u[k]);
+                            });
+                            // d(u sig) = sig + u sig (1 - sig)
+#pragma unroll
+                            for (int k = 0; k < H; ++k) {
+                                const Two sig = sigmoid_of(u[k]);
+                                du[k] = du[k] * fma(u[k] * sig, fma(sig, two(-1.0f, -1.0f), two(1.0f, 1.0f)), sig);
+                            }
+                        }
                         for_taps<K>(n, [&](int j) {
 #pragma unroll
-                            for (int k = 0; k < H; ++k) u[k] = fma(w[j][k], win[(i + K - j) % K][k], u[k]);
+                            for (int k = 0; k < H; ++k) dx[(i + K - j) % K][k] = fma(w[j][k], du[k], dx[(i + K - j) % K][k]);
                         });
-                        // d(u sig) = sig + u sig (1 - sig)
+                        if (mine) {
+                            for_taps<K>(n, [&](int j) {
+#pragma unroll
+                                for (int k = 0; k < H; ++k) dw[j][k] = fma(du[k], win[(i + K - j) % K][k], dw[j][k]);
+                            });
+#pragma unroll
+                            for (int k = 0; k < H; ++k) db[k] = db[k] + du[k];
+                        }
+                    }
+                    // slot s + i - (taps - 1) has all of its own
+                    const int done = s + i - (taps - 1);
+                    if (!tests || done >= s0) {
+                        Elements<T, V> out;
 #pragma unroll
                         for (int k = 0; k < H; ++k) {
-                            const Two sig = sigmoid_of(u[k]);
-                            du[k] = du[k] * fma(u[k] * sig, fma(sig, two(-1.0f, -1.0f), two(1.0f, 1.0f)), sig);
+                            Two v = dx[(i + 1) % K][k];
+                            if (K > 4) {
+#pragma unroll
+                                for (int j = 0; j < K; ++j) v.v = j == taps - 1 ? dx[(i + K - j) % K][k].v : v.v;
+                            }
+                            out.set_pair(2 * k, v);
                         }
-                    }
-                    for_taps<K>(n, [&](int j) {
-#pragma unroll
-                        for (int k = 0; k < H; ++k) dx[(i + K - j) % K][k] = fma(w[j][k], du[k], dx[(i + K - j) % K][k]);
-                    });
-                    if (mine) {
-                        for_taps<K>(n, [&](int j) {
-#pragma unroll
-                            for (int k = 0; k < H; ++k) dw[j][k] = fma(du[k], win[(i + K - j) % K][k], dw[j][k]);
-                        });
-#pragma unroll
-                        for (int k = 0; k < H; ++k) db[k] = db[k] + du[k];
+                        col.store_slot(out, dx0, a.dx.slot, done);
                     }
                 }
-                // slot s + i - (taps - 1) has all of its own
-                const int done = s + i - (taps - 1);
-                if (done >= s0) {
-                    Elements<T, V> out;
+            };
+            bool plain = s > s0 && s + U <= s1;
 #pragma unroll
-                    for (int k = 0; k < H; ++k) {
-                        Two v = dx[(i + 1) % K][k];
-                        if (K > 4) {
-#pragma unroll
-                            for (int j = 0; j < K; ++j) v.v = j == taps - 1 ? dx[(i + K - j) % K][k].v : v.v;
-                        }
-                        out.set_pair(2 * k, v);
-                    }
-                    col.store(out, dx0 + (int64_t)done * a.dx.slot);
-                }
-            }
+            for (int i = 0; i < U; ++i) plain = plain && here[i] >= taps - 1;
+            if (plain)
+                chunk(std::false_type());
+            else
+                chunk(std::true_type());
             slots.leave();
         }
         slots.finish();
     }
     if (p.work) {
-        float* const to = p.work + at * p.channels * (taps + 1);
+        float* const to = p.work + (int64_t)at * p.channels * (taps + 1);
 #pragma unroll
         for (int e = 0; e < V; ++e)
             if (e < col.there) {
@@ -403,8 +438,9 @@ template <typename T, int V, int K, bool WIDE>
 __global__ void __launch_bounds__(kThreads) k36_conv_step(const ConvParams p, int64_t rows, const T* state, T* next, const T* x, int64_t sx,
                                                          T* y, int64_t sy, int groups)
 {
-    const int64_t at = blockIdx.x / groups, row0 = at * kRowsAtOnce;
-    const Columns<T, V, K, WIDE> col(p.channels, (int)(blockIdx.x - at * groups));
+    const unsigned at = blockIdx.x / (unsigned)groups;
+    const int64_t row0 = (int64_t)at * kRowsAtOnce;
+    const Columns<T, V, K, WIDE> col(p.channels, (int)(blockIdx.x - at * (unsigned)groups));
     const int64_t keep = p.taps - 1, size = keep * p.channels;
     Elements<T, V> now[kRowsAtOnce], old[kRowsAtOnce][K - 1];  // old[j - 1]: j frames back
     int here[kRowsAtOnce];
@@ -414,11 +450,11 @@ __global__ void __launch_bounds__(kThreads) k36_conv_step(const ConvParams p, in
     for (int r = 0; r < kRowsAtOnce; ++r) {
         const bool on = row0 + r < rows;
         now[r].clear();
-        if (on && here[r] >= 0) col.load(now[r], x + (row0 + r) * sx);
+        if (on) col.load(now[r], x + (row0 + r) * sx);  // (whether or not it will be used: positions arrive no sooner)
 #pragma unroll
         for (int j = 1; j < K; ++j) {
             old[r][j - 1].clear();
-            if (on && j <= keep && (here[r] < 0 || j <= here[r])) col.load(old[r][j - 1], state + (row0 + r) * size + (keep - j) * p.channels);
+            if (on && j <= keep) col.load(old[r][j - 1], state + (row0 + r) * size + (keep - j) * p.channels);
         }
     }
     Two w[K][V / 2], bias[V / 2];
@@ -426,6 +462,11 @@ __global__ void __launch_bounds__(kThreads) k36_conv_step(const ConvParams p, in
 #pragma unroll
     for (int r = 0; r < kRowsAtOnce; ++r) {
         if (row0 + r >= rows) break;
+        if (here[r] >= 0 && here[r] < K - 1) {  // in front of the sequence there is nothing
+#pragma unroll
+            for (int j = 1; j < K; ++j)
+                if (j > here[r]) old[r][j - 1].clear();
+        }
         Two u[V / 2];
 #pragma unroll
         for (int k = 0; k < V / 2; ++k) u[k] = bias[k];
@@ -461,17 +502,19 @@ ConvTiles tiles_of(int64_t blocks, int32_t t, int64_t channels, int v)
     const int64_t units = (channels + v - 1) / v;
     x.threads = units >= kThreads ? kThreads : (int)((units + 31) / 32 * 32);
     x.groups = (int)((units + x.threads - 1) / x.threads);
-    // eight CTAs per SM, of at least 32 slots each
-    const int64_t wanted = 148 * 8 * kThreads / x.threads / x.groups, slots = wanted ? (blocks * t + wanted - 1) / wanted : t;
-    x.slots = (int)(slots < 32 ? 32 : slots > t ? t : slots);
+    // four CTAs per SM, as many as registers allow, in one wave; tiles of at least 32 slots
+    const int64_t wanted = (int64_t)148 * 4 * kThreads / x.threads / x.groups / blocks, slots = wanted > 1 ? (t + wanted - 1) / wanted : t;
+    x.slots = (int)(slots < 32 ? 32 : slots);
     x.tiles = (t + x.slots - 1) / x.slots;
     return x;
 }
 
+// pieces of V elements lie on boundaries of their size, and t slots span less than 2^32 bytes
 template <typename T, int V>
-bool on(const Channels<T>& x)
+bool on(const Channels<T>& x, int32_t t)
 {
     constexpr size_t n = V * sizeof(T) < 16 ? V * sizeof(T) : 16;
+    if ((uint64_t)x.slot * sizeof(T) >= ((uint64_t)1 << 31) / (uint64_t)t) return false;
     return reinterpret_cast<uintptr_t>(x.data) % n == 0 && x.block * sizeof(T) % n == 0 && x.slot * sizeof(T) % n == 0;
 }
 
@@ -505,7 +548,7 @@ cudaError_t launch_conv(const ConvParams& p, const ConvTensors<T>& a, cudaStream
     return with_taps(p.taps, [&](auto k) {
         constexpr int K = decltype(k)::value, V = kChannels<K, false, T>;
         const ConvTiles x = tiles_of(p.blocks, p.t, p.channels, V);
-        const bool wide = on<const T, V>(a.x) && on<T, V>(a.y) && p.channels % V == 0;
+        const bool wide = on<const T, V>(a.x, p.t) && on<T, V>(a.y, p.t) && p.channels % V == 0 && p.channels * (int64_t)sizeof(T) < ((int64_t)1 << 31);
         auto* kernel = wide ? k34_conv<T, V, K, true> : k34_conv<T, V, K, false>;
         constexpr int kShared = Slots<T, V, K, true, 1>::kShared;
         static std::atomic<uint64_t> allowed{0};
@@ -524,7 +567,7 @@ cudaError_t launch_conv_grad(const ConvParams& p, const ConvTensors<T>& a, cudaS
     const cudaError_t e = with_taps(p.taps, [&](auto k) {
         constexpr int K = decltype(k)::value, V = kChannels<K, true, T>;
         x = tiles_of(p.blocks, p.t, p.channels, V);
-        const bool wide = on<const T, V>(a.x) && on<const T, V>(a.dy) && on<T, V>(a.dx) && p.channels % V == 0;
+        const bool wide = on<const T, V>(a.x, p.t) && on<const T, V>(a.dy, p.t) && on<T, V>(a.dx, p.t) && p.channels % V == 0 && p.channels * (int64_t)sizeof(T) < ((int64_t)1 << 31);
         auto* kernel = wide ? k35_conv_grad<T, V, K, true> : k35_conv_grad<T, V, K, false>;
         constexpr int kShared = Slots<T, V, K, true, 2>::kShared;
         static std::atomic<uint64_t> allowed{0};
@@ -547,8 +590,8 @@ cudaError_t launch_conv_step(const ConvParams& p, int64_t rows, const T* state, 
         constexpr int K = decltype(k)::value, V = kChannels<K, true, T>;
         const int64_t units = (p.channels + V - 1) / V;
         const int threads = units >= kThreads ? kThreads : (int)((units + 31) / 32 * 32), groups = (int)((units + threads - 1) / threads);
-        auto fits = [&](const T* data, int64_t row) { return on<const T, V>(Channels<const T>{data, row, 0}); };
-        const bool wide = fits(state, p.channels) && fits(next, p.channels) && fits(x, sx) && fits(y, sy) && p.channels % V == 0;
+        auto fits = [&](const T* data, int64_t row) { return on<const T, V>(Channels<const T>{data, row, 0}, 1); };
+        const bool wide = fits(state, p.channels) && fits(next, p.channels) && fits(x, sx) && fits(y, sy) && p.channels % V == 0 && p.channels * (int64_t)sizeof(T) < ((int64_t)1 << 31);
         auto* kernel = wide ? k36_conv_step<T, V, K, true> : k36_conv_step<T, V, K, false>;
         kernel<<<(unsigned)((rows + kRowsAtOnce - 1) / kRowsAtOnce * groups), threads, 0, st>>>(p, rows, state, next, x, sx, y, sy, groups);
         count_launches(1);

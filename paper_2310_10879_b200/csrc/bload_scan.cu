@@ -139,11 +139,11 @@ struct Place {
         at[1] = (e + 1 - odd) * 8 + pair % 8;
         slot = threadIdx.x >> 3;
         m = threadIdx.x & 7;
-        const int64_t i = blockIdx.x / cuts.groups;
-        c0 = (int64_t)(blockIdx.x - i * cuts.groups) * S::kChannels;
+        const unsigned i = blockIdx.x / (unsigned)cuts.groups, walks = (unsigned)p.blocks;  // (a grid has less than 2^31 CTAs)
+        c0 = (int64_t)(blockIdx.x - i * (unsigned)cuts.groups) * S::kChannels;
         there = (int)max((int64_t)0, min(p.channels - c0 - m * S::kV, (int64_t)S::kV));
-        segment = (int)(i / p.blocks);
-        q = i - segment * p.blocks;
+        segment = (int)(i / walks);
+        q = i - segment * walks;
         begin = 0;
         stop = p.t;
         enters = leaves = false;
@@ -912,84 +912,94 @@ __global__ void __launch_bounds__(256) k40_scan_sums(const ScanParams p, const S
         a.dc.at(q, s)[n - all] = from_float<T>(v);
 }
 
-// A lane has four states of a channel, LANES of them the channel, and kRowsAtOnce rows one after the other, all loads under way.
+// A lane has four states of a channel, LANES of them the channel, in kStepRows rows, whose loads are all under way before the first is
+// used.  Bytes: the states, in and out.  WIDE: states and rows of b and c in pieces of four.
 constexpr int kStepRows = 4;
-template <typename T, int LANES>
-__global__ void __launch_bounds__(kThreads) k41_scan_step(const ScanStepParams p, const ScanStepTensors<T> a, int groups, bool wide)
+template <typename T, int LANES, bool WIDE>
+__global__ void __launch_bounds__(kThreads) k41_scan_step(const ScanStepParams p, const ScanStepTensors<T> a, unsigned groups)
 {
-    const int64_t at = blockIdx.x / groups, row0 = at * kStepRows;
+    const unsigned at = blockIdx.x / groups;
+    const int64_t row0 = (int64_t)at * kStepRows;
     const int part = threadIdx.x % LANES, n0 = part * 4;
-    const int64_t c = (blockIdx.x - at * groups) * (kThreads / LANES) + threadIdx.x / LANES;
-    const bool on = c < p.channels;
-    float h[kStepRows][4], b[kStepRows][4], cc[kStepRows][4], x[kStepRows], dt[kStepRows], z[kStepRows];
+    const int64_t c = (int64_t)(blockIdx.x - at * groups) * (kThreads / LANES) + threadIdx.x / LANES;
+    const bool on = c < p.channels && n0 < p.states, there = c < p.channels;
+    const int rows = (int)min(p.rows - row0, (int64_t)kStepRows);
+    const bool in_place = p.next == p.state;
     int here[kStepRows];
 #pragma unroll
-    for (int r = 0; r < kStepRows; ++r) here[r] = row0 + r < p.rows ? p.pos[row0 + r] : -1;
-    auto four = [&](const float* from, float (&to)[4]) {
-        if (wide) {
-            const float4 v = n0 < p.states ? *reinterpret_cast<const float4*>(from) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            to[0] = v.x;
-            to[1] = v.y;
-            to[2] = v.z;
-            to[3] = v.w;
-        } else {
+    for (int r = 0; r < kStepRows; ++r) here[r] = r < rows ? p.pos[row0 + r] : -1;
+
+    const int64_t per = p.channels * p.states, first = row0 * per + c * p.states + n0;
+    Elements<float, 4> h[kStepRows], decays;
+    Elements<T, 4> b[kStepRows], cc[kStepRows];
+    float x[kStepRows], dt[kStepRows], z[kStepRows];
+    const int left = p.states - n0;
+    {
+        const float* from = p.state + first;
+        const T *bp = a.b + row0 * a.sb + n0, *cp = a.c + row0 * a.sc + n0, *xp = a.x + row0 * a.sx + c, *dp = a.dt + row0 * a.sdt + c,
+                *zp = a.z ? a.z + row0 * a.sz + c : nullptr;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) to[i] = n0 + i < p.states ? from[i] : 0.0f;
+        for (int r = 0; r < kStepRows; ++r) {
+            h[r].clear();
+            b[r].clear();
+            cc[r].clear();
+            if (on && r < rows) {  // (whether or not they will be used: positions arrive no sooner)
+                h[r].load(from, WIDE ? 4 : left, WIDE);
+                b[r].load(bp, WIDE ? 4 : left, WIDE);
+                cc[r].load(cp, WIDE ? 4 : left, WIDE);
+            }
+            x[r] = there && r < rows ? to_float(*xp) : 0.0f;
+            dt[r] = there && r < rows ? to_float(*dp) : 0.0f;
+            z[r] = there && r < rows && a.z ? to_float(*zp) : 0.0f;
+            from += per;
+            bp += a.sb;
+            cp += a.sc;
+            xp += a.sx;
+            dp += a.sdt;
+            if (a.z) zp += a.sz;
         }
-    };
-#pragma unroll
-    for (int r = 0; r < kStepRows; ++r) {
-        const int64_t row = row0 + r;
-        const bool state = on && row < p.rows && (here[r] > 0 || (here[r] < 0 && p.next != p.state)), frame = on && here[r] >= 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h[r][i] = 0.0f;
-            b[r][i] = frame && n0 + i < p.states ? to_float(a.b[row * a.sb + n0 + i]) : 0.0f;
-            cc[r][i] = frame && n0 + i < p.states ? to_float(a.c[row * a.sc + n0 + i]) : 0.0f;
-        }
-        if (state) four(p.state + (row * p.channels + c) * p.states + n0, h[r]);
-        x[r] = frame ? to_float(a.x[row * a.sx + c]) : 0.0f;
-        dt[r] = frame ? to_float(a.dt[row * a.sdt + c]) : 0.0f;
-        z[r] = frame && a.z ? to_float(a.z[row * a.sz + c]) : 0.0f;
     }
-    float decays[4] = {0.0f, 0.0f, 0.0f, 0.0f}, bias = 0.0f, skip = 0.0f;
-    if (on) {
-        four(p.a + c * p.states + n0, decays);
+    decays.clear();
+    float bias = 0.0f, skip = 0.0f;
+    if (on) decays.load(p.a + c * p.states + n0, WIDE ? 4 : left, WIDE);
+    if (there) {
         bias = p.dt_bias ? p.dt_bias[c] : 0.0f;
         skip = p.d ? p.d[c] : 0.0f;
     }
+    Two a2[2] = {decays.pair(0) * two(kLog2E, kLog2E), decays.pair(2) * two(kLog2E, kLog2E)};
+    float* to = p.next + first;
+    T* yp = a.y + row0 * a.sy + c;
 #pragma unroll
-    for (int r = 0; r < kStepRows; ++r) {
-        const int64_t row = row0 + r;
-        if (row >= p.rows) break;
-        float delta = dt[r] + bias, y = 0.0f;
-        if (p.softplus) delta = one(softplus_of(two(delta, delta))).x;
-        const float u = delta * x[r];
-        if (here[r] >= 0) {
+    for (int r = 0; r < kStepRows; r += 2) {
+        // two rows' delta together
+        Two delta = two(dt[r] + bias, dt[r + 1] + bias);
+        if (p.softplus) delta = softplus_of(delta);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float push = u * b[r][i];
-                h[r][i] = here[r] > 0 ? fmaf(ex2(delta * (decays[i] * kLog2E)), h[r][i], push) : push;
-                y = fmaf(h[r][i], cc[r][i], y);
+        for (int i = 0; i < 2; ++i) {
+            const int k = r + i;
+            if (k >= rows) break;
+            const float d = i ? one(delta).y : one(delta).x;
+            const Two d2 = two(d, d), u = two(d * x[k], d * x[k]);
+            Two sum = zero();
+            if (here[k] >= 0) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const Two push = u * b[k].pair(2 * j), now = here[k] > 0 ? fma(decay(d2, a2[j]), h[k].pair(2 * j), push) : push;
+                    h[k].set_pair(2 * j, now);
+                    sum = fma(now, cc[k].pair(2 * j), sum);
+                }
             }
-        }
+            float y = one(sum).x + one(sum).y;
 #pragma unroll
-        for (int bit = LANES / 2; bit; bit /= 2) y += __shfl_xor_sync(0xffffffffu, y, bit);
-        if (!on) continue;
-        if (here[r] >= 0 || p.next != p.state) {
-            float* const to = p.next + (row * p.channels + c) * p.states + n0;
-            if (wide) {
-                if (n0 < p.states) *reinterpret_cast<float4*>(to) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (n0 + i < p.states) to[i] = h[r][i];
+            for (int bit = LANES / 2; bit; bit /= 2) y += __shfl_xor_sync(0xffffffffu, y, bit);
+            if (on && (here[k] >= 0 || !in_place)) h[k].store(to, WIDE ? 4 : left, WIDE);
+            if (there && part == 0) {
+                y = fmaf(skip, x[k], y);
+                if (a.z) y *= z[k] * sigmoid_of(z[k]);
+                *yp = from_float<T>(here[k] >= 0 ? y : 0.0f);
             }
-        }
-        if (part == 0) {
-            y = fmaf(skip, x[r], y);
-            if (a.z) y *= z[r] * sigmoid_of(z[r]);
-            a.y[row * a.sy + c] = from_float<T>(here[r] >= 0 ? y : 0.0f);
+            to += per;
+            yp += a.sy;
         }
     }
 }
@@ -1139,10 +1149,12 @@ cudaError_t launch_scan_step(const ScanStepParams& p, const ScanStepTensors<T>& 
 {
     auto go = [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
-        const int groups = (int)((p.channels + kThreads / L - 1) / (kThreads / L));
+        const unsigned groups = (unsigned)((p.channels + kThreads / L - 1) / (kThreads / L));
         auto on_16 = [](const float* x) { return reinterpret_cast<uintptr_t>(x) % 16 == 0; };
-        const bool wide = p.states % 4 == 0 && on_16(p.state) && on_16(p.next) && on_16(p.a);
-        k41_scan_step<T, L><<<(unsigned)((p.rows + kStepRows - 1) / kStepRows * groups), kThreads, 0, st>>>(p, a, groups, wide);
+        auto on_4 = [&](const T* x, int64_t row) { return reinterpret_cast<uintptr_t>(x) % (4 * sizeof(T)) == 0 && row % 4 == 0; };
+        const bool wide = p.states % 4 == 0 && on_16(p.state) && on_16(p.next) && on_16(p.a) && on_4(a.b, a.sb) && on_4(a.c, a.sc);
+        auto* kernel = wide ? k41_scan_step<T, L, true> : k41_scan_step<T, L, false>;
+        kernel<<<(unsigned)((p.rows + kStepRows - 1) / kStepRows) * groups, kThreads, 0, st>>>(p, a, groups);
         count_launches(1);
         return cudaGetLastError();
     };
