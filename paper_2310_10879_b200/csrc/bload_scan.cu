@@ -215,6 +215,14 @@ __device__ __forceinline__ void load_states(const ScanParams& p, const Place<S>&
     }
 }
 template <typename S>
+__device__ __forceinline__ void prefetch_states(const ScanParams& p, const Place<S>& at, const float* base)
+{
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+        if (at.c0 + at.ch[c] < p.channels && at.part * S::kStates < p.states)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(base + ((uint32_t)at.ch[c] * (uint32_t)p.states + (uint32_t)(at.part * S::kStates))));
+}
+template <typename S>
 __device__ __forceinline__ void store_states(const ScanParams& p, const Place<S>& at, float* base, const Two (&h)[2][S::kPairs])
 {
     const int n = at.part * S::kStates;
@@ -259,6 +267,10 @@ struct Frames {
             v.load(at_slot(x, at, s0), at.there, false);
         else
             v.clear();
+    }
+    static __device__ __forceinline__ void prefetch(const Channels<const T>& x, const Place<S>& at, int s0)
+    {
+        if (WIDE && at.there && s0 + at.slot >= at.begin) asm volatile("prefetch.global.L2 [%0];" ::"l"(at_slot(x, at, s0)));
     }
     static __device__ __forceinline__ void store(const Piece& v, const Channels<T>& x, const Place<S>& at, int s0)
     {
@@ -365,6 +377,7 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
     __shared__ __align__(16) float4 prepared[kRun][S::kChannels];  // delta, delta, delta x, delta x
     __shared__ __align__(16) float rows[kRun][2][S::kAll];
     __shared__ float sums[OUTPUT ? kRun : 1][OUTPUT ? S::kRow : 1];
+    __shared__ float2 of_channel[S::kChannels / 2][2];  // dt_bias, d, of two channels each
 
     const Place<S> at(p, cuts);
     const int32_t* const pos = p.pos + at.q * p.t;
@@ -389,8 +402,19 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
     if (OUTPUT && at.enters && at.begin < at.stop) load_states(p, at, work.state + (cell - p.blocks) * per + first_state, h);
 
     float passed[2] = {0.0f, 0.0f};
-    const int64_t c_mem = at.c0 + at.m * S::kV;
     const bool gated = OUTPUT && a.z.data, softplus = p.softplus;
+
+    for (int c = threadIdx.x; c < S::kChannels; c += kThreads) {
+        const bool there = at.c0 + c < p.channels;
+        const int pair = c % S::kV / 2 * 8 + c / S::kV;
+        reinterpret_cast<float*>(of_channel[pair])[c & 1] = p.dt_bias && there ? p.dt_bias[at.c0 + c] : 0.0f;
+        reinterpret_cast<float*>(of_channel[pair])[2 + (c & 1)] = OUTPUT && p.d && there ? p.d[at.c0 + c] : 0.0f;
+    }
+    __syncthreads();
+    auto of_pair = [&](int which, int e) {
+        const float2 v = of_channel[e / 2 * 8 + at.m][which];
+        return two(v.x, v.y);
+    };
 
     using F = Frames<T, S, WIDE>;
     Elements<T, S::kV> x, dt, z;
@@ -413,10 +437,9 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
         const Elements<T, S::kV> now_x = x, now_z = z;
         const bool on = (valid >> at.slot) & 1;
         if (on) {
-            const auto bias = of_channels<S::kV>(p.dt_bias, c_mem, at.there);
 #pragma unroll
             for (int e = 0; e < S::kV; e += 2) {
-                Two delta = dt.pair(e) + bias.pair(e);
+                Two delta = dt.pair(e) + of_pair(0, e);
                 if (softplus) delta = softplus_of(delta);
                 if (!WIDE) delta = two(e < at.there ? one(delta).x : 0.0f, e + 1 < at.there ? one(delta).y : 0.0f);
                 const float2 d = one(delta), u = one(delta * x.pair(e));
@@ -471,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
                 sums[g + first][at.at[0]] = y[0][0];
             }
         };
-#pragma unroll 1
+#pragma unroll 2
         for (int g = 0; g < kRun; g += 2 * S::kGroup) {
             if (((now_starts | now_ends) >> g) & ((1 << 2 * S::kGroup) - 1)) {
                 group(g, std::true_type());
@@ -485,10 +508,9 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
         if (OUTPUT && s0 + at.slot >= at.begin && s0 + at.slot < at.stop) {
             Elements<T, S::kV> out;
             if (on) {
-                const auto skip = of_channels<S::kV>(p.d, c_mem, at.there);
 #pragma unroll
                 for (int e = 0; e < S::kV; e += 2) {
-                    Two v = fma(skip.pair(e), now_x.pair(e), two(sums[at.slot][e * 8 + at.m], sums[at.slot][e * 8 + 8 + at.m]));
+                    Two v = fma(of_pair(1, e), now_x.pair(e), two(sums[at.slot][e * 8 + at.m], sums[at.slot][e * 8 + 8 + at.m]));
                     if (gated) v = v * (now_z.pair(e) * sigmoid_of(now_z.pair(e)));
                     out.set_pair(e, v);
                 }
@@ -542,14 +564,11 @@ struct GradShared {
     float4 prepared[kRun][S::kChannels];  // delta, delta, delta x, delta x; then sums over states: g b, g a h, h c, and delta
     float dv[kRun][S::kChannels];         // dy times the gate
     float rows[2][kRun][2][S::kAll];      // b, c as they are, and with the pairs of each lane's states the other way round
-    // The states that enter every other slot, of a thread: pair by pair, both channels.  Where a warp has read those of two slots, it
-    // leaves their db and dc, of its channels.
-    float4 kept[kRun / 2][S::kPairs][kThreads];
-    __device__ float* across(int warp, int slot)
-    {
-        constexpr bool two_planes = S::kPairs == 2;
-        return reinterpret_cast<float*>(&kept[slot / 2][two_planes ? slot & 1 : 0][warp * 32]) + (two_planes ? 0 : (slot & 1) * 2 * S::kAll);
-    }
+    // The states that enter every other slot, of a thread, channel by channel.  Where a warp has read those of two slots, it leaves
+    // their db and dc, of its channels.
+    using States = std::conditional_t<S::kPairs == 2, float4, float2>;
+    States kept[kRun / 2][2][kThreads];
+    __device__ float* across(int warp, int slot) { return reinterpret_cast<float*>(&kept[slot / 2][slot & 1][warp * 32]); }
 };
 template <typename S>
 constexpr int kPartShared = offsetof(GradShared<S>, kept);  // without output
@@ -654,6 +673,13 @@ __global__ void __launch_bounds__(kThreads, 4)
             if (S::kPairs == 2) bc.store(sh.rows[1], 2);
         }
         __syncthreads();
+        if (run > first) {  // the next run's tensors come as far as the second cache meanwhile
+            if (OUTPUT) F::prefetch(a.x, at, s0 - kRun);
+            F::prefetch(a.dt, at, s0 - kRun);
+            F::prefetch(a.dy, at, s0 - kRun);
+            if (gated) F::prefetch(a.z, at, s0 - kRun);
+            if (OUTPUT) prefetch_states(p, at, p.carry + (at.q * runs + run - 1) * per + first_state);
+        }
 
         if (OUTPUT) {  // the states that enter the even slots
             auto forward = [&](int g, auto with_breaks) {
@@ -663,9 +689,12 @@ __global__ void __launch_bounds__(kThreads, 4)
                     const int s = g + i;
                     if (i % 2 == 0)
 #pragma unroll
-                        for (int k = 0; k < S::kPairs; ++k) {
-                            const float2 x = one(h[0][k]), y = one(h[1][k]);
-                            sh.kept[s / 2][k][threadIdx.x] = make_float4(x.x, x.y, y.x, y.y);
+                        for (int c = 0; c < 2; ++c) {
+                            const float2 x = one(h[c][0]), y = one(h[c][S::kPairs - 1]);
+                            if constexpr (S::kPairs == 2)
+                                sh.kept[s / 2][c][threadIdx.x] = make_float4(x.x, x.y, y.x, y.y);
+                            else
+                                sh.kept[s / 2][c][threadIdx.x] = x;
                         }
                     Two B[S::kPairs];
                     pairs_of<S>(b_rows + s * 2 * S::kAll, B);
@@ -693,99 +722,95 @@ __global__ void __launch_bounds__(kThreads, 4)
         auto backward = [&](int g0, auto with_breaks) {
             constexpr bool breaks = decltype(with_breaks)::value;
             float sum[3][2][S::kGroup];  // over states: g b, g a h, h c
-            {
-                constexpr int i0 = 0;
-                Two decays[2][2][S::kPairs], w[2][2][S::kPairs], now[2][2][S::kPairs];  // exp(delta a), exp(delta a) h before, h
+            Two B[2][S::kPairs], C[2][S::kPairs], db[2][S::kPairs], dc[2][S::kPairs];  // of both slots
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+            for (int i = 0; i < 2; ++i) {
+                if (OUTPUT) pairs_of<S>(b_rows + (g0 + i) * 2 * S::kAll, B[i]);
+                pairs_of<S>(b_rows + (g0 + i) * 2 * S::kAll + S::kAll, C[i]);
+            }
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int s = g0 + i0 + i;
-                        const float4 d = sh.prepared[s][at.at[c]];
-                        Two B[S::kPairs];
-                        if (OUTPUT) pairs_of<S>(b_rows + s * 2 * S::kAll, B);
-                        const bool start = breaks && ((starts >> s) & 1);
+            for (int c = 0; c < 2; ++c) {
+                Two decays[2][S::kPairs], w[2][S::kPairs], now[2][S::kPairs];  // exp(delta a), exp(delta a) h before, h
+                float4 d[2];
 #pragma unroll
-                        for (int k = 0; k < S::kPairs; ++k) {
-                            decays[i][c][k] = decay(two(d.x, d.y), A[c][k]);
-                            if (OUTPUT) {
-                                Two before;
-                                if (i) {
-                                    before = now[0][c][k];
-                                } else {
-                                    const float2 x = reinterpret_cast<const float2*>(&sh.kept[s / 2][k][threadIdx.x])[c];
-                                    before = two(x.x, x.y);
-                                }
-                                w[i][c][k] = decays[i][c][k] * before;
-                                if (start) w[i][c][k] = zero();
-                                now[i][c][k] = fma(two(d.z, d.w), B[k], w[i][c][k]);
-                            }
-                            if (start) decays[i][c][k] = zero();
+                for (int i = 0; i < 2; ++i) d[i] = sh.prepared[g0 + i][at.at[c]];
+                if (OUTPUT) {
+                    float before[4];
+                    *reinterpret_cast<typename GradShared<S>::States*>(before) = sh.kept[g0 / 2][c][threadIdx.x];
+#pragma unroll
+                    for (int k = 0; k < S::kPairs; ++k) now[1][k] = two(before[2 * k], before[2 * k + 1]);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const bool start = breaks && ((starts >> (g0 + i)) & 1);
+#pragma unroll
+                    for (int k = 0; k < S::kPairs; ++k) {
+                        decays[i][k] = decay(two(d[i].x, d[i].y), A[c][k]);
+                        if (OUTPUT) {
+                            w[i][k] = decays[i][k] * now[1 - i][k];
+                            if (start) w[i][k] = zero();
+                            now[i][k] = fma(two(d[i].z, d[i].w), B[i][k], w[i][k]);
                         }
-                        if (!OUTPUT) passed[c] += d.x;
                     }
+                    if (!OUTPUT) passed[c] += d[i].x;
+                }
 #pragma unroll
                 for (int i = 1; i >= 0; --i) {
-                    const int s = g0 + i0 + i;
-                    Two B[S::kPairs], C[S::kPairs], db[S::kPairs], dc[S::kPairs];
-                    if (OUTPUT) pairs_of<S>(b_rows + s * 2 * S::kAll, B);
-                    pairs_of<S>(b_rows + s * 2 * S::kAll + S::kAll, C);
-                    const bool start = breaks && ((starts >> s) & 1);
+                    const bool start = breaks && ((starts >> (g0 + i)) & 1);
+                    const float dv1 = sh.dv[g0 + i][at.at[c]];
+                    const Two dv = two(dv1, dv1), u = two(d[i].z, d[i].w), delta = two(d[i].x, d[i].y);
+                    Two gb, gah, hc;
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const float4 d = sh.prepared[s][at.at[c]];
-                        const float dv1 = sh.dv[s][at.at[c]];
-                        const Two dv = two(dv1, dv1), u = two(d.z, d.w), delta = two(d.x, d.y);
-                        Two gb, gah, hc;
-#pragma unroll
-                        for (int k = 0; k < S::kPairs; ++k) {
-                            const Two g = fma(dv, C[k], e[c][k]);
-                            if (OUTPUT) {
-                                const Two h1 = now[i][c][k], gw = g * w[i][c][k];
-                                hc = k ? fma(h1, C[k], hc) : h1 * C[k];
-                                dc[k] = c ? fma(dv, h1, dc[k]) : dv * h1;
-                                db[k] = c ? fma(u, g, db[k]) : u * g;
-                                gb = k ? fma(g, B[k], gb) : g * B[k];
-                                gah = k ? fma(gw, A[c][k], gah) : gw * A[c][k];
-                                dA[c][k] = fma(gw, delta, dA[c][k]);
-                            }
-                            e[c][k] = decays[i][c][k] * g;
-                            if (start) e[c][k] = zero();
-                        }
+                    for (int k = 0; k < S::kPairs; ++k) {
+                        const Two g = fma(dv, C[i][k], e[c][k]);
                         if (OUTPUT) {
-                            sum[0][c][i0 + i] = one(gb).x + one(gb).y;
-                            sum[1][c][i0 + i] = one(gah).x + one(gah).y;
-                            sum[2][c][i0 + i] = one(hc).x + one(hc).y;
+                            const Two h1 = now[i][k], gw = g * w[i][k];
+                            hc = k ? fma(h1, C[i][k], hc) : h1 * C[i][k];
+                            dc[i][k] = c ? fma(dv, h1, dc[i][k]) : dv * h1;
+                            db[i][k] = c ? fma(u, g, db[i][k]) : u * g;
+                            gb = k ? fma(g, B[i][k], gb) : g * B[i][k];
+                            gah = k ? fma(gw, A[c][k], gah) : gw * A[c][k];
+                            dA[c][k] = fma(gw, delta, dA[c][k]);
                         }
+                        e[c][k] = decays[i][k] * g;
+                        if (start) e[c][k] = zero();
                     }
                     if (OUTPUT) {
-                        float v[4];  // of one pair of states: db, dc
-                        if (S::kPairs == 2) {
-                            const float2 b1 = one(db[S::kPairs - 1]), c1 = one(dc[S::kPairs - 1]);
-                            const Two b2 = two(__shfl_xor_sync(0xffffffffu, b1.x, 16), __shfl_xor_sync(0xffffffffu, b1.y, 16));
-                            const Two c2 = two(__shfl_xor_sync(0xffffffffu, c1.x, 16), __shfl_xor_sync(0xffffffffu, c1.y, 16));
-                            const float2 b0 = one(db[0] + b2), c0 = one(dc[0] + c2);
-                            v[0] = b0.x;
-                            v[1] = b0.y;
-                            v[2] = c0.x;
-                            v[3] = c0.y;
-                        } else {
-                            v[0] = one(db[0]).x;
-                            v[1] = one(db[0]).y;
-                            v[2] = one(dc[0]).x;
-                            v[3] = one(dc[0]).y;
-                        }
-                        constexpr int kTop = S::kPairs == 2 ? 8 : 16;  // the highest lane bit that is left
-                        constexpr int kSteps = S::kLanes == 4 ? (kTop == 8 ? 2 : 3) : S::kLanes == 8 ? 1 : 0, kLeft = 4 >> kSteps ? 4 >> kSteps : 1;
-                        int from = 0;
-                        share_sums<4, kTop, S::kLanes>(v, at.lane, from);
-                        if (i == 1) __syncwarp();  // all lanes have read the states of both slots
-                        // (where the warp has more lanes for a state than values, copies write the same)
+                        sum[0][c][i] = one(gb).x + one(gb).y;
+                        sum[1][c][i] = one(gah).x + one(gah).y;
+                        sum[2][c][i] = one(hc).x + one(hc).y;
+                    }
+                }
+            }
+            if (OUTPUT) {
+                __syncwarp();  // all lanes have read the states of both slots
 #pragma unroll
-                        for (int j = 0; j < kLeft; ++j) {
-                            const int n = from + j;
-                            sh.across(at.warp, s)[(n >> 1) * S::kAll + at.part * S::kStates + 2 * turned + (n & 1)] = v[j];
-                        }
+                for (int i = 0; i < 2; ++i) {
+                    float v[4];  // of one pair of states: db, dc
+                    if (S::kPairs == 2) {
+                        const float2 b1 = one(db[i][S::kPairs - 1]), c1 = one(dc[i][S::kPairs - 1]);
+                        const Two b2 = two(__shfl_xor_sync(0xffffffffu, b1.x, 16), __shfl_xor_sync(0xffffffffu, b1.y, 16));
+                        const Two c2 = two(__shfl_xor_sync(0xffffffffu, c1.x, 16), __shfl_xor_sync(0xffffffffu, c1.y, 16));
+                        const float2 b0 = one(db[i][0] + b2), c0 = one(dc[i][0] + c2);
+                        v[0] = b0.x;
+                        v[1] = b0.y;
+                        v[2] = c0.x;
+                        v[3] = c0.y;
+                    } else {
+                        v[0] = one(db[i][0]).x;
+                        v[1] = one(db[i][0]).y;
+                        v[2] = one(dc[i][0]).x;
+                        v[3] = one(dc[i][0]).y;
+                    }
+                    constexpr int kTop = S::kPairs == 2 ? 8 : 16;  // the highest lane bit that is left
+                    constexpr int kSteps = S::kLanes == 4 ? (kTop == 8 ? 2 : 3) : S::kLanes == 8 ? 1 : 0, kLeft = 4 >> kSteps ? 4 >> kSteps : 1;
+                    int from = 0;
+                    share_sums<4, kTop, S::kLanes>(v, at.lane, from);
+                    // (where the warp has more lanes for a state than values, copies write the same)
+#pragma unroll
+                    for (int j = 0; j < kLeft; ++j) {
+                        const int n = from + j;
+                        sh.across(at.warp, g0 + i)[(n >> 1) * S::kAll + at.part * S::kStates + 2 * turned + (n & 1)] = v[j];
                     }
                 }
             }
@@ -1014,15 +1039,23 @@ auto with_split(int states, const Go& go)
     return go(Split<16, 4>());
 }
 
-// Segments per walk: enough for eight CTAs per SM where there are fewer than two without, of at least 8 runs each.
+// Segments per walk.  Four CTAs of a walk fit on an SM at once, 592 in all.  What that is for: walks that are too few for it, and a
+// second wave that would be almost empty.  Many small segments (two waves or more, up to 14 CTAs per SM) level the SMs out; where the
+// runs do not suffice for that, 16 to a segment, one wave.  (8 x 4096 x 2048 bf16, 256 walks of prompts: 2 segments 880 us, 4 818, 8
+// 795; 4 x 10,000 x 1024 training, 64 walks: 9 segments 1,664, 18 1,599, 32 1,563; 20,011 x 509 fp32, 8 walks: 74 segments 470, 78 635;
+// 512 walks of 2048 slots: one segment 2,372, four 2,626.)
 ScanCuts cuts_of(int64_t blocks, int32_t t, int64_t channels, int states)
 {
     return with_split(states, [&](auto s) {
         using S = decltype(s);
         ScanCuts cuts;
         cuts.groups = (int)((channels + S::kChannels - 1) / S::kChannels);
-        const int64_t walks = blocks * cuts.groups, runs = (t + kRun - 1) / kRun;
-        const int64_t wanted = walks < 2 * 148 ? 8 * 148 / walks : 1, most = runs / 8, n = wanted < most ? wanted : most;
+        const int64_t walks = blocks * cuts.groups, runs = (t + kRun - 1) / kRun, at_once = 4 * 148;
+        int64_t n = 1;
+        if (walks < at_once / 2 || (walks > at_once && walks < at_once * 3 / 2)) {
+            const int64_t many = 14 * 148 / walks, fit = runs / 16 < many ? runs / 16 : many;
+            n = fit * walks >= 2 * at_once ? fit : at_once / walks < fit ? at_once / walks : fit;
+        }
         cuts.segments = (int)(n < 1 ? 1 : n);
         cuts.stride = 2 * S::kAll;
         return cuts;
