@@ -165,15 +165,23 @@ struct Place {
             }
         }
     }
+    // Position of the run's slot `lane`, up to the first slot behind the run; -1 in front of the segment and behind the block.
+    __device__ __forceinline__ int look(const int32_t* pos, int t, int s0) const
+    {
+        const int s = s0 + lane;
+        return lane <= kRun && s >= begin && s < t ? pos[s] : -1;
+    }
     // bit s of `valid`: slot s of the run is a frame of the segment, of `starts`: it starts a sequence (or is none), of `ends`:
     // its sequence ends with it
-    __device__ __forceinline__ void masks(const int32_t* pos, int t, int s0, unsigned& valid, unsigned& starts, unsigned* ends = nullptr) const
+    __device__ __forceinline__ void masks(int here, int s0, unsigned& valid, unsigned& starts, unsigned& ends) const
     {
-        const int s = s0 + lane, here = lane < kRun && s >= begin && s < stop ? pos[s] : -1;
-        valid = __ballot_sync(0xffffffffu, here >= 0);
-        starts = __ballot_sync(0xffffffffu, here <= 0);
-        if (ends) *ends = __ballot_sync(0xffffffffu, here >= 0 && (s + 1 >= t || pos[s + 1] <= 0));
+        const bool mine = lane < kRun && s0 + lane < stop;
+        valid = __ballot_sync(0xffffffffu, mine && here >= 0);
+        starts = __ballot_sync(0xffffffffu, !mine || here <= 0);
+        ends = valid & (__ballot_sync(0xffffffffu, here <= 0) >> 1);
     }
+    // whether this thread's slot of the run is the segment's
+    __device__ __forceinline__ bool inside(int s0) const { return s0 + slot >= begin && s0 + slot < stop; }
 };
 
 // a[channel][state], of the lane's two channels, as pairs of states; 0 where there is none
@@ -291,13 +299,16 @@ struct Rows {
     static constexpr int kV = 16 / sizeof(T) < S::kAll ? 16 / sizeof(T) : S::kAll, kPieces = kRun * S::kAll / kV;
     static constexpr int kEach = (kPieces + kThreads - 1) / kThreads;
     Elements<T, kV> b[B ? kEach : 1], c[C ? kEach : 1];
-    __device__ __forceinline__ void load(const ScanParams& p, const ScanTensors<T>& a, int64_t q, int s0, unsigned valid)
+    // ALL: of the segment's slots, otherwise of those in `wanted`
+    template <bool ALL>
+    __device__ __forceinline__ void load(const ScanParams& p, const ScanTensors<T>& a, const Place<S>& place, int s0, unsigned wanted = 0)
     {
-        const T *const b0 = a.b.data + q * a.b.block, *const c0 = a.c.data + q * a.c.block;
+        const T *const b0 = a.b.data + place.q * a.b.block, *const c0 = a.c.data + place.q * a.c.block;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int at = threadIdx.x + i * kThreads, slot = at / (S::kAll / kV), n = at % (S::kAll / kV) * kV;
-            const int there = slot < kRun && ((valid >> slot) & 1) ? p.states - n : 0;
+            const bool here = ALL ? s0 + slot >= place.begin && s0 + slot < place.stop : (wanted >> slot) & 1;
+            const int there = slot < kRun && here ? p.states - n : 0;
             b[B ? i : 0].clear();
             c[C ? i : 0].clear();
             if (there > 0 && p.rows_wide) {  // (blocks of less than 2^32 elements, too)
@@ -310,16 +321,18 @@ struct Rows {
         }
     }
     // `turn` 2: with the pairs of every four states the other way round
-    __device__ __forceinline__ void store(float (*to)[2][S::kAll], int turn = 0) const
+    __device__ __forceinline__ void store(float (*to)[2][S::kAll], unsigned valid, int turn = 0) const
     {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int at = threadIdx.x + i * kThreads, slot = at / (S::kAll / kV), n = at % (S::kAll / kV) * kV;
             if (slot >= kRun) break;
+            const bool on = (valid >> slot) & 1;
 #pragma unroll
             for (int e = 0; e < kV; e += 2) {
-                if (B) *reinterpret_cast<float2*>(&to[slot][0][n + (e ^ turn)]) = make_float2(b[B ? i : 0].get(e), b[B ? i : 0].get(e + 1));
-                if (C) *reinterpret_cast<float2*>(&to[slot][1][n + (e ^ turn)]) = make_float2(c[C ? i : 0].get(e), c[C ? i : 0].get(e + 1));
+                const float2 none = make_float2(0.0f, 0.0f);
+                if (B) *reinterpret_cast<float2*>(&to[slot][0][n + (e ^ turn)]) = on ? one(b[B ? i : 0].pair(e)) : none;
+                if (C) *reinterpret_cast<float2*>(&to[slot][1][n + (e ^ turn)]) = on ? one(c[C ? i : 0].pair(e)) : none;
             }
         }
     }
@@ -423,20 +436,22 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
     Elements<T, S::kV> x, dt, z;
     z.clear();
     Rows<T, S, true, OUTPUT> bc;
-    unsigned valid, starts, ends = 0;
-    auto fetch = [&](int r) {
+    int here;
+    auto fetch = [&](int r) {  // (padding as well: whether a slot is a frame is known only when its position has arrived)
         const int s0 = r * kRun;
-        at.masks(pos, p.t, s0, valid, starts, OUTPUT && p.last ? &ends : nullptr);
-        const bool on = (valid >> at.slot) & 1;
+        here = at.look(pos, p.t, s0);
+        const bool on = at.inside(s0);
         F::load(x, a.x, at, s0, on);
         F::load(dt, a.dt, at, s0, on);
         if (gated) F::load(z, a.z, at, s0, on);
-        bc.load(p, a, at.q, s0, valid);
+        bc.template load<true>(p, a, at, s0);
     };
     if (run < end) fetch(run);
     for (; run < end; ++run) {
         const int s0 = run * kRun;
-        const unsigned now_starts = starts, now_ends = ends;
+        unsigned valid, now_starts, now_ends;
+        at.masks(here, s0, valid, now_starts, now_ends);
+        if (!OUTPUT || !p.last) now_ends = 0;
         const Elements<T, S::kV> now_x = x, now_z = z;
         const bool on = (valid >> at.slot) & 1;
         if (on) {
@@ -453,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
 #pragma unroll
             for (int e = 0; e < S::kV; ++e) prepared[at.slot][e * 8 + at.m] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
-        bc.store(rows);
+        bc.store(rows, valid);
         if (OUTPUT && p.carry && s0 >= at.begin) store_states(p, at, p.carry + (at.q * runs + run) * per + first_state, h);
         __syncthreads();
         if (run + 1 < end) fetch(run + 1);
@@ -508,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
             }
         }
         __syncthreads();
-        if (OUTPUT && s0 + at.slot >= at.begin && s0 + at.slot < at.stop) {
+        if (OUTPUT && at.inside(s0)) {
             Elements<T, S::kV> out;
             if (on) {
 #pragma unroll
@@ -631,10 +646,11 @@ __global__ void __launch_bounds__(kThreads, 4)
     const bool gated = a.z.data != nullptr, softplus = p.softplus;
     using F = Frames<T, S, WIDE>;
 
+    int here = at.look(pos, p.t, run * kRun);
     for (; run >= first; --run) {
         const int s0 = run * kRun;
-        unsigned valid, starts;
-        at.masks(pos, p.t, s0, valid, starts);
+        unsigned valid, starts, ends;
+        at.masks(here, s0, valid, starts, ends);
         const bool on = (valid >> at.slot) & 1;
         Two h[2][S::kPairs];
         {
@@ -646,7 +662,8 @@ __global__ void __launch_bounds__(kThreads, 4)
             F::load(dy, a.dy, at, s0, on);
             if (gated) F::load(z, a.z, at, s0, on);
             Rows<T, S, OUTPUT, true> bc;
-            bc.load(p, a, at.q, s0, valid);
+            bc.template load<false>(p, a, at, s0, valid);
+            here = at.look(pos, p.t, s0 - kRun);  // of the next run
             if (OUTPUT) {
                 load_states(p, at, p.carry + (at.q * runs + run) * per + first_state, h);
                 turn(h);
@@ -672,8 +689,8 @@ __global__ void __launch_bounds__(kThreads, 4)
                     sh.dv[at.slot][i * 8 + at.m] = 0.0f;
                 }
             }
-            bc.store(sh.rows[0]);
-            if (S::kPairs == 2) bc.store(sh.rows[1], 2);
+            bc.store(sh.rows[0], ~0u);
+            if (S::kPairs == 2) bc.store(sh.rows[1], ~0u, 2);
         }
         __syncthreads();
         if (run > first) {  // the next run's tensors come as far as the second cache meanwhile
@@ -837,7 +854,7 @@ __global__ void __launch_bounds__(kThreads, 4)
         }
         __syncthreads();
         if (OUTPUT) {
-            if (s0 + at.slot >= at.begin && s0 + at.slot < at.stop) {
+            if (at.inside(s0)) {
                 Elements<T, S::kV> x, dt, z, dy;  // (once more: in registers meanwhile they would cost more)
                 x.clear();
                 dt.clear();
