@@ -115,17 +115,18 @@ __global__ void __launch_bounds__(kThreads, 2) k26_rotary(const RotaryParams p, 
     float freq[kPairs];
 #pragma unroll
     for (int e = 0; e < kPairs; ++e) freq[e] = turns ? p.inv_freq[unit * kPairs + e] : 0.0f;
-    const int32_t* along[AXES ? kPairs : 1];  // coordinates of each pair's axis
+    unsigned axes = 0;  // of the pairs, two bits each
     bool one_axis = true;
     if (AXES) {
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
             const int axis = turns ? p.axis[unit * kPairs + e] : 0, known = axis >= 0 && axis < p.axes ? axis : 0;
             if (known != axis) freq[e] = 0.0f;
-            along[AXES ? e : 0] = p.coords + known * p.slots;
-            one_axis = one_axis && along[AXES ? e : 0] == along[0];
+            axes |= (unsigned)known << 2 * e;
+            one_axis = one_axis && (axes >> 2 * e) == (axes & 3);
         }
     }
+    const int32_t* const along = AXES ? p.coords + (int64_t)(axes & 3) * p.slots : nullptr;  // coordinates of the first pair's axis
     const float factor = p.factor, back = p.gradient ? -p.factor : p.factor;
     const T* const x0 = x.data + h0 * x.head + at;
     T* const y0 = y.data + h0 * y.head + at;
@@ -136,13 +137,13 @@ __global__ void __launch_bounds__(kThreads, 2) k26_rotary(const RotaryParams p, 
     const int64_t step_q = step / p.t;
     int s = (int)(slot - q * p.t);
     const int step_s = (int)(step - step_q * p.t);
-    int next = slot < p.slots ? p.pos[slot] : 0, next_at = AXES && slot < p.slots ? along[0][slot] : 0;
+    int next = slot < p.slots ? p.pos[slot] : 0, next_at = AXES && slot < p.slots ? along[slot] : 0;
     for (; slot < p.slots; slot += step) {
         const int pos = next, first_at = next_at;
         int others[AXES ? kPairs : 1];
         if (AXES && !one_axis) {
 #pragma unroll
-            for (int e = 1; e < kPairs; ++e) others[AXES ? e : 0] = along[AXES ? e : 0][slot];
+            for (int e = 1; e < kPairs; ++e) others[AXES ? e : 0] = p.coords[(int64_t)((axes >> 2 * e) & 3) * p.slots + slot];
         }
         const T* from = x0 + q * x.block + s * x.slot;
         T* to = y0 + q * y.block + s * y.slot;
@@ -158,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 2) k26_rotary(const RotaryParams p, 
             }
         if (slot + step < p.slots) {
             next = p.pos[slot + step];
-            if (AXES) next_at = along[0][slot + step];
+            if (AXES) next_at = along[slot + step];
         }
         if (turns && pos >= 0) {
             float cs[kPairs], sn[kPairs];
