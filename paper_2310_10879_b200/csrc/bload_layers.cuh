@@ -293,6 +293,32 @@ struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Elements {
                 if (e < there) p[e] = x[e];
         }
     }
+    // WIDE loads that are predicated rather than branched around: a branch's two values meet in registers, and waiting for them there
+    // would keep a load that is issued early from overlapping with what follows.
+    __device__ __forceinline__ void load_if(const T* p, bool on)
+    {
+        if constexpr (kBytes % 16 == 0) {
+#pragma unroll
+            for (int k = 0; k < kBytes / 16; ++k) {
+                uint32_t w[4] = {0u, 0u, 0u, 0u};
+                asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                             : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3])
+                             : "l"(reinterpret_cast<const char*>(p) + 16 * k), "r"((uint32_t)on));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(x)[4 * k + i] = w[i];
+            }
+        } else if constexpr (kBytes == 8) {
+            uint32_t w[2] = {0u, 0u};
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\t@p ld.global.v2.u32 {%0, %1}, [%2];\n\t}" : "+r"(w[0]), "+r"(w[1]) : "l"(p), "r"((uint32_t)on));
+            reinterpret_cast<uint32_t*>(x)[0] = w[0];
+            reinterpret_cast<uint32_t*>(x)[1] = w[1];
+        } else {
+            static_assert(kBytes == 4, "4, 8 or whole pieces of 16 bytes");
+            uint32_t w = 0u;
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}" : "+r"(w) : "l"(p), "r"((uint32_t)on));
+            reinterpret_cast<uint32_t*>(x)[0] = w;
+        }
+    }
     // elements `step` apart
     __device__ __forceinline__ void load_apart(const T* p, int64_t step, int there)
     {

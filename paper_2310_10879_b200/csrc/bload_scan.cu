@@ -272,12 +272,13 @@ struct Frames {
     }
     static __device__ __forceinline__ void load(Piece& v, const Channels<const T>& x, const Place<S>& at, int s0, bool on)
     {
-        if (WIDE && on && at.there)
-            v.load(at_slot(x, at, s0), S::kV, true);
-        else if (!WIDE && on)
+        if constexpr (WIDE) {
+            v.load_if(at_slot(x, at, s0), on && at.there);
+        } else if (on) {
             v.load(at_slot(x, at, s0), at.there, false);
-        else
+        } else {
             v.clear();
+        }
     }
     static __device__ __forceinline__ void prefetch(const Channels<const T>& x, const Place<S>& at, int s0)
     {
@@ -309,12 +310,14 @@ struct Rows {
             const int at = threadIdx.x + i * kThreads, slot = at / (S::kAll / kV), n = at % (S::kAll / kV) * kV;
             const bool here = ALL ? s0 + slot >= place.begin && s0 + slot < place.stop : (wanted >> slot) & 1;
             const int there = slot < kRun && here ? p.states - n : 0;
+            if (p.rows_wide) {  // (blocks of less than 2^32 elements, too)
+                if (B) b[B ? i : 0].load_if(b0 + ((uint32_t)(s0 + slot) * (uint32_t)a.b.slot + (uint32_t)n), there > 0);
+                if (C) c[C ? i : 0].load_if(c0 + ((uint32_t)(s0 + slot) * (uint32_t)a.c.slot + (uint32_t)n), there > 0);
+                continue;
+            }
             b[B ? i : 0].clear();
             c[C ? i : 0].clear();
-            if (there > 0 && p.rows_wide) {  // (blocks of less than 2^32 elements, too)
-                if (B) b[B ? i : 0].load(b0 + ((uint32_t)(s0 + slot) * (uint32_t)a.b.slot + (uint32_t)n), kV, true);
-                if (C) c[C ? i : 0].load(c0 + ((uint32_t)(s0 + slot) * (uint32_t)a.c.slot + (uint32_t)n), kV, true);
-            } else if (there > 0) {
+            if (there > 0) {
                 if (B) b[B ? i : 0].load(b0 + (s0 + slot) * a.b.slot + n, there, false);
                 if (C) c[C ? i : 0].load(c0 + (s0 + slot) * a.c.slot + n, there, false);
             }
