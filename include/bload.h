@@ -658,7 +658,8 @@ BLOAD_API int bload_norm_grad(const bload_norm_t* a, void* stream);
  *   d_seq_id, n_seq, d_tails   forward: with all of them, the last taps - 1 inputs of every sequence k in [0, n_seq) of the batch
  *              are written to d_tails[k] ([n_seq, taps - 1, channels] of the element type, oldest first, 0 in front of the
  *              sequence): the state from which bload_conv_step goes on.  d_seq_id: int32 [block_count, t_block] as bload_pack
- *              writes it.  Other sequences' rows are left as they were.  d_tails NULL: not wanted
+ *              writes it.  Other sequences' rows are left as they were; a number that several pieces in the batch have (chunks of a
+ *              sequence) gets values of one or the other.  d_tails NULL: not wanted
  *   d_dweight, d_dbias         float, written by the gradient; NULL: not wanted
  *   d_work     scratch of bload_conv_work_bytes bytes for the gradient, 256-byte aligned (NULL when neither sum is wanted); calls
  *              that may overlap on the GPU need one each
@@ -708,7 +709,7 @@ BLOAD_API int bload_conv_step(int64_t rows, int64_t channels, int32_t dtype, int
  *                 each run of BLOAD_SCAN_RUN slots, written by the forward call (NULL: not kept) and read by the gradient
  *   d_seq_id, n_seq, d_last   forward: with all of them, the state behind the last frame of every sequence k in [0, n_seq) of the
  *                 batch is written to d_last[k] (float [n_seq, channels, states]), from which bload_scan_step goes on.  Other
- *                 rows are left as they were.  d_last NULL: not wanted
+ *                 rows are left as they were, numbers that several pieces have as in bload_conv.  d_last NULL: not wanted
  *   d_work        scratch of bload_scan_work_bytes(.., gradient) bytes, 256-byte aligned (NULL when that is 0); calls that may overlap
  *                 on the GPU need one each
  * bload_scan_step -- the same for one new frame of each of `rows` sequences; d_pos as in bload_conv_step.

@@ -9,6 +9,10 @@
 // The gradient walks the same way.  du_s goes to dx of the slots s - j, whose sums are in registers until slot s - (taps - 1) has
 // all of its own; the taps - 1 slots behind the tile are computed once more for it.  Sums over the frames (weights, bias) stay in
 // registers; a tile writes them once and k33 adds the tiles' in their order.
+//
+// 8 x 4096 x 2048 bf16, 4 taps, with the gate: 62 us forward (4.3 TB/s), 104 gradient (3.9 TB/s; 576 CTAs with all their registers); step of
+// 256 x 4096 fp16 7.7 us.  Bound by latency and issue: 30 instructions an element in the
+// gradient, 0.55 of the issue slots, half of what the multiply-adds allow.
 #include <type_traits>
 
 #include "bload_internal.cuh"

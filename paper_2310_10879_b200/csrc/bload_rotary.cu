@@ -9,7 +9,8 @@
 // the slots with its unit and heads fixed: with a thread per slot, unit and group of heads the divisions that place it cost as
 // much as the work (166 us).
 // AXES: the angle is a coordinate of the pair's axis times its frequency, with what the product's rounding loses.  A thread whose pairs
-// all have one axis loads one coordinate per slot; otherwise one per pair, which its neighbours load too.
+// all have one axis loads one coordinate per slot; otherwise one per pair, which its neighbours load too.  16 x 4096 slots
+// of 20 heads of 128, three axes: 124 us (5.4 TB/s); 4 x 5003 x 9 of 80 interleaved fp32, gradient: 29.
 // Pieces are as wide as alignment and the sizes of the turned part and of the rest allow: 16, 8 or 4 bytes, or one element.
 #include "bload_internal.cuh"
 #include "bload_layers.cuh"
