@@ -137,14 +137,14 @@ struct Place {
     __device__ __forceinline__ Place(const ScanParams& p, const ScanCuts& cuts)
     {
         lane = threadIdx.x & 31;
-        warp = threadIdx.x >> 5;
+        warp = (threadIdx.x >> 5) % kWarps;
         part = lane % S::kLanes;
         const int pair = warp * (S::kPerWarp / 2) + lane / S::kLanes, e = pair / 8 * 2, odd = part & 1;
         ch[0] = pair % 8 * S::kV + e + odd;
         ch[1] = pair % 8 * S::kV + e + 1 - odd;
         at[0] = (e + odd) * 8 + pair % 8;
         at[1] = (e + 1 - odd) * 8 + pair % 8;
-        slot = threadIdx.x >> 3;
+        slot = threadIdx.x % kThreads >> 3;
         m = threadIdx.x & 7;
         const unsigned i = blockIdx.x / (unsigned)cuts.groups, walks = (unsigned)p.blocks;  // (a grid has less than 2^31 CTAs)
         c0 = (int64_t)(blockIdx.x - i * (unsigned)cuts.groups) * S::kChannels;
@@ -311,7 +311,7 @@ struct Rows {
         const T *const b0 = a.b.data + place.q * a.b.block, *const c0 = a.c.data + place.q * a.c.block;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int at = threadIdx.x + i * kThreads, slot = at / (S::kAll / kV), n = at % (S::kAll / kV) * kV;
+            const int at = threadIdx.x % kThreads + i * kThreads, slot = at / (S::kAll / kV), n = at % (S::kAll / kV) * kV;
             const bool here = ALL ? s0 + slot >= place.begin && s0 + slot < place.stop : (wanted >> slot) & 1;
             const int there = slot < kRun && here ? p.states - n : 0;
             if (p.rows_wide) {  // (blocks of less than 2^32 elements, too)
@@ -332,7 +332,7 @@ struct Rows {
     {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int at = threadIdx.x + i * kThreads, slot = at / (S::kAll / kV), n = at % (S::kAll / kV) * kV;
+            const int at = threadIdx.x % kThreads + i * kThreads, slot = at / (S::kAll / kV), n = at % (S::kAll / kV) * kV;
             if (slot >= kRun) break;
             const bool on = (valid >> slot) & 1;
 #pragma unroll
@@ -393,13 +393,21 @@ __device__ __forceinline__ void lane_sums(float (&v)[2][S::kGroup], int lane, in
     }
 }
 
+// Named barriers between the two halves of a CTA: one half arrives, the other waits.
+__device__ __forceinline__ void half_arrives(int barrier) { asm volatile("barrier.cta.arrive %0, %1;" ::"r"(barrier), "n"(2 * kThreads) : "memory"); }
+__device__ __forceinline__ void half_waits(int barrier) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(barrier), "n"(2 * kThreads) : "memory"); }
+
+// 128 threads prepare, walk and finish a run in turn.  HALVES: of 256 threads half walk, while the other half finish the run in front and
+// prepare the one behind, in two buffers: a run takes less time (1.6 us instead of 2.3 alone on an SM), but fewer runs fit.
 // OUTPUT false: leaves what crosses the segment's end (kind, delta, state of ScanWork).
-template <typename T, typename S, bool WIDE, bool OUTPUT>
-__global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, const ScanTensors<T> a, const ScanCuts cuts, const ScanWork work)
+template <typename T, typename S, bool WIDE, bool OUTPUT, bool HALVES>
+__global__ void __launch_bounds__(HALVES ? 2 * kThreads : kThreads, HALVES ? 2 : 4)
+    k37_scan(const ScanParams p, const ScanTensors<T> a, const ScanCuts cuts, const ScanWork work)
 {
-    __shared__ __align__(16) float4 prepared[kRun][S::kChannels];  // delta, delta, delta x, delta x
-    __shared__ __align__(16) float rows[kRun][2][S::kAll];
-    __shared__ float sums[OUTPUT ? kRun : 1][OUTPUT ? S::kRow : 1];
+    constexpr int kBuffers = HALVES ? 2 : 1, kFull = 1, kDone = 3;  // barriers kFull, kDone + buffer
+    __shared__ __align__(16) float4 prepared[kBuffers][kRun][S::kChannels];  // delta, delta, delta x, delta x
+    __shared__ __align__(16) float rows[kBuffers][kRun][2][S::kAll];
+    __shared__ float sums[OUTPUT ? kBuffers : 1][OUTPUT ? kRun : 1][OUTPUT ? S::kRow : 1];
     __shared__ float2 of_channel[S::kChannels / 2][2];  // dt_bias, d, of two channels each
 
     const Place<S> at(p, cuts);
@@ -416,6 +424,102 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
         run = max(run, min(start / kRun, end - 1));
         if (threadIdx.x == 0) work.kind[cell] = start < at.begin ? 2 : 1;
     }
+    for (int c = threadIdx.x; c < S::kChannels; c += blockDim.x) {
+        const bool there = at.c0 + c < p.channels;
+        const int pair = c % S::kV / 2 * 8 + c / S::kV;
+        reinterpret_cast<float*>(of_channel[pair])[c & 1] = p.dt_bias && there ? p.dt_bias[at.c0 + c] : 0.0f;
+        reinterpret_cast<float*>(of_channel[pair])[2 + (c & 1)] = OUTPUT && p.d && there ? p.d[at.c0 + c] : 0.0f;
+    }
+    __syncthreads();
+
+    // what prepares and finishes: x, dt, z and y as they lie in memory
+    const bool gated = OUTPUT && a.z.data, softplus = p.softplus;
+    using F = Frames<T, S, WIDE>;
+    Elements<T, S::kV> x, dt, z;
+    z.clear();
+    Rows<T, S, true, OUTPUT> bc;
+    auto of_pair = [&](int which, int e) {
+        const float2 v = of_channel[e / 2 * 8 + at.m][which];
+        return two(v.x, v.y);
+    };
+    auto fetch = [&](int s0) {  // (padding as well: whether a slot is a frame is known only when its position has arrived)
+        const bool on = at.inside(s0);
+        F::load(x, a.x, at, s0, on);
+        F::load(dt, a.dt, at, s0, on);
+        if (gated) F::load(z, a.z, at, s0, on);
+        bc.template load<true>(p, a, at, s0);
+    };
+    auto prepare = [&](int buffer, unsigned valid) {
+        if ((valid >> at.slot) & 1) {
+#pragma unroll
+            for (int e = 0; e < S::kV; e += 2) {
+                Two delta = dt.pair(e) + of_pair(0, e);
+                if (softplus) delta = softplus_of(delta);
+                if (!WIDE) delta = two(e < at.there ? one(delta).x : 0.0f, e + 1 < at.there ? one(delta).y : 0.0f);
+                const float2 d = one(delta), u = one(delta * x.pair(e));
+                prepared[buffer][at.slot][e * 8 + at.m] = make_float4(d.x, d.x, u.x, u.x);
+                prepared[buffer][at.slot][e * 8 + 8 + at.m] = make_float4(d.y, d.y, u.y, u.y);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < S::kV; ++e) prepared[buffer][at.slot][e * 8 + at.m] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+        bc.store(rows[buffer], valid);
+    };
+    auto finish = [&](int buffer, int s0, unsigned valid, const Elements<T, S::kV>& xs, const Elements<T, S::kV>& zs) {
+        if (!at.inside(s0)) return;
+        Elements<T, S::kV> out;
+        if ((valid >> at.slot) & 1) {
+#pragma unroll
+            for (int e = 0; e < S::kV; e += 2) {
+                Two v = fma(of_pair(1, e), xs.pair(e), two(sums[buffer][at.slot][e * 8 + at.m], sums[buffer][at.slot][e * 8 + 8 + at.m]));
+                if (gated) v = v * (zs.pair(e) * sigmoid_of(zs.pair(e)));
+                out.set_pair(e, v);
+            }
+        } else {
+            out.clear();
+        }
+        F::store(out, a.y, at, s0);
+    };
+    if (HALVES && threadIdx.x >= kThreads) {
+        int buffer = 0;
+        unsigned before = 0;  // frames of the run in front
+        Elements<T, S::kV> before_x, before_z;
+        before_x.clear();
+        before_z.clear();
+        const int first = run;
+        int here = -1;
+        if (run < end) {
+            here = at.look(pos, p.t, run * kRun);
+            fetch(run * kRun);
+        }
+        for (; run < end; ++run) {
+            unsigned valid, starts, ends;
+            at.masks(here, run * kRun, valid, starts, ends);
+            prepare(buffer, valid);  // (the buffer is free: its last run has been finished)
+            half_arrives(kFull + buffer);
+            const Elements<T, S::kV> now_x = x, now_z = z;
+            if (run + 1 < end) {
+                here = at.look(pos, p.t, (run + 1) * kRun);
+                fetch((run + 1) * kRun);
+            }
+            buffer ^= 1;
+            if (run > first) {
+                half_waits(kDone + buffer);
+                finish(buffer, (run - 1) * kRun, before, before_x, before_z);
+            }
+            before = valid;
+            before_x = now_x;
+            before_z = now_z;
+        }
+        if (first < end) {
+            buffer ^= 1;
+            half_waits(kDone + buffer);
+            finish(buffer, (end - 1) * kRun, before, before_x, before_z);
+        }
+        return;
+    }
+
     Two A[2][S::kPairs], h[2][S::kPairs];
     load_a(p, at, kLog2E, A);
 #pragma unroll
@@ -423,62 +527,28 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
 #pragma unroll
         for (int k = 0; k < S::kPairs; ++k) h[c][k] = zero();
     if (OUTPUT && at.enters && at.begin < at.stop) load_states(p, at, work.state + (cell - p.blocks) * per + first_state, h);
-
     float passed[2] = {0.0f, 0.0f};
-    const bool gated = OUTPUT && a.z.data, softplus = p.softplus;
-
-    for (int c = threadIdx.x; c < S::kChannels; c += kThreads) {
-        const bool there = at.c0 + c < p.channels;
-        const int pair = c % S::kV / 2 * 8 + c / S::kV;
-        reinterpret_cast<float*>(of_channel[pair])[c & 1] = p.dt_bias && there ? p.dt_bias[at.c0 + c] : 0.0f;
-        reinterpret_cast<float*>(of_channel[pair])[2 + (c & 1)] = OUTPUT && p.d && there ? p.d[at.c0 + c] : 0.0f;
+    int here = -1, buffer = 0;
+    if (run < end) {
+        here = at.look(pos, p.t, run * kRun);
+        if (!HALVES) fetch(run * kRun);
     }
-    __syncthreads();
-    auto of_pair = [&](int which, int e) {
-        const float2 v = of_channel[e / 2 * 8 + at.m][which];
-        return two(v.x, v.y);
-    };
-
-    using F = Frames<T, S, WIDE>;
-    Elements<T, S::kV> x, dt, z;
-    z.clear();
-    Rows<T, S, true, OUTPUT> bc;
-    int here;
-    auto fetch = [&](int r) {  // (padding as well: whether a slot is a frame is known only when its position has arrived)
-        const int s0 = r * kRun;
-        here = at.look(pos, p.t, s0);
-        const bool on = at.inside(s0);
-        F::load(x, a.x, at, s0, on);
-        F::load(dt, a.dt, at, s0, on);
-        if (gated) F::load(z, a.z, at, s0, on);
-        bc.template load<true>(p, a, at, s0);
-    };
-    if (run < end) fetch(run);
     for (; run < end; ++run) {
         const int s0 = run * kRun;
         unsigned valid, now_starts, now_ends;
         at.masks(here, s0, valid, now_starts, now_ends);
         if (!OUTPUT || !p.last) now_ends = 0;
         const Elements<T, S::kV> now_x = x, now_z = z;
-        const bool on = (valid >> at.slot) & 1;
-        if (on) {
-#pragma unroll
-            for (int e = 0; e < S::kV; e += 2) {
-                Two delta = dt.pair(e) + of_pair(0, e);
-                if (softplus) delta = softplus_of(delta);
-                if (!WIDE) delta = two(e < at.there ? one(delta).x : 0.0f, e + 1 < at.there ? one(delta).y : 0.0f);
-                const float2 d = one(delta), u = one(delta * x.pair(e));
-                prepared[at.slot][e * 8 + at.m] = make_float4(d.x, d.x, u.x, u.x);
-                prepared[at.slot][e * 8 + 8 + at.m] = make_float4(d.y, d.y, u.y, u.y);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < S::kV; ++e) prepared[at.slot][e * 8 + at.m] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        }
-        bc.store(rows, valid);
+        if (!HALVES) prepare(buffer, valid);
         if (OUTPUT && p.carry && s0 >= at.begin) store_states(p, at, p.carry + (at.q * runs + run) * per + first_state, h);
-        __syncthreads();
-        if (run + 1 < end) fetch(run + 1);
+        if (HALVES)
+            half_waits(kFull + buffer);
+        else
+            __syncthreads();
+        if (run + 1 < end) {
+            here = at.look(pos, p.t, s0 + kRun);
+            if (!HALVES) fetch(s0 + kRun);
+        }
 
         auto group = [&](int g, auto with_breaks) {
             constexpr bool breaks = decltype(with_breaks)::value;
@@ -487,8 +557,8 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
             for (int i = 0; i < S::kGroup; ++i) {
                 const int s = g + i;
                 Two B[S::kPairs], C[S::kPairs];
-                pairs_of<S>(&rows[s][0][at.part * S::kStates], B);
-                if (OUTPUT) pairs_of<S>(&rows[s][1][at.part * S::kStates], C);
+                pairs_of<S>(&rows[buffer][s][0][at.part * S::kStates], B);
+                if (OUTPUT) pairs_of<S>(&rows[buffer][s][1][at.part * S::kStates], C);
                 if (breaks && ((now_starts >> s) & 1)) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
@@ -497,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
                 }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const float4 d = prepared[s][at.at[c]];
+                    const float4 d = prepared[buffer][s][at.at[c]];
                     const Two delta = two(d.x, d.y), u = two(d.z, d.w);
                     Two sum = zero();
 #pragma unroll
@@ -516,33 +586,30 @@ __global__ void __launch_bounds__(kThreads, 4) k37_scan(const ScanParams p, cons
             if (OUTPUT) {
                 int first;
                 lane_sums<S>(y, at.lane, first);
-                sums[g + first][at.at[0]] = y[0][0];
+                sums[buffer][g + first][at.at[0]] = y[0][0];
             }
         };
-#pragma unroll 2
-        for (int g = 0; g < kRun; g += 2 * S::kGroup) {
-            if (((now_starts | now_ends) >> g) & ((1 << 2 * S::kGroup) - 1)) {
-                group(g, std::true_type());
-                group(g + S::kGroup, std::true_type());
-            } else {
-                group(g, std::false_type());
-                group(g + S::kGroup, std::false_type());
+        if (HALVES && !(now_starts | now_ends)) {  // (in one piece: with two walks on an SM nothing else fills the gaps between groups)
+#pragma unroll
+            for (int g = 0; g < kRun; g += S::kGroup) group(g, std::false_type());
+        } else {
+#pragma unroll(HALVES ? 1 : 2)
+            for (int g = 0; g < kRun; g += 2 * S::kGroup) {
+                if (((now_starts | now_ends) >> g) & ((1 << 2 * S::kGroup) - 1)) {
+                    group(g, std::true_type());
+                    group(g + S::kGroup, std::true_type());
+                } else {
+                    group(g, std::false_type());
+                    group(g + S::kGroup, std::false_type());
+                }
             }
         }
-        __syncthreads();
-        if (OUTPUT && at.inside(s0)) {
-            Elements<T, S::kV> out;
-            if (on) {
-#pragma unroll
-                for (int e = 0; e < S::kV; e += 2) {
-                    Two v = fma(of_pair(1, e), now_x.pair(e), two(sums[at.slot][e * 8 + at.m], sums[at.slot][e * 8 + 8 + at.m]));
-                    if (gated) v = v * (now_z.pair(e) * sigmoid_of(now_z.pair(e)));
-                    out.set_pair(e, v);
-                }
-            } else {
-                out.clear();
-            }
-            F::store(out, a.y, at, s0);
+        if (HALVES) {
+            half_arrives(kDone + buffer);
+            buffer ^= 1;
+        } else {
+            __syncthreads();
+            if (OUTPUT) finish(buffer, s0, valid, now_x, now_z);
         }
     }
     if (!OUTPUT) {
@@ -1073,7 +1140,8 @@ auto with_split(int states, const Go& go)
 // 1,599, 32 1,563; 16 x 4096 x 2048 prompts, 512 walks: one segment 1,103, four 1,407; 20,011 x 509 fp32, 8 walks: 74 segments 470, 78 635;
 // 512 walks of 2048 slots, training: one segment 2,372, four 2,626.  Segments that end at a start anywhere in the next share, rather than in
 // its first half: 746 instead of 749 and 1,603 instead of 1,555: too unequal.)
-ScanCuts cuts_of(int64_t blocks, int32_t t, int64_t channels, int states)
+constexpr int64_t kHalves = 2 * 148;
+ScanCuts cuts_of(int64_t blocks, int32_t t, int64_t channels, int states, bool gradient)
 {
     return with_split(states, [&](auto s) {
         using S = decltype(s);
@@ -1081,7 +1149,8 @@ ScanCuts cuts_of(int64_t blocks, int32_t t, int64_t channels, int states)
         cuts.groups = (int)((channels + S::kChannels - 1) / S::kChannels);
         const int64_t walks = blocks * cuts.groups, runs = (t + kRun - 1) / kRun, at_once = 4 * 148;
         int64_t n = 1;
-        if (walks < at_once / 2 || (walks > at_once && walks < at_once * 3 / 2)) {
+        const bool halves = !gradient && walks > 148 && walks <= kHalves;
+        if (!halves && (walks < at_once / 2 || (walks > at_once && walks < at_once * 3 / 2))) {
             const int64_t many = 14 * 148 / walks, fit = runs / 16 < many ? runs / 16 : many;
             n = fit * walks >= 2 * at_once ? fit : at_once / walks < fit ? at_once / walks : fit;
         }
@@ -1139,7 +1208,7 @@ cudaError_t join(const ScanParams& p, const ScanCuts& cuts, const ScanWork& work
 
 size_t scan_work_bytes(int64_t blocks, int32_t t, int64_t channels, int32_t states, bool gradient)
 {
-    return work_of(nullptr, cuts_of(blocks, t, channels, states), blocks, t, channels, states, gradient).bytes;
+    return work_of(nullptr, cuts_of(blocks, t, channels, states, gradient), blocks, t, channels, states, gradient).bytes;
 }
 
 template <typename T>
@@ -1148,21 +1217,23 @@ cudaError_t launch_scan(const ScanParams& params, const ScanTensors<T>& a, cudaS
     const ScanParams p = with_rows(params, a);
     return with_split(p.states, [&](auto s) {
         using S = decltype(s);
-        const ScanCuts cuts = cuts_of(p.blocks, p.t, p.channels, p.states);
+        const ScanCuts cuts = cuts_of(p.blocks, p.t, p.channels, p.states, false);
         const ScanWork work = work_of(p.work, cuts, p.blocks, p.t, p.channels, p.states, false);
         constexpr size_t n = S::kV * sizeof(T);
         const bool wide = on(a.x, n, p.t) && on(a.dt, n, p.t) && on(a.z, n, p.t) && on(a.y, n, p.t) && p.channels % S::kV == 0;
         const unsigned grid = (unsigned)(cuts.segments * p.blocks * cuts.groups);
         if (cuts.segments > 1) {
-            auto* part = wide ? k37_scan<T, S, true, false> : k37_scan<T, S, false, false>;
+            auto* part = wide ? k37_scan<T, S, true, false, false> : k37_scan<T, S, false, false, false>;
             part<<<grid, kThreads, 0, st>>>(p, a, cuts, work);
             count_launches(1);
             cudaError_t e = cudaGetLastError();
             if (e == cudaSuccess) e = join(p, cuts, work, false, st);
             if (e != cudaSuccess) return e;
         }
-        auto* kernel = wide ? k37_scan<T, S, true, true> : k37_scan<T, S, false, true>;
-        kernel<<<grid, kThreads, 0, st>>>(p, a, cuts, work);
+        const bool halves = cuts.segments == 1 && grid <= kHalves;
+        auto* kernel = halves ? (wide ? k37_scan<T, S, true, true, true> : k37_scan<T, S, false, true, true>)
+                              : (wide ? k37_scan<T, S, true, true, false> : k37_scan<T, S, false, true, false>);
+        kernel<<<grid, halves ? 2 * kThreads : kThreads, 0, st>>>(p, a, cuts, work);
         count_launches(1);
         return cudaGetLastError();
     });
@@ -1174,7 +1245,7 @@ cudaError_t launch_scan_grad(const ScanParams& params, const ScanTensors<T>& a, 
     const ScanParams p = with_rows(params, a);
     return with_split(p.states, [&](auto s) {
         using S = decltype(s);
-        const ScanCuts cuts = cuts_of(p.blocks, p.t, p.channels, p.states);
+        const ScanCuts cuts = cuts_of(p.blocks, p.t, p.channels, p.states, true);
         const ScanWork work = work_of(p.work, cuts, p.blocks, p.t, p.channels, p.states, true);
         constexpr size_t n = S::kV * sizeof(T);
         const bool wide = on(a.x, n, p.t) && on(a.dt, n, p.t) && on(a.z, n, p.t) && on(a.dy, n, p.t) && on(a.dx, n, p.t) && on(a.ddt, n, p.t) && on(a.dz, n, p.t) &&
