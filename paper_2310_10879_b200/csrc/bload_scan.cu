@@ -8,7 +8,8 @@
 // neighbouring channels of a slot as they lie in memory, and go to the lanes through shared memory; sums over the states come back that
 // way.  The chain from slot to slot is one multiply-add per state.
 //
-// Where there are too few walks for the machine, the slots are cut into segments, a CTA each.  k37 and k39 first run over the part
+// Walks that fit on the machine at once, two to an SM, are bound by the latency of a run: there a second half of the CTA prepares and
+// finishes runs while the first walks.  Where there are fewer, the slots are cut into segments, a CTA each.  k37 and k39 first run over the part
 // of a segment that its successor hears of (from the last sequence start on; nothing if a sequence starts there) without output, k38
 // joins what they leave, and the walk proper starts from that.
 //
@@ -16,7 +17,7 @@
 // every other slot into shared memory (each thread its own), then goes through them from the last slot to the first.  Sums over
 // channels (db, dc) are shared out over the lanes of a warp, then over the CTA's warps, and written once per CTA; k40 adds the CTAs'.
 //
-// 8 x 4096 x 2048 x 16 bf16, prompts: 745 us (parts of segments 228, walk 508); 4 x 10,000 x 1024 x 16 training: 341 + 1,010 us for the
+// 8 x 4096 x 2048 x 16 bf16, prompts: 647 us (745 in segments: their parts 228, walk 508); 4 x 10,000 x 1024 x 16 training: 341 + 1,010 us for the
 // walks, 1,540 in all.  What bounds them is latency and issue (0.5 instructions a cycle and scheduler with 16 warps per SM, the exponentials
 // 40 to 55 % of their rate, shared memory 53 %).  Step of 256 x 4096 x 16: 36 us, 4.0 TB/s.
 #include <math.h>
@@ -1135,7 +1136,9 @@ auto with_split(int states, const Go& go)
 
 // Segments per walk.  Four CTAs of a walk fit on an SM at once, 592 in all.  What that is for: walks that are too few for it, and a
 // second wave that would be almost empty.  Many small segments (two waves or more, up to 14 CTAs per SM) level the SMs out; where the
-// runs do not suffice for that, 16 to a segment, one wave.  (8 x 4096 x 2048 bf16, 256 walks: prompts
+// runs do not suffice for that, 16 to a segment, one wave.  Forward, one wave of walks that take half a CTA more (kHalves) does without
+// segments where most SMs have two: 8 x 4096 x 2048 647 us instead of 745, but 4 x 4096 x 2048 440 to 483 instead of 416, and with 384 walks
+// 1,005 instead of 911.  (8 x 4096 x 2048 bf16, 256 walks: prompts
 // 1 segment 742 us, 2 775, 4 766, 8 749, training 3,051, 3,057, 2,833, 2,658; 4 x 10,000 x 1024 training, 64 walks: 9 segments 1,664, 18
 // 1,599, 32 1,563; 16 x 4096 x 2048 prompts, 512 walks: one segment 1,103, four 1,407; 20,011 x 509 fp32, 8 walks: 74 segments 470, 78 635;
 // 512 walks of 2048 slots, training: one segment 2,372, four 2,626.  Segments that end at a start anywhere in the next share, rather than in
