@@ -295,3 +295,25 @@ def test_no_blocks_and_refusals():
         with pytest.raises(B.BloadError) as e:
             bad()
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("dtype,c,n", [(BF, 2003, 16), (F32, 1999, 7), (FP, 1021, 24), (BF, 512, 64)])
+def test_one_wave_of_walks_in_one_piece_each(dtype, c, n):
+    """Between one and two walks for each of the machine's SMs, of many runs and an odd end; states of sequences that end in, at the end
+    of and across runs, two calls alike."""
+    blocks = [[203], [16, 32, 1, 100, 54], [-5, 150, 48], [31, 1, 171], [-203]]
+    pos = L.positions(203, blocks)
+    i = S.scan_inputs(5, 203, c, n, dtype, 12)
+    ids, count = S.sequence_numbers(pos)
+    args = {"d": i["d"], "dt_bias": i["dt_bias"], "z": i["z"]}
+    _, work = B.bload_scan_buffers(pos, i["x"], i["a"], gradient=False)
+    out = []
+    for _ in range(2):
+        y, last = torch.full_like(i["x"], 7.0), torch.full((count, c, n), 7.0, device=DEV)
+        B.bload_scan(pos, i["x"], i["dt"], i["a"], i["b"], i["c"], y, work=work, seq_id=ids, last=last, **args)
+        out.append((y, last))
+    torch.cuda.synchronize()
+    val, tol = S.scan(blocks, i["x"], i["dt"], i["a"], i["b"], i["c"], **args)
+    L.close(out[0][0], val["y"], tol["y"], "y")
+    L.close(out[0][1], val["last"], tol["last"], "last")
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
