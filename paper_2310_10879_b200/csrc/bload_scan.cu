@@ -560,7 +560,8 @@ __global__ void __launch_bounds__(HALVES ? 2 * kThreads : kThreads, HALVES ? 2 :
                 Two B[S::kPairs], C[S::kPairs];
                 pairs_of<S>(&rows[buffer][s][0][at.part * S::kStates], B);
                 if (OUTPUT) pairs_of<S>(&rows[buffer][s][1][at.part * S::kStates], C);
-                if (breaks && ((now_starts >> s) & 1)) {
+                const bool start = breaks && ((now_starts >> s) & 1);
+                if (start) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -569,7 +570,8 @@ __global__ void __launch_bounds__(HALVES ? 2 * kThreads : kThreads, HALVES ? 2 :
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const float4 d = prepared[buffer][s][at.at[c]];
-                    const Two delta = two(d.x, d.y), u = two(d.z, d.w);
+                    // (no state, no decay: one beyond 32 bits would make NaN of zero)
+                    const Two delta = start ? zero() : two(d.x, d.y), u = two(d.z, d.w);
                     Two sum = zero();
 #pragma unroll
                     for (int k = 0; k < S::kPairs; ++k) {
