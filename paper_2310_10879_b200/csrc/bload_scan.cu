@@ -648,7 +648,14 @@ __global__ void __launch_bounds__(256) k38_scan_join(const ScanParams p, const S
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             // (kind 0: nothing was written)
-            state = kind[j] == 0 ? 0.0f : kind[j] == 2 ? fmaf(ex2(delta[j] * a), state, own[j]) : own[j];
+            if (kind[j] == 2) {
+                // Decays are above 0 and finite slot by slot: where their product has left the 32-bit range, nothing still stays
+                // nothing, and an infinite state infinite.
+                const float left = state == 0.0f || isinf(state) ? state : ex2(delta[j] * a) * state;
+                state = left + own[j];
+            } else {
+                state = kind[j] == 0 ? 0.0f : own[j];
+            }
             if (kind[j] == 2) work.state[cell(j) * per + (i - q * per)] = state;
         }
     }
