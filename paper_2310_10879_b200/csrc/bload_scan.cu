@@ -9,7 +9,7 @@
 // way.  The chain from slot to slot is one multiply-add per state.
 //
 // Walks that fit on the machine at once, two to an SM, are bound by the latency of a run: there a second half of the CTA prepares and
-// finishes runs while the first walks.  Where there are fewer, the slots are cut into segments, a CTA each.  k37 and k39 first run over the part
+// finishes runs while the first walks.  Where they leave much of the machine empty, the slots are cut into segments, a CTA each.  k37 and k39 first run over the part
 // of a segment that its successor hears of (from the last sequence start on; nothing if a sequence starts there) without output, k38
 // joins what they leave, and the walk proper starts from that.
 //
@@ -1145,12 +1145,22 @@ auto with_split(int states, const Go& go)
 
 // Segments per walk.  Four CTAs of a walk fit on an SM at once, 592 in all.  What that is for: walks that are too few for it, and a
 // second wave that would be almost empty.  Many small segments (two waves or more, up to 14 CTAs per SM) level the SMs out; where the
-// runs do not suffice for that, 16 to a segment, one wave.  Forward, one wave of walks that take half a CTA more (kHalves) does without
-// segments where most SMs have two: 8 x 4096 x 2048 647 us instead of 745, but 4 x 4096 x 2048 440 to 483 instead of 416, and with 384 walks
-// 1,005 instead of 911.  (8 x 4096 x 2048 bf16, 256 walks: prompts
-// 1 segment 742 us, 2 775, 4 766, 8 749, training 3,051, 3,057, 2,833, 2,658; 4 x 10,000 x 1024 training, 64 walks: 9 segments 1,664, 18
+// runs do not suffice for that, 16 to a segment, one wave.
+// Forward, one wave of walks that take half a CTA more (kHalves, two to an SM) does without segments.  It takes as long as an SM with two
+// walks, however many SMs have only one; segments take time by the walks, and by how much of each its successor hears of.  So halves from
+// three quarters of the wave on; from two thirds on in blocks of less than 128 runs, where few segments fit and the last wave of them is
+// part empty; and always where a block makes two segments at most.  Halves / segments, us, 16 states bf16, with last states not wanted:
+//     4096 slots, packed tokens      149 walks 623 / 509, 192 635 / 583, 208 630 / 627, 222 635 / 646, 240 635 / 693, 256 634 / 726
+//     one sequence a block           149 621 / 525, 192 628 / 634, 208 628 / 697, 222 627 / 720, 256 629 / 826
+//     lengths of 30 in the middle    149 632 / 384, 192 639 / 468, 208 638 / 501, 222 643 / 523, 256 641 / 552
+//     1024 slots, packed tokens      149 165 / 161, 160 167 / 153, 192 168 / 159, 208 169 / 198, 222 169 / 191, 256 168 / 218
+//     640 slots                      149 107 / 107, 192 109 / 110, 208 109 / 134;    512: 149 87 / 103, 192 88 / 118, 222 89 / 120
+//     32,768 slots                   149 4,916 / 2,947, 192 4,959 / 3,576, 222 4,957 / 3,921, 256 4,954 / 4,330 (one sequence 6,368)
+// (Other walks, prompts of 8 x 4096 x 2048: one segment of whole CTAs 742, 2 775, 4 766, 8 749; training of the same
+// 1 segment 3,051, 2 3,057, 4 2,833, 8 2,658; 4 x 10,000 x 1024 training, 64 walks: 9 segments 1,664, 18
 // 1,599, 32 1,563; 16 x 4096 x 2048 prompts, 512 walks: one segment 1,103, four 1,407; 20,011 x 509 fp32, 8 walks: 74 segments 470, 78 635;
-// 512 walks of 2048 slots, training: one segment 2,372, four 2,626.  Segments that end at a start anywhere in the next share, rather than in
+// 512 walks of 2048 slots, training: one segment 2,372, four 2,626; halves: 4 x 4096 x 2048 440 to 483 instead of 416, 384 walks 1,005
+// instead of 911.  Segments that end at a start anywhere in the next share, rather than in
 // its first half: 746 instead of 749 and 1,603 instead of 1,555: too unequal.)
 constexpr int64_t kHalves = 2 * 148;
 ScanCuts cuts_of(int64_t blocks, int32_t t, int64_t channels, int states, bool gradient)
@@ -1161,7 +1171,8 @@ ScanCuts cuts_of(int64_t blocks, int32_t t, int64_t channels, int states, bool g
         cuts.groups = (int)((channels + S::kChannels - 1) / S::kChannels);
         const int64_t walks = blocks * cuts.groups, runs = (t + kRun - 1) / kRun, at_once = 4 * 148;
         int64_t n = 1;
-        const bool halves = !gradient && walks > 148 && walks <= kHalves;
+        const int64_t from = runs < 48 ? 149 : runs < 128 ? kHalves * 2 / 3 + 1 : kHalves * 3 / 4;
+        const bool halves = !gradient && walks >= from && walks <= kHalves;
         if (!halves && (walks < at_once / 2 || (walks > at_once && walks < at_once * 3 / 2))) {
             const int64_t many = 14 * 148 / walks, fit = runs / 16 < many ? runs / 16 : many;
             n = fit * walks >= 2 * at_once ? fit : at_once / walks < fit ? at_once / walks : fit;
