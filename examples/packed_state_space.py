@@ -68,7 +68,7 @@ class Conv(torch.autograd.Function):
 class Scan(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, dt, z, b, c, a, d, dt_bias, pos):
-        carry, work = B.bload_scan_buffers(pos, x, a)
+        carry, work = B.bload_scan_buffers(pos, x, a, gradient=False, carry=True)
         y = _new(x)
         B.bload_scan(pos, x, dt, a, b, c, y, d, dt_bias, z, carry=carry, work=work)
         ctx.save_for_backward(x, dt, z, b, c, a, d, dt_bias, pos, carry)
@@ -80,7 +80,7 @@ class Scan(torch.autograd.Function):
         x, dt, z, b, c, a, d, dt_bias, pos, carry = ctx.saved_tensors
         dx, ddt, dz, db, dc, da, dd, ddt_bias = (_new(v) for v in (x, dt, z, b, c, a, d, dt_bias))
         B.bload_scan_grad(pos, x, dt, a, b, c, carry, dy.contiguous(), dx, ddt, da, db, dc, d, dd, dt_bias, ddt_bias, z, dz,
-                          work=B.bload_scan_buffers(pos, x, a)[1])
+                          work=B.bload_scan_buffers(pos, x, a, carry=False)[1])
         return dx, ddt, dz, db, dc, da, dd, ddt_bias, None
 
 

@@ -968,14 +968,15 @@ def bload_conv_step(pos, state, x, y, weight, bias=None, silu: bool = True, next
 SCAN_RUN = 16
 
 
-def bload_scan_buffers(pos, x, a, gradient: bool = True):
-    """(carry, work) for bload_scan and, with gradient, bload_scan_grad on x [blocks, t_block, channels] and a [channels, states]: the
-    float32 states that the forward call keeps for the gradient, [blocks, ceil(t_block / 16), channels, states] (None without), and
-    scratch (None when none is needed).  Calls that may overlap on the GPU need a scratch each."""
+def bload_scan_buffers(pos, x, a, gradient: bool = True, carry: bool | None = None):
+    """(carry, work) for x [blocks, t_block, channels] and a [channels, states]: the float32 states that bload_scan keeps for the
+    gradient, [blocks, ceil(t_block / 16), channels, states], and scratch: of bload_scan_grad, which serves both calls, or with
+    gradient False of bload_scan alone, which needs less (None where none is needed).  carry: whether to make it (None: with
+    gradient).  Calls that may overlap on the GPU need a scratch each."""
     b, t = pos.shape
     c, states = x.shape[-1], a.shape[-1]
     n = load().bload_scan_work_bytes(b, t, c, states, 1 if gradient else 0)
-    return (x.new_empty((b, -(-t // SCAN_RUN), c, states), dtype=_torch()[2]) if gradient else None,
+    return (x.new_empty((b, -(-t // SCAN_RUN), c, states), dtype=_torch()[2]) if (gradient if carry is None else carry) else None,
             x.new_empty(n, dtype=_torch()[5]) if n else None)
 
 
