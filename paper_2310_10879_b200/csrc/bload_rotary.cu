@@ -67,7 +67,8 @@ struct alignas(V * sizeof(T)) Piece {
 // exact as long as k < 2^22), then the Taylor series of both to r^9 and r^8, and the quadrant.  Angles are below 3e5, where the 24 bits
 // of 2 / pi place k within 0.01 of a's multiple: |r| <= 0.8, and the series' remainders are below 3e-8 (over 2 million angles the result
 // was never off by more than 1e-7; up to 6e6 |r| grew to 1.03 and the error to 4.7e-7).  Larger angles go to sincosf.
-// REST: of the angle a + rest, where rest is below half a unit of a's last place.
+// REST: of the angle a + rest, where rest is at most half a unit of a's last place (2^-6 below 3e5), which counts for r but not for k:
+// |r| <= 0.82, remainders below 4e-8 (over 8 million products in each of 0 to 1e3, to 2^17, to 2^18 and to 3e5 never off by more than 1e-7).
 template <bool REST>
 __device__ __forceinline__ void sine_cosine(float a, float rest, float& sn, float& cs)
 {
