@@ -31,8 +31,8 @@ class Rotary(torch.autograd.Function):
     @staticmethod
     @once_differentiable  # (the gradient calls have no gradients of their own)
     def backward(ctx, dy):
-        dx = torch.empty_like(dy)
-        B.bload_rotary_grad(ctx.saved_tensors[0], dy, dx, ctx.saved_tensors[1])
+        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+        B.bload_rotary_grad(ctx.saved_tensors[0], dy.contiguous(), dx, ctx.saved_tensors[1])
         return dx, None, None
 
 

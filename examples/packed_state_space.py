@@ -97,7 +97,7 @@ class RotaryAxes(torch.autograd.Function):
     def backward(ctx, dy):
         pos, coords, axis, inv_freq = ctx.saved_tensors
         dx = _new(dy)
-        B.bload_rotary_axes_grad(pos, coords, axis, dy, dx, inv_freq)
+        B.bload_rotary_axes_grad(pos, coords, axis, dy.contiguous(), dx, inv_freq)
         return dx, None, None, None, None
 
 
