@@ -712,6 +712,11 @@ BLOAD_API int bload_conv_step(int64_t rows, int64_t channels, int32_t dtype, int
  *                 rows are left as they were, numbers that several pieces have as in bload_conv.  d_last NULL: not wanted
  *   d_work        scratch of bload_scan_work_bytes(.., gradient) bytes, 256-byte aligned (NULL when that is 0); calls that may overlap
  *                 on the GPU need one each
+ * What a call keeps grows with the states: d_carry as above (268 MB for 8 x 4096 slots of 2048 channels and 16 states), and in the
+ * gradient's scratch 8 bytes per slot, state and CTA of 64 channels (32 above 16 states, 16 above 32), states rounded up to 8, 16, 32 or
+ * 64, for the sums of db and dc: 134 MB there, 537 MB with 32 states, 2.1 GB with 64.
+ * An element of a frame that is infinite or NaN may make any value of its sequence's frames, and the sums over all frames, infinite or
+ * NaN (which of the two is not specified); y and states in front of it, and all frames of other sequences, are not concerned.
  * bload_scan_step -- the same for one new frame of each of `rows` sequences; d_pos as in bload_conv_step.
  *   state, next   float [rows, channels, states] contiguous: h before and after the call; next may be state itself
  *   x, dt, z, y   [rows, channels], b, c [rows, states], by block_stride (slot_stride unused)

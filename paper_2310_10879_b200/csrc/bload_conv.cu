@@ -11,7 +11,8 @@
 // registers; a tile writes them once and k33 adds the tiles' in their order.
 //
 // 8 x 4096 x 2048 bf16, 4 taps, with the gate: 62 us forward (4.3 TB/s), 104 gradient (3.9 TB/s; 576 CTAs with all their registers); step of
-// 256 x 4096 fp16 7.7 us.  Bound by latency and issue: 30 instructions an element in the
+// 256 x 4096 fp16 7.9 us; last inputs of 219 prompts kept as well: 3 us more; 2047 channels, rows off any boundary: 193 and 326 us, by
+// element loads when a slot's turn has come, nothing ahead.  Bound by latency and issue: 30 instructions an element in the
 // gradient, 0.55 of the issue slots, half of what the multiply-adds allow.
 #include <type_traits>
 

@@ -17,9 +17,11 @@
 // every other slot into shared memory (each thread its own), then goes through them from the last slot to the first.  Sums over
 // channels (db, dc) are shared out over the lanes of a warp, then over the CTA's warps, and written once per CTA; k40 adds the CTAs'.
 //
-// 8 x 4096 x 2048 x 16 bf16, prompts: 647 us (745 in segments: their parts 228, walk 508); 4 x 10,000 x 1024 x 16 training: 341 + 1,010 us for the
-// walks, 1,540 in all.  What bounds them is latency and issue (0.5 instructions a cycle and scheduler with 16 warps per SM, the exponentials
-// 40 to 55 % of their rate, shared memory 53 %).  Step of 256 x 4096 x 16: 36 us, 4.0 TB/s.
+// 8 x 4096 x 2048 x 16 bf16, prompts, in halves: 650 us (745 in segments: their parts 228, walk 508); 4 x 10,000 x 1024 x 16 training: 344 +
+// 1,020 us for the walks, 1,550 in all.  What bounds them is latency and issue: halves 0.44 instructions a cycle and scheduler, the exponentials at
+// 47 % of their rate, shared memory 51 %, 14 warps on an SM (the two halves wait for one another as often as for arithmetic);
+// segments 0.5, 40 to 55 %, 53 %, 16 warps.  More states, 8 x 4096 x 2048 bf16, 16 / 32 / 64 of them: forward 630 / 1,000 / 1,855 us,
+// training 2,570 / 4,240 / 7,990, of which the sums over CTAs' db and dc 30 / 93 / 344.  Step of 256 x 4096 x 16: 36 us, 4.0 TB/s.
 #include <math.h>
 #include <stddef.h>
 
